@@ -120,8 +120,32 @@ def lib() -> C.CDLL:
         L.rl_debug_split_k.argtypes = [C.c_int32, C.c_int32, C.c_int32, C.c_int32, C.c_int64, C.POINTER(C.c_int32), C.POINTER(C.c_int32),
                                        C.POINTER(C.c_int32)]
         L.rl_debug_split_k.restype = C.c_int
+        _declare_norm_linear(L)
         _lib = L
     return _lib
+
+
+def _declare_norm_linear(L):
+    """Signatures of include/rl_norm_linear.h."""
+    p, i, l, z, f = C.c_void_p, C.c_int32, C.c_int64, C.c_size_t, C.c_float
+    nbytes = C.POINTER(C.c_size_t)
+    for name, args in dict(
+            rl_layer_norm_forward=[p, l, i, l, i, p, p, i, f, p, l, p, p, p, i, p],
+            rl_layer_norm_backward_workspace_bytes=[l, i, nbytes],
+            rl_layer_norm_backward=[p, l, p, l, p, p, i, i, l, i, p, i, p, p, l, p, p, p, z, p],
+            rl_f8_pack=[p, l, i, l, i, i, p, p, p],
+            rl_f8_unpack=[p, p, i, l, i, p, l, i, p],
+            rl_f8_pack_weight=[p, l, i, i, i, i, p, p, p, p, p],
+            rl_f8_matmul_workspace_bytes=[l, i, i, nbytes],
+            rl_f8_matmul=[p, p, i, p, p, i, l, i, i, p, l, i, p, z, p],
+            rl_f8_linear_forward=[p, l, i, l, i, i, p, p, i, i, p, l, p, p, p, z, p],
+            rl_f8_linear_backward_workspace_bytes=[l, i, i, i, nbytes],
+            rl_f8_linear_backward=[p, l, i, l, i, i, i, p, p, i, p, p, i, p, l, p, l, i, p, z, p]).items():
+        fn = getattr(L, name)
+        fn.argtypes, fn.restype = args, C.c_int
+    for name in ("rl_f8_code_pitch", "rl_f8_scale_pitch"):
+        fn = getattr(L, name)
+        fn.argtypes, fn.restype = [i], l
 
 
 def _check(st: int):
@@ -417,3 +441,197 @@ def rl_rvq_encode(vectors, codebooks, norms=None, want_residual=True, count_exac
                                res.data_ptr() if want_residual else None, _stream_handle()))
     return codes, res
 
+
+# ------------------------------------------------------------------ layer norm, 8-bit rows, 8-bit linear layer
+F8_FORMATS = {"e4m3": 0, "e5m2": 1}
+F8_FEW_ROWS = 16
+
+
+@dataclass
+class F8Rows:
+    """A matrix [rows, cols] in 8-bit rows: codes uint8 [rows, cols rounded up to 128], scales uint8 [rows, blocks rounded up to 4]."""
+    codes: torch.Tensor
+    scales: torch.Tensor
+    cols: int
+    fmt: str = "e4m3"
+
+
+@dataclass
+class F8Weight:
+    """A packed weight [N, K] and its transpose [K, N] (None: forward only)."""
+    rows: F8Rows
+    cols: Optional[F8Rows] = None
+
+
+def _rows(t: torch.Tensor, name: str):
+    """(pointer, row stride, dtype code) of a [rows, columns] tensor whose columns are contiguous."""
+    if not t.is_cuda:
+        raise ValueError(f"{name} must live on the GPU")
+    if t.dim() != 2 or (t.stride(1) != 1 and t.shape[1] > 1):
+        raise ValueError(f"{name} must be [rows, columns] with contiguous columns")
+    ld = t.stride(0) if t.shape[0] > 1 else t.shape[1]
+    if ld < t.shape[1]:
+        raise ValueError(f"{name} must not have overlapping rows")
+    return t.data_ptr(), ld, _dtype_code(t)
+
+
+def _f8_pitch(cols: int):
+    return (cols + 127) // 128 * 128, ((cols + 127) // 128 + 3) // 4 * 4
+
+
+def _f8_empty(rows: int, cols: int, fmt: str, device) -> F8Rows:
+    if fmt not in F8_FORMATS:
+        raise ValueError(f"format must be one of {sorted(F8_FORMATS)}, got {fmt!r}")
+    kp, ks = _f8_pitch(cols)
+    return F8Rows(torch.empty((rows, kp), dtype=torch.uint8, device=device), torch.empty((rows, ks), dtype=torch.uint8, device=device), cols, fmt)
+
+
+def _f8(p: F8Rows, rows: int, cols: int, name: str):
+    """(codes, scales, format) of packed rows that must be [rows, cols]."""
+    kp, ks = _f8_pitch(cols)
+    if p.cols != cols or p.codes.shape != (rows, kp) or p.scales.shape != (rows, ks):
+        raise ValueError(f"{name} must be 8-bit rows of [{rows}, {cols}]")
+    return _ptr(p.codes, torch.uint8, name=name + ".codes"), _ptr(p.scales, torch.uint8, name=name + ".scales"), F8_FORMATS[p.fmt]
+
+
+def _f8_workspace(nbytes: int, device):
+    """(tensor to hold on to, address, bytes)"""
+    if nbytes == 0:
+        return None, None, 0
+    ws = _workspace(nbytes, device)
+    return ws, ws.data_ptr(), nbytes
+
+
+def rl_layer_norm_forward(x, gamma, beta=None, eps=1e-5, checkpoint=None, out=None):
+    """(y, stats, kept): y = (x - mean) rstd gamma + beta over the columns of x [R, H]; stats [R, 2] float32 (mean, rstd) for the backward pass;
+    kept: x in 8-bit rows of the format `checkpoint` ("e4m3" | "e5m2"), or None.  gamma, beta [H]: float32 or bfloat16, one type.
+    out: where y goes, x itself for instance."""
+    R, H = x.shape
+    px, ldx, dt = _rows(x, "x")
+    if beta is not None and beta.dtype != gamma.dtype:
+        raise ValueError("gamma and beta must have one dtype")
+    y = torch.empty((R, H), dtype=x.dtype, device=x.device) if out is None else out
+    if y.shape != x.shape or y.dtype != x.dtype:
+        raise ValueError("out must have the shape and dtype of x")
+    py, ldy, _ = _rows(y, "out")
+    stats = torch.empty((R, 2), dtype=torch.float32, device=x.device)
+    kept = None if checkpoint is None else _f8_empty(R, H, checkpoint, x.device)
+    codes, scales, fmt = (None, None, 0) if kept is None else (kept.codes.data_ptr(), kept.scales.data_ptr(), F8_FORMATS[kept.fmt])
+    _check(lib().rl_layer_norm_forward(px, ldx, dt, R, H, _ptr(gamma, numel=H, name="gamma"), _ptr(beta, numel=H, name="beta"), _dtype_code(gamma), float(eps),
+                                       py, ldy, stats.data_ptr(), codes, scales, fmt, _stream_handle()))
+    return y, stats, kept
+
+
+def rl_layer_norm_backward(dy, x, stats, gamma, want_beta=True, out=None):
+    """(dx, dgamma, dbeta) from dy [R, H], x or its checkpoint (F8Rows), and the statistics of the forward pass; dgamma, dbeta float32.
+    out: where dx goes, dy itself for instance."""
+    R, H = dy.shape
+    dev = dy.device
+    pdy, lddy, dt = _rows(dy, "dy")
+    px, ldx, codes, scales, fmt = None, 0, None, None, 0
+    if isinstance(x, F8Rows):
+        codes, scales, fmt = _f8(x, R, H, "x")
+    else:
+        if x.shape != dy.shape or x.dtype != dy.dtype:
+            raise ValueError("x must have the shape and dtype of dy")
+        px, ldx, _ = _rows(x, "x")
+    dx = torch.empty((R, H), dtype=dy.dtype, device=dev) if out is None else out
+    if dx.shape != dy.shape or dx.dtype != dy.dtype:
+        raise ValueError("out must have the shape and dtype of dy")
+    pdx, lddx, _ = _rows(dx, "out")
+    dgamma = torch.empty(H, dtype=torch.float32, device=dev)
+    dbeta = torch.empty(H, dtype=torch.float32, device=dev) if want_beta else None
+    need = C.c_size_t(0)
+    _check(lib().rl_layer_norm_backward_workspace_bytes(R, H, C.byref(need)))
+    ws, pws, nws = _f8_workspace(need.value, dev)
+    _check(lib().rl_layer_norm_backward(pdy, lddy, px, ldx, codes, scales, fmt, dt, R, H, _ptr(gamma, numel=H, name="gamma"), _dtype_code(gamma),
+                                        _ptr(stats, torch.float32, 2 * R, "stats"), pdx, lddx, dgamma.data_ptr(), dbeta.data_ptr() if want_beta else None,
+                                        pws, nws, _stream_handle()))
+    return dx, dgamma, dbeta
+
+
+def rl_f8_pack(x, fmt="e4m3") -> F8Rows:
+    """x [R, K] in 8-bit rows: a scale (a power of two) for 128 consecutive values of a row."""
+    R, K = x.shape
+    px, ldx, dt = _rows(x, "x")
+    p = _f8_empty(R, K, fmt, x.device)
+    _check(lib().rl_f8_pack(px, ldx, dt, R, K, F8_FORMATS[fmt], p.codes.data_ptr(), p.scales.data_ptr(), _stream_handle()))
+    return p
+
+
+def rl_f8_unpack(p: F8Rows, dtype=torch.bfloat16):
+    """The values [R, K] of 8-bit rows."""
+    R = p.codes.shape[0]
+    codes, scales, fmt = _f8(p, R, p.cols, "p")
+    x = torch.empty((R, p.cols), dtype=dtype, device=p.codes.device)
+    _check(lib().rl_f8_unpack(codes, scales, fmt, R, p.cols, x.data_ptr(), p.cols, _dtype_code(x), _stream_handle()))
+    return x
+
+
+def rl_f8_pack_weight(w, fmt="e4m3", transposed=True) -> F8Weight:
+    """A weight [N, K] packed for the linear layer, one scale for 128 x 128 values; with its transpose for the backward pass."""
+    N, K = w.shape
+    pw, ldw, dt = _rows(w, "w")
+    rows = _f8_empty(N, K, fmt, w.device)
+    cols = _f8_empty(K, N, fmt, w.device) if transposed else None
+    _check(lib().rl_f8_pack_weight(pw, ldw, dt, N, K, F8_FORMATS[fmt], rows.codes.data_ptr(), rows.scales.data_ptr(),
+                                   cols.codes.data_ptr() if transposed else None, cols.scales.data_ptr() if transposed else None, _stream_handle()))
+    return F8Weight(rows, cols)
+
+
+def rl_f8_matmul(a: F8Rows, b: F8Rows, dtype=torch.bfloat16):
+    """a [M, K] times the transpose of b [N, K], both in 8-bit rows; sums in float32."""
+    M, N, K = a.codes.shape[0], b.codes.shape[0], a.cols
+    ca, sa, fa = _f8(a, M, K, "a")
+    cb, sb, fb = _f8(b, N, K, "b")
+    y = torch.empty((M, N), dtype=dtype, device=a.codes.device)
+    need = C.c_size_t(0)
+    _check(lib().rl_f8_matmul_workspace_bytes(M, N, K, C.byref(need)))
+    ws, pws, nws = _f8_workspace(need.value, y.device)
+    _check(lib().rl_f8_matmul(ca, sa, fa, cb, sb, fb, M, N, K, y.data_ptr(), N, _dtype_code(y), pws, nws, _stream_handle()))
+    return y
+
+
+def rl_f8_linear_forward(x, w: F8Weight, fmt="e4m3", keep=True):
+    """(y, kept): y = pack(x) W^T in the dtype of x, and the packed x for the backward pass (keep=False: None)."""
+    M, K = x.shape
+    N = w.rows.codes.shape[0]
+    px, ldx, dt = _rows(x, "x")
+    cw, sw, fw = _f8(w.rows, N, K, "w.rows")
+    kept = _f8_empty(M, K, fmt, x.device) if keep or M > F8_FEW_ROWS else None
+    y = torch.empty((M, N), dtype=x.dtype, device=x.device)
+    need = C.c_size_t(0)
+    _check(lib().rl_f8_matmul_workspace_bytes(M, N, K, C.byref(need)))
+    ws, pws, nws = _f8_workspace(need.value, x.device)
+    if fmt not in F8_FORMATS:
+        raise ValueError(f"format must be one of {sorted(F8_FORMATS)}, got {fmt!r}")
+    _check(lib().rl_f8_linear_forward(px, ldx, dt, M, K, F8_FORMATS[fmt], cw, sw, fw, N, y.data_ptr(), N,
+                                      kept.codes.data_ptr() if kept else None, kept.scales.data_ptr() if kept else None, pws, nws, _stream_handle()))
+    return y, kept if keep else None
+
+
+def rl_f8_linear_backward(dy, kept: F8Rows, w: F8Weight, fmt="e5m2", want_dx=True, want_dw=True, dw=None):
+    """(dx, dw): dx = pack(dy) W in the dtype of dy, with dy packed in `fmt`; dw = dy^T x in float32 from the kept x, added to `dw` if that is given."""
+    M, N = dy.shape
+    K = kept.cols if kept is not None else w.rows.cols
+    dev = dy.device
+    pdy, lddy, dt = _rows(dy, "dy")
+    if fmt not in F8_FORMATS:
+        raise ValueError(f"format must be one of {sorted(F8_FORMATS)}, got {fmt!r}")
+    if want_dx and (w is None or w.cols is None):
+        raise ValueError("dx needs the packed transpose of the weight")
+    cx, sx, fx = _f8(kept, M, K, "kept") if want_dw else (None, None, 0)
+    ct, st, fw = _f8(w.cols, K, N, "w.cols") if want_dx else (None, None, 0)
+    dx = torch.empty((M, K), dtype=dy.dtype, device=dev) if want_dx else None
+    accumulate = dw is not None
+    if want_dw and dw is None:
+        dw = torch.empty((N, K), dtype=torch.float32, device=dev)
+    if want_dw and (dw.shape != (N, K) or dw.dtype != torch.float32):
+        raise ValueError(f"dw must be float32 [{N}, {K}]")
+    pdw, lddw, _ = _rows(dw, "dw") if want_dw else (None, K, 0)
+    need = C.c_size_t(0)
+    _check(lib().rl_f8_linear_backward_workspace_bytes(M, N, K, dt, C.byref(need)))
+    ws, pws, nws = _f8_workspace(need.value, dev)
+    _check(lib().rl_f8_linear_backward(pdy, lddy, dt, M, N, K, F8_FORMATS[fmt], cx, sx, fx, ct, st, fw, dx.data_ptr() if want_dx else None, K,
+                                       pdw, lddw, 1 if accumulate else 0, pws, nws, _stream_handle()))
+    return dx, dw if want_dw else None

@@ -1,0 +1,290 @@
+// gemm_f8.h - product of two matrices of 8-bit rows (f8_rows.h):  y[m, n] = sum_k x[m, k] w[n, k]
+//
+// A slab is one block of 128 k: 128 bytes of a row, one 16x16x128 MFMA a block of the tile, which multiplies the two blocks' scales in by itself
+// (v_mfma_scale_f32_16x16x128_f8f6f4; operands in either format) and adds in f32.  Rows are padded to whole blocks with zeros, so K has no tail.
+// An operand is 32 bytes a lane: row l % 16, and which 32 of the 128 k a lane group l / 16 holds is free as long as both operands agree (the sum does not care,
+// and the scale is one for all 128).
+// That MFMA adds eight products at a time on a common exponent, what is below about 2^-13 of the largest of the eight being cut off, and in f32 from there on
+// (measured: 2.6e-5 of the result at K = 128).  Where y is bf16 that is a hundredth of y's own rounding, and taken; where y is f32 the operands are restored to bf16, which is
+// exact, on their way to 16x16x32 bf16 MFMAs, whose products and sums are those of f32, at half the rate (kExact).
+// The operands are exchanged (w first): a lane then holds four consecutive n of one row of y.
+//
+//  * f8_gemm_kernel  general: BM x BN tile, four wavefronts, two LDS stages of one slab, cut along K where there are few tiles.
+//  * f8_few_kernel   up to 16 rows of x: bound by reading w, which goes from memory straight into MFMA operands; eight wavefronts share K.  x may come
+//                    as it is: a lane holds 32 consecutive values of a block, which it packs in registers.
+#pragma once
+#include <type_traits>
+
+#include "f8_rows.h"
+
+namespace rlk {
+
+typedef int i32x8_t __attribute__((ext_vector_type(8)));
+typedef int i32x4_t __attribute__((ext_vector_type(4)));
+
+struct F8Operand { const uint8_t* codes; const uint8_t* scales; int rows, Kp, Ks; };
+
+// acc += x-block * w-block; byte 0 of sx / sw: the scales of the lane's row
+template <int FX, int FW> __device__ __attribute__((always_inline)) inline void mfma_f8(floatx4& acc, const i32x8_t& w, const i32x8_t& x, unsigned sw, unsigned sx) {
+  acc = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(w, x, acc, FW, FX, 0, (int)sw, 0, (int)sx);
+}
+
+// The 32 codes of an operand and their scale as four operands of 16x16x32 bf16 MFMAs.
+struct ExactOperand { u32x4_t v[4]; };
+template <int F> __device__ __attribute__((always_inline)) inline ExactOperand exact_operand(const i32x8_t& c, unsigned scale) {
+  const float s = f8_scale_value(scale & 255u);
+  ExactOperand o;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    bf16x2 lo, hi;
+    if constexpr (F == kE4M3) { lo = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((unsigned)c[i], s, false); hi = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((unsigned)c[i], s, true); }
+    else { lo = __builtin_amdgcn_cvt_scalef32_pk_bf16_bf8((unsigned)c[i], s, false); hi = __builtin_amdgcn_cvt_scalef32_pk_bf16_bf8((unsigned)c[i], s, true); }
+    o.v[i >> 1][(i & 1) * 2] = __builtin_bit_cast(unsigned, lo); o.v[i >> 1][(i & 1) * 2 + 1] = __builtin_bit_cast(unsigned, hi);
+  }
+  return o;
+}
+__device__ __attribute__((always_inline)) inline void mfma_exact(floatx4& acc, const ExactOperand& w, const ExactOperand& x) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, w.v[i]), __builtin_bit_cast(bf16x8, x.v[i]), acc, 0, 0, 0);
+}
+template <class T> constexpr bool kExact = sizeof(T) == 4;
+
+// Four consecutive values of a row of y, at most `left` of them.
+typedef float floatx4_el4 __attribute__((ext_vector_type(4), aligned(4)));
+typedef __bf16 bf16x4_el2 __attribute__((ext_vector_type(4), aligned(2)));
+template <class T> __device__ __attribute__((always_inline)) inline void store4(T* p, int left, const floatx4& v) {
+  if (left >= 4) {
+    if constexpr (sizeof(T) == 4) *reinterpret_cast<floatx4_el4*>(p) = v;
+    else *reinterpret_cast<bf16x4_el2*>(p) = bf16x4_el2{(bf16_t)v[0], (bf16_t)v[1], (bf16_t)v[2], (bf16_t)v[3]};
+  } else {
+#pragma unroll
+    for (int i = 0; i < 3; ++i) if (i < left) p[i] = (T)v[i];
+  }
+}
+
+template <class T> struct F8Product {
+  F8Operand x, w;
+  T* y; int64_t ldy;
+  int M, N, nk;                      // nk: blocks of k
+  int slices, per;                   // cut along K: slices of `per` blocks (a multiple of four), whose sums go to part [slices][M][Np] instead of y
+  float* part; int Np;
+};
+
+template <int FX, int FW, class T, int BM, int BN>
+__global__ __launch_bounds__(256, 2) void f8_gemm_kernel(F8Product<T> j) {
+  constexpr int MB = BM / 32, NB = BN / 32, STAGE = (BM + BN) * kSlabBytes, LOADS = (BM + BN) / 32;      // loads of a wavefront and slab, 8 rows each
+  __shared__ __attribute__((aligned(1024))) unsigned char smem[2 * STAGE];
+  const int tiles_m = (j.M + BM - 1) / BM, tiles_n = (j.N + BN - 1) / BN;
+  int t;
+  if (!run_of_block(blockIdx.x, tiles_m * tiles_n * j.slices, t)) return;
+  const int slice = t / (tiles_m * tiles_n);
+  t -= slice * (tiles_m * tiles_n);
+  const int tn = t / tiles_m, tm = t - tn * tiles_m;
+  const int k0 = slice * j.per, nk = j.nk - k0 < j.per ? j.nk - k0 : j.per;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wm = wave >> 1, wn = wave & 1;
+
+  const uint8_t* src[LOADS];
+#pragma unroll
+  for (int i = 0; i < LOADS; ++i) {
+    const int lr = (wave * LOADS + i) * 8 + (lane >> 3);             // row of the stage: x rows, then w rows
+    const int c = (lane & 7) ^ ((lr >> 1) & 7);
+    const bool is_x = lr < BM;                                       // (uniform: BM is a multiple of 8)
+    int r = is_x ? tm * BM + lr : tn * BN + lr - BM;
+    const int last = (is_x ? j.M : j.N) - 1;
+    r = r < last ? r : last;
+    src[i] = (is_x ? j.x.codes + (int64_t)r * j.x.Kp : j.w.codes + (int64_t)r * j.w.Kp) + (int64_t)k0 * 128 + c * 16;
+  }
+  auto issue = [&](int kt) __attribute__((always_inline)) {
+#pragma unroll
+    for (int i = 0; i < LOADS; ++i) load16_to_lds_lanes(src[i] + (int64_t)kt * 128, smem + (kt & 1) * STAGE + (wave * LOADS + i) * 1024);
+  };
+  const int frow = lane & 15, g = lane >> 4;
+  const unsigned* xs[MB];
+  const unsigned* ws[NB];
+#pragma unroll
+  for (int i = 0; i < MB; ++i) {
+    int r = tm * BM + wm * (BM / 2) + i * 16 + frow; r = r < j.M ? r : j.M - 1;
+    xs[i] = reinterpret_cast<const unsigned*>(j.x.scales + (int64_t)r * j.x.Ks + k0);
+  }
+#pragma unroll
+  for (int i = 0; i < NB; ++i) {
+    int r = tn * BN + wn * (BN / 2) + i * 16 + frow; r = r < j.N ? r : j.N - 1;
+    ws[i] = reinterpret_cast<const unsigned*>(j.w.scales + (int64_t)r * j.w.Ks + k0);
+  }
+  floatx4 acc[MB][NB];
+#pragma unroll
+  for (int i = 0; i < MB; ++i)
+#pragma unroll
+    for (int b = 0; b < NB; ++b) acc[i][b] = floatx4{0.f, 0.f, 0.f, 0.f};
+
+  unsigned sx[MB], sw[NB];
+  issue(0);
+  for (int kt = 0; kt < nk; ++kt) {
+    if ((kt & 3) == 0) {                                             // the scales of four slabs
+#pragma unroll
+      for (int i = 0; i < MB; ++i) sx[i] = xs[i][kt >> 2];
+#pragma unroll
+      for (int i = 0; i < NB; ++i) sw[i] = ws[i][kt >> 2];
+    }
+    __builtin_amdgcn_s_waitcnt(0x0F70);                              // vmcnt(0): this slab has landed ...
+    __syncthreads();                                                 // ... everybody's, and nobody reads the other stage any more
+    if (kt + 1 < nk) issue(kt + 1);
+    const unsigned char* xa = smem + (kt & 1) * STAGE;
+    std::conditional_t<kExact<T>, ExactOperand, i32x8_t> fx[MB];
+#pragma unroll
+    for (int i = 0; i < MB; ++i) {
+      const int r = wm * (BM / 2) + i * 16 + frow;
+      const i32x4_t lo = *reinterpret_cast<const i32x4_t*>(xa + lds_off(r, g)), hi = *reinterpret_cast<const i32x4_t*>(xa + lds_off(r, g + 4));
+      const i32x8_t c = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+      if constexpr (kExact<T>) fx[i] = exact_operand<FX>(c, sx[i]); else fx[i] = c;
+    }
+#pragma unroll
+    for (int b = 0; b < NB; ++b) {
+      const int r = BM + wn * (BN / 2) + b * 16 + frow;
+      const i32x4_t lo = *reinterpret_cast<const i32x4_t*>(xa + lds_off(r, g)), hi = *reinterpret_cast<const i32x4_t*>(xa + lds_off(r, g + 4));
+      const i32x8_t fw = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+      if constexpr (kExact<T>) {
+        const ExactOperand ew = exact_operand<FW>(fw, sw[b]);
+#pragma unroll
+        for (int i = 0; i < MB; ++i) mfma_exact(acc[i][b], ew, fx[i]);
+      } else {
+#pragma unroll
+        for (int i = 0; i < MB; ++i) mfma_f8<FX, FW>(acc[i][b], fw, fx[i], sw[b], sx[i]);
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < MB; ++i) sx[i] >>= 8;
+#pragma unroll
+    for (int i = 0; i < NB; ++i) sw[i] >>= 8;
+  }
+#pragma unroll
+  for (int i = 0; i < MB; ++i) {
+    const int m = tm * BM + wm * (BM / 2) + i * 16 + frow;
+    if (m >= j.M) continue;
+#pragma unroll
+    for (int b = 0; b < NB; ++b) {
+      const int n = tn * BN + wn * (BN / 2) + b * 16 + g * 4;
+      if (j.slices > 1) { if (n < j.Np) *reinterpret_cast<floatx4*>(j.part + ((int64_t)slice * j.M + m) * j.Np + n) = acc[i][b]; }
+      else store4(j.y + (int64_t)m * j.ldy + n, j.N - n, acc[i][b]);
+    }
+  }
+}
+
+// The slices of a cut product, added in order.
+template <class T>
+__global__ __launch_bounds__(256) void f8_slices_kernel(const float* part, int slices, int M, int N, int Np, T* y, int64_t ldy) {
+  const int n4 = Np / 4;
+  const int64_t all = (int64_t)M * n4, stride = (int64_t)M * Np;
+  for (int64_t q = (int64_t)blockIdx.x * 256 + threadIdx.x; q < all; q += (int64_t)gridDim.x * 256) {
+    const int64_t m = q / n4;
+    const int n = (int)(q - m * n4) * 4;
+    const float* p = part + m * Np + n;
+    floatx4 s = *reinterpret_cast<const floatx4*>(p);
+    for (int k0 = 1; k0 < slices; k0 += 4) {
+      floatx4 v[4];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) v[k] = k0 + k < slices ? *reinterpret_cast<const floatx4*>(p + (k0 + k) * stride) : floatx4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int k = 0; k < 4; ++k) s += v[k];
+    }
+    store4(y + m * ldy + n, N - n, s);
+  }
+}
+
+// ------------------------------------------------------------------ few rows
+constexpr int kF8FewRows = 16, kF8FewWaves = 8;
+
+// x as it is: 32 consecutive values of the lane's row and block to codes and their block's scale byte (the four lanes of a row have the block).
+template <class T> __device__ __attribute__((always_inline)) inline unsigned f8_pack_operand(const Raw8<T> (&r)[4], int fmt, i32x8_t& code) {
+  unsigned a = 0;
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+#pragma unroll
+    for (int e = 0; e < 8; ++e) { const unsigned b = finite_bits(raw_get(r[i], e)); a = a > b ? a : b; }
+  for (int d = 16; d < 64; d <<= 1) { const unsigned b = (unsigned)__shfl_xor((int)a, d); a = a > b ? a : b; }
+  const unsigned s = f8_scale(a, fmt);
+  const float inv = f8_scale_inverse(s);
+  const bool last = f8_scale_is_last(s, fmt);
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      float v[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) v[e] = raw_get(r[i], 4 * h + e);
+      if (last) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = f8_below_end(v[e], fmt);
+      }
+      code[2 * i + h] = (int)f8_code4(v[0] * inv, v[1] * inv, v[2] * inv, v[3] * inv, fmt);
+    }
+  return s;
+}
+
+template <class T> struct F8Few {
+  F8Operand x, w;                    // x.codes: read them, or, where raw is set, written by the first workgroup (nullptr: not wanted)
+  const T* raw; int64_t ldx; int K;
+  T* y; int64_t ldy;
+  int M, N, nk;
+};
+
+template <int FX, int FW, class T, bool RAW>
+__global__ __launch_bounds__(kF8FewWaves * 64) void f8_few_kernel(F8Few<T> j) {
+  __shared__ floatx4 sums[kF8FewWaves][64];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), frow = lane & 15, g = lane >> 4;
+  const int n0 = blockIdx.x * 16;
+  const int nr = n0 + frow < j.N ? n0 + frow : j.N - 1, mr = frow < j.M ? frow : j.M - 1;
+  const uint8_t* wp = j.w.codes + (int64_t)nr * j.w.Kp + g * 32;
+  const uint8_t* wsp = j.w.scales + (int64_t)nr * j.w.Ks;
+  floatx4 acc = {0.f, 0.f, 0.f, 0.f};
+  constexpr int U = 4;                                               // slabs in flight
+  for (int k0 = wave; k0 < j.nk; k0 += kF8FewWaves * U) {
+    i32x4_t wc[U][2];
+    unsigned sw[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      int k = k0 + u * kF8FewWaves; k = k < j.nk ? k : j.nk - 1;
+      wc[u][0] = *reinterpret_cast<const i32x4_t*>(wp + (int64_t)k * 128); wc[u][1] = *reinterpret_cast<const i32x4_t*>(wp + (int64_t)k * 128 + 16);
+      sw[u] = wsp[k];
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int k = k0 + u * kF8FewWaves;
+      if (k >= j.nk) break;
+      i32x8_t xc;
+      unsigned sx;
+      if constexpr (RAW) {
+        Raw8<T> r[4];
+        const int col = k * 128 + g * 32;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) r[i] = raw_load(j.raw + (int64_t)mr * j.ldx + col + i * 8, frow < j.M ? j.K - col - i * 8 : 0);
+        sx = f8_pack_operand(r, FX, xc);
+        if (j.x.codes && blockIdx.x == 0 && frow < j.M) {
+          uint8_t* cp = const_cast<uint8_t*>(j.x.codes) + (int64_t)frow * j.x.Kp + col;
+          *reinterpret_cast<i32x4_t*>(cp) = __builtin_shufflevector(xc, xc, 0, 1, 2, 3);
+          *reinterpret_cast<i32x4_t*>(cp + 16) = __builtin_shufflevector(xc, xc, 4, 5, 6, 7);
+          uint8_t* sp = const_cast<uint8_t*>(j.x.scales) + (int64_t)frow * j.x.Ks;
+          if (g == 0) {
+            sp[k] = (uint8_t)sx;
+            if (k == j.nk - 1) for (int b = j.nk; b < j.x.Ks; ++b) sp[b] = 127;
+          }
+        }
+      } else {
+        const uint8_t* xp = j.x.codes + (int64_t)mr * j.x.Kp + k * 128 + g * 32;
+        xc = __builtin_shufflevector(*reinterpret_cast<const i32x4_t*>(xp), *reinterpret_cast<const i32x4_t*>(xp + 16), 0, 1, 2, 3, 4, 5, 6, 7);
+        sx = j.x.scales[(int64_t)mr * j.x.Ks + k];
+      }
+      const i32x8_t wf = __builtin_shufflevector(wc[u][0], wc[u][1], 0, 1, 2, 3, 4, 5, 6, 7);
+      if constexpr (kExact<T>) mfma_exact(acc, exact_operand<FW>(wf, sw[u]), exact_operand<FX>(xc, sx));
+      else mfma_f8<FX, FW>(acc, wf, xc, sw[u], sx);
+    }
+  }
+  sums[wave][lane] = acc;
+  __syncthreads();
+  if (wave > 0) return;
+#pragma unroll
+  for (int i = 1; i < kF8FewWaves; ++i) acc += sums[i][lane];
+  if (frow < j.M) store4(j.y + (int64_t)frow * j.ldy + n0 + g * 4, j.N - n0 - g * 4, acc);
+}
+
+}  // namespace rlk

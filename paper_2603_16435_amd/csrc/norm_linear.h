@@ -1,0 +1,363 @@
+// norm_linear.h - host side and C entry points of layer norm, 8-bit rows and the 8-bit linear layer (include/rl_norm_linear.h).
+#pragma once
+#include "../../include/rl_norm_linear.h"
+#include "f8_grad.h"
+#include "f8_rows.h"
+#include "gemm_f8.h"
+#include "layer_norm.h"
+
+namespace rlk {
+
+static_assert((int)kE4M3 == (int)RL_E4M3 && (int)kE5M2 == (int)RL_E5M2 && kF8FewRows == RL_F8_FEW_ROWS && kNormMaxH == RL_LAYER_NORM_MAX_H, "header");
+constexpr int64_t kMaxRows = ((int64_t)1 << 31) - (1 << 16);
+constexpr int kMaxCols = 1 << 22;                             // columns of an 8-bit operand, and rows of a weight
+
+static bool known(int32_t dtype) { return dtype == RL_F32 || dtype == RL_BF16; }
+static bool known_f8(int32_t f) { return f == RL_E4M3 || f == RL_E5M2; }
+static size_t size_of(int32_t dtype) { return dtype == RL_F32 ? 4 : 2; }
+static bool off(const void* p, size_t align) { return reinterpret_cast<uintptr_t>(p) % align != 0; }
+static bool bad_rows(const void* p, int64_t ld, int32_t dtype, int64_t R, int64_t cols) {
+  return R < 0 || R >= kMaxRows || cols < 1 || ld < cols || ld > ((int64_t)1 << 40) / (R > 0 ? R : 1) || off(p, size_of(dtype));
+}
+static bool bad_ws(const void* ws, size_t bytes, size_t need) { return need && (!ws || off(ws, 256) || bytes < need); }
+static rl_status launched() { return hipGetLastError() == hipSuccess ? RL_OK : RL_ERR_HIP; }
+static unsigned blocks_of(int64_t n, int64_t most) { return (unsigned)(n < most ? (n > 0 ? n : 1) : most); }
+static F8Out f8_out(void* codes, void* scales, int fmt, int K) { return F8Out{(uint8_t*)codes, (uint8_t*)scales, fmt, f8_code_pitch(K), f8_scale_pitch(K)}; }
+static F8Operand f8_operand(const void* codes, const void* scales, int64_t rows, int K) {
+  return F8Operand{(const uint8_t*)codes, (const uint8_t*)scales, (int)rows, f8_code_pitch(K), f8_scale_pitch(K)};
+}
+
+// (a launch has at most 2^32 threads, of 256 a tile of 64 x 64 or more)
+static bool bad_product(int64_t M, int64_t N, int64_t K) {
+  return M < 0 || M >= kMaxRows || N < 1 || N > kMaxCols || K < 1 || K > kMaxCols || ((M + 63) / 64) * ((N + 63) / 64) > (1 << 23);
+}
+
+// ------------------------------------------------------------------ layer norm
+template <class T>
+static void run_norm_forward(const NormFwd<T>& j, hipStream_t s) {
+  auto go = [&](auto kern, int threads, int teams) { kern<<<blocks_of((j.R + teams - 1) / teams, 1 << 20), threads, 0, s>>>(j); };
+  const int H = j.H;
+  if (H <= 512) go(ln_forward_kernel<T, 1, 1>, 256, 4);
+  else if (H <= 4096 && j.R >= 2048) {
+    if (H <= 1024) go(ln_forward_kernel<T, 1, 2>, 256, 4);
+    else if (H <= 2048) go(ln_forward_kernel<T, 1, 4>, 256, 4);
+    else go(ln_forward_kernel<T, 1, 8>, 256, 4);
+  } else if (H <= 2048) go(ln_forward_kernel<T, 4, 1>, 256, 1);
+  else if (H <= 4096) go(ln_forward_kernel<T, 4, 2>, 256, 1);
+  else if (H <= 8192) go(ln_forward_kernel<T, 4, 4>, 256, 1);
+  else go(ln_forward_kernel<T, 16, 2>, 1024, 1);
+}
+
+constexpr int kNormBlocks = 512;
+struct NormTeams { int per_block, rows, blocks; };
+static NormTeams norm_teams(int64_t R, int H) {
+  NormTeams t;
+  t.per_block = H <= 1024 ? 4 : 1;
+  t.rows = H <= 4096 ? 4 : H <= 8192 ? 2 : 1;
+  const int64_t n = (R + t.rows * t.per_block - 1) / (t.rows * t.per_block);
+  t.blocks = (int)(n < kNormBlocks ? n : kNormBlocks);
+  return t;
+}
+static int norm_pitch(int H) { return (H + 7) / 8 * 8; }
+static size_t norm_part_bytes(int64_t R, int H) {
+  const NormTeams t = norm_teams(R, H);
+  return up256((size_t)t.blocks * t.per_block * 2 * norm_pitch(H) * 4);
+}
+
+template <class T, bool CK>
+static void run_norm_backward(const NormBwd<T>& j, float* dgamma, float* dbeta, hipStream_t s) {
+  const NormTeams t = norm_teams(j.R, j.H);
+  auto go = [&](auto kern, int threads) { kern<<<t.blocks, threads, 0, s>>>(j); };
+  if (t.blocks > 0) {
+    if (j.H <= 512) go(ln_backward_kernel<T, CK, 1, 1, 4>, 256);
+    else if (j.H <= 1024) go(ln_backward_kernel<T, CK, 1, 2, 4>, 256);
+    else if (j.H <= 2048) go(ln_backward_kernel<T, CK, 4, 1, 4>, 256);
+    else if (j.H <= 4096) go(ln_backward_kernel<T, CK, 4, 2, 4>, 256);
+    else if (j.H <= 8192) go(ln_backward_kernel<T, CK, 4, 4, 2>, 256);
+    else go(ln_backward_kernel<T, CK, 16, 2, 1>, 1024);
+  }
+  ln_sum_kernel<<<(2 * j.Hp + 63) / 64, 256, 0, s>>>(j.part, t.blocks * t.per_block, j.Hp, j.H, dgamma, dbeta);
+}
+
+// ------------------------------------------------------------------ products
+constexpr int kF8Slots = 512;             // general kernel: two workgroups a CU
+struct F8Plan { int bm, slices, per; size_t part; int Np; };
+static F8Plan f8_plan(int64_t M, int N, int K) {
+  F8Plan p{128, 1, 0, 0, (N + 3) / 4 * 4};
+  const int nk = f8_blocks(K);
+  auto tiles = [&](int b) { return ((M + b - 1) / b) * ((N + b - 1) / b); };
+  if (tiles(128) < kF8Slots / 2) p.bm = 64;
+  const int64_t t = tiles(p.bm);
+  int64_t want = t < kF8Slots ? kF8Slots / (t > 0 ? t : 1) : 1;
+  if (want > nk / 4) want = nk / 4;                                // a slice has four blocks at least: one word of scales a row
+  p.per = want > 1 ? (int)((nk + want - 1) / want + 3) / 4 * 4 : (nk + 3) / 4 * 4;
+  p.slices = (nk + p.per - 1) / p.per;
+  if (p.slices > 1) p.part = up256((size_t)p.slices * M * p.Np * 4);
+  return p;
+}
+
+template <int FX, int FW, class T>
+static void run_f8_matmul_of(const F8Operand& x, const F8Operand& w, int K, T* y, int64_t ldy, void* ws, hipStream_t s) {
+  const F8Plan p = f8_plan(x.rows, w.rows, K);
+  F8Product<T> j{x, w, y, ldy, x.rows, w.rows, f8_blocks(K), p.slices, p.per, (float*)ws, p.Np};
+  const int64_t tiles = (int64_t)((x.rows + p.bm - 1) / p.bm) * ((w.rows + p.bm - 1) / p.bm) * p.slices;
+  const unsigned blocks = (unsigned)((tiles + kXcds - 1) / kXcds * kXcds);
+  if (p.bm == 128) f8_gemm_kernel<FX, FW, T, 128, 128><<<blocks, 256, 0, s>>>(j);
+  else f8_gemm_kernel<FX, FW, T, 64, 64><<<blocks, 256, 0, s>>>(j);
+  if (p.slices > 1) f8_slices_kernel<T><<<blocks_of(((int64_t)x.rows * p.Np / 4 + 255) / 256, 4096), 256, 0, s>>>(j.part, p.slices, j.M, j.N, p.Np, y, ldy);
+}
+template <int FX, int FW, class T>
+static void run_f8_few_of(const F8Operand& x, const F8Operand& w, const T* raw, int64_t ldx, int K, T* y, int64_t ldy, hipStream_t s) {
+  const F8Few<T> j{x, w, raw, ldx, K, y, ldy, x.rows, w.rows, f8_blocks(K)};
+  const int blocks = (w.rows + 15) / 16;
+  if (raw) f8_few_kernel<FX, FW, T, true><<<blocks, kF8FewWaves * 64, 0, s>>>(j);
+  else f8_few_kernel<FX, FW, T, false><<<blocks, kF8FewWaves * 64, 0, s>>>(j);
+}
+// raw: x as it is, up to kF8FewRows rows
+template <class T>
+static void run_f8_product(const F8Operand& x, int fx, const F8Operand& w, int fw, const T* raw, int64_t ldx, int K, T* y, int64_t ldy, void* ws, hipStream_t s) {
+  auto go = [&](auto FX, auto FW) {
+    if (x.rows <= kF8FewRows) run_f8_few_of<FX.value, FW.value, T>(x, w, raw, ldx, K, y, ldy, s);
+    else run_f8_matmul_of<FX.value, FW.value, T>(x, w, K, y, ldy, ws, s);
+  };
+  typedef std::integral_constant<int, 0> E4;
+  typedef std::integral_constant<int, 1> E5;
+  if (fx == RL_E4M3) { if (fw == RL_E4M3) go(E4(), E4()); else go(E4(), E5()); }
+  else { if (fw == RL_E4M3) go(E5(), E4()); else go(E5(), E5()); }
+}
+template <class T> static void run_f8_pack(const T* x, int64_t ldx, int64_t R, int K, const F8Out& o, hipStream_t s) {
+  const int segs = (o.Ks / 4 + kF8Steps - 1) / kF8Steps;
+  f8_pack_kernel<T><<<blocks_of((R * segs + 3) / 4, 1 << 16), 256, 0, s>>>(x, R, ldx, K, o);
+}
+
+// ------------------------------------------------------------------ backward of the linear layer
+struct F8GradPlan { size_t codes, scales, mm, xt, terms, part, total; int chunk, Np; };
+static F8GradPlan f8_grad_plan(int64_t M, int N, int K, int32_t dtype) {
+  F8GradPlan p{};
+  size_t o = 0;
+  auto take = [&](size_t n) { const size_t at = o; o += up256(n); return at; };
+  p.codes = take((size_t)M * f8_code_pitch(N));
+  p.scales = take((size_t)M * f8_scale_pitch(N));
+  size_t mm = 0;
+  if (M > kF8FewRows) mm = f8_plan(M, K, N).part;
+  p.mm = take(mm);
+  p.chunk = (int)(M < kGradChunk ? (M + 127) / 128 * 128 : kGradChunk);
+  p.Np = (N + 7) / 8 * 8;
+  p.xt = take((size_t)p.chunk * ((K + 255) / 256 * 256) * 2);
+  p.terms = take((size_t)(dtype == RL_F32 ? 3 : 1) * p.chunk * p.Np * 2);
+  const int tm = (K + kBM - 1) / kBM, tn = (p.Np + kBN - 1) / kBN;
+  const int64_t slices = (int64_t)tm * tn < 2 * kHotSlots ? 2 * kHotSlots / (tm * tn) : 1;
+  p.part = take(slices > 1 ? (size_t)(slices < kMaxSplit ? slices : kMaxSplit) * N * ((K + 3) / 4 * 4) * 4 : 0);
+  p.total = o;
+  return p;
+}
+
+template <class T>
+static void run_f8_weight_grad(const T* dy, int64_t lddy, int64_t M, int N, int K, const F8Operand& x, int fx, float* dW, int64_t lddw, bool accumulate,
+                               unsigned char* ws, const F8GradPlan& p, hipStream_t s) {
+  bf16_t* xt = (bf16_t*)(ws + p.xt);
+  bf16_t* terms = (bf16_t*)(ws + p.terms);
+  const bool direct = sizeof(T) == 2 && N % 8 == 0 && lddy % 8 == 0 && !off(dy, 16) && lddy < (1 << 23);
+  for (int64_t t0 = 0; t0 < M; t0 += p.chunk) {
+    const int tokens = (int)(M - t0 < p.chunk ? M - t0 : p.chunk), pad = (tokens + 127) / 128 * 128;
+    f8_restore_t_kernel<<<dim3(pad / 64, f8_blocks(K)), 256, 0, s>>>(x.codes + t0 * x.Kp, x.scales + t0 * x.Ks, fx, tokens, x.Kp, x.Ks, xt, pad);
+    if (!direct) f8_grad_terms_kernel<T><<<blocks_of(((int64_t)tokens * p.Np / 8 + 255) / 256, 8192), 256, 0, s>>>(dy + t0 * lddy, lddy, tokens, N, p.Np, terms);
+    for (int k = sizeof(T) == 4 ? 2 : 0; k >= 0; --k) {            // the smallest term first
+      GemmDims d{};
+      d.M = K; d.N = direct ? N : p.Np; d.K = pad; d.lda = pad; d.ldb = direct ? lddy : p.Np;
+      d.group_m = 8; d.split_slots = kHotSlots; d.b_k_rows = tokens;
+      const bf16_t* B = direct ? (const bf16_t*)(dy + t0 * lddy) : terms + (int64_t)k * tokens * p.Np;
+      const bool add = accumulate || t0 > 0 || (sizeof(T) == 4 && k < 2);
+      const int tm = (d.M + kBM - 1) / kBM, tn = (d.N + kBN - 1) / kBN;
+      const SplitK sk = split_k_host(tm * tn, pad / 64 / 2, kHotSlots, 0);
+      const int64_t ldp = (K + 3) / 4 * 4;
+      const EpiF8Grad e{dW, lddw, N, K, add, (float*)(ws + p.part), ldp};
+      f8_grad_kernel<TuneDX><<<split_launch(tm, tn, kHotSlots), 256, 0, s>>>(xt, B, d, e);
+      if (sk.slices > 1) f8_grad_slices_kernel<<<blocks_of(((int64_t)N * (ldp / 4) + 255) / 256, 4096), 256, 0, s>>>(e.part, sk.slices, N, K, ldp, dW, lddw, add);
+    }
+  }
+}
+
+__global__ __launch_bounds__(256) void f8_zero_kernel(float* dW, int64_t ld, int N, int K) {
+  for (int64_t q = (int64_t)blockIdx.x * 256 + threadIdx.x; q < (int64_t)N * K; q += (int64_t)gridDim.x * 256) dW[q / K * ld + q % K] = 0.f;
+}
+
+}  // namespace rlk
+
+// ------------------------------------------------------------------ C entry points
+using namespace rlk;
+
+extern "C" {
+
+int64_t rl_f8_code_pitch(int32_t K) { return K > 0 && K <= kMaxCols ? f8_code_pitch(K) : 0; }
+int64_t rl_f8_scale_pitch(int32_t K) { return K > 0 && K <= kMaxCols ? f8_scale_pitch(K) : 0; }
+
+rl_status rl_layer_norm_forward(const void* x, int64_t ldx, int32_t dtype, int64_t R, int32_t H, const void* gamma, const void* beta,
+                                int32_t param_dtype, float eps, void* y, int64_t ldy, float* stats, void* codes, void* scales,
+                                int32_t format, void* stream) {
+  if (!gamma || (R != 0 && (!x || !y)) || !codes != !scales) return RL_ERR_NULL;
+  if (!known(dtype) || !known(param_dtype) || (codes && !known_f8(format))) return RL_ERR_DTYPE;
+  if (H > kNormMaxH || bad_rows(x, ldx, dtype, R, H) || bad_rows(y, ldy, dtype, R, H) || off(gamma, size_of(param_dtype)) ||
+      off(beta, size_of(param_dtype)) || off(codes, 16) || off(scales, 16) || off(stats, 8)) return RL_ERR_SHAPE;
+  if (!(eps >= 0.f) || !__builtin_isfinite(eps)) return RL_ERR_RANGE;
+  if (R == 0) return RL_OK;
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  (void)hipGetLastError();
+  const NormParams p{gamma, beta, param_dtype == RL_BF16};
+  const F8Out o = f8_out(codes, scales, format, H);
+  if (dtype == RL_BF16) run_norm_forward(NormFwd<bf16_t>{(const bf16_t*)x, (bf16_t*)y, R, ldx, ldy, H, eps, p, (float2*)stats, o}, s);
+  else run_norm_forward(NormFwd<float>{(const float*)x, (float*)y, R, ldx, ldy, H, eps, p, (float2*)stats, o}, s);
+  return launched();
+}
+
+rl_status rl_layer_norm_backward_workspace_bytes(int64_t R, int32_t H, size_t* bytes) {
+  if (!bytes) return RL_ERR_NULL;
+  if (R < 0 || R >= kMaxRows || H < 1 || H > kNormMaxH) return RL_ERR_SHAPE;
+  *bytes = norm_part_bytes(R, H);
+  return RL_OK;
+}
+
+rl_status rl_layer_norm_backward(const void* dy, int64_t lddy, const void* x, int64_t ldx, const void* codes, const void* scales, int32_t format,
+                                 int32_t dtype, int64_t R, int32_t H, const void* gamma, int32_t param_dtype, const float* stats,
+                                 void* dx, int64_t lddx, float* dgamma, float* dbeta, void* ws, size_t ws_bytes, void* stream) {
+  if (!gamma || !dgamma || (R != 0 && (!dy || !dx || !stats || (!x && (!codes || !scales))))) return RL_ERR_NULL;
+  if (x && (codes || scales)) return RL_ERR_NULL;                  // one of the two
+  if (!known(dtype) || !known(param_dtype) || (codes && !known_f8(format))) return RL_ERR_DTYPE;
+  if (H > kNormMaxH || bad_rows(dy, lddy, dtype, R, H) || bad_rows(dx, lddx, dtype, R, H) || (x && bad_rows(x, ldx, dtype, R, H)) ||
+      off(gamma, size_of(param_dtype)) || off(codes, 16) || off(scales, 16) || off(stats, 8) || off(dgamma, 16) || off(dbeta, 16)) return RL_ERR_SHAPE;
+  if (bad_ws(ws, ws_bytes, norm_part_bytes(R, H))) return RL_ERR_WORKSPACE;
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  (void)hipGetLastError();
+  auto go = [&](auto zero) {
+    typedef decltype(zero) T;
+    const NormBwd<T> j{(const T*)dy, (const T*)x, (T*)dx, R, lddy, ldx, lddx, H, (const uint8_t*)codes, (const uint8_t*)scales, format,
+                       f8_code_pitch(H), f8_scale_pitch(H), NormParams{gamma, nullptr, param_dtype == RL_BF16}, (const float2*)stats, (float*)ws, norm_pitch(H)};
+    if (codes) run_norm_backward<T, true>(j, dgamma, dbeta, s); else run_norm_backward<T, false>(j, dgamma, dbeta, s);
+  };
+  if (dtype == RL_BF16) go(bf16_t()); else go(float());
+  return launched();
+}
+
+rl_status rl_f8_pack(const void* x, int64_t ldx, int32_t dtype, int64_t R, int32_t K, int32_t format, void* codes, void* scales, void* stream) {
+  if (R != 0 && (!x || !codes || !scales)) return RL_ERR_NULL;
+  if (!known(dtype) || !known_f8(format)) return RL_ERR_DTYPE;
+  if (K > kMaxCols || bad_rows(x, ldx, dtype, R, K) || off(codes, 16) || off(scales, 16)) return RL_ERR_SHAPE;
+  if (R == 0) return RL_OK;
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  (void)hipGetLastError();
+  const F8Out o = f8_out(codes, scales, format, K);
+  if (dtype == RL_BF16) run_f8_pack((const bf16_t*)x, ldx, R, K, o, s); else run_f8_pack((const float*)x, ldx, R, K, o, s);
+  return launched();
+}
+
+rl_status rl_f8_unpack(const void* codes, const void* scales, int32_t format, int64_t R, int32_t K, void* x, int64_t ldx, int32_t dtype, void* stream) {
+  if (R != 0 && (!x || !codes || !scales)) return RL_ERR_NULL;
+  if (!known(dtype) || !known_f8(format)) return RL_ERR_DTYPE;
+  if (K > kMaxCols || bad_rows(x, ldx, dtype, R, K) || off(codes, 16) || off(scales, 16)) return RL_ERR_SHAPE;
+  if (R == 0) return RL_OK;
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  (void)hipGetLastError();
+  const int segs = (f8_scale_pitch(K) / 4 + kF8Steps - 1) / kF8Steps;
+  const unsigned blocks = blocks_of((R * segs + 3) / 4, 1 << 16);
+  if (dtype == RL_BF16) f8_restore_kernel<bf16_t><<<blocks, 256, 0, s>>>((const uint8_t*)codes, (const uint8_t*)scales, format, R, K, (bf16_t*)x, ldx);
+  else f8_restore_kernel<float><<<blocks, 256, 0, s>>>((const uint8_t*)codes, (const uint8_t*)scales, format, R, K, (float*)x, ldx);
+  return launched();
+}
+
+rl_status rl_f8_pack_weight(const void* w, int64_t ldw, int32_t dtype, int32_t N, int32_t K, int32_t format, void* codes, void* scales,
+                            void* codes_t, void* scales_t, void* stream) {
+  if (!w || !codes || !scales || !codes_t != !scales_t) return RL_ERR_NULL;
+  if (!known(dtype) || !known_f8(format)) return RL_ERR_DTYPE;
+  if (N < 1 || N > kMaxCols || K > kMaxCols || bad_rows(w, ldw, dtype, N, K) || off(codes, 16) || off(scales, 16) || off(codes_t, 16) || off(scales_t, 16)) return RL_ERR_SHAPE;
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  (void)hipGetLastError();
+  const dim3 grid(f8_blocks(K), f8_blocks(N));
+  const F8Out o = f8_out(codes, scales, format, K), t = f8_out(codes_t, scales_t, format, N);
+  if (dtype == RL_BF16) f8_pack_weight_kernel<bf16_t><<<grid, 256, 0, s>>>((const bf16_t*)w, ldw, N, K, o, t);
+  else f8_pack_weight_kernel<float><<<grid, 256, 0, s>>>((const float*)w, ldw, N, K, o, t);
+  return launched();
+}
+
+rl_status rl_f8_matmul_workspace_bytes(int64_t M, int32_t N, int32_t K, size_t* bytes) {
+  if (!bytes) return RL_ERR_NULL;
+  if (bad_product(M, N, K)) return RL_ERR_SHAPE;
+  *bytes = M > kF8FewRows ? f8_plan(M, N, K).part : 0;
+  return RL_OK;
+}
+
+rl_status rl_f8_matmul(const void* x_codes, const void* x_scales, int32_t x_format, const void* w_codes, const void* w_scales, int32_t w_format,
+                       int64_t M, int32_t N, int32_t K, void* y, int64_t ldy, int32_t dtype, void* ws, size_t ws_bytes, void* stream) {
+  if (!w_codes || !w_scales || (M != 0 && (!x_codes || !x_scales || !y))) return RL_ERR_NULL;
+  if (!known(dtype) || !known_f8(x_format) || !known_f8(w_format)) return RL_ERR_DTYPE;
+  size_t need = 0;
+  if (rl_f8_matmul_workspace_bytes(M, N, K, &need) != RL_OK || bad_rows(y, ldy, dtype, M, N) || off(x_codes, 16) || off(x_scales, 16) || off(w_codes, 16) || off(w_scales, 16))
+    return RL_ERR_SHAPE;
+  if (bad_ws(ws, ws_bytes, need)) return RL_ERR_WORKSPACE;
+  if (M == 0) return RL_OK;
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  (void)hipGetLastError();
+  const F8Operand x = f8_operand(x_codes, x_scales, M, K), w = f8_operand(w_codes, w_scales, N, K);
+  if (dtype == RL_BF16) run_f8_product<bf16_t>(x, x_format, w, w_format, nullptr, 0, K, (bf16_t*)y, ldy, ws, s);
+  else run_f8_product<float>(x, x_format, w, w_format, nullptr, 0, K, (float*)y, ldy, ws, s);
+  return launched();
+}
+
+rl_status rl_f8_linear_forward(const void* x, int64_t ldx, int32_t dtype, int64_t M, int32_t K, int32_t x_format, const void* w_codes,
+                               const void* w_scales, int32_t w_format, int32_t N, void* y, int64_t ldy, void* x_codes, void* x_scales,
+                               void* ws, size_t ws_bytes, void* stream) {
+  if (!w_codes || !w_scales || (M != 0 && (!x || !y)) || !x_codes != !x_scales || (M > kF8FewRows && !x_codes)) return RL_ERR_NULL;
+  if (!known(dtype) || !known_f8(x_format) || !known_f8(w_format)) return RL_ERR_DTYPE;
+  size_t need = 0;
+  if (rl_f8_matmul_workspace_bytes(M, N, K, &need) != RL_OK || bad_rows(x, ldx, dtype, M, K) || bad_rows(y, ldy, dtype, M, N) || off(x_codes, 16) || off(x_scales, 16) ||
+      off(w_codes, 16) || off(w_scales, 16)) return RL_ERR_SHAPE;
+  if (bad_ws(ws, ws_bytes, need)) return RL_ERR_WORKSPACE;
+  if (M == 0) return RL_OK;
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  (void)hipGetLastError();
+  const F8Operand xo = f8_operand(x_codes, x_scales, M, K), w = f8_operand(w_codes, w_scales, N, K);
+  auto go = [&](auto zero) {
+    typedef decltype(zero) T;
+    if (M > kF8FewRows) run_f8_pack((const T*)x, ldx, M, K, f8_out(x_codes, x_scales, x_format, K), s);
+    run_f8_product<T>(xo, x_format, w, w_format, (const T*)x, ldx, K, (T*)y, ldy, ws, s);
+  };
+  if (dtype == RL_BF16) go(bf16_t()); else go(float());
+  return launched();
+}
+
+rl_status rl_f8_linear_backward_workspace_bytes(int64_t M, int32_t N, int32_t K, int32_t dtype, size_t* bytes) {
+  if (!bytes) return RL_ERR_NULL;
+  if (!known(dtype)) return RL_ERR_DTYPE;
+  if (bad_product(M, N, K) || bad_product(M, K, N)) return RL_ERR_SHAPE;
+  *bytes = f8_grad_plan(M, N, K, dtype).total;
+  return RL_OK;
+}
+
+rl_status rl_f8_linear_backward(const void* dy, int64_t lddy, int32_t dtype, int64_t M, int32_t N, int32_t K, int32_t dy_format,
+                                const void* x_codes, const void* x_scales, int32_t x_format, const void* wt_codes, const void* wt_scales, int32_t w_format,
+                                void* dx, int64_t lddx, float* dW, int64_t lddw, int32_t accumulate, void* ws, size_t ws_bytes, void* stream) {
+  if ((!dx && !dW && M != 0) || (M != 0 && !dy) || (dx && (!wt_codes || !wt_scales)) || (dW && M != 0 && (!x_codes || !x_scales))) return RL_ERR_NULL;
+  if (!known(dtype) || (dx && (!known_f8(dy_format) || !known_f8(w_format))) || (dW && !known_f8(x_format))) return RL_ERR_DTYPE;
+  if (bad_product(M, N, K) || bad_product(M, K, N) || bad_rows(dy, lddy, dtype, M, N) || (dx && bad_rows(dx, lddx, dtype, M, K)) ||
+      (dW && (lddw < K || off(dW, 4))) || off(x_codes, 16) || off(x_scales, 16) || off(wt_codes, 16) || off(wt_scales, 16)) return RL_ERR_SHAPE;
+  const F8GradPlan p = f8_grad_plan(M, N, K, dtype);
+  if (bad_ws(ws, ws_bytes, p.total)) return RL_ERR_WORKSPACE;
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  (void)hipGetLastError();
+  if (M == 0) {
+    if (dW && !accumulate) f8_zero_kernel<<<blocks_of(((int64_t)N * K + 255) / 256, 4096), 256, 0, s>>>(dW, lddw, N, K);
+    return launched();
+  }
+  unsigned char* w = static_cast<unsigned char*>(ws);
+  auto go = [&](auto zero) {
+    typedef decltype(zero) T;
+    if (dx) {
+      run_f8_pack((const T*)dy, lddy, M, N, f8_out(w + p.codes, w + p.scales, dy_format, N), s);
+      run_f8_product<T>(f8_operand(w + p.codes, w + p.scales, M, N), dy_format, f8_operand(wt_codes, wt_scales, K, N), w_format, nullptr, 0, N, (T*)dx, lddx, w + p.mm, s);
+    }
+    if (dW) run_f8_weight_grad((const T*)dy, lddy, M, N, K, f8_operand(x_codes, x_scales, M, K), x_format, dW, lddw, accumulate != 0, w, p, s);
+  };
+  if (dtype == RL_BF16) go(bf16_t()); else go(float());
+  return launched();
+}
+
+}  // extern "C"

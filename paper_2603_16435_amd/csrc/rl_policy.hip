@@ -2193,3 +2193,5 @@ rl_status rl_rvq_encode_counted(const void* vectors, const void* codebooks, cons
 }
 
 }  // extern "C"
+
+#include "norm_linear.h"

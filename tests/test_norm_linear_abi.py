@@ -1,0 +1,169 @@
+"""Layer norm, 8-bit rows and the 8-bit linear layer: what the C entry points refuse (no GPU: nothing reaches a kernel), and the oracle against
+independent statements of the same (bit patterns of torch's 8-bit types, finite differences)."""
+import ctypes as C
+import os
+
+import numpy as np
+import pytest
+import torch
+
+from oracle import norm_linear_oracle as orc
+from paper_2603_16435_amd import binding
+
+OK, NULL, SHAPE, DTYPE, RANGE, WORKSPACE = 0, 1, 2, 3, 4, 5
+P = 0x10000                                          # any aligned non-null address: never dereferenced
+
+
+@pytest.fixture(scope="module")
+def lib():
+    if not os.path.exists(binding.LIB_PATH):
+        from paper_2603_16435_amd import build
+        build.build(verbose=False)
+    return binding.lib()
+
+
+def _call(fn, names, defaults, over):
+    a = dict(defaults)
+    assert set(over) <= set(a), over
+    a.update(over)
+    return fn(*[a[n] for n in names])
+
+
+def _caller(fn, **defaults):
+    return lambda **over: _call(fn, list(defaults), defaults, over)
+
+
+def test_pitches(lib):
+    for k, c, s in ((1, 128, 4), (128, 128, 4), (129, 256, 4), (512, 512, 4), (513, 640, 8), (3584, 3584, 28), (0, 0, 0), (-5, 0, 0)):
+        assert lib.rl_f8_code_pitch(k) == c and lib.rl_f8_scale_pitch(k) == s
+    assert binding._f8_pitch(513) == (640, 8)
+
+
+def test_layer_norm_refusals(lib):
+    f = _caller(lib.rl_layer_norm_forward, x=P, ldx=64, dtype=1, R=0, H=64, gamma=P, beta=P, param_dtype=0, eps=1e-5, y=P, ldy=64, stats=P, codes=P,
+                scales=P, format=0, stream=None)
+    assert f() == OK                                  # no rows: nothing to do
+    assert f(x=None, y=None) == OK
+    for over, st in ((dict(gamma=None), NULL), (dict(R=4, x=None), NULL), (dict(R=4, y=None), NULL), (dict(codes=None), NULL), (dict(scales=None), NULL),
+                     (dict(dtype=2), DTYPE), (dict(param_dtype=9), DTYPE), (dict(format=2), DTYPE), (dict(H=0), SHAPE), (dict(H=16385), SHAPE),
+                     (dict(R=-1), SHAPE), (dict(R=1 << 31), SHAPE), (dict(ldx=63), SHAPE), (dict(ldy=63), SHAPE), (dict(ldx=1 << 41), SHAPE),
+                     (dict(x=P + 1), SHAPE), (dict(y=P + 1), SHAPE), (dict(gamma=P + 2), SHAPE), (dict(beta=P + 2), SHAPE), (dict(codes=P + 8), SHAPE),
+                     (dict(scales=P + 4), SHAPE), (dict(stats=P + 4), SHAPE), (dict(dtype=0, x=P + 2), SHAPE), (dict(eps=-1.0), RANGE),
+                     (dict(eps=float("nan")), RANGE), (dict(eps=float("inf")), RANGE)):
+        assert f(**over) == st, over
+    n = C.c_size_t(0)
+    assert lib.rl_layer_norm_backward_workspace_bytes(1000, 512, C.byref(n)) == OK and n.value > 0 and n.value % 256 == 0
+    need = n.value
+    assert lib.rl_layer_norm_backward_workspace_bytes(0, 512, C.byref(n)) == OK and n.value == 0
+    for R, H in ((-1, 8), (1, 0), (1, 16385), (1 << 31, 8)):
+        assert lib.rl_layer_norm_backward_workspace_bytes(R, H, C.byref(n)) == SHAPE
+    assert lib.rl_layer_norm_backward_workspace_bytes(1, 8, None) == NULL
+    b = _caller(lib.rl_layer_norm_backward, dy=P, lddy=512, x=P, ldx=512, codes=None, scales=None, format=0, dtype=1, R=1000, H=512, gamma=P, param_dtype=0,
+                stats=P, dx=P, lddx=512, dgamma=P, dbeta=P, workspace=P, workspace_bytes=need, stream=None)
+    packed = dict(x=None, codes=P, scales=P)
+    for over, st in ((dict(dy=None), NULL), (dict(dx=None), NULL), (dict(stats=None), NULL), (dict(dgamma=None), NULL), (dict(gamma=None), NULL),
+                     (dict(x=None), NULL), (dict(x=None, codes=P), NULL), (dict(codes=P, scales=P), NULL), (dict(dtype=5), DTYPE),
+                     (dict(packed, format=7), DTYPE), (dict(H=0), SHAPE), (dict(H=16385), SHAPE), (dict(lddy=511), SHAPE), (dict(lddx=511), SHAPE),
+                     (dict(ldx=511), SHAPE), (dict(dy=P + 1), SHAPE), (dict(packed, codes=P + 4), SHAPE), (dict(dgamma=P + 4), SHAPE), (dict(dbeta=P + 4), SHAPE),
+                     (dict(workspace=None), WORKSPACE), (dict(workspace=P + 16), WORKSPACE), (dict(workspace_bytes=need - 1), WORKSPACE)):
+        assert b(**over) == st, over
+
+
+def test_packing_refusals(lib):
+    pack = _caller(lib.rl_f8_pack, x=P, ldx=64, dtype=1, R=0, K=64, format=0, codes=P, scales=P, stream=None)
+    unpack = _caller(lib.rl_f8_unpack, codes=P, scales=P, format=0, R=0, K=64, x=P, ldx=64, dtype=1, stream=None)
+    for f in (pack, unpack):
+        assert f() == OK
+        for over, st in ((dict(R=1, x=None), NULL), (dict(R=1, codes=None), NULL), (dict(R=1, scales=None), NULL), (dict(dtype=3), DTYPE), (dict(format=-1), DTYPE),
+                         (dict(K=0), SHAPE), (dict(K=(1 << 22) + 1, ldx=1 << 30), SHAPE), (dict(ldx=63), SHAPE), (dict(R=-2), SHAPE), (dict(x=P + 1), SHAPE),
+                         (dict(codes=P + 8), SHAPE), (dict(scales=P + 2), SHAPE)):
+            assert f(**over) == st, over
+    w = _caller(lib.rl_f8_pack_weight, w=P, ldw=64, dtype=0, N=8, K=64, format=0, codes=P, scales=P, codes_t=P, scales_t=P, stream=None)
+    for over, st in ((dict(w=None), NULL), (dict(codes=None), NULL), (dict(codes_t=None), NULL), (dict(scales_t=None), NULL), (dict(dtype=2), DTYPE),
+                     (dict(format=2), DTYPE), (dict(N=0), SHAPE), (dict(K=0), SHAPE), (dict(ldw=63), SHAPE), (dict(w=P + 2), SHAPE), (dict(codes_t=P + 1), SHAPE)):
+        assert w(**over) == st, over
+
+
+def test_product_refusals(lib):
+    n = C.c_size_t(0)
+    assert lib.rl_f8_matmul_workspace_bytes(0, 8, 8, C.byref(n)) == OK and n.value == 0
+    assert lib.rl_f8_matmul_workspace_bytes(100, 64, 8192, C.byref(n)) == OK
+    need = n.value
+    for M, N, K in ((-1, 8, 8), (8, 0, 8), (8, 8, 0), (1 << 31, 8, 8), (8, (1 << 22) + 1, 8), (8, 8, (1 << 22) + 1), (1 << 30, 1 << 22, 8)):
+        assert lib.rl_f8_matmul_workspace_bytes(M, N, K, C.byref(n)) == SHAPE, (M, N, K)
+    assert lib.rl_f8_matmul_workspace_bytes(8, 8, 8, None) == NULL
+    mm = _caller(lib.rl_f8_matmul, x_codes=P, x_scales=P, x_format=0, w_codes=P, w_scales=P, w_format=1, M=0, N=64, K=8192, y=P, ldy=64, dtype=1,
+                 workspace=P, workspace_bytes=need, stream=None)
+    assert mm() == OK and mm(x_codes=None, y=None) == OK
+    common = ((dict(w_codes=None), NULL), (dict(w_scales=None), NULL), (dict(M=100, x_codes=None), NULL), (dict(M=100, x_scales=None), NULL),
+              (dict(M=100, y=None), NULL), (dict(dtype=4), DTYPE), (dict(x_format=2), DTYPE), (dict(w_format=2), DTYPE), (dict(N=0), SHAPE), (dict(K=-1), SHAPE),
+              (dict(ldy=63), SHAPE), (dict(y=P + 1), SHAPE), (dict(w_codes=P + 8), SHAPE), (dict(x_scales=P + 8), SHAPE))
+    for over, st in common + (((dict(M=100, workspace=None), WORKSPACE), (dict(M=100, workspace_bytes=need - 1), WORKSPACE)) if need else ()):
+        assert mm(**over) == st, over
+    lin = _caller(lib.rl_f8_linear_forward, x=P, ldx=8192, dtype=1, M=0, K=8192, x_format=0, w_codes=P, w_scales=P, w_format=0, N=64, y=P, ldy=64, x_codes=P,
+                  x_scales=P, workspace=P, workspace_bytes=need, stream=None)
+    assert lin() == OK
+    for over, st in ((dict(M=100, x=None), NULL), (dict(x_codes=None), NULL), (dict(M=17, x_codes=None, x_scales=None), NULL), (dict(w_codes=None), NULL),
+                     (dict(dtype=4), DTYPE), (dict(x_format=2), DTYPE), (dict(ldx=8191), SHAPE), (dict(ldy=63), SHAPE), (dict(x=P + 1), SHAPE), (dict(w_scales=P + 1), SHAPE)):
+        assert lin(**over) == st, over
+    assert lib.rl_f8_linear_backward_workspace_bytes(100, 64, 256, 0, C.byref(n)) == OK and n.value % 256 == 0
+    need = n.value
+    assert lib.rl_f8_linear_backward_workspace_bytes(100, 64, 256, 1, C.byref(n)) == OK and n.value < need          # bf16 dy needs one term, f32 three
+    assert lib.rl_f8_linear_backward_workspace_bytes(100, 64, 256, 2, C.byref(n)) == DTYPE
+    assert lib.rl_f8_linear_backward_workspace_bytes(-1, 64, 256, 1, C.byref(n)) == SHAPE
+    assert lib.rl_f8_linear_backward_workspace_bytes(1, 64, 256, 1, None) == NULL
+    bw = _caller(lib.rl_f8_linear_backward, dy=P, lddy=64, dtype=0, M=100, N=64, K=256, dy_format=1, x_codes=P, x_scales=P, x_format=0, wt_codes=P, wt_scales=P,
+                 w_format=0, dx=P, lddx=256, dW=P, lddw=256, accumulate=0, workspace=P, workspace_bytes=need, stream=None)
+    for over, st in ((dict(dx=None, dW=None), NULL), (dict(dy=None), NULL), (dict(wt_codes=None), NULL), (dict(x_scales=None), NULL), (dict(dtype=2), DTYPE),
+                     (dict(dy_format=2), DTYPE), (dict(x_format=2), DTYPE), (dict(w_format=-1), DTYPE), (dict(N=0), SHAPE), (dict(K=0), SHAPE), (dict(lddy=63), SHAPE),
+                     (dict(lddx=255), SHAPE), (dict(lddw=255), SHAPE), (dict(dW=P + 2), SHAPE), (dict(x_codes=P + 8), SHAPE), (dict(workspace=None), WORKSPACE),
+                     (dict(workspace=P + 128), WORKSPACE), (dict(workspace_bytes=need - 1), WORKSPACE)):
+        assert bw(**over) == st, over
+
+
+def test_binding_refuses_what_the_library_cannot_see():
+    x = torch.zeros(4, 8)
+    with pytest.raises(ValueError, match="GPU"):
+        binding.rl_f8_pack(x)
+    with pytest.raises(ValueError, match="GPU"):
+        binding.rl_layer_norm_forward(x, torch.ones(8))
+
+
+@pytest.mark.parametrize("fmt, t", [("e4m3", torch.float8_e4m3fn), ("e5m2", torch.float8_e5m2)])
+def test_oracle_values_and_rounding_are_those_of_the_format(fmt, t):
+    v = orc.values(fmt)
+    assert np.array_equal(torch.arange(len(v), dtype=torch.uint8).view(t).double().numpy(), v)
+    x = np.concatenate([v, (v[1:] + v[:-1]) / 2, np.random.default_rng(1).uniform(0, v[-1], 5000)])         # values, ties, anything between
+    x = np.concatenate([x, -x]).astype(np.float32).astype(np.float64)
+    got, e = orc.round_block(x, fmt)
+    assert e == 0 and np.array_equal(got, torch.from_numpy(x).float().to(t).double().numpy())
+
+
+@pytest.mark.parametrize("fmt", ["e4m3", "e5m2"])
+def test_oracle_scale_is_the_smallest_that_holds_the_block(fmt):
+    top = orc.values(fmt)[-1]
+    for a in (1.0, top, np.nextafter(top, 0), np.nextafter(top, 1e9), top * 2.0 ** 20, 1e-3, 3.4e38, 1e-30):
+        e = orc.scale_exponent(a, fmt)
+        assert a <= top * 2.0 ** e and a > top * 2.0 ** (e - 1)
+    assert orc.scale_exponent(0.0, fmt) == 0
+
+
+def test_oracle_norm_gradients_against_differences():
+    rng = np.random.default_rng(3)
+    x, dy, gamma, beta = rng.normal(size=(3, 9)), rng.normal(size=(3, 9)), rng.normal(size=9), rng.normal(size=9)
+    _, mean, rstd = orc.norm_forward(x, gamma, beta, 1e-3)
+    dx, dg, db = orc.norm_backward(dy, x, mean, rstd, gamma)
+    loss = lambda x, g, b: (dy * orc.norm_forward(x, g, b, 1e-3)[0]).sum()
+    h = 1e-6
+
+    def diff(a, f):
+        out = np.empty_like(a)
+        for i in np.ndindex(a.shape):
+            up, dn = a.copy(), a.copy()
+            up[i] += h
+            dn[i] -= h
+            out[i] = (f(up) - f(dn)) / (2 * h)
+        return out
+    assert np.allclose(dx, diff(x, lambda a: loss(a, gamma, beta)), atol=1e-7)
+    assert np.allclose(dg, diff(gamma, lambda a: loss(x, a, beta)), atol=1e-7)
+    assert np.allclose(db, diff(beta, lambda a: loss(x, gamma, a)), atol=1e-7)
