@@ -214,7 +214,8 @@ def _workspace(nbytes: int, device) -> torch.Tensor:
 
 
 def _stream_handle() -> int:
-    return torch.cuda.current_stream().cuda_stream
+    """The current stream of the current device (torch.cuda.current_stream().cuda_stream, without the stream object: 0.3 us instead of 2.8)."""
+    return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
 
 
 def rl_token_logprob(hidden, weight, token_ids, mask, cu_seqlens=None, workspace=None):
@@ -469,8 +470,10 @@ def _rows(t: torch.Tensor, name: str):
         raise ValueError(f"{name} must live on the GPU")
     if t.dim() != 2 or (t.stride(1) != 1 and t.shape[1] > 1):
         raise ValueError(f"{name} must be [rows, columns] with contiguous columns")
-    ld = t.stride(0) if t.shape[0] > 1 else t.shape[1]
-    if ld < t.shape[1]:
+    (rows, cols), (ld, _) = t.shape, t.stride()
+    if rows < 2:
+        ld = cols
+    elif ld < cols:
         raise ValueError(f"{name} must not have overlapping rows")
     return t.data_ptr(), ld, _dtype_code(t)
 
@@ -494,12 +497,31 @@ def _f8(p: F8Rows, rows: int, cols: int, name: str):
     return _ptr(p.codes, torch.uint8, name=name + ".codes"), _ptr(p.scales, torch.uint8, name=name + ".scales"), F8_FORMATS[p.fmt]
 
 
-def _f8_workspace(nbytes: int, device):
-    """(tensor to hold on to, address, bytes)"""
-    if nbytes == 0:
+def _f8_workspace(query, *args):
+    """(tensor to hold on to, address, bytes) of the workspace that a *_workspace_bytes call asks for; the last argument is the device."""
+    need = C.c_size_t(0)
+    _check(query(*args[:-1], C.byref(need)))
+    if need.value == 0:
         return None, None, 0
-    ws = _workspace(nbytes, device)
-    return ws, ws.data_ptr(), nbytes
+    ws = torch.empty(need.value, dtype=torch.uint8, device=args[-1])
+    if ws.data_ptr() % 256:
+        ws = _workspace(need.value, args[-1])
+    return ws, ws.data_ptr(), need.value
+
+
+def _like(x: torch.Tensor) -> torch.Tensor:
+    """A contiguous tensor of x's shape and dtype."""
+    return torch.empty_like(x) if x.is_contiguous() else x.new_empty(x.shape)
+
+
+def _output(out, x):
+    """(tensor, address, row stride) of a result of x's shape and dtype, in `out` if that is given."""
+    if out is None:
+        y = _like(x)
+        return y, y.data_ptr(), x.shape[1]
+    if out.shape != x.shape or out.dtype != x.dtype:
+        raise ValueError("out must have the shape and dtype of the input")
+    return (out,) + _rows(out, "out")[:2]
 
 
 def rl_layer_norm_forward(x, gamma, beta=None, eps=1e-5, checkpoint=None, out=None):
@@ -510,11 +532,8 @@ def rl_layer_norm_forward(x, gamma, beta=None, eps=1e-5, checkpoint=None, out=No
     px, ldx, dt = _rows(x, "x")
     if beta is not None and beta.dtype != gamma.dtype:
         raise ValueError("gamma and beta must have one dtype")
-    y = torch.empty((R, H), dtype=x.dtype, device=x.device) if out is None else out
-    if y.shape != x.shape or y.dtype != x.dtype:
-        raise ValueError("out must have the shape and dtype of x")
-    py, ldy, _ = _rows(y, "out")
-    stats = torch.empty((R, 2), dtype=torch.float32, device=x.device)
+    y, py, ldy = _output(out, x)
+    stats = x.new_empty((R, 2), dtype=torch.float32)
     kept = None if checkpoint is None else _f8_empty(R, H, checkpoint, x.device)
     codes, scales, fmt = (None, None, 0) if kept is None else (kept.codes.data_ptr(), kept.scales.data_ptr(), F8_FORMATS[kept.fmt])
     _check(lib().rl_layer_norm_forward(px, ldx, dt, R, H, _ptr(gamma, numel=H, name="gamma"), _ptr(beta, numel=H, name="beta"), _dtype_code(gamma), float(eps),
@@ -535,15 +554,10 @@ def rl_layer_norm_backward(dy, x, stats, gamma, want_beta=True, out=None):
         if x.shape != dy.shape or x.dtype != dy.dtype:
             raise ValueError("x must have the shape and dtype of dy")
         px, ldx, _ = _rows(x, "x")
-    dx = torch.empty((R, H), dtype=dy.dtype, device=dev) if out is None else out
-    if dx.shape != dy.shape or dx.dtype != dy.dtype:
-        raise ValueError("out must have the shape and dtype of dy")
-    pdx, lddx, _ = _rows(dx, "out")
+    dx, pdx, lddx = _output(out, dy)
     dgamma = torch.empty(H, dtype=torch.float32, device=dev)
     dbeta = torch.empty(H, dtype=torch.float32, device=dev) if want_beta else None
-    need = C.c_size_t(0)
-    _check(lib().rl_layer_norm_backward_workspace_bytes(R, H, C.byref(need)))
-    ws, pws, nws = _f8_workspace(need.value, dev)
+    ws, pws, nws = _f8_workspace(lib().rl_layer_norm_backward_workspace_bytes, R, H, dev)
     _check(lib().rl_layer_norm_backward(pdy, lddy, px, ldx, codes, scales, fmt, dt, R, H, _ptr(gamma, numel=H, name="gamma"), _dtype_code(gamma),
                                         _ptr(stats, torch.float32, 2 * R, "stats"), pdx, lddx, dgamma.data_ptr(), dbeta.data_ptr() if want_beta else None,
                                         pws, nws, _stream_handle()))
@@ -585,9 +599,7 @@ def rl_f8_matmul(a: F8Rows, b: F8Rows, dtype=torch.bfloat16):
     ca, sa, fa = _f8(a, M, K, "a")
     cb, sb, fb = _f8(b, N, K, "b")
     y = torch.empty((M, N), dtype=dtype, device=a.codes.device)
-    need = C.c_size_t(0)
-    _check(lib().rl_f8_matmul_workspace_bytes(M, N, K, C.byref(need)))
-    ws, pws, nws = _f8_workspace(need.value, y.device)
+    ws, pws, nws = _f8_workspace(lib().rl_f8_matmul_workspace_bytes, M, N, K, y.device)
     _check(lib().rl_f8_matmul(ca, sa, fa, cb, sb, fb, M, N, K, y.data_ptr(), N, _dtype_code(y), pws, nws, _stream_handle()))
     return y
 
@@ -600,9 +612,7 @@ def rl_f8_linear_forward(x, w: F8Weight, fmt="e4m3", keep=True):
     cw, sw, fw = _f8(w.rows, N, K, "w.rows")
     kept = _f8_empty(M, K, fmt, x.device) if keep or M > F8_FEW_ROWS else None
     y = torch.empty((M, N), dtype=x.dtype, device=x.device)
-    need = C.c_size_t(0)
-    _check(lib().rl_f8_matmul_workspace_bytes(M, N, K, C.byref(need)))
-    ws, pws, nws = _f8_workspace(need.value, x.device)
+    ws, pws, nws = _f8_workspace(lib().rl_f8_matmul_workspace_bytes, M, N, K, x.device)
     if fmt not in F8_FORMATS:
         raise ValueError(f"format must be one of {sorted(F8_FORMATS)}, got {fmt!r}")
     _check(lib().rl_f8_linear_forward(px, ldx, dt, M, K, F8_FORMATS[fmt], cw, sw, fw, N, y.data_ptr(), N,
@@ -629,9 +639,7 @@ def rl_f8_linear_backward(dy, kept: F8Rows, w: F8Weight, fmt="e5m2", want_dx=Tru
     if want_dw and (dw.shape != (N, K) or dw.dtype != torch.float32):
         raise ValueError(f"dw must be float32 [{N}, {K}]")
     pdw, lddw, _ = _rows(dw, "dw") if want_dw else (None, K, 0)
-    need = C.c_size_t(0)
-    _check(lib().rl_f8_linear_backward_workspace_bytes(M, N, K, dt, C.byref(need)))
-    ws, pws, nws = _f8_workspace(need.value, dev)
+    ws, pws, nws = _f8_workspace(lib().rl_f8_linear_backward_workspace_bytes, M, N, K, dt, dev)
     _check(lib().rl_f8_linear_backward(pdy, lddy, dt, M, N, K, F8_FORMATS[fmt], cx, sx, fx, ct, st, fw, dx.data_ptr() if want_dx else None, K,
                                        pdw, lddw, 1 if accumulate else 0, pws, nws, _stream_handle()))
     return dx, dw if want_dw else None

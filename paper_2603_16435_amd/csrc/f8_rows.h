@@ -33,21 +33,26 @@ template <class T> __device__ __attribute__((always_inline)) inline Raw8<T> raw_
   if constexpr (sizeof(T) == 4) r.w = r.v;
   return r;
 }
+template <class T> __device__ __attribute__((always_inline)) inline Raw8<T> raw_load8(const T* p) {
+  Raw8<T> r;
+  r.v = *reinterpret_cast<const u32x4_el2*>(p);
+  if constexpr (sizeof(T) == 4) r.w = *reinterpret_cast<const u32x4_el2*>(p + 4);
+  return r;
+}
+template <class T> __device__ __attribute__((always_inline)) inline Raw8<T> raw_load_part(const T* p, int n) {       // the first n of 8
+  Raw8<T> r = raw_zero<T>();
+#pragma unroll
+  for (int i = 0; i < 7; ++i)
+    if (i < n) {
+      if constexpr (sizeof(T) == 4) { (i < 4 ? r.v : r.w)[i & 3] = __float_as_uint(p[i]); }
+      else r.v[i >> 1] |= (unsigned)reinterpret_cast<const uint16_t*>(p)[i] << ((i & 1) * 16);
+    }
+  return r;
+}
 // `left`: values that the row still has from p on (8 or more: all of them, none: zeros)
 template <class T> __device__ __attribute__((always_inline)) inline Raw8<T> raw_load(const T* p, int left) {
-  Raw8<T> r = raw_zero<T>();
-  if (left >= 8) {
-    r.v = *reinterpret_cast<const u32x4_el2*>(p);
-    if constexpr (sizeof(T) == 4) r.w = *reinterpret_cast<const u32x4_el2*>(p + 4);
-  } else if (left > 0) {
-#pragma unroll
-    for (int i = 0; i < 8; ++i)
-      if (i < left) {
-        if constexpr (sizeof(T) == 4) { (i < 4 ? r.v : r.w)[i & 3] = __float_as_uint(p[i]); }
-        else r.v[i >> 1] |= (unsigned)reinterpret_cast<const uint16_t*>(p)[i] << ((i & 1) * 16);
-      }
-  }
-  return r;
+  if (left >= 8) return raw_load8(p);
+  return left > 0 ? raw_load_part(p, left) : raw_zero<T>();
 }
 template <class T> __device__ __attribute__((always_inline)) inline float raw_get(const Raw8<T>& r, int i) {
   if constexpr (sizeof(T) == 4) return __uint_as_float((i < 4 ? r.v : r.w)[i & 3]);
@@ -68,18 +73,21 @@ template <class T> __device__ __attribute__((always_inline)) inline Raw8<T> raw_
   }
   return r;
 }
-template <class T> __device__ __attribute__((always_inline)) inline void raw_store(T* p, int left, const Raw8<T>& r) {
-  if (left >= 8) {
-    *reinterpret_cast<u32x4_el2*>(p) = r.v;
-    if constexpr (sizeof(T) == 4) *reinterpret_cast<u32x4_el2*>(p + 4) = r.w;
-  } else if (left > 0) {
+template <class T> __device__ __attribute__((always_inline)) inline void raw_store8(T* p, const Raw8<T>& r) {
+  *reinterpret_cast<u32x4_el2*>(p) = r.v;
+  if constexpr (sizeof(T) == 4) *reinterpret_cast<u32x4_el2*>(p + 4) = r.w;
+}
+template <class T> __device__ __attribute__((always_inline)) inline void raw_store_part(T* p, int n, const Raw8<T>& r) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i)
-      if (i < left) {
-        if constexpr (sizeof(T) == 4) p[i] = __uint_as_float((i < 4 ? r.v : r.w)[i & 3]);
-        else reinterpret_cast<uint16_t*>(p)[i] = (uint16_t)(r.v[i >> 1] >> ((i & 1) * 16));
-      }
-  }
+  for (int i = 0; i < 7; ++i)
+    if (i < n) {
+      if constexpr (sizeof(T) == 4) p[i] = __uint_as_float((i < 4 ? r.v : r.w)[i & 3]);
+      else reinterpret_cast<uint16_t*>(p)[i] = (uint16_t)(r.v[i >> 1] >> ((i & 1) * 16));
+    }
+}
+template <class T> __device__ __attribute__((always_inline)) inline void raw_store(T* p, int left, const Raw8<T>& r) {
+  if (left >= 8) raw_store8(p, r);
+  else if (left > 0) raw_store_part(p, left, r);
 }
 
 // ------------------------------------------------------------------ codes

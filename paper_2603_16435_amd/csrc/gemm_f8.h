@@ -191,6 +191,174 @@ __global__ __launch_bounds__(256) void f8_slices_kernel(const float* part, int s
   }
 }
 
+// ------------------------------------------------------------------ hot kernel
+// 256 x 256 tile, four wavefronts of 128 x 128 (256 accumulators a lane, in AGPRs), y in bf16.  A slab's 64 MFMAs of 32 cycles are as long as those of a slab of the bf16
+// hot kernel (gemm_nt.h), on the same bytes, so it is built like that one: slabs go straight into two LDS stages, every MFMA is fenced, fragment reads, slab
+// loads and one L2 prefetch are dealt out between them.  A slab is two phases: all eight blocks of x against blocks 0..3 of w, then against 4..7.  The
+// workgroup meets between them, when the last fragments of the slab have been read: the second phase runs from registers, covers the first fragment reads of the next slab (an
+// x block is fetched as soon as the last MFMA that reads its registers is out) and the first loads of the slab after it.
+// Scales: one word a row holds four slabs' bytes; shifted by a byte a slab, and fetched a group ahead.
+// LDS row 16 b + 4 g + e of w holds column 32 (b / 2) + 8 g + 4 (b % 2) + e of the tile's half (perm_row), so that a lane ends up with eight consecutive columns in a pair of
+// blocks: 16-byte stores.
+template <int FX, int FW> __device__ __attribute__((always_inline)) inline void mfma_f8_acc(floatx4& acc, const i32x8_t& w, const i32x8_t& x, unsigned sw, unsigned sx) {
+  asm volatile("v_mfma_scale_f32_16x16x128_f8f6f4 %0, %1, %2, %0, %3, %4 op_sel_hi:[0,0,0] cbsz:%5 blgp:%6"
+               : "+a"(acc) : "v"(w), "v"(x), "v"(sw), "v"(sx), "n"(FW), "n"(FX));
+}
+
+struct F8Hot { F8Operand x, w; bf16_t* y; int64_t ldy; int M, N, nk; };
+constexpr int kF8Band = 8;
+
+template <int FX, int FW>
+__global__ __launch_bounds__(256) void f8_hot_kernel(F8Hot j) {
+  __shared__ __attribute__((aligned(1024))) unsigned char stage0[kHotStageBytes];
+  __shared__ __attribute__((aligned(1024))) unsigned char stage1[kHotStageBytes];
+  constexpr int A_BYTES = 256 * kSlabBytes;
+  const int tiles_m = (j.M + 255) / 256, tiles_n = (j.N + 255) / 256;
+  int tm, tn;
+  if (!tile_of_block(blockIdx.x, tiles_m, tiles_n, kF8Band, false, tm, tn)) return;
+  tm = __builtin_amdgcn_readfirstlane(tm); tn = __builtin_amdgcn_readfirstlane(tn);
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wm = wave >> 1, wn = wave & 1;
+  const int nk = j.nk;
+
+  // slab loads: wavefront w fills rows [64 w, 64 w + 64) of x and of w, eight rows a load; the tile's rows are within 32 bits of its first
+  const uint8_t* xbase = uniform_ptr(j.x.codes + (int64_t)tm * 256 * j.x.Kp);
+  const uint8_t* wbase = uniform_ptr(j.w.codes + (int64_t)tn * 256 * j.w.Kp);
+  unsigned xoff[8], woff[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const int lr = wave * 64 + i * 8 + (lane >> 3), c = (lane & 7) ^ ((lr >> 1) & 7);
+    int m = lr, n = perm_lds_row_a(lr);
+    m = tm * 256 + m < j.M ? m : j.M - 1 - tm * 256; n = tn * 256 + n < j.N ? n : j.N - 1 - tn * 256;
+    xoff[i] = (unsigned)m * (unsigned)j.x.Kp + c * 16; woff[i] = (unsigned)n * (unsigned)j.w.Kp + c * 16;
+  }
+  auto issue = [&](int slab, unsigned char* stage, int i) __attribute__((always_inline)) {
+    unsigned char* dst = stage + wave * 64 * kSlabBytes + (i & 7) * 8 * kSlabBytes + (i < 8 ? 0 : A_BYTES);
+    if (i < 8) load16_to_lds_uniform(xbase + (int64_t)slab * 128, xoff[i & 7], dst);
+    else load16_to_lds_uniform(wbase + (int64_t)slab * 128, woff[i & 7], dst);
+  };
+  const int frow = lane & 15, g = lane >> 4;
+  const unsigned *xs[8], *ws[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    int m = tm * 256 + wm * 128 + i * 16 + frow, n = tn * 256 + wn * 128 + perm_row(i, frow >> 2, frow & 3);
+    m = m < j.M ? m : j.M - 1; n = n < j.N ? n : j.N - 1;
+    xs[i] = reinterpret_cast<const unsigned*>(j.x.scales + (int64_t)m * j.x.Ks);
+    ws[i] = reinterpret_cast<const unsigned*>(j.w.scales + (int64_t)n * j.w.Ks);
+  }
+  const int groups = (nk + 3) / 4;
+  unsigned sx[8], sw[8], nx[8], nw[8];
+  auto fetch_scales = [&](int group) __attribute__((always_inline)) {
+    group = group < groups ? group : groups - 1;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) { nx[i] = xs[i][group]; nw[i] = ws[i][group]; }
+  };
+  // L2 prefetch two slabs ahead, a quarter of the tile's x rows by one wavefront, an eighth of its w rows by another: the workgroups that an XCD runs at a time share
+  // the panels (as in gemm_nt.h)
+  const uint8_t* pf_ptr;
+  int pf_stride = 128;
+  if (wave == 0) {
+    int m = tm * 256 + 64 * (tn & 3) + lane; m = m < j.M ? m : j.M - 1;
+    pf_ptr = j.x.codes + (int64_t)m * j.x.Kp;
+  } else if (wave == 1) {
+    int n = tn * 256 + 32 * (tm & 7) + (lane & 31); n = n < j.N ? n : j.N - 1;
+    pf_ptr = j.w.codes + (int64_t)n * j.w.Kp;
+  } else { pf_ptr = j.x.codes; pf_stride = 0; }
+  unsigned pf0 = 0, pf1 = 0, pf_sink = 0;
+  auto prefetch = [&](unsigned& slot, int kt) __attribute__((always_inline)) {
+    pf_sink ^= slot;
+    const int k = kt + 3 < nk ? kt + 3 : nk - 1;
+    typedef const __attribute__((address_space(1))) unsigned* line_ptr;
+    line_ptr p = (line_ptr)(pf_ptr + (int64_t)k * pf_stride);
+    asm volatile("" : "+v"(p));
+    slot = *p;
+    asm volatile("" ::: "memory");
+  };
+
+  floatx4 acc[8][8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i)
+#pragma unroll
+    for (int b = 0; b < 8; ++b) acc[i][b] = floatx4{0.f, 0.f, 0.f, 0.f};
+  i32x8_t fx[8], fw[2][4];
+  const int xrow = (wm * 128 + frow) * kSlabBytes, wrow = A_BYTES + (wn * 128 + frow) * kSlabBytes, swz = (frow >> 1) & 7;
+  const int slot0 = (g ^ swz) << 4, slot1 = ((g + 4) ^ swz) << 4;
+  auto read = [&](const unsigned char* p) __attribute__((always_inline)) {
+    const i32x4_t lo = *reinterpret_cast<const i32x4_t*>(p + slot0), hi = *reinterpret_cast<const i32x4_t*>(p + slot1);
+    return (i32x8_t)__builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+  };
+  // Slab kt is in `cur`; fx and fw[0] hold its x blocks and w blocks 0..3, loads 0..7 of slab kt + 1 are on their way to `nxt`.
+  auto slab = [&](unsigned char* cur, unsigned char* nxt, int kt, unsigned& pfslot) __attribute__((always_inline)) {
+    if ((kt & 3) == 0) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) { sx[i] = nx[i]; sw[i] = nw[i]; }
+    }
+    const int k1 = kt + 1 < nk ? kt + 1 : nk - 1, k2 = kt + 2 < nk ? kt + 2 : nk - 1;
+#pragma unroll
+    for (int q = 0; q < 32; ++q) {
+      const int i = q >> 2, b = i & 1 ? 3 - (q & 3) : q & 3;
+      mfma_f8_acc<FX, FW>(acc[i][b], fw[0][b], fx[i], sw[b], sx[i]);
+      if (q % 2 == 0 && q < 8) fw[1][q / 2] = read(cur + wrow + (4 + q / 2) * 16 * kSlabBytes);
+      if (q % 3 == 1 && q < 24) issue(k1, nxt, 8 + q / 3);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    if ((kt & 3) == 1) fetch_scales((kt >> 2) + 1);
+    prefetch(pfslot, kt);
+    __builtin_amdgcn_s_waitcnt(0x0071);       // all but the prefetch; own fragment reads
+    __syncthreads();
+#pragma unroll
+    for (int q = 0; q < 32; ++q) {
+      const int i = q >> 2, b = i & 1 ? 3 - (q & 3) : q & 3;
+      mfma_f8_acc<FX, FW>(acc[i][4 + b], fw[1][b], fx[i], sw[4 + b], sx[i]);
+      if ((q & 3) == 3) fx[i] = read(nxt + xrow + i * 16 * kSlabBytes);
+      else if (q % 8 == 1) fw[0][q / 8] = read(nxt + wrow + (q / 8) * 16 * kSlabBytes);
+      if (q % 4 == 2) issue(k2, cur, q / 4);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) { sx[i] >>= 8; sw[i] >>= 8; }
+  };
+
+#pragma unroll
+  for (int i = 0; i < 16; ++i) issue(0, stage0, i);
+  fetch_scales(0);
+#pragma unroll
+  for (int i = 0; i < 8; ++i)
+#pragma unroll
+    for (int b = 0; b < 8; ++b) asm volatile("" : "+a"(acc[i][b]));
+  __builtin_amdgcn_s_waitcnt(0x0F70);
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < 8; ++i) issue(nk > 1 ? 1 : 0, stage1, i);
+#pragma unroll
+  for (int i = 0; i < 8; ++i) fx[i] = read(stage0 + xrow + i * 16 * kSlabBytes);
+#pragma unroll
+  for (int b = 0; b < 4; ++b) fw[0][b] = read(stage0 + wrow + b * 16 * kSlabBytes);
+  int kt = 0;
+  for (; kt + 1 < nk; kt += 2) {
+    slab(stage0, stage1, kt, pf0);
+    slab(stage1, stage0, kt + 1, pf1);
+  }
+  if (kt < nk) slab(stage0, stage1, kt, pf0);
+  __builtin_amdgcn_s_waitcnt(0x0070);         // the loads past the end
+  mfma_drain();
+
+  const bool edge = tm * 256 + 256 > j.M || tn * 256 + 256 > j.N;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const int m = tm * 256 + wm * 128 + i * 16 + frow;
+    if (edge && m >= j.M) continue;
+#pragma unroll
+    for (int b = 0; b < 8; b += 2) {
+      const int n = tn * 256 + wn * 128 + b * 16 + g * 8;
+      float v[8];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) { v[e] = acc_read<true>(acc[i][b], e); v[4 + e] = acc_read<true>(acc[i][b + 1], e); }
+      raw_store(j.y + (int64_t)m * j.ldy + n, edge ? j.N - n : 8, raw_make<bf16_t>(v));
+    }
+  }
+  if ((pf_sink ^ pf0 ^ pf1) == 0x9E3779B9u && nk < 0) j.y[0] = (bf16_t)0.f;        // never true: keeps the prefetch loads
+}
+
 // ------------------------------------------------------------------ few rows
 constexpr int kF8FewRows = 16, kF8FewWaves = 8;
 

@@ -4,12 +4,14 @@
 //   g = dy gamma,  dx = rstd (g - mean(g) - xh mean(g xh)),  dgamma = sum_rows dy xh,  dbeta = sum_rows dy
 //
 // Bound by HBM: forward x and y, backward x (or its codes), dy and dx, each once.  A row is held by a team of TW wavefronts, in registers, eight
-// consecutive values a lane and CH such pieces a lane, so that mean and variance are taken one after the other (no sum of squares whose difference would
-// cancel) without a second read.  Statistics and sums are f32.
+// consecutive values a lane and CH such pieces a lane (two at most: four made registers of 300, and 5120 columns ran at 3.9 TB/s); a team walks rows far apart with the
+// parameters of its columns in registers.  Sums are f32.  (Two or four rows at a time: no faster, fewer wavefronts fit a CU.)
 //
-// Backward: a team walks rows far apart and keeps its columns' sums of dgamma and dbeta in registers the whole way; ROWS rows at a time, so that their
-// loads are all in flight and one exchange between the wavefronts serves them all.  Each team's sums go to the workspace and ln_sum_kernel adds
-// the teams' in order (no atomics: same bits every run).
+// Mean and variance: a wavefront's own values give its sum and the sum of squares about its own mean, which are joined exactly
+// (sum_w [q_w + n_w (mean_w - mean)^2]): no difference of large sums, and one exchange instead of two.
+//
+// Backward: a team keeps its columns' sums of dgamma and dbeta in registers the whole way; they go to the workspace and ln_sum_kernel adds the teams' in
+// order (no atomics: same bits every run).  Few rows: one launch, in which further workgroups form those sums column by column out of a second read of x and dy.
 #pragma once
 #include "f8_rows.h"
 
@@ -27,85 +29,149 @@ __device__ __attribute__((always_inline)) inline float wave_sum(float x) {
   return __uint_as_float((unsigned)__builtin_amdgcn_readlane((int)__float_as_uint(x), 63));
 }
 
-struct NormParams { const void* gamma; const void* beta; int bf16; };
-// eight parameters from column `col` on, zeros past the end
-__device__ __attribute__((always_inline)) inline void norm_params(const void* p, int bf16, int col, int H, float (&v)[8]) {
-  if (bf16) {
-    const Raw8<bf16_t> r = raw_load((const bf16_t*)p + col, H - col);
-#pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = raw_get(r, i);
-  } else {
-    const Raw8<float> r = raw_load((const float*)p + col, H - col);
-#pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = raw_get(r, i);
+// Which columns of a row a lane holds: pieces of eight from c0 + c * TW * 512 on.  Where H is no multiple of eight, one lane of one wavefront has a piece
+// that is not whole; it is loaded and stored by element, apart from the others.
+template <int TW, int CH> struct Pieces {
+  int c0, H, part;                   // part: columns of the lane's piece that is not whole, 0 if it has none
+  int part_c;                        // that piece
+  __device__ Pieces(int w, int lane, int H_) : c0((w * 64 + lane) * 8), H(H_) {
+    const int p = H / 8;
+    part_c = p / (TW * 64);
+    part = p % (TW * 64) == w * 64 + lane ? H % 8 : 0;
   }
-}
+  __device__ __attribute__((always_inline)) int col(int c) const { return c0 + c * TW * 512; }
+  __device__ __attribute__((always_inline)) bool whole(int c) const { return col(c) + 8 <= H; }
+  template <class T> __device__ __attribute__((always_inline)) void load(const T* row, bool there, Raw8<T> (&r)[CH]) const {
+#pragma unroll
+    for (int c = 0; c < CH; ++c) {
+      r[c] = raw_zero<T>();
+      if (there && whole(c)) r[c] = raw_load8(row + col(c));
+    }
+    if (there && part) {
+      const Raw8<T> t = raw_load_part(row + col(part_c), part);
+#pragma unroll
+      for (int c = 0; c < CH; ++c) if (c == part_c) r[c] = t;
+    }
+  }
+  template <class T> __device__ __attribute__((always_inline)) void store(T* row, const Raw8<T> (&r)[CH]) const {
+#pragma unroll
+    for (int c = 0; c < CH; ++c) if (whole(c)) raw_store8(row + col(c), r[c]);
+    if (part) {
+      Raw8<T> t = r[0];
+#pragma unroll
+      for (int c = 1; c < CH; ++c) if (c == part_c) t = r[c];
+      raw_store_part(row + col(part_c), part, t);
+    }
+  }
+  // parameters of the lane's columns, zeros past the end
+  __device__ __attribute__((always_inline)) void params(const void* p, int bf16, float (&v)[CH][8]) const {
+    if (bf16) {
+      Raw8<bf16_t> r[CH];
+      load((const bf16_t*)p, p != nullptr, r);
+#pragma unroll
+      for (int c = 0; c < CH; ++c)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[c][e] = raw_get(r[c], e);
+    } else {
+      Raw8<float> r[CH];
+      load((const float*)p, p != nullptr, r);
+#pragma unroll
+      for (int c = 0; c < CH; ++c)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[c][e] = raw_get(r[c], e);
+    }
+  }
+};
 
+constexpr int norm_threads(int tw) { return tw > 4 ? tw * 64 : 256; }
+
+struct NormParams { const void* gamma; const void* beta; int bf16; };
 template <class T> struct NormFwd {
   const T* x; T* y; int64_t R, ldx, ldy; int H; float eps;
   NormParams p; float2* stats; F8Out ckpt;
 };
 
 template <class T, int TW, int CH>
-__global__ __launch_bounds__(TW > 4 ? TW * 64 : 256) void ln_forward_kernel(NormFwd<T> j) {
-  constexpr int NT = TW > 4 ? TW * 64 : 256, TEAMS = NT / (TW * 64);
-  __shared__ float red[2][TW > 1 ? TW : 1];
+__global__ __launch_bounds__(norm_threads(TW)) void ln_forward_kernel(NormFwd<T> j) {
+  constexpr int TEAMS = norm_threads(TW) / (TW * 64);
+  __shared__ float2 red[2][TW];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int w = wave % TW, team = wave / TW;
-  const int c0 = (w * 64 + lane) * 8;
+  const int w = wave % TW, team = blockIdx.x * TEAMS + wave / TW, teams = gridDim.x * TEAMS;
+  const Pieces<TW, CH> at(w, lane, j.H);
   const float inv_h = 1.f / (float)j.H;
-  auto team_sum = [&](float s, int slot) __attribute__((always_inline)) {
-    s = wave_sum(s);
-    if constexpr (TW > 1) {
-      if (lane == 0) red[slot][w] = s;
-      __syncthreads();
-      s = red[slot][0];
+  // columns that wavefront i of the team holds: of every run of TW * 512 its 512
+  auto columns = [&](int i) __attribute__((always_inline)) {
+    int n = 0;
 #pragma unroll
-      for (int i = 1; i < TW; ++i) s += red[slot][i];
-    }
-    return s;
+    for (int c = 0; c < CH; ++c) { const int left = j.H - (c * TW + i) * 512; n += left < 0 ? 0 : left < 512 ? left : 512; }
+    return n;
   };
-  for (int64_t row = (int64_t)blockIdx.x * TEAMS + team; row < j.R; row += (int64_t)gridDim.x * TEAMS) {
+  const int mine = columns(w);
+  const float inv_mine = mine > 0 ? 1.f / (float)mine : 0.f;
+  float gamma[CH][8], beta[CH][8];
+  at.params(j.p.gamma, j.p.bf16, gamma);
+  at.params(j.p.beta, j.p.bf16, beta);
+  int flip = 0;
+  for (int64_t row = team; row < j.R; row += teams) {
     Raw8<T> r[CH];
-#pragma unroll
-    for (int c = 0; c < CH; ++c) r[c] = raw_load(j.x + row * j.ldx + c0 + c * TW * 512, j.H - c0 - c * TW * 512);
-    float s = 0.f;
+    at.load(j.x + row * j.ldx, true, r);
+    float a = 0.f;
 #pragma unroll
     for (int c = 0; c < CH; ++c)
 #pragma unroll
-      for (int e = 0; e < 8; ++e) s += raw_get(r[c], e);
-    const float mean = team_sum(s, 0) * inv_h;
-    s = 0.f;
+      for (int e = 0; e < 8; ++e) a += raw_get(r[c], e);
+    const float sum = wave_sum(a), m = sum * inv_mine;
+    a = 0.f;
 #pragma unroll
     for (int c = 0; c < CH; ++c) {
-      const int left = j.H - c0 - c * TW * 512;
+      float t = 0.f;
 #pragma unroll
-      for (int e = 0; e < 8; ++e) { const float d = raw_get(r[c], e) - mean; s += e < left ? d * d : 0.f; }
+      for (int e = 0; e < 8; ++e) { const float d = raw_get(r[c], e) - m; t += d * d; }
+      a += at.whole(c) ? t : 0.f;
     }
-    const float var = team_sum(s, 1) * inv_h;
-    const float rstd = 1.f / sqrtf(var + j.eps);
-    if (j.stats && w == 0 && lane == 0) j.stats[row] = make_float2(mean, rstd);
+    if (at.part) {
+      Raw8<T> t = r[0];
 #pragma unroll
-    for (int c = 0; c < CH; ++c) {
-      const int col = c0 + c * TW * 512, left = j.H - col;
-      float g[8], b[8], v[8];
-      norm_params(j.p.gamma, j.p.bf16, col, j.H, g);
-      if (j.p.beta) norm_params(j.p.beta, j.p.bf16, col, j.H, b);
-      else {
+      for (int c = 1; c < CH; ++c) if (c == at.part_c) t = r[c];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) b[e] = 0.f;
+      for (int e = 0; e < 7; ++e) { const float d = raw_get(t, e) - m; a += e < at.part ? d * d : 0.f; }
+    }
+    float mean = m, sq = wave_sum(a);
+    if constexpr (TW > 1) {
+      if (lane == 0) red[flip][w] = make_float2(sum, sq);
+      __syncthreads();
+      float2 p[TW];
+      float all = 0.f;
+#pragma unroll
+      for (int i = 0; i < TW; ++i) { p[i] = red[flip][i]; all += p[i].x; }
+      mean = all * inv_h; sq = 0.f;
+#pragma unroll
+      for (int i = 0; i < TW; ++i) {
+        const int n = columns(i);
+        const float d = n > 0 ? p[i].x * (1.f / (float)n) - mean : 0.f;
+        sq += p[i].y + (float)n * d * d;
       }
+      flip ^= 1;                                     // two sets: a wavefront that is ahead writes the other one
+    }
+    const float rstd = 1.f / sqrtf(sq * inv_h + j.eps);
+    if (j.stats && w == 0 && lane == 0) j.stats[row] = make_float2(mean, rstd);
+    if (j.ckpt.codes) {
 #pragma unroll
-      for (int e = 0; e < 8; ++e) v[e] = (raw_get(r[c], e) - mean) * rstd * g[e] + b[e];
-      if (j.ckpt.codes) {
+      for (int c = 0; c < CH; ++c) {
         float x[8];
 #pragma unroll
         for (int e = 0; e < 8; ++e) x[e] = raw_get(r[c], e);
-        f8_pack_wave(j.ckpt, row, col, lane, x);
+        f8_pack_wave(j.ckpt, row, at.col(c), lane, x);
       }
-      raw_store(j.y + row * j.ldy + col, left, raw_make<T>(v));
     }
-    // (the next row's first sum is in another slot than this row's last, and one barrier lies between a slot's reads and its next writes)
+#pragma unroll
+    for (int c = 0; c < CH; ++c) {
+      float v[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[e] = (raw_get(r[c], e) - mean) * rstd * gamma[c][e] + beta[c][e];
+      r[c] = raw_make<T>(v);
+    }
+    at.store(j.y + row * j.ldy, r);
   }
 }
 
@@ -114,116 +180,158 @@ template <class T> struct NormBwd {
   const uint8_t *codes, *scales; int fmt, Kp, Ks;
   NormParams p; const float2* stats;
   float* part; int Hp;            // [teams][2][Hp]: sums of dgamma and dbeta
+  float *dgamma, *dbeta; int row_blocks;          // few rows
 };
 
-template <class T, bool CK, int TW, int CH, int ROWS>
-__global__ __launch_bounds__(TW > 4 ? TW * 64 : 256) void ln_backward_kernel(NormBwd<T> j) {
-  constexpr int NT = TW > 4 ? TW * 64 : 256, TEAMS = NT / (TW * 64);
-  __shared__ float red[2][2 * ROWS][TW > 1 ? TW : 1];
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int w = wave % TW, team = blockIdx.x * TEAMS + wave / TW, teams = gridDim.x * TEAMS;
-  const int c0 = (w * 64 + lane) * 8;
+// Team `team` of `teams`.  SUMS: dgamma, dbeta of its rows to the workspace.
+template <class T, bool CK, int TW, int CH, bool SUMS>
+__device__ __attribute__((always_inline)) inline void ln_backward_rows(const NormBwd<T>& j, int team, int teams, int w, int lane, float2 (&red)[2][TW]) {
+  const Pieces<TW, CH> at(w, lane, j.H);
   const float inv_h = 1.f / (float)j.H;
-  float gamma[CH][8], dg[CH][8], db[CH][8];
+  float gamma[CH][8], dg[SUMS ? CH : 1][8], db[SUMS ? CH : 1][8];
+  at.params(j.p.gamma, j.p.bf16, gamma);
 #pragma unroll
-  for (int c = 0; c < CH; ++c) {
-    norm_params(j.p.gamma, j.p.bf16, c0 + c * TW * 512, j.H, gamma[c]);
+  for (int c = 0; c < (SUMS ? CH : 1); ++c)
 #pragma unroll
     for (int e = 0; e < 8; ++e) dg[c][e] = db[c][e] = 0.f;
-  }
   int flip = 0;
-  for (int64_t first = (int64_t)team * ROWS; first < j.R; first += (int64_t)teams * ROWS) {
-    Raw8<T> rx[CK ? 1 : ROWS][CK ? 1 : CH], ry[ROWS][CH];
-    u32x2_t code[CK ? ROWS : 1][CK ? CH : 1];
-    unsigned scale[CK ? ROWS : 1][CK ? CH : 1];
-    float2 st[ROWS];
-#pragma unroll
-    for (int q = 0; q < ROWS; ++q) {
-      const bool there = first + q < j.R;
-      const int64_t row = there ? first + q : first;
-      st[q] = j.stats[row];
+  for (int64_t row = team; row < j.R; row += teams) {
+    Raw8<T> rx[CH], ry[CH];
+    u32x2_t code[CK ? CH : 1];
+    unsigned scale[CK ? CH : 1];
+    const float2 st = j.stats[row];
+    at.load(j.dy + row * j.lddy, true, ry);
+    if constexpr (CK) {
 #pragma unroll
       for (int c = 0; c < CH; ++c) {
-        const int col = c0 + c * TW * 512, left = j.H - col;
-        ry[q][c] = raw_load(j.dy + row * j.lddy + col, there ? left : 0);
-        if constexpr (CK) {
-          code[q][c] = u32x2_t{0, 0}; scale[q][c] = 127;
-          if (col < j.Kp) {
-            code[q][c] = *reinterpret_cast<const u32x2_t*>(j.codes + row * j.Kp + col);
-            scale[q][c] = j.scales[row * j.Ks + col / kF8Block];
-          }
-        } else rx[q][c] = raw_load(j.x + row * j.ldx + col, left);
-      }
-    }
-    auto values = [&](int q, int c, float (&xh)[8]) __attribute__((always_inline)) {
-      if constexpr (CK) f8_restore8(code[q][c], scale[q][c], j.fmt, xh);
-      else {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) xh[e] = raw_get(rx[q][c], e);
-      }
-#pragma unroll
-      for (int e = 0; e < 8; ++e) xh[e] = (xh[e] - st[q].x) * st[q].y;
-    };
-    float a[ROWS], b[ROWS];                          // mean(g), mean(g xh)
-#pragma unroll
-    for (int q = 0; q < ROWS; ++q) {
-      a[q] = b[q] = 0.f;
-      if (first + q < j.R) {                         // (a row that is read in the place of one that is not there adds nothing, whatever it holds)
-#pragma unroll
-        for (int c = 0; c < CH; ++c) {
-          float xh[8];
-          values(q, c, xh);
-#pragma unroll
-          for (int e = 0; e < 8; ++e) {
-            const float d = raw_get(ry[q][c], e), g = d * gamma[c][e];
-            const float p = xh[e];
-            a[q] += g; b[q] += g * p;
-            dg[c][e] += d * p; db[c][e] += d;
-          }
+        const int col = at.col(c);
+        code[c] = u32x2_t{0, 0}; scale[c] = 127;
+        if (col < j.Kp) {
+          code[c] = *reinterpret_cast<const u32x2_t*>(j.codes + row * j.Kp + col);
+          scale[c] = j.scales[row * j.Ks + col / kF8Block];
         }
       }
-      a[q] = wave_sum(a[q]); b[q] = wave_sum(b[q]);
+    } else at.load(j.x + row * j.ldx, true, rx);
+    auto normal = [&](int c, float (&xh)[8]) __attribute__((always_inline)) {
+      if constexpr (CK) f8_restore8(code[c], scale[c], j.fmt, xh);
+      else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) xh[e] = raw_get(rx[c], e);
+      }
+#pragma unroll
+      for (int e = 0; e < 8; ++e) xh[e] = (xh[e] - st.x) * st.y;
+    };
+    float a = 0.f, b = 0.f;                          // mean(g), mean(g xh)
+#pragma unroll
+    for (int c = 0; c < CH; ++c) {
+      float xh[8];
+      normal(c, xh);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const float d = raw_get(ry[c], e), g = d * gamma[c][e];
+        a += g; b += g * xh[e];
+        if constexpr (SUMS) { dg[c][e] += d * xh[e]; db[c][e] += d; }
+      }
     }
+    a = wave_sum(a); b = wave_sum(b);
     if constexpr (TW > 1) {
-      if (lane == 0) {
-#pragma unroll
-        for (int q = 0; q < ROWS; ++q) { red[flip][2 * q][w] = a[q]; red[flip][2 * q + 1][w] = b[q]; }
-      }
+      if (lane == 0) red[flip][w] = make_float2(a, b);
       __syncthreads();
+      a = red[flip][0].x; b = red[flip][0].y;
 #pragma unroll
-      for (int q = 0; q < ROWS; ++q) {
-        a[q] = red[flip][2 * q][0]; b[q] = red[flip][2 * q + 1][0];
+      for (int i = 1; i < TW; ++i) { a += red[flip][i].x; b += red[flip][i].y; }
+      flip ^= 1;
+    }
+    const float ma = a * inv_h, mb = b * inv_h;
+    Raw8<T> out[CH];
 #pragma unroll
-        for (int i = 1; i < TW; ++i) { a[q] += red[flip][2 * q][i]; b[q] += red[flip][2 * q + 1][i]; }
+    for (int c = 0; c < CH; ++c) {
+      float xh[8], v[8];
+      normal(c, xh);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[e] = st.y * (raw_get(ry[c], e) * gamma[c][e] - ma - xh[e] * mb);
+      out[c] = raw_make<T>(v);
+    }
+    at.store(j.dx + row * j.lddx, out);
+  }
+  if constexpr (SUMS) {
+#pragma unroll
+    for (int c = 0; c < CH; ++c) {
+      const int col = at.col(c);
+      if (col >= j.Hp) continue;
+      float* p = j.part + (int64_t)team * 2 * j.Hp + col;
+#pragma unroll
+      for (int e = 0; e < 8; e += 4) {
+        *reinterpret_cast<floatx4*>(p + e) = floatx4{dg[c][e], dg[c][e + 1], dg[c][e + 2], dg[c][e + 3]};
+        *reinterpret_cast<floatx4*>(p + j.Hp + e) = floatx4{db[c][e], db[c][e + 1], db[c][e + 2], db[c][e + 3]};
       }
-      flip ^= 1;                                     // two sets: a wavefront that is ahead writes the other one
+    }
+  }
+}
+
+template <class T, bool CK, int TW, int CH>
+__global__ __launch_bounds__(norm_threads(TW)) void ln_backward_kernel(NormBwd<T> j) {
+  constexpr int TEAMS = norm_threads(TW) / (TW * 64);
+  __shared__ float2 red[2][TW];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  ln_backward_rows<T, CK, TW, CH, true>(j, blockIdx.x * TEAMS + wave / TW, gridDim.x * TEAMS, wave % TW, lane, red);
+}
+
+// dgamma, dbeta of 128 columns: sixteen lanes of eight columns, the rows dealt out among groups of such lanes.
+template <class T, bool CK, int NT>
+__device__ __attribute__((always_inline)) inline void ln_backward_columns(const NormBwd<T>& j, int block, float (&sums)[NT / 16][2][128]) {
+  constexpr int GROUPS = NT / 16, U = 4;
+  const int q = threadIdx.x & 15, grp = threadIdx.x >> 4, col = block * 128 + q * 8, left = j.H - col;
+  float dg[8], db[8];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) dg[e] = db[e] = 0.f;
+  for (int64_t r0 = grp; r0 < j.R; r0 += GROUPS * U) {
+    Raw8<T> ry[U], rx[U];
+    u32x2_t code[U];
+    unsigned scale[U];
+    float2 st[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int64_t r = r0 + u * GROUPS, row = r < j.R ? r : r0;
+      st[u] = j.stats[row];
+      ry[u] = raw_load(j.dy + row * j.lddy + col, left);
+      if constexpr (CK) { code[u] = *reinterpret_cast<const u32x2_t*>(j.codes + row * j.Kp + col); scale[u] = j.scales[row * j.Ks + block]; }
+      else rx[u] = raw_load(j.x + row * j.ldx + col, left);
     }
 #pragma unroll
-    for (int q = 0; q < ROWS; ++q) {
-      if (first + q >= j.R) break;
-      const float ma = a[q] * inv_h, mb = b[q] * inv_h;
+    for (int u = 0; u < U; ++u) {
+      if (r0 + u * GROUPS >= j.R) break;
+      float xh[8];
+      if constexpr (CK) f8_restore8(code[u], scale[u], j.fmt, xh);
 #pragma unroll
-      for (int c = 0; c < CH; ++c) {
-        const int col = c0 + c * TW * 512;
-        float xh[8], v[8];
-        values(q, c, xh);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] = st[q].y * (raw_get(ry[q][c], e) * gamma[c][e] - ma - xh[e] * mb);
-        raw_store(j.dx + (first + q) * j.lddx + col, j.H - col, raw_make<T>(v));
+      for (int e = 0; e < 8; ++e) {
+        if constexpr (!CK) xh[e] = raw_get(rx[u], e);
+        const float d = raw_get(ry[u], e);
+        dg[e] += d * ((xh[e] - st[u].x) * st[u].y); db[e] += d;
       }
     }
   }
 #pragma unroll
-  for (int c = 0; c < CH; ++c) {
-    const int col = c0 + c * TW * 512;
-    if (col >= j.Hp) continue;
-    float* p = j.part + (int64_t)team * 2 * j.Hp + col;
-#pragma unroll
-    for (int e = 0; e < 8; e += 4) {
-      *reinterpret_cast<floatx4*>(p + e) = floatx4{dg[c][e], dg[c][e + 1], dg[c][e + 2], dg[c][e + 3]};
-      *reinterpret_cast<floatx4*>(p + j.Hp + e) = floatx4{db[c][e], db[c][e + 1], db[c][e + 2], db[c][e + 3]};
-    }
+  for (int e = 0; e < 8; ++e) { sums[grp][0][q * 8 + e] = dg[e]; sums[grp][1][q * 8 + e] = db[e]; }
+  __syncthreads();
+  for (int i = threadIdx.x; i < 256; i += NT) {
+    const int k = i >> 7, h = block * 128 + (i & 127);
+    float v = sums[0][k][i & 127];
+    for (int g = 1; g < GROUPS; ++g) v += sums[g][k][i & 127];
+    float* o = k ? j.dbeta : j.dgamma;
+    if (o && h < j.H) o[h] = v;
   }
+}
+
+template <class T, bool CK, int TW, int CH>
+__global__ __launch_bounds__(norm_threads(TW)) void ln_backward_few_kernel(NormBwd<T> j) {
+  constexpr int NT = norm_threads(TW), TEAMS = NT / (TW * 64);
+  __shared__ float2 red[2][TW];
+  __shared__ float sums[NT / 16][2][128];
+  if ((int)blockIdx.x < j.row_blocks) {
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    ln_backward_rows<T, CK, TW, CH, false>(j, blockIdx.x * TEAMS + wave / TW, j.row_blocks * TEAMS, wave % TW, lane, red);
+  } else ln_backward_columns<T, CK, NT>(j, (int)blockIdx.x - j.row_blocks, sums);
 }
 
 // Sums over the teams: a workgroup takes 64 columns of [teams][2 Hp], sixteen slices of the teams each.

@@ -33,50 +33,60 @@ static bool bad_product(int64_t M, int64_t N, int64_t K) {
 }
 
 // ------------------------------------------------------------------ layer norm
+// Calls f with the team of a row of H columns: wavefronts and pieces a lane as constants.
+template <class F> static void with_team(int H, F f) {
+  typedef std::integral_constant<int, 1> I1; typedef std::integral_constant<int, 2> I2;
+  if (H <= 512) f(I1(), I1());
+  else if (H <= 1024) f(I1(), I2());
+  else if (H <= 2048) f(std::integral_constant<int, 4>(), I1());
+  else if (H <= 4096) f(std::integral_constant<int, 4>(), I2());
+  else if (H <= 8192) f(std::integral_constant<int, 8>(), I2());
+  else f(std::integral_constant<int, 16>(), I2());
+}
+
+// Workgroups: as many as are of use to cover the loads' latency, few enough that most walk equally many rows.  us, bf16, 512 / 1024 / 2048 / 4096 workgroups: 32749 rows of
+// 3584 120 / 94 / 93 / 92, with the checkpoint 170 / 124 / 124 / 118 (one a row: 162); 5003 rows of 1160 12.9 / 10.7 / 10.1, one a row 11.7.
 template <class T>
 static void run_norm_forward(const NormFwd<T>& j, hipStream_t s) {
-  auto go = [&](auto kern, int threads, int teams) { kern<<<blocks_of((j.R + teams - 1) / teams, 1 << 20), threads, 0, s>>>(j); };
-  const int H = j.H;
-  if (H <= 512) go(ln_forward_kernel<T, 1, 1>, 256, 4);
-  else if (H <= 4096 && j.R >= 2048) {
-    if (H <= 1024) go(ln_forward_kernel<T, 1, 2>, 256, 4);
-    else if (H <= 2048) go(ln_forward_kernel<T, 1, 4>, 256, 4);
-    else go(ln_forward_kernel<T, 1, 8>, 256, 4);
-  } else if (H <= 2048) go(ln_forward_kernel<T, 4, 1>, 256, 1);
-  else if (H <= 4096) go(ln_forward_kernel<T, 4, 2>, 256, 1);
-  else if (H <= 8192) go(ln_forward_kernel<T, 4, 4>, 256, 1);
-  else go(ln_forward_kernel<T, 16, 2>, 1024, 1);
+  with_team(j.H, [&](auto tw, auto ch) {
+    constexpr int TW = tw.value, CH = ch.value, NT = norm_threads(TW), TEAMS = NT / (TW * 64);
+    const int64_t blocks = (j.R + TEAMS - 1) / TEAMS;
+    ln_forward_kernel<T, TW, CH><<<blocks_of(blocks, blocks > 8192 ? 4096 : 2048), NT, 0, s>>>(j);
+  });
 }
 
-constexpr int kNormBlocks = 512;
-struct NormTeams { int per_block, rows, blocks; };
-static NormTeams norm_teams(int64_t R, int H) {
-  NormTeams t;
-  t.per_block = H <= 1024 ? 4 : 1;
-  t.rows = H <= 4096 ? 4 : H <= 8192 ? 2 : 1;
-  const int64_t n = (R + t.rows * t.per_block - 1) / (t.rows * t.per_block);
-  t.blocks = (int)(n < kNormBlocks ? n : kNormBlocks);
+// Backward: one launch up to kNormFewRows rows.  us, 3584 columns, one launch / two: 128 rows 3.8 / 4.3 + 2.7, 256 5.6 / 5.3 + 3.0, 512 8.9 / 7.3 + 3.4, 1024 21.3 / 8.8 + 3.5;
+// 768 columns, 512 rows 8.0 / 3.9 + 3.4; the host takes 3.5 for a launch.
+// Beyond, the teams' sums cost 8 bytes a column and workgroup, twice: two workgroups a CU from x, three from a checkpoint, whose loads are shorter (32749 rows of 3584,
+// 384 / 512 / 768 / 1024 workgroups: 148 / 126 / 134 / 140 and 169 / 133 / 114 / 141), and four rows a team at least where a wavefront has a row to itself (2175 rows of 768, f32:
+// 128 / 256 / 384 workgroups 6.7 + 3.3 / 5.8 + 4.2 / 6.1 + 5.2).
+constexpr int kNormFewRows = 512;
+static int norm_pitch(int H) { return (H + 7) / 8 * 8; }
+struct NormTeams { int blocks, teams; };
+static NormTeams norm_teams(int64_t R, int H, bool ck) {
+  NormTeams t{0, 0};
+  if (R > kNormFewRows) with_team(H, [&](auto tw, auto) {
+    constexpr int TEAMS = norm_threads(tw.value) / (tw.value * 64), PER = TEAMS > 1 ? 4 * TEAMS : 1;
+    t.blocks = (int)blocks_of((R + PER - 1) / PER, ck ? 768 : 512);
+    t.teams = t.blocks * TEAMS;
+  });
   return t;
 }
-static int norm_pitch(int H) { return (H + 7) / 8 * 8; }
-static size_t norm_part_bytes(int64_t R, int H) {
-  const NormTeams t = norm_teams(R, H);
-  return up256((size_t)t.blocks * t.per_block * 2 * norm_pitch(H) * 4);
-}
+static size_t norm_part_bytes(int64_t R, int H) { return up256((size_t)norm_teams(R, H, true).teams * 2 * norm_pitch(H) * 4); }
 
 template <class T, bool CK>
-static void run_norm_backward(const NormBwd<T>& j, float* dgamma, float* dbeta, hipStream_t s) {
-  const NormTeams t = norm_teams(j.R, j.H);
-  auto go = [&](auto kern, int threads) { kern<<<t.blocks, threads, 0, s>>>(j); };
-  if (t.blocks > 0) {
-    if (j.H <= 512) go(ln_backward_kernel<T, CK, 1, 1, 4>, 256);
-    else if (j.H <= 1024) go(ln_backward_kernel<T, CK, 1, 2, 4>, 256);
-    else if (j.H <= 2048) go(ln_backward_kernel<T, CK, 4, 1, 4>, 256);
-    else if (j.H <= 4096) go(ln_backward_kernel<T, CK, 4, 2, 4>, 256);
-    else if (j.H <= 8192) go(ln_backward_kernel<T, CK, 4, 4, 2>, 256);
-    else go(ln_backward_kernel<T, CK, 16, 2, 1>, 1024);
-  }
-  ln_sum_kernel<<<(2 * j.Hp + 63) / 64, 256, 0, s>>>(j.part, t.blocks * t.per_block, j.Hp, j.H, dgamma, dbeta);
+static void run_norm_backward(NormBwd<T> j, hipStream_t s) {
+  const NormTeams t = norm_teams(j.R, j.H, CK);
+  with_team(j.H, [&](auto tw, auto ch) {
+    constexpr int TW = tw.value, CH = ch.value, NT = norm_threads(TW), TEAMS = NT / (TW * 64);
+    if (t.blocks) {
+      ln_backward_kernel<T, CK, TW, CH><<<t.blocks, NT, 0, s>>>(j);
+      ln_sum_kernel<<<(2 * j.Hp + 63) / 64, 256, 0, s>>>(j.part, t.teams, j.Hp, j.H, j.dgamma, j.dbeta);
+    } else {
+      j.row_blocks = (int)((j.R + TEAMS - 1) / TEAMS);
+      ln_backward_few_kernel<T, CK, TW, CH><<<j.row_blocks + f8_blocks(j.H), NT, 0, s>>>(j);
+    }
+  });
 }
 
 // ------------------------------------------------------------------ products
@@ -96,8 +106,16 @@ static F8Plan f8_plan(int64_t M, int N, int K) {
   return p;
 }
 
+static bool f8_hot(int64_t M, int N) { return ((M + 255) / 256) * ((N + 255) / 256) >= 256; }
+
 template <int FX, int FW, class T>
 static void run_f8_matmul_of(const F8Operand& x, const F8Operand& w, int K, T* y, int64_t ldy, void* ws, hipStream_t s) {
+  if constexpr (!kExact<T>)
+    if (f8_hot(x.rows, w.rows)) {
+      const int tm = (x.rows + 255) / 256, tn = (w.rows + 255) / 256;
+      f8_hot_kernel<FX, FW><<<launch_tiles(tm, tn), 256, 0, s>>>(F8Hot{x, w, y, ldy, x.rows, w.rows, f8_blocks(K)});
+      return;
+    }
   const F8Plan p = f8_plan(x.rows, w.rows, K);
   F8Product<T> j{x, w, y, ldy, x.rows, w.rows, f8_blocks(K), p.slices, p.per, (float*)ws, p.Np};
   const int64_t tiles = (int64_t)((x.rows + p.bm - 1) / p.bm) * ((w.rows + p.bm - 1) / p.bm) * p.slices;
@@ -231,8 +249,8 @@ rl_status rl_layer_norm_backward(const void* dy, int64_t lddy, const void* x, in
   auto go = [&](auto zero) {
     typedef decltype(zero) T;
     const NormBwd<T> j{(const T*)dy, (const T*)x, (T*)dx, R, lddy, ldx, lddx, H, (const uint8_t*)codes, (const uint8_t*)scales, format,
-                       f8_code_pitch(H), f8_scale_pitch(H), NormParams{gamma, nullptr, param_dtype == RL_BF16}, (const float2*)stats, (float*)ws, norm_pitch(H)};
-    if (codes) run_norm_backward<T, true>(j, dgamma, dbeta, s); else run_norm_backward<T, false>(j, dgamma, dbeta, s);
+                       f8_code_pitch(H), f8_scale_pitch(H), NormParams{gamma, nullptr, param_dtype == RL_BF16}, (const float2*)stats, (float*)ws, norm_pitch(H), dgamma, dbeta, 0};
+    if (codes) run_norm_backward<T, true>(j, s); else run_norm_backward<T, false>(j, s);
   };
   if (dtype == RL_BF16) go(bf16_t()); else go(float());
   return launched();

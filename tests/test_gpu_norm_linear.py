@@ -247,6 +247,29 @@ def test_matmul_of_single_products_is_exact(fa, fb):
             assert np.array_equal(f64(binding.rl_f8_matmul(pa, pb, t)), want)
 
 
+@pytest.mark.parametrize("M, N, K", [(4096, 4096, 100), (4000, 4200, 384), (3900, 4099, 640), (8200, 2310, 1157)])
+@pytest.mark.parametrize("fa, fb", [("e4m3", "e4m3"), ("e5m2", "e4m3"), ("e4m3", "e5m2"), ("e5m2", "e5m2")])
+def test_matmul_of_many_tiles(M, N, K, fa, fb):
+    # 1, 3, 5 and 10 blocks of k; single products first, exact whatever the path; then sums, within the tolerance of the 8-bit matrix unit
+    rng = np.random.default_rng(K)
+    a = rng.normal(size=(M, K)) * 2.0 ** rng.integers(-9, 9, size=(M, 1))
+    b = np.zeros((N, K))
+    b[np.arange(N), rng.integers(0, K, size=N)] = rng.choice([-1.0, 2.0, 0.5, 8.0], size=N)
+    pa, pb = binding.rl_f8_pack(rows(a, torch.float32), fa), binding.rl_f8_pack(rows(b, torch.float32), fb)
+    va = f64(binding.rl_f8_unpack(pa, torch.float32))
+    want = va[:, np.abs(b).argmax(1)] * b[np.arange(N), np.abs(b).argmax(1)]
+    assert np.array_equal(f64(binding.rl_f8_matmul(pa, pb)), want)
+    pb = binding.rl_f8_pack(rows(rng.normal(size=(N, K)) / K ** 0.5, torch.float32), fb)
+    vb = f64(binding.rl_f8_unpack(pb, torch.float32))
+    y = binding.rl_f8_matmul(pa, pb)
+    for r in (slice(0, 40), slice(M // 2, M // 2 + 40), slice(M - 40, M)):
+        want = va[r] @ vb.T
+        tol = (2 * (K + 32) * U + CUT["bf16"]) * (np.abs(va[r]) @ np.abs(vb).T) + half_step(torch.bfloat16, want)
+        assert np.all(np.abs(f64(y[r]) - want) <= tol)
+        assert np.linalg.norm(f64(y[r]) - want) <= 2.0 ** -8 * np.linalg.norm(want)
+    assert torch.equal(y, binding.rl_f8_matmul(pa, pb))
+
+
 def test_matmul_keeps_what_is_not_finite_in_its_row():
     rng = np.random.default_rng(2)
     for M in (9, 33, 300):
