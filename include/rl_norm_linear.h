@@ -60,9 +60,9 @@ rl_status rl_f8_matmul_workspace_bytes(int64_t M, int32_t N, int32_t K, size_t* 
 rl_status rl_f8_matmul(const void* x_codes, const void* x_scales, int32_t x_format, const void* w_codes, const void* w_scales, int32_t w_format,
                        int64_t M, int32_t N, int32_t K, void* y, int64_t ldy, int32_t dtype, void* workspace, size_t workspace_bytes, void* stream);
 
-/* The linear layer.  Forward: x [M, K] is packed into x_codes, x_scales (the checkpoint of the backward pass; both may be NULL up to
- * RL_F8_FEW_ROWS rows) and multiplied with the packed weight.  Workspace: rl_f8_matmul_workspace_bytes. */
-#define RL_F8_FEW_ROWS 16
+/* The linear layer.  Forward: x [M, K] is packed into x_codes, x_scales (the checkpoint of the backward pass; both NULL: not kept) and multiplied with the packed
+ * weight.  Workspace: with the packed x kept (keep != 0) or not. */
+rl_status rl_f8_linear_forward_workspace_bytes(int64_t M, int32_t N, int32_t K, int32_t keep, size_t* bytes);
 rl_status rl_f8_linear_forward(const void* x, int64_t ldx, int32_t dtype, int64_t M, int32_t K, int32_t x_format, const void* w_codes,
                                const void* w_scales, int32_t w_format, int32_t N, void* y, int64_t ldy, void* x_codes, void* x_scales,
                                void* workspace, size_t workspace_bytes, void* stream);

@@ -138,6 +138,7 @@ def _declare_norm_linear(L):
             rl_f8_pack_weight=[p, l, i, i, i, i, p, p, p, p, p],
             rl_f8_matmul_workspace_bytes=[l, i, i, nbytes],
             rl_f8_matmul=[p, p, i, p, p, i, l, i, i, p, l, i, p, z, p],
+            rl_f8_linear_forward_workspace_bytes=[l, i, i, i, nbytes],
             rl_f8_linear_forward=[p, l, i, l, i, i, p, p, i, i, p, l, p, p, p, z, p],
             rl_f8_linear_backward_workspace_bytes=[l, i, i, i, nbytes],
             rl_f8_linear_backward=[p, l, i, l, i, i, i, p, p, i, p, p, i, p, l, p, l, i, p, z, p]).items():
@@ -445,7 +446,6 @@ def rl_rvq_encode(vectors, codebooks, norms=None, want_residual=True, count_exac
 
 # ------------------------------------------------------------------ layer norm, 8-bit rows, 8-bit linear layer
 F8_FORMATS = {"e4m3": 0, "e5m2": 1}
-F8_FEW_ROWS = 16
 
 
 @dataclass
@@ -610,14 +610,14 @@ def rl_f8_linear_forward(x, w: F8Weight, fmt="e4m3", keep=True):
     N = w.rows.codes.shape[0]
     px, ldx, dt = _rows(x, "x")
     cw, sw, fw = _f8(w.rows, N, K, "w.rows")
-    kept = _f8_empty(M, K, fmt, x.device) if keep or M > F8_FEW_ROWS else None
-    y = torch.empty((M, N), dtype=x.dtype, device=x.device)
-    ws, pws, nws = _f8_workspace(lib().rl_f8_matmul_workspace_bytes, M, N, K, x.device)
     if fmt not in F8_FORMATS:
         raise ValueError(f"format must be one of {sorted(F8_FORMATS)}, got {fmt!r}")
+    kept = _f8_empty(M, K, fmt, x.device) if keep else None
+    y = x.new_empty((M, N))
+    ws, pws, nws = _f8_workspace(lib().rl_f8_linear_forward_workspace_bytes, M, N, K, 1 if keep else 0, x.device)
     _check(lib().rl_f8_linear_forward(px, ldx, dt, M, K, F8_FORMATS[fmt], cw, sw, fw, N, y.data_ptr(), N,
-                                      kept.codes.data_ptr() if kept else None, kept.scales.data_ptr() if kept else None, pws, nws, _stream_handle()))
-    return y, kept if keep else None
+                                      kept.codes.data_ptr() if keep else None, kept.scales.data_ptr() if keep else None, pws, nws, _stream_handle()))
+    return y, kept
 
 
 def rl_f8_linear_backward(dy, kept: F8Rows, w: F8Weight, fmt="e5m2", want_dx=True, want_dw=True, dw=None):

@@ -152,20 +152,23 @@ __device__ __attribute__((always_inline)) inline void f8_restore8(u32x2_t c, uns
 
 struct F8Out { uint8_t* codes; uint8_t* scales; int fmt, Kp, Ks; };    // codes == nullptr: not wanted
 
+// Eight consecutive values of a block that sixteen lanes hold, `a` being the bits of the lane's largest finite magnitude: codes and the block's scale byte.
+__device__ __attribute__((always_inline)) inline u32x2_t f8_pack8(float (&v)[8], unsigned a, int fmt, unsigned& s) {
+  s = f8_scale(max_of_16(a), fmt);
+  const float inv = f8_scale_inverse(s);
+  if (f8_scale_is_last(s, fmt)) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = f8_below_end(v[i], fmt);
+  }
+  return u32x2_t{f8_code4(v[0] * inv, v[1] * inv, v[2] * inv, v[3] * inv, fmt), f8_code4(v[4] * inv, v[5] * inv, v[6] * inv, v[7] * inv, fmt)};
+}
+
 // 512 consecutive values of a row, eight a lane starting at column `col` = first column + 8 lane (values past the row's end are zeros): codes and the word of scales.
 __device__ __attribute__((always_inline)) inline void f8_pack_wave(const F8Out& o, int64_t row, int col, int lane, float (&v)[8]) {
-  unsigned a = 0;
+  unsigned a = 0, s;
 #pragma unroll
   for (int i = 0; i < 8; ++i) { const unsigned b = finite_bits(v[i]); a = a > b ? a : b; }
-  const unsigned s = f8_scale(max_of_16(a), o.fmt);
-  const float inv = f8_scale_inverse(s);
-  if (f8_scale_is_last(s, o.fmt)) {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = f8_below_end(v[i], o.fmt);
-  }
-  u32x2_t c;
-  c[0] = f8_code4(v[0] * inv, v[1] * inv, v[2] * inv, v[3] * inv, o.fmt);
-  c[1] = f8_code4(v[4] * inv, v[5] * inv, v[6] * inv, v[7] * inv, o.fmt);
+  const u32x2_t c = f8_pack8(v, a, o.fmt, s);
   const unsigned word = (unsigned)__builtin_amdgcn_readlane((int)s, 0) | (unsigned)__builtin_amdgcn_readlane((int)s, 16) << 8 |
                         (unsigned)__builtin_amdgcn_readlane((int)s, 32) << 16 | (unsigned)__builtin_amdgcn_readlane((int)s, 48) << 24;
   if (col < o.Kp) *reinterpret_cast<u32x2_t*>(o.codes + row * o.Kp + col) = c;

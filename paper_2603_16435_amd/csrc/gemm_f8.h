@@ -10,8 +10,8 @@
 // The operands are exchanged (w first): a lane then holds four consecutive n of one row of y.
 //
 //  * f8_gemm_kernel  general: BM x BN tile, four wavefronts, two LDS stages of one slab, cut along K where there are few tiles.
-//  * f8_few_kernel   up to 16 rows of x: bound by reading w, which goes from memory straight into MFMA operands; eight wavefronts share K.  x may come
-//                    as it is: a lane holds 32 consecutive values of a block, which it packs in registers.
+//  * f8_hot_kernel   256 x 256 tile, for many tiles and bf16 outputs.
+//  * f8_few_kernel   up to 64 rows of x: bound by reading w.
 #pragma once
 #include <type_traits>
 
@@ -360,99 +360,102 @@ __global__ __launch_bounds__(256) void f8_hot_kernel(F8Hot j) {
 }
 
 // ------------------------------------------------------------------ few rows
-constexpr int kF8FewRows = 16, kF8FewWaves = 8;
-
-// x as it is: 32 consecutive values of the lane's row and block to codes and their block's scale byte (the four lanes of a row have the block).
-template <class T> __device__ __attribute__((always_inline)) inline unsigned f8_pack_operand(const Raw8<T> (&r)[4], int fmt, i32x8_t& code) {
-  unsigned a = 0;
-#pragma unroll
-  for (int i = 0; i < 4; ++i)
-#pragma unroll
-    for (int e = 0; e < 8; ++e) { const unsigned b = finite_bits(raw_get(r[i], e)); a = a > b ? a : b; }
-  for (int d = 16; d < 64; d <<= 1) { const unsigned b = (unsigned)__shfl_xor((int)a, d); a = a > b ? a : b; }
-  const unsigned s = f8_scale(a, fmt);
-  const float inv = f8_scale_inverse(s);
-  const bool last = f8_scale_is_last(s, fmt);
-#pragma unroll
-  for (int i = 0; i < 4; ++i)
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      float v[4];
-#pragma unroll
-      for (int e = 0; e < 4; ++e) v[e] = raw_get(r[i], 4 * h + e);
-      if (last) {
-#pragma unroll
-        for (int e = 0; e < 4; ++e) v[e] = f8_below_end(v[e], fmt);
-      }
-      code[2 * i + h] = (int)f8_code4(v[0] * inv, v[1] * inv, v[2] * inv, v[3] * inv, fmt);
-    }
-  return s;
-}
+// Up to 64 rows of x in MT blocks of sixteen: sixteen rows of w a workgroup, whose codes go from memory straight into MFMA operands (32 consecutive bytes a lane: the lanes of a row
+// have its line), four slabs of a wavefront on their way; eight wavefronts take every eighth slab and their sums are added at the end.  x, or the part of it that a
+// wavefront is at, comes out of the L2.
+// RAW: x as it is, where its codes fit the LDS (kF8RawBytes): each workgroup packs all of it there while its first codes of w are on their way, which takes a
+// launch less.
+constexpr int kF8FewRows = 64, kF8FewWaves = 8, kF8RawRows = 16, kF8RawBytes = 32768;
 
 template <class T> struct F8Few {
-  F8Operand x, w;                    // x.codes: read them, or, where raw is set, written by the first workgroup (nullptr: not wanted)
+  F8Operand x, w;                    // x: read; or, where raw is set, written by the first workgroup (codes nullptr: not wanted)
   const T* raw; int64_t ldx; int K;
   T* y; int64_t ldy;
   int M, N, nk;
 };
+__host__ __device__ inline int f8_raw_pitch(int Kp) { return Kp + 32; }                     // bytes of a row in LDS: rows in other banks
 
-template <int FX, int FW, class T, bool RAW>
+template <int FX, int FW, class T, int MT, bool RAW>
 __global__ __launch_bounds__(kF8FewWaves * 64) void f8_few_kernel(F8Few<T> j) {
-  __shared__ floatx4 sums[kF8FewWaves][64];
+  __shared__ floatx4 sums[kF8FewWaves][MT][64];
+  extern __shared__ __attribute__((aligned(16))) uint8_t xlds[];              // RAW: codes [M][pitch], scales [M][Ks]
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), frow = lane & 15, g = lane >> 4;
-  const int n0 = blockIdx.x * 16;
-  const int nr = n0 + frow < j.N ? n0 + frow : j.N - 1, mr = frow < j.M ? frow : j.M - 1;
+  const int n0 = blockIdx.x * 16, pitch = f8_raw_pitch(j.x.Kp);
+  const int nr = n0 + frow < j.N ? n0 + frow : j.N - 1;
   const uint8_t* wp = j.w.codes + (int64_t)nr * j.w.Kp + g * 32;
   const uint8_t* wsp = j.w.scales + (int64_t)nr * j.w.Ks;
-  floatx4 acc = {0.f, 0.f, 0.f, 0.f};
+  int mr[MT];
+#pragma unroll
+  for (int i = 0; i < MT; ++i) mr[i] = i * 16 + frow < j.M ? i * 16 + frow : j.M - 1;       // (rows that are not there: their results are not stored)
+  floatx4 acc[MT];
+#pragma unroll
+  for (int i = 0; i < MT; ++i) acc[i] = floatx4{0.f, 0.f, 0.f, 0.f};
   constexpr int U = 4;                                               // slabs in flight
-  for (int k0 = wave; k0 < j.nk; k0 += kF8FewWaves * U) {
-    i32x4_t wc[U][2];
-    unsigned sw[U];
+  i32x4_t wc[U][2];
+  unsigned sw[U];
+  auto fetch = [&](int k0) __attribute__((always_inline)) {
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       int k = k0 + u * kF8FewWaves; k = k < j.nk ? k : j.nk - 1;
       wc[u][0] = *reinterpret_cast<const i32x4_t*>(wp + (int64_t)k * 128); wc[u][1] = *reinterpret_cast<const i32x4_t*>(wp + (int64_t)k * 128 + 16);
       sw[u] = wsp[k];
     }
+    asm volatile("" ::: "memory");                                   // (all of them out before anything else: the compiler would move each to where it is used)
+  };
+  fetch(wave);
+  if constexpr (RAW) {
+    uint8_t* slds = xlds + j.M * pitch;
+    const int per = j.x.Kp / 8;                                      // pieces of a row: sixteen lanes have a block
+    for (int p = threadIdx.x; p < j.M * per; p += kF8FewWaves * 64) {
+      const int r = p / per, col = (p - r * per) * 8;
+      const Raw8<T> raw = raw_load(j.raw + (int64_t)r * j.ldx + col, j.K - col);
+      float v[8];
+      unsigned a = 0;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) { v[e] = raw_get(raw, e); const unsigned b = finite_bits(v[e]); a = a > b ? a : b; }
+      unsigned s;
+      const u32x2_t c = f8_pack8(v, a, FX, s);
+      *reinterpret_cast<u32x2_t*>(xlds + r * pitch + col) = c;
+      if ((threadIdx.x & 15) == 0) slds[r * j.x.Ks + col / kF8Block] = (uint8_t)s;
+      if (j.x.codes && blockIdx.x == 0) {
+        *reinterpret_cast<u32x2_t*>(const_cast<uint8_t*>(j.x.codes) + (int64_t)r * j.x.Kp + col) = c;
+        if ((threadIdx.x & 15) == 0) {
+          uint8_t* q = const_cast<uint8_t*>(j.x.scales) + (int64_t)r * j.x.Ks;
+          q[col / kF8Block] = (uint8_t)s;
+          if (col / kF8Block == j.nk - 1) for (int b = j.nk; b < j.x.Ks; ++b) q[b] = 127;
+        }
+      }
+    }
+    __syncthreads();
+  }
+  for (int k0 = wave; k0 < j.nk; k0 += kF8FewWaves * U) {
+    if (k0 != wave) fetch(k0);
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      const int k = k0 + u * kF8FewWaves;
-      if (k >= j.nk) break;
-      i32x8_t xc;
-      unsigned sx;
-      if constexpr (RAW) {
-        Raw8<T> r[4];
-        const int col = k * 128 + g * 32;
+      const bool there = k0 + u * kF8FewWaves < j.nk;                // (no branch around the loads of x: a slab past the end is the last one, times zero)
+      const int k = there ? k0 + u * kF8FewWaves : j.nk - 1;
+      i32x8_t wf = __builtin_shufflevector(wc[u][0], wc[u][1], 0, 1, 2, 3, 4, 5, 6, 7);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) r[i] = raw_load(j.raw + (int64_t)mr * j.ldx + col + i * 8, frow < j.M ? j.K - col - i * 8 : 0);
-        sx = f8_pack_operand(r, FX, xc);
-        if (j.x.codes && blockIdx.x == 0 && frow < j.M) {
-          uint8_t* cp = const_cast<uint8_t*>(j.x.codes) + (int64_t)frow * j.x.Kp + col;
-          *reinterpret_cast<i32x4_t*>(cp) = __builtin_shufflevector(xc, xc, 0, 1, 2, 3);
-          *reinterpret_cast<i32x4_t*>(cp + 16) = __builtin_shufflevector(xc, xc, 4, 5, 6, 7);
-          uint8_t* sp = const_cast<uint8_t*>(j.x.scales) + (int64_t)frow * j.x.Ks;
-          if (g == 0) {
-            sp[k] = (uint8_t)sx;
-            if (k == j.nk - 1) for (int b = j.nk; b < j.x.Ks; ++b) sp[b] = 127;
-          }
-        }
-      } else {
-        const uint8_t* xp = j.x.codes + (int64_t)mr * j.x.Kp + k * 128 + g * 32;
-        xc = __builtin_shufflevector(*reinterpret_cast<const i32x4_t*>(xp), *reinterpret_cast<const i32x4_t*>(xp + 16), 0, 1, 2, 3, 4, 5, 6, 7);
-        sx = j.x.scales[(int64_t)mr * j.x.Ks + k];
+      for (int e = 0; e < 8; ++e) wf[e] = there ? wf[e] : 0;
+#pragma unroll
+      for (int i = 0; i < MT; ++i) {
+        const uint8_t* xp = RAW ? xlds + mr[i] * pitch + k * 128 + g * 32 : j.x.codes + (int64_t)mr[i] * j.x.Kp + k * 128 + g * 32;
+        const i32x8_t xc = __builtin_shufflevector(*reinterpret_cast<const i32x4_t*>(xp), *reinterpret_cast<const i32x4_t*>(xp + 16), 0, 1, 2, 3, 4, 5, 6, 7);
+        const unsigned sx = RAW ? xlds[j.M * pitch + mr[i] * j.x.Ks + k] : j.x.scales[(int64_t)mr[i] * j.x.Ks + k];
+        if constexpr (kExact<T>) mfma_exact(acc[i], exact_operand<FW>(wf, sw[u]), exact_operand<FX>(xc, sx));
+        else mfma_f8<FX, FW>(acc[i], wf, xc, sw[u], sx);
       }
-      const i32x8_t wf = __builtin_shufflevector(wc[u][0], wc[u][1], 0, 1, 2, 3, 4, 5, 6, 7);
-      if constexpr (kExact<T>) mfma_exact(acc, exact_operand<FW>(wf, sw[u]), exact_operand<FX>(xc, sx));
-      else mfma_f8<FX, FW>(acc, wf, xc, sw[u], sx);
     }
   }
-  sums[wave][lane] = acc;
-  __syncthreads();
-  if (wave > 0) return;
 #pragma unroll
-  for (int i = 1; i < kF8FewWaves; ++i) acc += sums[i][lane];
-  if (frow < j.M) store4(j.y + (int64_t)frow * j.ldy + n0 + g * 4, j.N - n0 - g * 4, acc);
+  for (int i = 0; i < MT; ++i) sums[wave][i][lane] = acc[i];
+  __syncthreads();
+  if (wave >= MT) return;                                            // wavefront i adds and stores block i
+  floatx4 v = sums[0][wave][lane];
+#pragma unroll
+  for (int i = 1; i < kF8FewWaves; ++i) v += sums[i][wave][lane];
+  const int m = wave * 16 + frow;
+  if (m < j.M) store4(j.y + (int64_t)m * j.ldy + n0 + g * 4, j.N - n0 - g * 4, v);
 }
 
 }  // namespace rlk

@@ -8,7 +8,7 @@
 
 namespace rlk {
 
-static_assert((int)kE4M3 == (int)RL_E4M3 && (int)kE5M2 == (int)RL_E5M2 && kF8FewRows == RL_F8_FEW_ROWS && kNormMaxH == RL_LAYER_NORM_MAX_H, "header");
+static_assert((int)kE4M3 == (int)RL_E4M3 && (int)kE5M2 == (int)RL_E5M2 && kNormMaxH == RL_LAYER_NORM_MAX_H, "header");
 constexpr int64_t kMaxRows = ((int64_t)1 << 31) - (1 << 16);
 constexpr int kMaxCols = 1 << 22;                             // columns of an 8-bit operand, and rows of a weight
 
@@ -127,11 +127,14 @@ static void run_f8_matmul_of(const F8Operand& x, const F8Operand& w, int K, T* y
 template <int FX, int FW, class T>
 static void run_f8_few_of(const F8Operand& x, const F8Operand& w, const T* raw, int64_t ldx, int K, T* y, int64_t ldy, hipStream_t s) {
   const F8Few<T> j{x, w, raw, ldx, K, y, ldy, x.rows, w.rows, f8_blocks(K)};
-  const int blocks = (w.rows + 15) / 16;
-  if (raw) f8_few_kernel<FX, FW, T, true><<<blocks, kF8FewWaves * 64, 0, s>>>(j);
-  else f8_few_kernel<FX, FW, T, false><<<blocks, kF8FewWaves * 64, 0, s>>>(j);
+  const int blocks = (w.rows + 15) / 16, nt = kF8FewWaves * 64;
+  if (raw) f8_few_kernel<FX, FW, T, 1, true><<<blocks, nt, x.rows * (f8_raw_pitch(x.Kp) + x.Ks), s>>>(j);
+  else if (x.rows <= 16) f8_few_kernel<FX, FW, T, 1, false><<<blocks, nt, 0, s>>>(j);
+  else if (x.rows <= 32) f8_few_kernel<FX, FW, T, 2, false><<<blocks, nt, 0, s>>>(j);
+  else f8_few_kernel<FX, FW, T, 4, false><<<blocks, nt, 0, s>>>(j);
 }
-// raw: x as it is, up to kF8FewRows rows
+// raw: x as it is (f8_takes_raw)
+static bool f8_takes_raw(int64_t M, int K) { return M <= kF8RawRows && M * (f8_raw_pitch(f8_code_pitch(K)) + f8_scale_pitch(K)) <= kF8RawBytes; }
 template <class T>
 static void run_f8_product(const F8Operand& x, int fx, const F8Operand& w, int fw, const T* raw, int64_t ldx, int K, T* y, int64_t ldy, void* ws, hipStream_t s) {
   auto go = [&](auto FX, auto FW) {
@@ -143,6 +146,15 @@ static void run_f8_product(const F8Operand& x, int fx, const F8Operand& w, int f
   if (fx == RL_E4M3) { if (fw == RL_E4M3) go(E4(), E4()); else go(E4(), E5()); }
   else { if (fw == RL_E4M3) go(E5(), E4()); else go(E5(), E5()); }
 }
+struct F8ForwardPlan { size_t codes, scales, mm, total; bool raw; };
+static F8ForwardPlan f8_forward_plan(int64_t M, int N, int K, bool keep) {
+  F8ForwardPlan p{};
+  p.raw = f8_takes_raw(M, K);
+  if (!keep && !p.raw) { p.scales = up256((size_t)M * f8_code_pitch(K)); p.mm = p.scales + up256((size_t)M * f8_scale_pitch(K)); }
+  p.total = p.mm + (M > kF8FewRows ? f8_plan(M, N, K).part : 0);
+  return p;
+}
+
 template <class T> static void run_f8_pack(const T* x, int64_t ldx, int64_t R, int K, const F8Out& o, hipStream_t s) {
   const int segs = (o.Ks / 4 + kF8Steps - 1) / kF8Steps;
   f8_pack_kernel<T><<<blocks_of((R * segs + 3) / 4, 1 << 16), 256, 0, s>>>(x, R, ldx, K, o);
@@ -320,23 +332,32 @@ rl_status rl_f8_matmul(const void* x_codes, const void* x_scales, int32_t x_form
   return launched();
 }
 
+rl_status rl_f8_linear_forward_workspace_bytes(int64_t M, int32_t N, int32_t K, int32_t keep, size_t* bytes) {
+  if (!bytes) return RL_ERR_NULL;
+  if (bad_product(M, N, K)) return RL_ERR_SHAPE;
+  *bytes = f8_forward_plan(M, N, K, keep != 0).total;
+  return RL_OK;
+}
+
 rl_status rl_f8_linear_forward(const void* x, int64_t ldx, int32_t dtype, int64_t M, int32_t K, int32_t x_format, const void* w_codes,
                                const void* w_scales, int32_t w_format, int32_t N, void* y, int64_t ldy, void* x_codes, void* x_scales,
                                void* ws, size_t ws_bytes, void* stream) {
-  if (!w_codes || !w_scales || (M != 0 && (!x || !y)) || !x_codes != !x_scales || (M > kF8FewRows && !x_codes)) return RL_ERR_NULL;
+  if (!w_codes || !w_scales || (M != 0 && (!x || !y)) || !x_codes != !x_scales) return RL_ERR_NULL;
   if (!known(dtype) || !known_f8(x_format) || !known_f8(w_format)) return RL_ERR_DTYPE;
-  size_t need = 0;
-  if (rl_f8_matmul_workspace_bytes(M, N, K, &need) != RL_OK || bad_rows(x, ldx, dtype, M, K) || bad_rows(y, ldy, dtype, M, N) || off(x_codes, 16) || off(x_scales, 16) ||
+  if (bad_product(M, N, K) || bad_rows(x, ldx, dtype, M, K) || bad_rows(y, ldy, dtype, M, N) || off(x_codes, 16) || off(x_scales, 16) ||
       off(w_codes, 16) || off(w_scales, 16)) return RL_ERR_SHAPE;
-  if (bad_ws(ws, ws_bytes, need)) return RL_ERR_WORKSPACE;
+  const F8ForwardPlan p = f8_forward_plan(M, N, K, x_codes != nullptr);
+  if (bad_ws(ws, ws_bytes, p.total)) return RL_ERR_WORKSPACE;
   if (M == 0) return RL_OK;
   hipStream_t s = static_cast<hipStream_t>(stream);
   (void)hipGetLastError();
+  unsigned char* o = static_cast<unsigned char*>(ws);
+  if (!x_codes && !p.raw) { x_codes = o + p.codes; x_scales = o + p.scales; }
   const F8Operand xo = f8_operand(x_codes, x_scales, M, K), w = f8_operand(w_codes, w_scales, N, K);
   auto go = [&](auto zero) {
     typedef decltype(zero) T;
-    if (M > kF8FewRows) run_f8_pack((const T*)x, ldx, M, K, f8_out(x_codes, x_scales, x_format, K), s);
-    run_f8_product<T>(xo, x_format, w, w_format, (const T*)x, ldx, K, (T*)y, ldy, ws, s);
+    if (!p.raw) run_f8_pack((const T*)x, ldx, M, K, f8_out(x_codes, x_scales, x_format, K), s);
+    run_f8_product<T>(xo, x_format, w, w_format, p.raw ? (const T*)x : nullptr, ldx, K, (T*)y, ldy, o + p.mm, s);
   };
   if (dtype == RL_BF16) go(bf16_t()); else go(float());
   return launched();

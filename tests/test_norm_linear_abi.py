@@ -100,10 +100,15 @@ def test_product_refusals(lib):
               (dict(ldy=63), SHAPE), (dict(y=P + 1), SHAPE), (dict(w_codes=P + 8), SHAPE), (dict(x_scales=P + 8), SHAPE))
     for over, st in common + (((dict(M=100, workspace=None), WORKSPACE), (dict(M=100, workspace_bytes=need - 1), WORKSPACE)) if need else ()):
         assert mm(**over) == st, over
+    assert lib.rl_f8_linear_forward_workspace_bytes(100, 64, 8192, 1, C.byref(n)) == OK and n.value == need
+    assert lib.rl_f8_linear_forward_workspace_bytes(100, 64, 8192, 0, C.byref(n)) == OK and n.value >= need + 100 * (8192 + 64)         # room for the packed x
+    assert lib.rl_f8_linear_forward_workspace_bytes(1, 64, 8192, 0, C.byref(n)) == OK and n.value == 0                                  # packed on the way
+    assert lib.rl_f8_linear_forward_workspace_bytes(-1, 64, 8192, 0, C.byref(n)) == SHAPE
+    assert lib.rl_f8_linear_forward_workspace_bytes(1, 64, 8192, 0, None) == NULL
     lin = _caller(lib.rl_f8_linear_forward, x=P, ldx=8192, dtype=1, M=0, K=8192, x_format=0, w_codes=P, w_scales=P, w_format=0, N=64, y=P, ldy=64, x_codes=P,
                   x_scales=P, workspace=P, workspace_bytes=need, stream=None)
-    assert lin() == OK
-    for over, st in ((dict(M=100, x=None), NULL), (dict(x_codes=None), NULL), (dict(M=17, x_codes=None, x_scales=None), NULL), (dict(w_codes=None), NULL),
+    assert lin() == OK and lin(x_codes=None, x_scales=None) == OK
+    for over, st in ((dict(M=100, x=None), NULL), (dict(x_codes=None), NULL), (dict(M=17, x_codes=None, x_scales=None, workspace_bytes=0), WORKSPACE), (dict(w_codes=None), NULL),
                      (dict(dtype=4), DTYPE), (dict(x_format=2), DTYPE), (dict(ldx=8191), SHAPE), (dict(ldy=63), SHAPE), (dict(x=P + 1), SHAPE), (dict(w_scales=P + 1), SHAPE)):
         assert lin(**over) == st, over
     assert lib.rl_f8_linear_backward_workspace_bytes(100, 64, 256, 0, C.byref(n)) == OK and n.value % 256 == 0
