@@ -4,18 +4,20 @@
 // significant bits times a power of two), so that the products of the bf16 MFMA are exact.  The checkpoint is restored, transposed, into the slab-tiled work buffer
 // that the hot kernel's A operand is read from (x^T [k][t], zeros past the last token), dy is its K-major B operand as it is stored:
 //     C[k, n] = sum_t x^T[k, t] dy[t, n] = dW[n, k],   a lane holding four consecutive k of one row of dW.
-// f32 dy goes as three bf16 terms, dy = d0 + d1 + d2 to 2^-24 of it, three contractions added up: each product is exact, and three at the rate of
-// the bf16 pipes take a third of the time of one on the f32 pipes.  Tokens are taken a chunk at a time.
+// f32 dy goes as three bf16 terms, dy = d0 + d1 + d2 to 2^-24 of it, one contraction over three times the tokens, the smallest term first: each product is exact, and
+// three at the rate of the bf16 pipes take a third of the time of one on the f32 pipes.  (Three launches of a third each: 95 us where one takes a fraction, 3001 tokens of 1157 x 1163.)  Tokens are
+// taken a chunk at a time.
 #pragma once
 #include "epilogues.h"
 #include "f8_rows.h"
 
 namespace rlk {
 
-constexpr int kGradChunk = 32768;         // tokens restored at a time
+constexpr int kGradChunk = 32768;         // tokens restored at a time, with their copies
+constexpr int kGradTerms = 3;
 
-// x^T of a chunk: a workgroup restores 64 tokens x 128 k and writes 128 rows of 64 tokens, whole lines.  `pad` tokens in all, a multiple of 128.
-__global__ __launch_bounds__(256) void f8_restore_t_kernel(const uint8_t* codes, const uint8_t* scales, int fmt, int tokens, int Kp, int Ks, bf16_t* xt, int pad) {
+// x^T of a chunk: a workgroup restores 64 tokens x 128 k and writes 128 rows of 64 tokens, whole lines.  `pad` tokens in all, a multiple of 128; `copies` of them side by side.
+__global__ __launch_bounds__(256) void f8_restore_t_kernel(const uint8_t* codes, const uint8_t* scales, int fmt, int tokens, int Kp, int Ks, bf16_t* xt, int pad, int copies) {
   constexpr int kPitch = 66;              // elements of a row in LDS
   __shared__ bf16_t lds[128 * kPitch];
   const int t0 = blockIdx.x * 64, k0 = blockIdx.y * 128, tid = threadIdx.x, c = (tid & 15) * 8;
@@ -39,27 +41,29 @@ __global__ __launch_bounds__(256) void f8_restore_t_kernel(const uint8_t* codes,
   for (int i = 0; i < 4; ++i) {
     const int k = i * 32 + (tid >> 3), t = (tid & 7) * 8;
     const unsigned* p = reinterpret_cast<const unsigned*>(lds + k * kPitch + t);       // (4-byte aligned: the pitch is even)
-    *reinterpret_cast<u32x4_t*>(xt + tiled_index(k0 + k, t0 + t, pad)) = u32x4_t{p[0], p[1], p[2], p[3]};
+    const u32x4_t v = {p[0], p[1], p[2], p[3]};
+    for (int c = 0; c < copies; ++c) *reinterpret_cast<u32x4_t*>(xt + tiled_index(k0 + k, c * pad + t0 + t, (int64_t)copies * pad)) = v;
   }
 }
 
-// dy of a chunk into aligned rows of bf16: as it is (terms == 1), or in three terms of `tokens` rows each.
+// dy of a chunk into aligned rows of bf16, `pad` of them with zeros past the last token: as it is, or in three terms of as many rows each, the smallest first.
 template <class T>
-__global__ __launch_bounds__(256) void f8_grad_terms_kernel(const T* dy, int64_t ld, int tokens, int N, int Np, bf16_t* out) {
+__global__ __launch_bounds__(256) void f8_grad_terms_kernel(const T* dy, int64_t ld, int tokens, int pad, int N, int Np, bf16_t* out) {
+  constexpr int TERMS = sizeof(T) == 4 ? kGradTerms : 1;
   const int chunks = Np / 8;
-  const int64_t all = (int64_t)tokens * chunks, term = (int64_t)tokens * Np;
+  const int64_t all = (int64_t)pad * chunks, term = (int64_t)pad * Np;
   for (int64_t q = (int64_t)blockIdx.x * 256 + threadIdx.x; q < all; q += (int64_t)gridDim.x * 256) {
     const int64_t t = q / chunks;
     const int n = (int)(q - t * chunks) * 8;
-    const Raw8<T> r = raw_load(dy + t * ld + n, N - n);
+    const Raw8<T> r = raw_load(dy + t * ld + n, t < tokens ? N - n : 0);
     float v[8];
 #pragma unroll
     for (int e = 0; e < 8; ++e) v[e] = raw_get(r, e);
 #pragma unroll
-    for (int k = 0; k < (sizeof(T) == 4 ? 3 : 1); ++k) {
+    for (int k = TERMS - 1; k >= 0; --k) {
       const Raw8<bf16_t> b = raw_make<bf16_t>(v);
       *reinterpret_cast<u32x4_t*>(out + k * term + t * Np + n) = b.v;
-      if constexpr (sizeof(T) == 4) {
+      if constexpr (TERMS > 1) {
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
           const float hi = raw_get(b, e);

@@ -9,9 +9,9 @@
 // exact, on their way to 16x16x32 bf16 MFMAs, whose products and sums are those of f32, at half the rate (kExact).
 // The operands are exchanged (w first): a lane then holds four consecutive n of one row of y.
 //
-//  * f8_gemm_kernel  general: BM x BN tile, four wavefronts, two LDS stages of one slab, cut along K where there are few tiles.
+//  * f8_gemm_kernel  general: BM x BN tile, four wavefronts, cut along K where there are few tiles.
 //  * f8_hot_kernel   256 x 256 tile, for many tiles and bf16 outputs.
-//  * f8_few_kernel   up to 64 rows of x: bound by reading w.
+//  * f8_few_kernel   up to 16 rows of x: bound by reading w.
 #pragma once
 #include <type_traits>
 
@@ -23,6 +23,12 @@ typedef int i32x8_t __attribute__((ext_vector_type(8)));
 typedef int i32x4_t __attribute__((ext_vector_type(4)));
 
 struct F8Operand { const uint8_t* codes; const uint8_t* scales; int rows, Kp, Ks; };
+
+// 64 lanes x 4 bytes, an address per lane, to 256 bytes of LDS at l
+__device__ __attribute__((always_inline)) inline void load4_to_lds_lanes(const void* g, void* l) {
+  const unsigned lds = (unsigned)(size_t)(lds_ptr_t)l;      // uniform
+  asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dword %0, off" :: "v"(g), "s"(lds) : "memory");
+}
 
 // acc += x-block * w-block; byte 0 of sx / sw: the scales of the lane's row
 template <int FX, int FW> __device__ __attribute__((always_inline)) inline void mfma_f8(floatx4& acc, const i32x8_t& w, const i32x8_t& x, unsigned sw, unsigned sx) {
@@ -70,10 +76,15 @@ template <class T> struct F8Product {
   float* part; int Np;
 };
 
-template <int FX, int FW, class T, int BM, int BN>
+// S stages of a slab: S - 1 slabs are on their way while one is multiplied.  A stage holds the slab of x, that of w and a word of scales for each of their rows (four slabs'
+// bytes: fetched with every slab, so that each has as many loads).
+template <int BM, int BN> constexpr int f8_stage_bytes() { return (BM + BN) * kSlabBytes + 1024; }
+template <int FX, int FW, class T, int BM, int BN, int S>
 __global__ __launch_bounds__(256, 2) void f8_gemm_kernel(F8Product<T> j) {
-  constexpr int MB = BM / 32, NB = BN / 32, STAGE = (BM + BN) * kSlabBytes, LOADS = (BM + BN) / 32;      // loads of a wavefront and slab, 8 rows each
-  __shared__ __attribute__((aligned(1024))) unsigned char smem[2 * STAGE];
+  constexpr int MB = BM / 32, NB = BN / 32, STAGE = f8_stage_bytes<BM, BN>(), ROWS = (BM + BN) / 4, LOADS = ROWS / 8;      // of a wavefront and slab: rows, loads of eight rows
+  constexpr int WAIT = (S - 2) * (LOADS + 1);
+  static_assert(ROWS <= 64 && ROWS % 8 == 0 && WAIT < 64, "tile");
+  __shared__ __attribute__((aligned(1024))) unsigned char smem[S * STAGE];
   const int tiles_m = (j.M + BM - 1) / BM, tiles_n = (j.N + BN - 1) / BN;
   int t;
   if (!run_of_block(blockIdx.x, tiles_m * tiles_n * j.slices, t)) return;
@@ -83,79 +94,78 @@ __global__ __launch_bounds__(256, 2) void f8_gemm_kernel(F8Product<T> j) {
   const int k0 = slice * j.per, nk = j.nk - k0 < j.per ? j.nk - k0 : j.per;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wm = wave >> 1, wn = wave & 1;
 
+  // row lr of a stage: x rows, then w rows
+  auto row_of = [&](int lr, bool& is_x) __attribute__((always_inline)) {
+    is_x = lr < BM;
+    const int r = is_x ? tm * BM + lr : tn * BN + lr - BM, last = (is_x ? j.M : j.N) - 1;
+    return r < last ? r : last;
+  };
   const uint8_t* src[LOADS];
 #pragma unroll
   for (int i = 0; i < LOADS; ++i) {
-    const int lr = (wave * LOADS + i) * 8 + (lane >> 3);             // row of the stage: x rows, then w rows
-    const int c = (lane & 7) ^ ((lr >> 1) & 7);
-    const bool is_x = lr < BM;                                       // (uniform: BM is a multiple of 8)
-    int r = is_x ? tm * BM + lr : tn * BN + lr - BM;
-    const int last = (is_x ? j.M : j.N) - 1;
-    r = r < last ? r : last;
+    const int lr = wave * ROWS + i * 8 + (lane >> 3), c = (lane & 7) ^ ((lr >> 1) & 7);
+    bool is_x;
+    const int r = row_of(lr, is_x);
     src[i] = (is_x ? j.x.codes + (int64_t)r * j.x.Kp : j.w.codes + (int64_t)r * j.w.Kp) + (int64_t)k0 * 128 + c * 16;
   }
-  auto issue = [&](int kt) __attribute__((always_inline)) {
+  const uint8_t* scales;
+  {
+    bool is_x;
+    const int r = row_of(wave * ROWS + (lane < ROWS ? lane : ROWS - 1), is_x);
+    scales = (is_x ? j.x.scales + (int64_t)r * j.x.Ks : j.w.scales + (int64_t)r * j.w.Ks) + k0;          // (k0 is a multiple of four)
+  }
+  auto issue = [&](int kt, int stage) __attribute__((always_inline)) {
+    unsigned char* to = smem + stage * STAGE;
 #pragma unroll
-    for (int i = 0; i < LOADS; ++i) load16_to_lds_lanes(src[i] + (int64_t)kt * 128, smem + (kt & 1) * STAGE + (wave * LOADS + i) * 1024);
+    for (int i = 0; i < LOADS; ++i) load16_to_lds_lanes(src[i] + (int64_t)kt * 128, to + (wave * LOADS + i) * 1024);
+    load4_to_lds_lanes(scales + (kt & ~3), to + (BM + BN) * kSlabBytes + wave * 256);
   };
   const int frow = lane & 15, g = lane >> 4;
-  const unsigned* xs[MB];
-  const unsigned* ws[NB];
-#pragma unroll
-  for (int i = 0; i < MB; ++i) {
-    int r = tm * BM + wm * (BM / 2) + i * 16 + frow; r = r < j.M ? r : j.M - 1;
-    xs[i] = reinterpret_cast<const unsigned*>(j.x.scales + (int64_t)r * j.x.Ks + k0);
-  }
-#pragma unroll
-  for (int i = 0; i < NB; ++i) {
-    int r = tn * BN + wn * (BN / 2) + i * 16 + frow; r = r < j.N ? r : j.N - 1;
-    ws[i] = reinterpret_cast<const unsigned*>(j.w.scales + (int64_t)r * j.w.Ks + k0);
-  }
   floatx4 acc[MB][NB];
 #pragma unroll
   for (int i = 0; i < MB; ++i)
 #pragma unroll
     for (int b = 0; b < NB; ++b) acc[i][b] = floatx4{0.f, 0.f, 0.f, 0.f};
 
-  unsigned sx[MB], sw[NB];
-  issue(0);
+#pragma unroll
+  for (int i = 0; i < S - 1; ++i) if (i < nk) issue(i, i);
+  int at = 0, next = S - 1;                                          // stage of slab kt, and of slab kt + S - 1
   for (int kt = 0; kt < nk; ++kt) {
-    if ((kt & 3) == 0) {                                             // the scales of four slabs
-#pragma unroll
-      for (int i = 0; i < MB; ++i) sx[i] = xs[i][kt >> 2];
-#pragma unroll
-      for (int i = 0; i < NB; ++i) sw[i] = ws[i][kt >> 2];
-    }
-    __builtin_amdgcn_s_waitcnt(0x0F70);                              // vmcnt(0): this slab has landed ...
-    __syncthreads();                                                 // ... everybody's, and nobody reads the other stage any more
-    if (kt + 1 < nk) issue(kt + 1);
-    const unsigned char* xa = smem + (kt & 1) * STAGE;
+    if (kt + S - 2 < nk) __builtin_amdgcn_s_waitcnt(0x0F70 | (WAIT & 15) | (WAIT >> 4) << 14);          // this slab has landed ...
+    else __builtin_amdgcn_s_waitcnt(0x0F70);
+    __syncthreads();                                                 // ... everybody's, and nobody reads the stage of the slab before it any more
+    if (kt + S - 1 < nk) issue(kt + S - 1, next);
+    const unsigned char* xa = smem + at * STAGE;
+    const unsigned* words = reinterpret_cast<const unsigned*>(xa + (BM + BN) * kSlabBytes);
+    const int shift = (kt & 3) * 8;
+    auto scale = [&](int r) __attribute__((always_inline)) { return words[r / ROWS * 64 + r % ROWS] >> shift; };
+    auto codes = [&](int r) __attribute__((always_inline)) {
+      const i32x4_t lo = *reinterpret_cast<const i32x4_t*>(xa + lds_off(r, g)), hi = *reinterpret_cast<const i32x4_t*>(xa + lds_off(r, g + 4));
+      return (i32x8_t)__builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+    };
     std::conditional_t<kExact<T>, ExactOperand, i32x8_t> fx[MB];
+    unsigned sx[MB];
 #pragma unroll
     for (int i = 0; i < MB; ++i) {
       const int r = wm * (BM / 2) + i * 16 + frow;
-      const i32x4_t lo = *reinterpret_cast<const i32x4_t*>(xa + lds_off(r, g)), hi = *reinterpret_cast<const i32x4_t*>(xa + lds_off(r, g + 4));
-      const i32x8_t c = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
-      if constexpr (kExact<T>) fx[i] = exact_operand<FX>(c, sx[i]); else fx[i] = c;
+      sx[i] = scale(r);
+      if constexpr (kExact<T>) fx[i] = exact_operand<FX>(codes(r), sx[i]); else fx[i] = codes(r);
     }
 #pragma unroll
     for (int b = 0; b < NB; ++b) {
       const int r = BM + wn * (BN / 2) + b * 16 + frow;
-      const i32x4_t lo = *reinterpret_cast<const i32x4_t*>(xa + lds_off(r, g)), hi = *reinterpret_cast<const i32x4_t*>(xa + lds_off(r, g + 4));
-      const i32x8_t fw = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+      const unsigned sw = scale(r);
+      const i32x8_t fw = codes(r);
       if constexpr (kExact<T>) {
-        const ExactOperand ew = exact_operand<FW>(fw, sw[b]);
+        const ExactOperand ew = exact_operand<FW>(fw, sw);
 #pragma unroll
         for (int i = 0; i < MB; ++i) mfma_exact(acc[i][b], ew, fx[i]);
       } else {
 #pragma unroll
-        for (int i = 0; i < MB; ++i) mfma_f8<FX, FW>(acc[i][b], fw, fx[i], sw[b], sx[i]);
+        for (int i = 0; i < MB; ++i) mfma_f8<FX, FW>(acc[i][b], fw, fx[i], sw, sx[i]);
       }
     }
-#pragma unroll
-    for (int i = 0; i < MB; ++i) sx[i] >>= 8;
-#pragma unroll
-    for (int i = 0; i < NB; ++i) sw[i] >>= 8;
+    at = at + 1 == S ? 0 : at + 1; next = next + 1 == S ? 0 : next + 1;
   }
 #pragma unroll
   for (int i = 0; i < MB; ++i) {
@@ -194,17 +204,17 @@ __global__ __launch_bounds__(256) void f8_slices_kernel(const float* part, int s
 // ------------------------------------------------------------------ hot kernel
 // 256 x 256 tile, four wavefronts of 128 x 128 (256 accumulators a lane, in AGPRs), y in bf16.  A slab's 64 MFMAs of 32 cycles are as long as those of a slab of the bf16
 // hot kernel (gemm_nt.h), on the same bytes, so it is built like that one: slabs go straight into two LDS stages, every MFMA is fenced, fragment reads, slab
-// loads and one L2 prefetch are dealt out between them.  A slab is two phases: all eight blocks of x against blocks 0..3 of w, then against 4..7.  The
+// loads are dealt out between them.  A slab is two phases: all eight blocks of x against blocks 0..3 of w, then against 4..7.  The
 // workgroup meets between them, when the last fragments of the slab have been read: the second phase runs from registers, covers the first fragment reads of the next slab (an
 // x block is fetched as soon as the last MFMA that reads its registers is out) and the first loads of the slab after it.
-// Scales: one word a row holds four slabs' bytes; shifted by a byte a slab, and fetched a group ahead.
+// Scales: one word a row holds four slabs' bytes, of which the MFMA picks one; the words come through LDS as well, a group of slabs ahead.
 // LDS row 16 b + 4 g + e of w holds column 32 (b / 2) + 8 g + 4 (b % 2) + e of the tile's half (perm_row), so that a lane ends up with eight consecutive columns in a pair of
 // blocks: 16-byte stores.
-template <int FX, int FW> __device__ __attribute__((always_inline)) inline void mfma_f8_acc(floatx4& acc, const i32x8_t& w, const i32x8_t& x, unsigned sw, unsigned sx) {
-  asm volatile("v_mfma_scale_f32_16x16x128_f8f6f4 %0, %1, %2, %0, %3, %4 op_sel_hi:[0,0,0] cbsz:%5 blgp:%6"
-               : "+a"(acc) : "v"(w), "v"(x), "v"(sw), "v"(sx), "n"(FW), "n"(FX));
+// B: which byte of sw and sx
+template <int FX, int FW, int B> __device__ __attribute__((always_inline)) inline void mfma_f8_acc(floatx4& acc, const i32x8_t& w, const i32x8_t& x, unsigned sw, unsigned sx) {
+  asm volatile("v_mfma_scale_f32_16x16x128_f8f6f4 %0, %1, %2, %0, %3, %4 op_sel:[%7,%7,0] op_sel_hi:[%8,%8,0] cbsz:%5 blgp:%6"
+               : "+a"(acc) : "v"(w), "v"(x), "v"(sw), "v"(sx), "n"(FW), "n"(FX), "n"(B & 1), "n"(B >> 1));
 }
-
 struct F8Hot { F8Operand x, w; bf16_t* y; int64_t ldy; int M, N, nk; };
 constexpr int kF8Band = 8;
 
@@ -212,6 +222,8 @@ template <int FX, int FW>
 __global__ __launch_bounds__(256) void f8_hot_kernel(F8Hot j) {
   __shared__ __attribute__((aligned(1024))) unsigned char stage0[kHotStageBytes];
   __shared__ __attribute__((aligned(1024))) unsigned char stage1[kHotStageBytes];
+  __shared__ __attribute__((aligned(1024))) unsigned scales0[512];          // a word a row, x then w: the scales of four slabs
+  __shared__ __attribute__((aligned(1024))) unsigned scales1[512];
   constexpr int A_BYTES = 256 * kSlabBytes;
   const int tiles_m = (j.M + 255) / 256, tiles_n = (j.N + 255) / 256;
   int tm, tn;
@@ -237,42 +249,21 @@ __global__ __launch_bounds__(256) void f8_hot_kernel(F8Hot j) {
     else load16_to_lds_uniform(wbase + (int64_t)slab * 128, woff[i & 7], dst);
   };
   const int frow = lane & 15, g = lane >> 4;
-  const unsigned *xs[8], *ws[8];
-#pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    int m = tm * 256 + wm * 128 + i * 16 + frow, n = tn * 256 + wn * 128 + perm_row(i, frow >> 2, frow & 3);
-    m = m < j.M ? m : j.M - 1; n = n < j.N ? n : j.N - 1;
-    xs[i] = reinterpret_cast<const unsigned*>(j.x.scales + (int64_t)m * j.x.Ks);
-    ws[i] = reinterpret_cast<const unsigned*>(j.w.scales + (int64_t)n * j.w.Ks);
-  }
+  // scales: wavefront w fetches the words of its 64 rows of x and of w
   const int groups = (nk + 3) / 4;
-  unsigned sx[8], sw[8], nx[8], nw[8];
-  auto fetch_scales = [&](int group) __attribute__((always_inline)) {
+  const unsigned *xs, *ws;
+  {
+    int m = tm * 256 + wave * 64 + lane, n = tn * 256 + perm_lds_row_a(wave * 64 + lane);
+    m = m < j.M ? m : j.M - 1; n = n < j.N ? n : j.N - 1;
+    xs = reinterpret_cast<const unsigned*>(j.x.scales + (int64_t)m * j.x.Ks);
+    ws = reinterpret_cast<const unsigned*>(j.w.scales + (int64_t)n * j.w.Ks);
+  }
+  auto issue_scales = [&](int group, unsigned* to) __attribute__((always_inline)) {
     group = group < groups ? group : groups - 1;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) { nx[i] = xs[i][group]; nw[i] = ws[i][group]; }
+    load4_to_lds_lanes(xs + group, to + wave * 64);
+    load4_to_lds_lanes(ws + group, to + 256 + wave * 64);
   };
-  // L2 prefetch two slabs ahead, a quarter of the tile's x rows by one wavefront, an eighth of its w rows by another: the workgroups that an XCD runs at a time share
-  // the panels (as in gemm_nt.h)
-  const uint8_t* pf_ptr;
-  int pf_stride = 128;
-  if (wave == 0) {
-    int m = tm * 256 + 64 * (tn & 3) + lane; m = m < j.M ? m : j.M - 1;
-    pf_ptr = j.x.codes + (int64_t)m * j.x.Kp;
-  } else if (wave == 1) {
-    int n = tn * 256 + 32 * (tm & 7) + (lane & 31); n = n < j.N ? n : j.N - 1;
-    pf_ptr = j.w.codes + (int64_t)n * j.w.Kp;
-  } else { pf_ptr = j.x.codes; pf_stride = 0; }
-  unsigned pf0 = 0, pf1 = 0, pf_sink = 0;
-  auto prefetch = [&](unsigned& slot, int kt) __attribute__((always_inline)) {
-    pf_sink ^= slot;
-    const int k = kt + 3 < nk ? kt + 3 : nk - 1;
-    typedef const __attribute__((address_space(1))) unsigned* line_ptr;
-    line_ptr p = (line_ptr)(pf_ptr + (int64_t)k * pf_stride);
-    asm volatile("" : "+v"(p));
-    slot = *p;
-    asm volatile("" ::: "memory");
-  };
+  unsigned sx[8], sw[8];
 
   floatx4 acc[8][8];
 #pragma unroll
@@ -286,41 +277,45 @@ __global__ __launch_bounds__(256) void f8_hot_kernel(F8Hot j) {
     const i32x4_t lo = *reinterpret_cast<const i32x4_t*>(p + slot0), hi = *reinterpret_cast<const i32x4_t*>(p + slot1);
     return (i32x8_t)__builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
   };
-  // Slab kt is in `cur`; fx and fw[0] hold its x blocks and w blocks 0..3, loads 0..7 of slab kt + 1 are on their way to `nxt`.
-  auto slab = [&](unsigned char* cur, unsigned char* nxt, int kt, unsigned& pfslot) __attribute__((always_inline)) {
-    if ((kt & 3) == 0) {
-#pragma unroll
-      for (int i = 0; i < 8; ++i) { sx[i] = nx[i]; sw[i] = nw[i]; }
-    }
-    const int k1 = kt + 1 < nk ? kt + 1 : nk - 1, k2 = kt + 2 < nk ? kt + 2 : nk - 1;
+  auto read_sx = [&](const unsigned* from, int i) __attribute__((always_inline)) { sx[i] = from[wm * 128 + i * 16 + frow]; };
+  auto read_sw = [&](const unsigned* from, int i) __attribute__((always_inline)) { sw[i] = from[256 + wn * 128 + i * 16 + frow]; };
+  // Slab kt = B modulo 4 is in `cur`; fx and fw[0] hold its x blocks and w blocks 0..3, the loads of slab kt + 1 are on their way to `nxt`.  `scales`: where the words of
+  // the next group go.
+  auto slab = [&](auto B, unsigned char* cur, unsigned char* nxt, int kt, unsigned* scales) __attribute__((always_inline)) {
+    const int k2 = kt + 2 < nk ? kt + 2 : nk - 1;
 #pragma unroll
     for (int q = 0; q < 32; ++q) {
       const int i = q >> 2, b = i & 1 ? 3 - (q & 3) : q & 3;
-      mfma_f8_acc<FX, FW>(acc[i][b], fw[0][b], fx[i], sw[b], sx[i]);
+      mfma_f8_acc<FX, FW, B.value>(acc[i][b], fw[0][b], fx[i], sw[b], sx[i]);
       if (q % 2 == 0 && q < 8) fw[1][q / 2] = read(cur + wrow + (4 + q / 2) * 16 * kSlabBytes);
-      if (q % 3 == 1 && q < 24) issue(k1, nxt, 8 + q / 3);
       __builtin_amdgcn_sched_barrier(0);
     }
-    if ((kt & 3) == 1) fetch_scales((kt >> 2) + 1);
-    prefetch(pfslot, kt);
-    __builtin_amdgcn_s_waitcnt(0x0071);       // all but the prefetch; own fragment reads
+    __builtin_amdgcn_s_waitcnt(0x0070);       // own loads have landed, own fragment reads are done
     __syncthreads();
 #pragma unroll
     for (int q = 0; q < 32; ++q) {
       const int i = q >> 2, b = i & 1 ? 3 - (q & 3) : q & 3;
-      mfma_f8_acc<FX, FW>(acc[i][4 + b], fw[1][b], fx[i], sw[4 + b], sx[i]);
-      if ((q & 3) == 3) fx[i] = read(nxt + xrow + i * 16 * kSlabBytes);
-      else if (q % 8 == 1) fw[0][q / 8] = read(nxt + wrow + (q / 8) * 16 * kSlabBytes);
-      if (q % 4 == 2) issue(k2, cur, q / 4);
+      mfma_f8_acc<FX, FW, B.value>(acc[i][4 + b], fw[1][b], fx[i], sw[4 + b], sx[i]);
+      if ((q & 3) == 3) {
+        fx[i] = read(nxt + xrow + i * 16 * kSlabBytes);
+        if (B.value == 3) read_sx(scales, i);
+      } else if (q % 8 == 1) {
+        fw[0][q / 8] = read(nxt + wrow + (q / 8) * 16 * kSlabBytes);
+        if (B.value == 3) read_sw(scales, q / 8);
+      }
+      if (q % 2 == 0) issue(k2, cur, q / 2);
+      if (B.value == 0 && q == 0) issue_scales(kt / 4 + 1, scales);
       __builtin_amdgcn_sched_barrier(0);
     }
+    if (B.value == 3) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) { sx[i] >>= 8; sw[i] >>= 8; }
+      for (int i = 4; i < 8; ++i) read_sw(scales, i);
+    }
   };
 
 #pragma unroll
   for (int i = 0; i < 16; ++i) issue(0, stage0, i);
-  fetch_scales(0);
+  issue_scales(0, scales0);
 #pragma unroll
   for (int i = 0; i < 8; ++i)
 #pragma unroll
@@ -328,17 +323,22 @@ __global__ __launch_bounds__(256) void f8_hot_kernel(F8Hot j) {
   __builtin_amdgcn_s_waitcnt(0x0F70);
   __syncthreads();
 #pragma unroll
-  for (int i = 0; i < 8; ++i) issue(nk > 1 ? 1 : 0, stage1, i);
+  for (int i = 0; i < 16; ++i) issue(nk > 1 ? 1 : 0, stage1, i);
 #pragma unroll
-  for (int i = 0; i < 8; ++i) fx[i] = read(stage0 + xrow + i * 16 * kSlabBytes);
+  for (int i = 0; i < 8; ++i) { fx[i] = read(stage0 + xrow + i * 16 * kSlabBytes); read_sx(scales0, i); read_sw(scales0, i); }
 #pragma unroll
   for (int b = 0; b < 4; ++b) fw[0][b] = read(stage0 + wrow + b * 16 * kSlabBytes);
+  typedef std::integral_constant<int, 0> B0; typedef std::integral_constant<int, 1> B1; typedef std::integral_constant<int, 2> B2; typedef std::integral_constant<int, 3> B3;
   int kt = 0;
-  for (; kt + 1 < nk; kt += 2) {
-    slab(stage0, stage1, kt, pf0);
-    slab(stage1, stage0, kt + 1, pf1);
+  for (; kt + 3 < nk; kt += 4) {
+    slab(B0(), stage0, stage1, kt, scales1);
+    slab(B1(), stage1, stage0, kt + 1, scales1);
+    slab(B2(), stage0, stage1, kt + 2, scales1);
+    slab(B3(), stage1, stage0, kt + 3, scales1);
   }
-  if (kt < nk) slab(stage0, stage1, kt, pf0);
+  if (kt < nk) slab(B0(), stage0, stage1, kt, scales1);
+  if (kt + 1 < nk) slab(B1(), stage1, stage0, kt + 1, scales1);
+  if (kt + 2 < nk) slab(B2(), stage0, stage1, kt + 2, scales1);
   __builtin_amdgcn_s_waitcnt(0x0070);         // the loads past the end
   mfma_drain();
 
@@ -356,16 +356,14 @@ __global__ __launch_bounds__(256) void f8_hot_kernel(F8Hot j) {
       raw_store(j.y + (int64_t)m * j.ldy + n, edge ? j.N - n : 8, raw_make<bf16_t>(v));
     }
   }
-  if ((pf_sink ^ pf0 ^ pf1) == 0x9E3779B9u && nk < 0) j.y[0] = (bf16_t)0.f;        // never true: keeps the prefetch loads
 }
 
 // ------------------------------------------------------------------ few rows
-// Up to 64 rows of x in MT blocks of sixteen: sixteen rows of w a workgroup, whose codes go from memory straight into MFMA operands (32 consecutive bytes a lane: the lanes of a row
-// have its line), four slabs of a wavefront on their way; eight wavefronts take every eighth slab and their sums are added at the end.  x, or the part of it that a
-// wavefront is at, comes out of the L2.
-// RAW: x as it is, where its codes fit the LDS (kF8RawBytes): each workgroup packs all of it there while its first codes of w are on their way, which takes a
-// launch less.
-constexpr int kF8FewRows = 64, kF8FewWaves = 8, kF8RawRows = 16, kF8RawBytes = 32768;
+// Up to 16 rows of x: sixteen rows of w a workgroup, whose codes go from memory straight into MFMA operands (32 consecutive bytes a lane: the lanes of a row
+// have its line), four slabs of a wavefront on their way; eight wavefronts take every eighth slab and their sums are added at the end.  x comes out of the L2.
+// Faster than the general kernel's tiles while a CU has one workgroup (8 rows of 3584, 3584 rows of w 5.4 us and 7.2; 14336 rows of w 15.5 and 10.9).
+// RAW: x as it is: each workgroup packs all of it into LDS while its first codes of w are on their way, which takes a launch less.
+constexpr int kF8FewRows = 16, kF8FewWaves = 8;
 
 template <class T> struct F8Few {
   F8Operand x, w;                    // x: read; or, where raw is set, written by the first workgroup (codes nullptr: not wanted)
@@ -375,21 +373,17 @@ template <class T> struct F8Few {
 };
 __host__ __device__ inline int f8_raw_pitch(int Kp) { return Kp + 32; }                     // bytes of a row in LDS: rows in other banks
 
-template <int FX, int FW, class T, int MT, bool RAW>
+template <int FX, int FW, class T, bool RAW>
 __global__ __launch_bounds__(kF8FewWaves * 64) void f8_few_kernel(F8Few<T> j) {
-  __shared__ floatx4 sums[kF8FewWaves][MT][64];
+  __shared__ floatx4 sums[kF8FewWaves][64];
   extern __shared__ __attribute__((aligned(16))) uint8_t xlds[];              // RAW: codes [M][pitch], scales [M][Ks]
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), frow = lane & 15, g = lane >> 4;
   const int n0 = blockIdx.x * 16, pitch = f8_raw_pitch(j.x.Kp);
   const int nr = n0 + frow < j.N ? n0 + frow : j.N - 1;
   const uint8_t* wp = j.w.codes + (int64_t)nr * j.w.Kp + g * 32;
   const uint8_t* wsp = j.w.scales + (int64_t)nr * j.w.Ks;
-  int mr[MT];
-#pragma unroll
-  for (int i = 0; i < MT; ++i) mr[i] = i * 16 + frow < j.M ? i * 16 + frow : j.M - 1;       // (rows that are not there: their results are not stored)
-  floatx4 acc[MT];
-#pragma unroll
-  for (int i = 0; i < MT; ++i) acc[i] = floatx4{0.f, 0.f, 0.f, 0.f};
+  const int mr = frow < j.M ? frow : j.M - 1;                        // (rows that are not there: their results are not stored)
+  floatx4 acc = {0.f, 0.f, 0.f, 0.f};
   constexpr int U = 4;                                               // slabs in flight
   i32x4_t wc[U][2];
   unsigned sw[U];
@@ -437,25 +431,19 @@ __global__ __launch_bounds__(kF8FewWaves * 64) void f8_few_kernel(F8Few<T> j) {
       i32x8_t wf = __builtin_shufflevector(wc[u][0], wc[u][1], 0, 1, 2, 3, 4, 5, 6, 7);
 #pragma unroll
       for (int e = 0; e < 8; ++e) wf[e] = there ? wf[e] : 0;
-#pragma unroll
-      for (int i = 0; i < MT; ++i) {
-        const uint8_t* xp = RAW ? xlds + mr[i] * pitch + k * 128 + g * 32 : j.x.codes + (int64_t)mr[i] * j.x.Kp + k * 128 + g * 32;
-        const i32x8_t xc = __builtin_shufflevector(*reinterpret_cast<const i32x4_t*>(xp), *reinterpret_cast<const i32x4_t*>(xp + 16), 0, 1, 2, 3, 4, 5, 6, 7);
-        const unsigned sx = RAW ? xlds[j.M * pitch + mr[i] * j.x.Ks + k] : j.x.scales[(int64_t)mr[i] * j.x.Ks + k];
-        if constexpr (kExact<T>) mfma_exact(acc[i], exact_operand<FW>(wf, sw[u]), exact_operand<FX>(xc, sx));
-        else mfma_f8<FX, FW>(acc[i], wf, xc, sw[u], sx);
-      }
+      const uint8_t* xp = RAW ? xlds + mr * pitch + k * 128 + g * 32 : j.x.codes + (int64_t)mr * j.x.Kp + k * 128 + g * 32;
+      const i32x8_t xc = __builtin_shufflevector(*reinterpret_cast<const i32x4_t*>(xp), *reinterpret_cast<const i32x4_t*>(xp + 16), 0, 1, 2, 3, 4, 5, 6, 7);
+      const unsigned sx = RAW ? xlds[j.M * pitch + mr * j.x.Ks + k] : j.x.scales[(int64_t)mr * j.x.Ks + k];
+      if constexpr (kExact<T>) mfma_exact(acc, exact_operand<FW>(wf, sw[u]), exact_operand<FX>(xc, sx));
+      else mfma_f8<FX, FW>(acc, wf, xc, sw[u], sx);
     }
   }
-#pragma unroll
-  for (int i = 0; i < MT; ++i) sums[wave][i][lane] = acc[i];
+  sums[wave][lane] = acc;
   __syncthreads();
-  if (wave >= MT) return;                                            // wavefront i adds and stores block i
-  floatx4 v = sums[0][wave][lane];
+  if (wave > 0) return;
 #pragma unroll
-  for (int i = 1; i < kF8FewWaves; ++i) v += sums[i][wave][lane];
-  const int m = wave * 16 + frow;
-  if (m < j.M) store4(j.y + (int64_t)m * j.ldy + n0 + g * 4, j.N - n0 - g * 4, v);
+  for (int i = 1; i < kF8FewWaves; ++i) acc += sums[i][lane];
+  if (frow < j.M) store4(j.y + (int64_t)frow * j.ldy + n0 + g * 4, j.N - n0 - g * 4, acc);
 }
 
 }  // namespace rlk

@@ -27,9 +27,9 @@ static F8Operand f8_operand(const void* codes, const void* scales, int64_t rows,
   return F8Operand{(const uint8_t*)codes, (const uint8_t*)scales, (int)rows, f8_code_pitch(K), f8_scale_pitch(K)};
 }
 
-// (a launch has at most 2^32 threads, of 256 a tile of 64 x 64 or more)
+// (a launch has at most 2^32 threads; products of so many rows take tiles of 128 x 128 or more, 256 threads each)
 static bool bad_product(int64_t M, int64_t N, int64_t K) {
-  return M < 0 || M >= kMaxRows || N < 1 || N > kMaxCols || K < 1 || K > kMaxCols || ((M + 63) / 64) * ((N + 63) / 64) > (1 << 23);
+  return M < 0 || M >= kMaxRows || N < 1 || N > kMaxCols || K < 1 || K > kMaxCols || ((M + 127) / 128) * ((N + 127) / 128) > (1 << 23);
 }
 
 // ------------------------------------------------------------------ layer norm
@@ -90,68 +90,99 @@ static void run_norm_backward(NormBwd<T> j, hipStream_t s) {
 }
 
 // ------------------------------------------------------------------ products
-constexpr int kF8Slots = 512;             // general kernel: two workgroups a CU
-struct F8Plan { int bm, slices, per; size_t part; int Np; };
-static F8Plan f8_plan(int64_t M, int N, int K) {
-  F8Plan p{128, 1, 0, 0, (N + 3) / 4 * 4};
-  const int nk = f8_blocks(K);
-  auto tiles = [&](int b) { return ((M + b - 1) / b) * ((N + b - 1) / b); };
-  if (tiles(128) < kF8Slots / 2) p.bm = 64;
-  const int64_t t = tiles(p.bm);
-  int64_t want = t < kF8Slots ? kF8Slots / (t > 0 ? t : 1) : 1;
-  if (want > nk / 4) want = nk / 4;                                // a slice has four blocks at least: one word of scales a row
-  p.per = want > 1 ? (int)((nk + want - 1) / want + 3) / 4 * 4 : (nk + 3) / 4 * 4;
-  p.slices = (nk + p.per - 1) / p.per;
-  if (p.slices > 1) p.part = up256((size_t)p.slices * M * p.Np * 4);
-  return p;
+// Tile and cut along K of a product.  A workgroup takes `start` us and `one` us a slab, `two` where a CU has two of them (measured, in rounds that fill the chip or part of it;
+// bf16 outputs and f32 ones, whose MFMAs run at half the rate); a cut product takes a second launch and a pass over the slices.  The cheapest by that account is
+// taken: within 10 % of the fastest of all tiles and cuts measured over 8 to 4000 rows and seven weights of 300 x 5000 to 14336 x 3584 (us, by tiles of 32 x 32 / 64 x 64 /
+// 64 x 128 / 128 x 128 / 256 x 256: 48 rows, 4096 x 2048 5.9 / 7.8 / - / - / -; 250, 14336 x 3584 53.7 / 27.4 / 23.0 / 24.5 / 35.1; 1000, 3584 x 3584 - / 27.8 / 22.2 / 24.9 / 35.3;
+// 2000, 3584 x 3584 - / 53.4 / 42.5 / 33.6 / 36.1; 4000 - / 117 / 79 / 63.5 / 37.1).
+struct F8Tile { int bm, bn; float start[2], one[2], two[2]; };
+constexpr F8Tile kF8Tiles[] = {
+    {32, 32, {2.6f, 2.6f}, {0.205f, 0.275f}, {0.25f, 0.36f}},
+    {64, 64, {3.0f, 3.2f}, {0.32f, 0.43f}, {0.45f, 0.70f}},
+    {64, 128, {3.4f, 3.8f}, {0.465f, 0.79f}, {0.69f, 1.18f}},
+    {128, 128, {4.3f, 5.0f}, {0.68f, 1.15f}, {1.05f, 1.82f}},
+    {256, 256, {7.0f, 0.f}, {1.15f, 0.f}, {0.f, 0.f}},               // hot kernel: bf16 outputs, one workgroup a CU, not cut
+};
+constexpr int kF8Hot = 4;
+struct F8Plan { int tile, slices, per; size_t part; int Np; };
+static F8Plan f8_plan(int64_t M, int N, int K, bool exact) {
+  const int nk = f8_blocks(K), whole = (nk + 3) / 4 * 4;
+  F8Plan best{0, 1, whole, 0, (N + 3) / 4 * 4};
+  float least = 3e38f;
+  for (int t = 0; t <= kF8Hot - (exact ? 1 : 0); ++t) {
+    const F8Tile& c = kF8Tiles[t];
+    const int64_t tiles = ((M + c.bm - 1) / c.bm) * ((N + c.bn - 1) / c.bn);
+    for (int slices = 1; slices <= 16 && slices <= (nk + 3) / 4; ++slices) {
+      if (slices > 1 && (t == kF8Hot || tiles * slices > 512)) break;
+      const int per = slices > 1 ? ((nk + slices - 1) / slices + 3) / 4 * 4 : whole;          // whole words of scales
+      if ((nk + per - 1) / per != slices) continue;
+      const int64_t n = tiles * slices;
+      const float len = (float)(slices > 1 ? per : nk), one = c.start[exact] + c.one[exact] * len, two = c.start[exact] + c.two[exact] * len;
+      float us;
+      if (t == kF8Hot) us = (float)((n + 255) / 256) * one;
+      else { const int64_t left = n % 512; us = (float)(n / 512) * two + (left == 0 ? 0.f : left <= 256 ? one : two); }
+      if (slices > 1) us += 2.4f + (float)M * (float)N * (float)(slices + 1) * 1e-6f;
+      if (us < least) { least = us; best.tile = t; best.slices = slices; best.per = per; }
+    }
+  }
+  if (best.slices > 1) best.part = up256((size_t)best.slices * M * best.Np * 4);
+  return best;
 }
-
-static bool f8_hot(int64_t M, int N) { return ((M + 255) / 256) * ((N + 255) / 256) >= 256; }
 
 template <int FX, int FW, class T>
-static void run_f8_matmul_of(const F8Operand& x, const F8Operand& w, int K, T* y, int64_t ldy, void* ws, hipStream_t s) {
+static void run_f8_tiles(const F8Operand& x, const F8Operand& w, int K, T* y, int64_t ldy, void* ws, hipStream_t s) {
+  const F8Plan p = f8_plan(x.rows, w.rows, K, kExact<T>);
   if constexpr (!kExact<T>)
-    if (f8_hot(x.rows, w.rows)) {
-      const int tm = (x.rows + 255) / 256, tn = (w.rows + 255) / 256;
-      f8_hot_kernel<FX, FW><<<launch_tiles(tm, tn), 256, 0, s>>>(F8Hot{x, w, y, ldy, x.rows, w.rows, f8_blocks(K)});
+    if (p.tile == kF8Hot) {
+      f8_hot_kernel<FX, FW><<<launch_tiles((x.rows + 255) / 256, (w.rows + 255) / 256), 256, 0, s>>>(F8Hot{x, w, y, ldy, x.rows, w.rows, f8_blocks(K)});
       return;
     }
-  const F8Plan p = f8_plan(x.rows, w.rows, K);
-  F8Product<T> j{x, w, y, ldy, x.rows, w.rows, f8_blocks(K), p.slices, p.per, (float*)ws, p.Np};
-  const int64_t tiles = (int64_t)((x.rows + p.bm - 1) / p.bm) * ((w.rows + p.bm - 1) / p.bm) * p.slices;
-  const unsigned blocks = (unsigned)((tiles + kXcds - 1) / kXcds * kXcds);
-  if (p.bm == 128) f8_gemm_kernel<FX, FW, T, 128, 128><<<blocks, 256, 0, s>>>(j);
-  else f8_gemm_kernel<FX, FW, T, 64, 64><<<blocks, 256, 0, s>>>(j);
+  const F8Product<T> j{x, w, y, ldy, x.rows, w.rows, f8_blocks(K), p.slices, p.per, (float*)ws, p.Np};
+  const F8Tile& c = kF8Tiles[p.tile];
+  const int64_t n = (int64_t)((x.rows + c.bm - 1) / c.bm) * ((w.rows + c.bn - 1) / c.bn) * p.slices;
+  const unsigned blocks = (unsigned)((n + kXcds - 1) / kXcds * kXcds);
+  if (p.tile == 0) f8_gemm_kernel<FX, FW, T, 32, 32, 6><<<blocks, 256, 0, s>>>(j);
+  else if (p.tile == 1) f8_gemm_kernel<FX, FW, T, 64, 64, 4><<<blocks, 256, 0, s>>>(j);
+  else if (p.tile == 2) f8_gemm_kernel<FX, FW, T, 64, 128, 3><<<blocks, 256, 0, s>>>(j);
+  else f8_gemm_kernel<FX, FW, T, 128, 128, 2><<<blocks, 256, 0, s>>>(j);
   if (p.slices > 1) f8_slices_kernel<T><<<blocks_of(((int64_t)x.rows * p.Np / 4 + 255) / 256, 4096), 256, 0, s>>>(j.part, p.slices, j.M, j.N, p.Np, y, ldy);
 }
+// One workgroup of the few-rows kernel a CU; with more slabs than its wavefronts have on their way the tiles do better.
+static bool f8_few(int64_t M, int N, int K) { return M <= kF8FewRows && N <= 16 * 256 && f8_blocks(K) <= 32; }
+// Packing x in every workgroup instead of a launch ahead: up to so many bytes of codes, times the rounds of workgroups (3584 columns; 3584 rows of w: 4 rows of x 6.2 us and 5.2 + 3.3,
+// 8 rows 8.4 and 5.4 + 3.3; 14336: 1 row 12.3 and 10.9 + 3.3, 4 rows 15.7).
+static bool f8_takes_raw(int64_t M, int N, int K) { return M <= kF8FewRows && M * f8_raw_pitch(f8_code_pitch(K)) * ((N + 4095) / 4096) <= 28800; }
 template <int FX, int FW, class T>
 static void run_f8_few_of(const F8Operand& x, const F8Operand& w, const T* raw, int64_t ldx, int K, T* y, int64_t ldy, hipStream_t s) {
   const F8Few<T> j{x, w, raw, ldx, K, y, ldy, x.rows, w.rows, f8_blocks(K)};
   const int blocks = (w.rows + 15) / 16, nt = kF8FewWaves * 64;
-  if (raw) f8_few_kernel<FX, FW, T, 1, true><<<blocks, nt, x.rows * (f8_raw_pitch(x.Kp) + x.Ks), s>>>(j);
-  else if (x.rows <= 16) f8_few_kernel<FX, FW, T, 1, false><<<blocks, nt, 0, s>>>(j);
-  else if (x.rows <= 32) f8_few_kernel<FX, FW, T, 2, false><<<blocks, nt, 0, s>>>(j);
-  else f8_few_kernel<FX, FW, T, 4, false><<<blocks, nt, 0, s>>>(j);
+  if (raw) f8_few_kernel<FX, FW, T, true><<<blocks, nt, x.rows * (f8_raw_pitch(x.Kp) + x.Ks), s>>>(j);
+  else f8_few_kernel<FX, FW, T, false><<<blocks, nt, 0, s>>>(j);
 }
-// raw: x as it is (f8_takes_raw)
-static bool f8_takes_raw(int64_t M, int K) { return M <= kF8RawRows && M * (f8_raw_pitch(f8_code_pitch(K)) + f8_scale_pitch(K)) <= kF8RawBytes; }
+// raw: x as it is (f8_takes_raw), or nullptr
 template <class T>
 static void run_f8_product(const F8Operand& x, int fx, const F8Operand& w, int fw, const T* raw, int64_t ldx, int K, T* y, int64_t ldy, void* ws, hipStream_t s) {
   auto go = [&](auto FX, auto FW) {
-    if (x.rows <= kF8FewRows) run_f8_few_of<FX.value, FW.value, T>(x, w, raw, ldx, K, y, ldy, s);
-    else run_f8_matmul_of<FX.value, FW.value, T>(x, w, K, y, ldy, ws, s);
+    if (raw || f8_few(x.rows, w.rows, K)) run_f8_few_of<FX.value, FW.value, T>(x, w, raw, ldx, K, y, ldy, s);
+    else run_f8_tiles<FX.value, FW.value, T>(x, w, K, y, ldy, ws, s);
   };
   typedef std::integral_constant<int, 0> E4;
   typedef std::integral_constant<int, 1> E5;
   if (fx == RL_E4M3) { if (fw == RL_E4M3) go(E4(), E4()); else go(E4(), E5()); }
   else { if (fw == RL_E4M3) go(E5(), E4()); else go(E5(), E5()); }
 }
+// (either type of y: the larger of the two)
+static size_t f8_product_bytes(int64_t M, int N, int K) {
+  if (f8_few(M, N, K)) return 0;
+  const size_t a = f8_plan(M, N, K, false).part, b = f8_plan(M, N, K, true).part;
+  return a > b ? a : b;
+}
 struct F8ForwardPlan { size_t codes, scales, mm, total; bool raw; };
 static F8ForwardPlan f8_forward_plan(int64_t M, int N, int K, bool keep) {
   F8ForwardPlan p{};
-  p.raw = f8_takes_raw(M, K);
+  p.raw = f8_takes_raw(M, N, K);
   if (!keep && !p.raw) { p.scales = up256((size_t)M * f8_code_pitch(K)); p.mm = p.scales + up256((size_t)M * f8_scale_pitch(K)); }
-  p.total = p.mm + (M > kF8FewRows ? f8_plan(M, N, K).part : 0);
+  p.total = p.mm + (p.raw ? 0 : f8_product_bytes(M, N, K));
   return p;
 }
 
@@ -161,20 +192,20 @@ template <class T> static void run_f8_pack(const T* x, int64_t ldx, int64_t R, i
 }
 
 // ------------------------------------------------------------------ backward of the linear layer
-struct F8GradPlan { size_t codes, scales, mm, xt, terms, part, total; int chunk, Np; };
+struct F8GradPlan { size_t codes, scales, mm, xt, terms, part, total; int chunk, copies, Np; };
 static F8GradPlan f8_grad_plan(int64_t M, int N, int K, int32_t dtype) {
   F8GradPlan p{};
   size_t o = 0;
   auto take = [&](size_t n) { const size_t at = o; o += up256(n); return at; };
   p.codes = take((size_t)M * f8_code_pitch(N));
   p.scales = take((size_t)M * f8_scale_pitch(N));
-  size_t mm = 0;
-  if (M > kF8FewRows) mm = f8_plan(M, K, N).part;
-  p.mm = take(mm);
-  p.chunk = (int)(M < kGradChunk ? (M + 127) / 128 * 128 : kGradChunk);
+  p.mm = take(f8_product_bytes(M, K, N));
+  p.copies = dtype == RL_F32 ? kGradTerms : 1;
+  const int most = kGradChunk / p.copies / 128 * 128;
+  p.chunk = (int)(M < most ? (M + 127) / 128 * 128 : most);
   p.Np = (N + 7) / 8 * 8;
-  p.xt = take((size_t)p.chunk * ((K + 255) / 256 * 256) * 2);
-  p.terms = take((size_t)(dtype == RL_F32 ? 3 : 1) * p.chunk * p.Np * 2);
+  p.xt = take((size_t)p.copies * p.chunk * ((K + 255) / 256 * 256) * 2);
+  p.terms = take((size_t)p.copies * p.chunk * p.Np * 2);
   const int tm = (K + kBM - 1) / kBM, tn = (p.Np + kBN - 1) / kBN;
   const int64_t slices = (int64_t)tm * tn < 2 * kHotSlots ? 2 * kHotSlots / (tm * tn) : 1;
   p.part = take(slices > 1 ? (size_t)(slices < kMaxSplit ? slices : kMaxSplit) * N * ((K + 3) / 4 * 4) * 4 : 0);
@@ -187,24 +218,22 @@ static void run_f8_weight_grad(const T* dy, int64_t lddy, int64_t M, int N, int 
                                unsigned char* ws, const F8GradPlan& p, hipStream_t s) {
   bf16_t* xt = (bf16_t*)(ws + p.xt);
   bf16_t* terms = (bf16_t*)(ws + p.terms);
+  // bf16 rows that lie on 16 bytes are read where they are, others and f32 go through the workspace
   const bool direct = sizeof(T) == 2 && N % 8 == 0 && lddy % 8 == 0 && !off(dy, 16) && lddy < (1 << 23);
   for (int64_t t0 = 0; t0 < M; t0 += p.chunk) {
     const int tokens = (int)(M - t0 < p.chunk ? M - t0 : p.chunk), pad = (tokens + 127) / 128 * 128;
-    f8_restore_t_kernel<<<dim3(pad / 64, f8_blocks(K)), 256, 0, s>>>(x.codes + t0 * x.Kp, x.scales + t0 * x.Ks, fx, tokens, x.Kp, x.Ks, xt, pad);
-    if (!direct) f8_grad_terms_kernel<T><<<blocks_of(((int64_t)tokens * p.Np / 8 + 255) / 256, 8192), 256, 0, s>>>(dy + t0 * lddy, lddy, tokens, N, p.Np, terms);
-    for (int k = sizeof(T) == 4 ? 2 : 0; k >= 0; --k) {            // the smallest term first
-      GemmDims d{};
-      d.M = K; d.N = direct ? N : p.Np; d.K = pad; d.lda = pad; d.ldb = direct ? lddy : p.Np;
-      d.group_m = 8; d.split_slots = kHotSlots; d.b_k_rows = tokens;
-      const bf16_t* B = direct ? (const bf16_t*)(dy + t0 * lddy) : terms + (int64_t)k * tokens * p.Np;
-      const bool add = accumulate || t0 > 0 || (sizeof(T) == 4 && k < 2);
-      const int tm = (d.M + kBM - 1) / kBM, tn = (d.N + kBN - 1) / kBN;
-      const SplitK sk = split_k_host(tm * tn, pad / 64 / 2, kHotSlots, 0);
-      const int64_t ldp = (K + 3) / 4 * 4;
-      const EpiF8Grad e{dW, lddw, N, K, add, (float*)(ws + p.part), ldp};
-      f8_grad_kernel<TuneDX><<<split_launch(tm, tn, kHotSlots), 256, 0, s>>>(xt, B, d, e);
-      if (sk.slices > 1) f8_grad_slices_kernel<<<blocks_of(((int64_t)N * (ldp / 4) + 255) / 256, 4096), 256, 0, s>>>(e.part, sk.slices, N, K, ldp, dW, lddw, add);
-    }
+    f8_restore_t_kernel<<<dim3(pad / 64, f8_blocks(K)), 256, 0, s>>>(x.codes + t0 * x.Kp, x.scales + t0 * x.Ks, fx, tokens, x.Kp, x.Ks, xt, pad, p.copies);
+    if (!direct) f8_grad_terms_kernel<T><<<blocks_of(((int64_t)pad * p.Np / 8 + 255) / 256, 8192), 256, 0, s>>>(dy + t0 * lddy, lddy, tokens, pad, N, p.Np, terms);
+    GemmDims d{};
+    d.M = K; d.N = direct ? N : p.Np; d.K = p.copies * pad; d.lda = d.K; d.ldb = direct ? lddy : p.Np;
+    d.group_m = 8; d.split_slots = kHotSlots; d.b_k_rows = direct ? tokens : d.K;
+    const bool add = accumulate || t0 > 0;
+    const int tm = (d.M + kBM - 1) / kBM, tn = (d.N + kBN - 1) / kBN;
+    const SplitK sk = split_k_host(tm * tn, d.K / 64 / 2, kHotSlots, 0);
+    const int64_t ldp = (K + 3) / 4 * 4;
+    const EpiF8Grad e{dW, lddw, N, K, add, (float*)(ws + p.part), ldp};
+    f8_grad_kernel<TuneDX><<<split_launch(tm, tn, kHotSlots), 256, 0, s>>>(xt, direct ? (const bf16_t*)(dy + t0 * lddy) : terms, d, e);
+    if (sk.slices > 1) f8_grad_slices_kernel<<<blocks_of(((int64_t)N * (ldp / 4) + 255) / 256, 4096), 256, 0, s>>>(e.part, sk.slices, N, K, ldp, dW, lddw, add);
   }
 }
 
@@ -311,7 +340,7 @@ rl_status rl_f8_pack_weight(const void* w, int64_t ldw, int32_t dtype, int32_t N
 rl_status rl_f8_matmul_workspace_bytes(int64_t M, int32_t N, int32_t K, size_t* bytes) {
   if (!bytes) return RL_ERR_NULL;
   if (bad_product(M, N, K)) return RL_ERR_SHAPE;
-  *bytes = M > kF8FewRows ? f8_plan(M, N, K).part : 0;
+  *bytes = f8_product_bytes(M, N, K);
   return RL_OK;
 }
 
