@@ -448,13 +448,60 @@ def rl_rvq_encode(vectors, codebooks, norms=None, want_residual=True, count_exac
 F8_FORMATS = {"e4m3": 0, "e5m2": 1}
 
 
-@dataclass
+def _f8_pitch(cols: int):
+    """Bytes of a row of codes and of scales."""
+    blocks = (cols + 127) // 128
+    return blocks * 128, (blocks + 3) // 4 * 4
+
+
 class F8Rows:
-    """A matrix [rows, cols] in 8-bit rows: codes uint8 [rows, cols rounded up to 128], scales uint8 [rows, blocks rounded up to 4]."""
-    codes: torch.Tensor
-    scales: torch.Tensor
-    cols: int
-    fmt: str = "e4m3"
+    """A matrix [rows, cols] in 8-bit rows: codes uint8 [rows, cols rounded up to 128], scales uint8 [rows, blocks rounded up to 4].  What the library packs
+    lies in one buffer (an allocation less a call), of which `codes` and `scales` are views."""
+    __slots__ = ("rows", "cols", "fmt", "_codes", "_scales", "_buffer")
+
+    def __init__(self, codes: torch.Tensor, scales: torch.Tensor, cols: int, fmt: str = "e4m3"):
+        if fmt not in F8_FORMATS:
+            raise ValueError(f"format must be one of {sorted(F8_FORMATS)}, got {fmt!r}")
+        self.rows, self.cols, self.fmt, self._codes, self._scales, self._buffer = codes.shape[0], cols, fmt, codes, scales, None
+
+    @classmethod
+    def empty(cls, rows: int, cols: int, fmt: str, like: torch.Tensor) -> "F8Rows":
+        """Room for such a matrix on the device of `like`."""
+        if fmt not in F8_FORMATS:
+            raise ValueError(f"format must be one of {sorted(F8_FORMATS)}, got {fmt!r}")
+        p = cls.__new__(cls)
+        kp, ks = _f8_pitch(cols)
+        p.rows, p.cols, p.fmt, p._codes, p._scales = rows, cols, fmt, None, None
+        p._buffer = like.new_empty(rows * (kp + ks), dtype=torch.uint8)
+        return p
+
+    @property
+    def codes(self) -> torch.Tensor:
+        if self._codes is None:
+            kp = _f8_pitch(self.cols)[0]
+            self._codes = self._buffer[:self.rows * kp].view(self.rows, kp)
+        return self._codes
+
+    @property
+    def scales(self) -> torch.Tensor:
+        if self._scales is None:
+            kp, ks = _f8_pitch(self.cols)
+            self._scales = self._buffer[self.rows * kp:].view(self.rows, ks)
+        return self._scales
+
+    @property
+    def device(self):
+        return (self._codes if self._buffer is None else self._buffer).device
+
+    def _pointers(self, name: str):
+        """(codes, scales, format code)"""
+        kp, ks = _f8_pitch(self.cols)
+        if self._buffer is not None:
+            at = self._buffer.data_ptr()
+            return (at, at + self.rows * kp, F8_FORMATS[self.fmt]) if self.rows else (None, None, F8_FORMATS[self.fmt])
+        if self._codes.shape != (self.rows, kp) or self._scales.shape != (self.rows, ks):
+            raise ValueError(f"{name} must have codes [rows, {kp}] and scales [rows, {ks}]")
+        return _ptr(self._codes, torch.uint8, name=name + ".codes"), _ptr(self._scales, torch.uint8, name=name + ".scales"), F8_FORMATS[self.fmt]
 
 
 @dataclass
@@ -478,23 +525,11 @@ def _rows(t: torch.Tensor, name: str):
     return t.data_ptr(), ld, _dtype_code(t)
 
 
-def _f8_pitch(cols: int):
-    return (cols + 127) // 128 * 128, ((cols + 127) // 128 + 3) // 4 * 4
-
-
-def _f8_empty(rows: int, cols: int, fmt: str, device) -> F8Rows:
-    if fmt not in F8_FORMATS:
-        raise ValueError(f"format must be one of {sorted(F8_FORMATS)}, got {fmt!r}")
-    kp, ks = _f8_pitch(cols)
-    return F8Rows(torch.empty((rows, kp), dtype=torch.uint8, device=device), torch.empty((rows, ks), dtype=torch.uint8, device=device), cols, fmt)
-
-
 def _f8(p: F8Rows, rows: int, cols: int, name: str):
-    """(codes, scales, format) of packed rows that must be [rows, cols]."""
-    kp, ks = _f8_pitch(cols)
-    if p.cols != cols or p.codes.shape != (rows, kp) or p.scales.shape != (rows, ks):
-        raise ValueError(f"{name} must be 8-bit rows of [{rows}, {cols}]")
-    return _ptr(p.codes, torch.uint8, name=name + ".codes"), _ptr(p.scales, torch.uint8, name=name + ".scales"), F8_FORMATS[p.fmt]
+    """(codes, scales, format code) of packed rows that must be [rows, cols]."""
+    if p.cols != cols or p.rows != rows:
+        raise ValueError(f"{name} must be 8-bit rows of [{rows}, {cols}], got [{p.rows}, {p.cols}]")
+    return p._pointers(name)
 
 
 def _f8_workspace(query, *args):
@@ -534,8 +569,8 @@ def rl_layer_norm_forward(x, gamma, beta=None, eps=1e-5, checkpoint=None, out=No
         raise ValueError("gamma and beta must have one dtype")
     y, py, ldy = _output(out, x)
     stats = x.new_empty((R, 2), dtype=torch.float32)
-    kept = None if checkpoint is None else _f8_empty(R, H, checkpoint, x.device)
-    codes, scales, fmt = (None, None, 0) if kept is None else (kept.codes.data_ptr(), kept.scales.data_ptr(), F8_FORMATS[kept.fmt])
+    kept = None if checkpoint is None else F8Rows.empty(R, H, checkpoint, x)
+    codes, scales, fmt = (None, None, 0) if kept is None else kept._pointers("checkpoint")
     _check(lib().rl_layer_norm_forward(px, ldx, dt, R, H, _ptr(gamma, numel=H, name="gamma"), _ptr(beta, numel=H, name="beta"), _dtype_code(gamma), float(eps),
                                        py, ldy, stats.data_ptr(), codes, scales, fmt, _stream_handle()))
     return y, stats, kept
@@ -568,17 +603,17 @@ def rl_f8_pack(x, fmt="e4m3") -> F8Rows:
     """x [R, K] in 8-bit rows: a scale (a power of two) for 128 consecutive values of a row."""
     R, K = x.shape
     px, ldx, dt = _rows(x, "x")
-    p = _f8_empty(R, K, fmt, x.device)
-    _check(lib().rl_f8_pack(px, ldx, dt, R, K, F8_FORMATS[fmt], p.codes.data_ptr(), p.scales.data_ptr(), _stream_handle()))
+    p = F8Rows.empty(R, K, fmt, x)
+    codes, scales, code = p._pointers("p")
+    _check(lib().rl_f8_pack(px, ldx, dt, R, K, code, codes, scales, _stream_handle()))
     return p
 
 
 def rl_f8_unpack(p: F8Rows, dtype=torch.bfloat16):
     """The values [R, K] of 8-bit rows."""
-    R = p.codes.shape[0]
-    codes, scales, fmt = _f8(p, R, p.cols, "p")
-    x = torch.empty((R, p.cols), dtype=dtype, device=p.codes.device)
-    _check(lib().rl_f8_unpack(codes, scales, fmt, R, p.cols, x.data_ptr(), p.cols, _dtype_code(x), _stream_handle()))
+    codes, scales, fmt = p._pointers("p")
+    x = torch.empty((p.rows, p.cols), dtype=dtype, device=p.device)
+    _check(lib().rl_f8_unpack(codes, scales, fmt, p.rows, p.cols, x.data_ptr(), p.cols, _dtype_code(x), _stream_handle()))
     return x
 
 
@@ -586,19 +621,20 @@ def rl_f8_pack_weight(w, fmt="e4m3", transposed=True) -> F8Weight:
     """A weight [N, K] packed for the linear layer, one scale for 128 x 128 values; with its transpose for the backward pass."""
     N, K = w.shape
     pw, ldw, dt = _rows(w, "w")
-    rows = _f8_empty(N, K, fmt, w.device)
-    cols = _f8_empty(K, N, fmt, w.device) if transposed else None
-    _check(lib().rl_f8_pack_weight(pw, ldw, dt, N, K, F8_FORMATS[fmt], rows.codes.data_ptr(), rows.scales.data_ptr(),
-                                   cols.codes.data_ptr() if transposed else None, cols.scales.data_ptr() if transposed else None, _stream_handle()))
+    rows = F8Rows.empty(N, K, fmt, w)
+    cols = F8Rows.empty(K, N, fmt, w) if transposed else None
+    codes, scales, code = rows._pointers("w")
+    codes_t, scales_t, _ = cols._pointers("w") if transposed else (None, None, 0)
+    _check(lib().rl_f8_pack_weight(pw, ldw, dt, N, K, code, codes, scales, codes_t, scales_t, _stream_handle()))
     return F8Weight(rows, cols)
 
 
 def rl_f8_matmul(a: F8Rows, b: F8Rows, dtype=torch.bfloat16):
     """a [M, K] times the transpose of b [N, K], both in 8-bit rows; sums in float32."""
-    M, N, K = a.codes.shape[0], b.codes.shape[0], a.cols
+    M, N, K = a.rows, b.rows, a.cols
     ca, sa, fa = _f8(a, M, K, "a")
     cb, sb, fb = _f8(b, N, K, "b")
-    y = torch.empty((M, N), dtype=dtype, device=a.codes.device)
+    y = torch.empty((M, N), dtype=dtype, device=a.device)
     ws, pws, nws = _f8_workspace(lib().rl_f8_matmul_workspace_bytes, M, N, K, y.device)
     _check(lib().rl_f8_matmul(ca, sa, fa, cb, sb, fb, M, N, K, y.data_ptr(), N, _dtype_code(y), pws, nws, _stream_handle()))
     return y
@@ -607,16 +643,17 @@ def rl_f8_matmul(a: F8Rows, b: F8Rows, dtype=torch.bfloat16):
 def rl_f8_linear_forward(x, w: F8Weight, fmt="e4m3", keep=True):
     """(y, kept): y = pack(x) W^T in the dtype of x, and the packed x for the backward pass (keep=False: None)."""
     M, K = x.shape
-    N = w.rows.codes.shape[0]
+    N = w.rows.rows
     px, ldx, dt = _rows(x, "x")
     cw, sw, fw = _f8(w.rows, N, K, "w.rows")
     if fmt not in F8_FORMATS:
         raise ValueError(f"format must be one of {sorted(F8_FORMATS)}, got {fmt!r}")
-    kept = _f8_empty(M, K, fmt, x.device) if keep else None
+    kept = F8Rows.empty(M, K, fmt, x) if keep else None
+    codes, scales, _ = kept._pointers("kept") if keep else (None, None, 0)
     y = x.new_empty((M, N))
     ws, pws, nws = _f8_workspace(lib().rl_f8_linear_forward_workspace_bytes, M, N, K, 1 if keep else 0, x.device)
     _check(lib().rl_f8_linear_forward(px, ldx, dt, M, K, F8_FORMATS[fmt], cw, sw, fw, N, y.data_ptr(), N,
-                                      kept.codes.data_ptr() if keep else None, kept.scales.data_ptr() if keep else None, pws, nws, _stream_handle()))
+                                      codes, scales, pws, nws, _stream_handle()))
     return y, kept
 
 
