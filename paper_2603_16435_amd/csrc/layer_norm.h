@@ -34,13 +34,20 @@ __device__ __attribute__((always_inline)) inline float wave_sum(float x) {
 template <int TW, int CH> struct Pieces {
   int c0, H, part;                   // part: columns of the lane's piece that is not whole, 0 if it has none
   int part_c;                        // that piece
+  int held;                          // pieces of the wavefront that hold any column (uniform); the others are left out where that pays
   __device__ Pieces(int w, int lane, int H_) : c0((w * 64 + lane) * 8), H(H_) {
     const int p = H / 8;
+    held = 0;
+#pragma unroll
+    for (int c = 0; c < CH; ++c) held += (c * TW + w) * 512 < H ? 1 : 0;
     part_c = p / (TW * 64);
     part = p % (TW * 64) == w * 64 + lane ? H % 8 : 0;
   }
   __device__ __attribute__((always_inline)) int col(int c) const { return c0 + c * TW * 512; }
   __device__ __attribute__((always_inline)) bool whole(int c) const { return col(c) + 8 <= H; }
+  // Eight wavefronts a team: with 5120 columns six of them have one piece (16000 rows, forward 72 -> 66 us).  Fewer: the branch costs more than it saves (3584 columns, backward from
+  // a checkpoint 114 -> 128).
+  __device__ __attribute__((always_inline)) bool has(int c) const { return TW < 8 || c < held; }
   template <class T> __device__ __attribute__((always_inline)) void load(const T* row, bool there, Raw8<T> (&r)[CH]) const {
 #pragma unroll
     for (int c = 0; c < CH; ++c) {
@@ -108,27 +115,39 @@ __global__ __launch_bounds__(norm_threads(TW)) void ln_forward_kernel(NormFwd<T>
   };
   const int mine = columns(w);
   const float inv_mine = mine > 0 ? 1.f / (float)mine : 0.f;
+  const int peer = lane < TW ? columns(lane) : 0;    // lane i joins what wavefront i found
+  const float peer_n = (float)peer, inv_peer = peer > 0 ? 1.f / peer_n : 0.f;
   float gamma[CH][8], beta[CH][8];
   at.params(j.p.gamma, j.p.bf16, gamma);
   at.params(j.p.beta, j.p.bf16, beta);
   int flip = 0;
+  constexpr bool AHEAD = TW == 8;                    // the next row on its way while one is worked on: 16000 rows of 5120 72 -> 65 us; 32749 of 3584 88 -> 93
+  Raw8<T> ahead[AHEAD ? CH : 1];
+  if constexpr (AHEAD) at.load(j.x + (int64_t)(team < j.R ? team : 0) * j.ldx, true, ahead);
   for (int64_t row = team; row < j.R; row += teams) {
     Raw8<T> r[CH];
-    at.load(j.x + row * j.ldx, true, r);
+    if constexpr (AHEAD) {
+#pragma unroll
+      for (int c = 0; c < CH; ++c) r[c] = ahead[c];
+      if (row + teams < j.R) at.load(j.x + (row + teams) * j.ldx, true, ahead);
+    } else at.load(j.x + row * j.ldx, true, r);
     float a = 0.f;
 #pragma unroll
     for (int c = 0; c < CH; ++c)
+      if (at.has(c)) {
 #pragma unroll
-      for (int e = 0; e < 8; ++e) a += raw_get(r[c], e);
+        for (int e = 0; e < 8; ++e) a += raw_get(r[c], e);
+      }
     const float sum = wave_sum(a), m = sum * inv_mine;
     a = 0.f;
 #pragma unroll
-    for (int c = 0; c < CH; ++c) {
-      float t = 0.f;
+    for (int c = 0; c < CH; ++c)
+      if (at.has(c)) {
+        float t = 0.f;
 #pragma unroll
-      for (int e = 0; e < 8; ++e) { const float d = raw_get(r[c], e) - m; t += d * d; }
-      a += at.whole(c) ? t : 0.f;
-    }
+        for (int e = 0; e < 8; ++e) { const float d = raw_get(r[c], e) - m; t += d * d; }
+        a += at.whole(c) ? t : 0.f;
+      }
     if (at.part) {
       Raw8<T> t = r[0];
 #pragma unroll
@@ -140,37 +159,32 @@ __global__ __launch_bounds__(norm_threads(TW)) void ln_forward_kernel(NormFwd<T>
     if constexpr (TW > 1) {
       if (lane == 0) red[flip][w] = make_float2(sum, sq);
       __syncthreads();
-      float2 p[TW];
-      float all = 0.f;
-#pragma unroll
-      for (int i = 0; i < TW; ++i) { p[i] = red[flip][i]; all += p[i].x; }
-      mean = all * inv_h; sq = 0.f;
-#pragma unroll
-      for (int i = 0; i < TW; ++i) {
-        const int n = columns(i);
-        const float d = n > 0 ? p[i].x * (1.f / (float)n) - mean : 0.f;
-        sq += p[i].y + (float)n * d * d;
-      }
+      const float2 p = red[flip][lane < TW ? lane : 0];
+      mean = wave_sum(lane < TW ? p.x : 0.f) * inv_h;
+      const float d = p.x * inv_peer - mean;
+      sq = wave_sum(peer > 0 ? p.y + peer_n * d * d : 0.f);
       flip ^= 1;                                     // two sets: a wavefront that is ahead writes the other one
     }
     const float rstd = 1.f / sqrtf(sq * inv_h + j.eps);
     if (j.stats && w == 0 && lane == 0) j.stats[row] = make_float2(mean, rstd);
     if (j.ckpt.codes) {
 #pragma unroll
-      for (int c = 0; c < CH; ++c) {
-        float x[8];
+      for (int c = 0; c < CH; ++c)
+        if (at.has(c)) {
+          float x[8];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) x[e] = raw_get(r[c], e);
-        f8_pack_wave(j.ckpt, row, at.col(c), lane, x);
+          for (int e = 0; e < 8; ++e) x[e] = raw_get(r[c], e);
+          f8_pack_wave(j.ckpt, row, at.col(c), lane, x);
+        }
+    }
+#pragma unroll
+    for (int c = 0; c < CH; ++c)
+      if (at.has(c)) {
+        float v[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = (raw_get(r[c], e) - mean) * rstd * gamma[c][e] + beta[c][e];
+        r[c] = raw_make<T>(v);
       }
-    }
-#pragma unroll
-    for (int c = 0; c < CH; ++c) {
-      float v[8];
-#pragma unroll
-      for (int e = 0; e < 8; ++e) v[e] = (raw_get(r[c], e) - mean) * rstd * gamma[c][e] + beta[c][e];
-      r[c] = raw_make<T>(v);
-    }
     at.store(j.y + row * j.ldy, r);
   }
 }
@@ -223,16 +237,17 @@ __device__ __attribute__((always_inline)) inline void ln_backward_rows(const Nor
     };
     float a = 0.f, b = 0.f;                          // mean(g), mean(g xh)
 #pragma unroll
-    for (int c = 0; c < CH; ++c) {
-      float xh[8];
-      normal(c, xh);
+    for (int c = 0; c < CH; ++c)
+      if (at.has(c)) {
+        float xh[8];
+        normal(c, xh);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const float d = raw_get(ry[c], e), g = d * gamma[c][e];
-        a += g; b += g * xh[e];
-        if constexpr (SUMS) { dg[c][e] += d * xh[e]; db[c][e] += d; }
+        for (int e = 0; e < 8; ++e) {
+          const float d = raw_get(ry[c], e), g = d * gamma[c][e];
+          a += g; b += g * xh[e];
+          if constexpr (SUMS) { dg[c][e] += d * xh[e]; db[c][e] += d; }
+        }
       }
-    }
     a = wave_sum(a); b = wave_sum(b);
     if constexpr (TW > 1) {
       if (lane == 0) red[flip][w] = make_float2(a, b);
@@ -245,13 +260,14 @@ __device__ __attribute__((always_inline)) inline void ln_backward_rows(const Nor
     const float ma = a * inv_h, mb = b * inv_h;
     Raw8<T> out[CH];
 #pragma unroll
-    for (int c = 0; c < CH; ++c) {
-      float xh[8], v[8];
-      normal(c, xh);
+    for (int c = 0; c < CH; ++c)
+      if (at.has(c)) {
+        float xh[8], v[8];
+        normal(c, xh);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) v[e] = st.y * (raw_get(ry[c], e) * gamma[c][e] - ma - xh[e] * mb);
-      out[c] = raw_make<T>(v);
-    }
+        for (int e = 0; e < 8; ++e) v[e] = st.y * (raw_get(ry[c], e) * gamma[c][e] - ma - xh[e] * mb);
+        out[c] = raw_make<T>(v);
+      }
     at.store(j.dx + row * j.lddx, out);
   }
   if constexpr (SUMS) {

@@ -44,30 +44,33 @@ template <class F> static void with_team(int H, F f) {
   else f(std::integral_constant<int, 16>(), I2());
 }
 
-// Workgroups: as many as are of use to cover the loads' latency, few enough that most walk equally many rows.  us, bf16, 512 / 1024 / 2048 / 4096 workgroups: 32749 rows of
-// 3584 120 / 94 / 93 / 92, with the checkpoint 170 / 124 / 124 / 118 (one a row: 162); 5003 rows of 1160 12.9 / 10.7 / 10.1, one a row 11.7.
+// Workgroups: five a CU, each walking rows.  us, bf16, 768 / 1024 / 1280 workgroups: 32749 rows of 3584 89 / 88 / 87, with the checkpoint 124 / 117 / 118 (2048: 124, one a row: 162);
+// 5003 rows of 1157 13.6 / 12.5 / 11.5 and 17.0 / 15.2 / 14.6; 3000 rows of 3584 11.3 / 10.5 / 9.9 and 14.8 / 14.2 / 13.1; 16000 rows of 5120 66 / 65 / 65 and 102 / 94 / 98.
+constexpr int kNormBlocks = 1280;
 template <class T>
 static void run_norm_forward(const NormFwd<T>& j, hipStream_t s) {
   with_team(j.H, [&](auto tw, auto ch) {
     constexpr int TW = tw.value, CH = ch.value, NT = norm_threads(TW), TEAMS = NT / (TW * 64);
     const int64_t blocks = (j.R + TEAMS - 1) / TEAMS;
-    ln_forward_kernel<T, TW, CH><<<blocks_of(blocks, blocks > 8192 ? 4096 : 2048), NT, 0, s>>>(j);
+    ln_forward_kernel<T, TW, CH><<<blocks_of(blocks, kNormBlocks), NT, 0, s>>>(j);
   });
 }
 
 // Backward: one launch up to kNormFewRows rows.  us, 3584 columns, one launch / two: 128 rows 3.8 / 4.3 + 2.7, 256 5.6 / 5.3 + 3.0, 512 8.9 / 7.3 + 3.4, 1024 21.3 / 8.8 + 3.5;
 // 768 columns, 512 rows 8.0 / 3.9 + 3.4; the host takes 3.5 for a launch.
-// Beyond, the teams' sums cost 8 bytes a column and workgroup, twice: two workgroups a CU from x, three from a checkpoint, whose loads are shorter (32749 rows of 3584,
-// 384 / 512 / 768 / 1024 workgroups: 148 / 126 / 134 / 140 and 169 / 133 / 114 / 141), and four rows a team at least where a wavefront has a row to itself (2175 rows of 768, f32:
-// 128 / 256 / 384 workgroups 6.7 + 3.3 / 5.8 + 4.2 / 6.1 + 5.2).
+// Beyond, the teams' sums cost 8 bytes a column and workgroup, twice, so there are only as many workgroups as keep the loads going: by the registers of a lane, four a CU up to 2048
+// columns (5003 rows of 1157, 512 / 768 / 1024 workgroups 24.9 / 20.6 / 17.7 us, from a checkpoint 20.3 / 16.9 / 15.2), two up to 4096 (32749 rows of 3584 125 / 134 / 138), three from a
+// checkpoint, whose loads are shorter (133 / 114 / 141), two up to 8192 (16000 rows of 5120 93 / 107 / 101 and 95 / 112 / 98), one beyond (6000 rows of 12000, 256 / 512 92 / 98); two where
+// a wavefront has a row to itself (20000 rows of 1000 22.4 / 23.3 / 24.4), with four rows each at least (2175 rows of 768, f32, 128 / 256 / 384 workgroups, with the sum 6.7 + 3.3 / 5.8 + 4.2 /
+// 6.1 + 5.2).
 constexpr int kNormFewRows = 512;
 static int norm_pitch(int H) { return (H + 7) / 8 * 8; }
 struct NormTeams { int blocks, teams; };
 static NormTeams norm_teams(int64_t R, int H, bool ck) {
   NormTeams t{0, 0};
-  if (R > kNormFewRows) with_team(H, [&](auto tw, auto) {
-    constexpr int TEAMS = norm_threads(tw.value) / (tw.value * 64), PER = TEAMS > 1 ? 4 * TEAMS : 1;
-    t.blocks = (int)blocks_of((R + PER - 1) / PER, ck ? 768 : 512);
+  if (R > kNormFewRows) with_team(H, [&](auto tw, auto ch) {
+    constexpr int TW = tw.value, TEAMS = norm_threads(TW) / (TW * 64), PER = TEAMS > 1 ? 4 * TEAMS : 1;
+    t.blocks = (int)blocks_of((R + PER - 1) / PER, TW == 16 ? 256 : TW != 4 ? 512 : ch.value == 1 ? 1024 : ck ? 768 : 512);
     t.teams = t.blocks * TEAMS;
   });
   return t;
