@@ -16,23 +16,29 @@ namespace rlk {
 constexpr int kGradChunk = 32768;         // tokens restored at a time, with their copies
 constexpr int kGradTerms = 3;
 
-// x^T of a chunk: a workgroup restores 64 tokens x 128 k and writes 128 rows of 64 tokens, whole lines.  `pad` tokens in all, a multiple of 128; `copies` of them side by side.
-__global__ __launch_bounds__(256) void f8_restore_t_kernel(const uint8_t* codes, const uint8_t* scales, int fmt, int tokens, int Kp, int Ks, bf16_t* xt, int pad, int copies) {
+// What the two contractions of the backward pass read, in one launch: workgroups [0, pack_blocks) pack dy, the next restore_blocks restore x^T of a chunk, the rest copy dy.
+template <class T> struct F8GradPrep {
+  const T* dy; int64_t lddy, M; int N; F8Out packed; int pack_blocks;          // all rows of dy
+  const uint8_t *codes, *scales; int fmt, tokens, Kp, Ks; bf16_t* xt; int pad, copies, restore_blocks;          // `pad` tokens, a multiple of 128; `copies` of them side by side
+  const T* chunk; int Np; bf16_t* terms;                                       // rows of dy of the chunk
+};
+
+// x^T: a workgroup restores 64 tokens x 128 k and writes 128 rows of 64 tokens, whole lines.
+template <class T> __device__ __attribute__((always_inline)) inline void f8_restore_t(const F8GradPrep<T>& j, int block, bf16_t* lds) {
   constexpr int kPitch = 66;              // elements of a row in LDS
-  __shared__ bf16_t lds[128 * kPitch];
-  const int t0 = blockIdx.x * 64, k0 = blockIdx.y * 128, tid = threadIdx.x, c = (tid & 15) * 8;
+  const int across = j.pad / 64, kb = block / across, t0 = (block - kb * across) * 64, k0 = kb * 128, tid = threadIdx.x, c = (tid & 15) * 8;
   u32x2_t code[4];
   unsigned s[4];
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     const int t = t0 + i * 16 + (tid >> 4);
     code[i] = u32x2_t{0, 0}; s[i] = 127;
-    if (t < tokens) { code[i] = *reinterpret_cast<const u32x2_t*>(codes + (int64_t)t * Kp + k0 + c); s[i] = scales[(int64_t)t * Ks + blockIdx.y]; }
+    if (t < j.tokens) { code[i] = *reinterpret_cast<const u32x2_t*>(j.codes + (int64_t)t * j.Kp + k0 + c); s[i] = j.scales[(int64_t)t * j.Ks + kb]; }
   }
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     float v[8];
-    f8_restore8(code[i], s[i], fmt, v);
+    f8_restore8(code[i], s[i], j.fmt, v);
 #pragma unroll
     for (int e = 0; e < 8; ++e) lds[(c + e) * kPitch + i * 16 + (tid >> 4)] = (bf16_t)v[e];
   }
@@ -42,27 +48,26 @@ __global__ __launch_bounds__(256) void f8_restore_t_kernel(const uint8_t* codes,
     const int k = i * 32 + (tid >> 3), t = (tid & 7) * 8;
     const unsigned* p = reinterpret_cast<const unsigned*>(lds + k * kPitch + t);       // (4-byte aligned: the pitch is even)
     const u32x4_t v = {p[0], p[1], p[2], p[3]};
-    for (int c = 0; c < copies; ++c) *reinterpret_cast<u32x4_t*>(xt + tiled_index(k0 + k, c * pad + t0 + t, (int64_t)copies * pad)) = v;
+    for (int q = 0; q < j.copies; ++q) *reinterpret_cast<u32x4_t*>(j.xt + tiled_index(k0 + k, q * j.pad + t0 + t, (int64_t)j.copies * j.pad)) = v;
   }
 }
 
 // dy of a chunk into aligned rows of bf16, `pad` of them with zeros past the last token: as it is, or in three terms of as many rows each, the smallest first.
-template <class T>
-__global__ __launch_bounds__(256) void f8_grad_terms_kernel(const T* dy, int64_t ld, int tokens, int pad, int N, int Np, bf16_t* out) {
+template <class T> __device__ __attribute__((always_inline)) inline void f8_grad_terms(const F8GradPrep<T>& j, int block, int blocks) {
   constexpr int TERMS = sizeof(T) == 4 ? kGradTerms : 1;
-  const int chunks = Np / 8;
-  const int64_t all = (int64_t)pad * chunks, term = (int64_t)pad * Np;
-  for (int64_t q = (int64_t)blockIdx.x * 256 + threadIdx.x; q < all; q += (int64_t)gridDim.x * 256) {
+  const int chunks = j.Np / 8;
+  const int64_t all = (int64_t)j.pad * chunks, term = (int64_t)j.pad * j.Np;
+  for (int64_t q = (int64_t)block * 256 + threadIdx.x; q < all; q += (int64_t)blocks * 256) {
     const int64_t t = q / chunks;
     const int n = (int)(q - t * chunks) * 8;
-    const Raw8<T> r = raw_load(dy + t * ld + n, t < tokens ? N - n : 0);
+    const Raw8<T> r = raw_load(j.chunk + t * j.lddy + n, t < j.tokens ? j.N - n : 0);
     float v[8];
 #pragma unroll
     for (int e = 0; e < 8; ++e) v[e] = raw_get(r, e);
 #pragma unroll
     for (int k = TERMS - 1; k >= 0; --k) {
       const Raw8<bf16_t> b = raw_make<bf16_t>(v);
-      *reinterpret_cast<u32x4_t*>(out + k * term + t * Np + n) = b.v;
+      *reinterpret_cast<u32x4_t*>(j.terms + k * term + t * j.Np + n) = b.v;
       if constexpr (TERMS > 1) {
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
@@ -74,6 +79,15 @@ __global__ __launch_bounds__(256) void f8_grad_terms_kernel(const T* dy, int64_t
   }
 }
 
+template <class T>
+__global__ __launch_bounds__(256) void f8_grad_prep_kernel(F8GradPrep<T> j) {
+  __shared__ bf16_t lds[128 * 66];
+  const int b = blockIdx.x;
+  if (b < j.pack_blocks) f8_pack_rows(j.dy, j.M, j.lddy, j.N, j.packed, b, j.pack_blocks);
+  else if (b < j.pack_blocks + j.restore_blocks) f8_restore_t(j, b - j.pack_blocks, lds);
+  else f8_grad_terms(j, b - j.pack_blocks - j.restore_blocks, (int)gridDim.x - j.pack_blocks - j.restore_blocks);
+}
+
 // Tile of dW^T, written as dW; or a slice's share of it to the workspace, [slice][N][ldw] likewise.
 struct EpiF8Grad {
   typedef NoPre Pre;
@@ -83,33 +97,47 @@ struct EpiF8Grad {
   float* dW; int64_t ldw; int N, K; int accumulate;
   float* part; int64_t ldp;                   // slices: rows of ldp floats
 
-  template <int MB, int NB, bool ACC, bool EDGE>
+  // A lane holds four consecutive k of one row of dW in each of two neighbouring blocks, a pair of lanes thus two rows: they swap halves, so that a store writes eight rows
+  // in whole lines of 128 bytes instead of sixteen in halves, past the caches (NT) where the rows lie on lines.  256 KB a tile: with few tokens it is what a tile waits for.
+  template <int MB, int NB, bool ACC, bool EDGE, bool NT>
   __device__ __attribute__((always_inline)) void tile(floatx4 (&acc)[MB][NB], const TileCtx& c, float* out, int64_t ld) const {
-    const int col = c.lane & 15, g = c.lane >> 4;
+    const int r = c.lane & 15, p = r & 1, k0 = c.m0 + p * 16 + (c.lane >> 4) * 4;
 #pragma unroll
     for (int bj = 0; bj < NB; ++bj) {
-      const int n = c.n0 + bj * 16 + col;
-      float* q = out + (int64_t)n * ld + c.m0 + g * 4;
-      floatx4 old[MB];
+      const int n = c.n0 + bj * 16 + (r & ~1);                       // the pair's first row
+      float* const q[2] = {out + (int64_t)n * ld + k0, out + (int64_t)(n + 1) * ld + k0};
+      auto left = [&](int w, int i) __attribute__((always_inline)) { return !EDGE ? 4 : n + w < N ? K - k0 - i * 32 : 0; };
+      floatx4 old[2][MB / 2];
       if (ACC) {
 #pragma unroll
-        for (int bi = 0; bi < MB; ++bi) {
-          if (!EDGE) old[bi] = *reinterpret_cast<const floatx4_any*>(q + bi * 16);
-          else {
+        for (int i = 0; i < MB / 2; ++i)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) old[bi][e] = n < N && c.m0 + bi * 16 + g * 4 + e < K ? q[bi * 16 + e] : 0.f;
+          for (int w = 0; w < 2; ++w) {
+            if (left(w, i) >= 4) old[w][i] = *reinterpret_cast<const floatx4_any*>(q[w] + i * 32);
+            else {
+#pragma unroll
+              for (int e = 0; e < 4; ++e) old[w][i][e] = e < left(w, i) ? q[w][i * 32 + e] : 0.f;
+            }
           }
-        }
       }
 #pragma unroll
-      for (int bi = 0; bi < MB; ++bi) {
-        floatx4 v;
+      for (int i = 0; i < MB / 2; ++i) {
+        floatx4 v[2];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) { v[e] = acc_read<true>(acc[bi][bj], e); if (ACC) v[e] += old[bi][e]; }
-        if (!EDGE) *reinterpret_cast<floatx4_any*>(q + bi * 16) = v;
-        else {
+        for (int e = 0; e < 4; ++e) {
+          const float a = acc_read<true>(acc[2 * i][bj], e), b = acc_read<true>(acc[2 * i + 1][bj], e);
+          const float recv = __uint_as_float((unsigned)__builtin_amdgcn_mov_dpp((int)__float_as_uint(p ? a : b), 0xB1, 0xF, 0xF, true));
+          v[0][e] = p ? recv : a; v[1][e] = p ? b : recv;
+          if (ACC) { v[0][e] += old[0][i][e]; v[1][e] += old[1][i][e]; }
+        }
 #pragma unroll
-          for (int e = 0; e < 4; ++e) if (n < N && c.m0 + bi * 16 + g * 4 + e < K) q[bi * 16 + e] = v[e];
+        for (int w = 0; w < 2; ++w) {
+          if (NT) __builtin_nontemporal_store(v[w], reinterpret_cast<floatx4*>(q[w] + i * 32));
+          else if (left(w, i) >= 4) *reinterpret_cast<floatx4_any*>(q[w] + i * 32) = v[w];
+          else {
+#pragma unroll
+            for (int e = 0; e < 3; ++e) if (e < left(w, i)) q[w][i * 32 + e] = v[w][e];
+          }
         }
       }
     }
@@ -119,11 +147,12 @@ struct EpiF8Grad {
     const bool edge = c.m0 + MB * 16 > K || c.n0 + NB * 16 > N;
     if (c.slices > 1) {
       float* p = part + (int64_t)c.slice * N * ldp;
-      if (edge) tile<MB, NB, false, true>(acc, c, p, ldp); else tile<MB, NB, false, false>(acc, c, p, ldp);
+      if (edge) tile<MB, NB, false, true, false>(acc, c, p, ldp); else tile<MB, NB, false, false, false>(acc, c, p, ldp);
     } else if (accumulate) {
-      if (edge) tile<MB, NB, true, true>(acc, c, dW, ldw); else tile<MB, NB, true, false>(acc, c, dW, ldw);
+      if (edge) tile<MB, NB, true, true, false>(acc, c, dW, ldw); else tile<MB, NB, true, false, false>(acc, c, dW, ldw);
     } else {
-      if (edge) tile<MB, NB, false, true>(acc, c, dW, ldw); else tile<MB, NB, false, false>(acc, c, dW, ldw);
+      const bool lines = ldw % 32 == 0 && (reinterpret_cast<uintptr_t>(dW) & 127) == 0;
+      if (edge) tile<MB, NB, false, true, false>(acc, c, dW, ldw); else if (lines) tile<MB, NB, false, false, true>(acc, c, dW, ldw); else tile<MB, NB, false, false, false>(acc, c, dW, ldw);
     }
   }
 };

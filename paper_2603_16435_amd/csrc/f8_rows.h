@@ -180,10 +180,10 @@ __device__ __attribute__((always_inline)) inline void f8_pack_wave(const F8Out& 
 constexpr int kF8Steps = 4;
 
 template <class T>
-__global__ __launch_bounds__(256) void f8_pack_kernel(const T* x, int64_t R, int64_t ldx, int K, F8Out o) {
+__device__ __attribute__((always_inline)) inline void f8_pack_rows(const T* x, int64_t R, int64_t ldx, int K, const F8Out& o, int block, int blocks) {
   const int lane = threadIdx.x & 63, segs = (o.Ks / 4 + kF8Steps - 1) / kF8Steps;
   const int64_t items = R * segs;
-  for (int64_t it = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6); it < items; it += (int64_t)gridDim.x * 4) {
+  for (int64_t it = (int64_t)block * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6); it < items; it += (int64_t)blocks * 4) {
     const int64_t row = it / segs;
     const int c0 = (int)(it - row * segs) * kF8Steps * 512 + lane * 8;
     Raw8<T> r[kF8Steps];
@@ -199,6 +199,9 @@ __global__ __launch_bounds__(256) void f8_pack_kernel(const T* x, int64_t R, int
     }
   }
 }
+
+template <class T>
+__global__ __launch_bounds__(256) void f8_pack_kernel(const T* x, int64_t R, int64_t ldx, int K, F8Out o) { f8_pack_rows(x, R, ldx, K, o, blockIdx.x, gridDim.x); }
 
 template <class T>
 __global__ __launch_bounds__(256) void f8_restore_kernel(const uint8_t* codes, const uint8_t* scales, int fmt, int64_t R, int K, T* x, int64_t ldx) {

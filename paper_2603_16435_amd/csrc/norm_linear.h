@@ -216,17 +216,31 @@ static F8GradPlan f8_grad_plan(int64_t M, int N, int K, int32_t dtype) {
   return p;
 }
 
+// One launch prepares both contractions of the first chunk; a chunk that follows has its x^T and dy prepared ahead of its contraction.
 template <class T>
-static void run_f8_weight_grad(const T* dy, int64_t lddy, int64_t M, int N, int K, const F8Operand& x, int fx, float* dW, int64_t lddw, bool accumulate,
-                               unsigned char* ws, const F8GradPlan& p, hipStream_t s) {
+static void run_f8_backward(const T* dy, int64_t lddy, int64_t M, int N, int K, int fdy, const F8Operand& x, int fx, const F8Operand& wt, int fw, T* dx, int64_t lddx,
+                            float* dW, int64_t lddw, bool accumulate, unsigned char* ws, const F8GradPlan& p, hipStream_t s) {
   bf16_t* xt = (bf16_t*)(ws + p.xt);
   bf16_t* terms = (bf16_t*)(ws + p.terms);
   // bf16 rows that lie on 16 bytes are read where they are, others and f32 go through the workspace
   const bool direct = sizeof(T) == 2 && N % 8 == 0 && lddy % 8 == 0 && !off(dy, 16) && lddy < (1 << 23);
+  const bool raw = dx && f8_takes_raw(M, K, N);                    // (packed where it is multiplied)
   for (int64_t t0 = 0; t0 < M; t0 += p.chunk) {
     const int tokens = (int)(M - t0 < p.chunk ? M - t0 : p.chunk), pad = (tokens + 127) / 128 * 128;
-    f8_restore_t_kernel<<<dim3(pad / 64, f8_blocks(K)), 256, 0, s>>>(x.codes + t0 * x.Kp, x.scales + t0 * x.Ks, fx, tokens, x.Kp, x.Ks, xt, pad, p.copies);
-    if (!direct) f8_grad_terms_kernel<T><<<blocks_of(((int64_t)pad * p.Np / 8 + 255) / 256, 8192), 256, 0, s>>>(dy + t0 * lddy, lddy, tokens, pad, N, p.Np, terms);
+    F8GradPrep<T> j{};
+    j.dy = dy; j.lddy = lddy; j.M = M; j.N = N; j.packed = f8_out(ws + p.codes, ws + p.scales, fdy, N);
+    if (dx && t0 == 0 && !raw) j.pack_blocks = (int)blocks_of((M * ((j.packed.Ks / 4 + kF8Steps - 1) / kF8Steps) + 3) / 4, 1 << 16);
+    int copy_blocks = 0;
+    if (dW) {
+      j.codes = x.codes + t0 * x.Kp; j.scales = x.scales + t0 * x.Ks; j.fmt = fx; j.tokens = tokens; j.Kp = x.Kp; j.Ks = x.Ks;
+      j.xt = xt; j.pad = pad; j.copies = p.copies; j.restore_blocks = pad / 64 * f8_blocks(K);
+      j.chunk = dy + t0 * lddy; j.Np = p.Np; j.terms = terms;
+      if (!direct) copy_blocks = (int)blocks_of(((int64_t)pad * p.Np / 8 + 255) / 256, 8192);
+    }
+    const int blocks = j.pack_blocks + j.restore_blocks + copy_blocks;
+    if (blocks) f8_grad_prep_kernel<T><<<blocks, 256, 0, s>>>(j);
+    if (dx && t0 == 0) run_f8_product<T>(f8_operand(raw ? nullptr : ws + p.codes, raw ? nullptr : ws + p.scales, M, N), fdy, wt, fw, raw ? dy : nullptr, lddy, N, dx, lddx, ws + p.mm, s);
+    if (!dW) return;
     GemmDims d{};
     d.M = K; d.N = direct ? N : p.Np; d.K = p.copies * pad; d.lda = d.K; d.ldb = direct ? lddy : p.Np;
     d.group_m = 8; d.split_slots = kHotSlots; d.b_k_rows = direct ? tokens : d.K;
@@ -421,11 +435,8 @@ rl_status rl_f8_linear_backward(const void* dy, int64_t lddy, int32_t dtype, int
   unsigned char* w = static_cast<unsigned char*>(ws);
   auto go = [&](auto zero) {
     typedef decltype(zero) T;
-    if (dx) {
-      run_f8_pack((const T*)dy, lddy, M, N, f8_out(w + p.codes, w + p.scales, dy_format, N), s);
-      run_f8_product<T>(f8_operand(w + p.codes, w + p.scales, M, N), dy_format, f8_operand(wt_codes, wt_scales, K, N), w_format, nullptr, 0, N, (T*)dx, lddx, w + p.mm, s);
-    }
-    if (dW) run_f8_weight_grad((const T*)dy, lddy, M, N, K, f8_operand(x_codes, x_scales, M, K), x_format, dW, lddw, accumulate != 0, w, p, s);
+    run_f8_backward((const T*)dy, lddy, M, N, K, dy_format, f8_operand(x_codes, x_scales, M, K), x_format, f8_operand(wt_codes, wt_scales, K, N), w_format, (T*)dx, lddx,
+                    dW, lddw, accumulate != 0, w, p, s);
   };
   if (dtype == RL_BF16) go(bf16_t()); else go(float());
   return launched();
