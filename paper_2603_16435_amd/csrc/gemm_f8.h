@@ -426,13 +426,13 @@ __global__ __launch_bounds__(kF8FewWaves * 64) void f8_few_kernel(F8Few<T> j) {
     if (k0 != wave) fetch(k0);
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      const bool there = k0 + u * kF8FewWaves < j.nk;                // (no branch around the loads of x: a slab past the end is the last one, times zero)
+      const bool there = k0 + u * kF8FewWaves < j.nk;                // (no branch around the loads of x: a slab past the end is the last one, both operands zeroed)
       const int k = there ? k0 + u * kF8FewWaves : j.nk - 1;
       i32x8_t wf = __builtin_shufflevector(wc[u][0], wc[u][1], 0, 1, 2, 3, 4, 5, 6, 7);
-#pragma unroll
-      for (int e = 0; e < 8; ++e) wf[e] = there ? wf[e] : 0;
       const uint8_t* xp = RAW ? xlds + mr * pitch + k * 128 + g * 32 : j.x.codes + (int64_t)mr * j.x.Kp + k * 128 + g * 32;
-      const i32x8_t xc = __builtin_shufflevector(*reinterpret_cast<const i32x4_t*>(xp), *reinterpret_cast<const i32x4_t*>(xp + 16), 0, 1, 2, 3, 4, 5, 6, 7);
+      i32x8_t xc = __builtin_shufflevector(*reinterpret_cast<const i32x4_t*>(xp), *reinterpret_cast<const i32x4_t*>(xp + 16), 0, 1, 2, 3, 4, 5, 6, 7);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) { wf[e] = there ? wf[e] : 0; xc[e] = there ? xc[e] : 0; }
       const unsigned sx = RAW ? xlds[j.M * pitch + mr * j.x.Ks + k] : j.x.scales[(int64_t)mr * j.x.Ks + k];
       if constexpr (kExact<T>) mfma_exact(acc, exact_operand<FW>(wf, sw[u]), exact_operand<FX>(xc, sx));
       else mfma_f8<FX, FW>(acc, wf, xc, sw[u], sx);

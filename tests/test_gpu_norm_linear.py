@@ -282,6 +282,34 @@ def test_matmul_keeps_what_is_not_finite_in_its_row():
         assert np.array_equal(np.isnan(y).all(1), bad) and np.isfinite(y[~bad]).all()
 
 
+def test_matmul_keeps_infinities_of_e5m2():
+    rng = np.random.default_rng(12)
+    for M in (9, 33, 300):
+        a = rng.normal(size=(M, 300))
+        a[4, 299], a[6, 0] = -np.inf, np.inf
+        b = rng.choice([-1.0, 1.0], size=(80, 300)) * rng.uniform(0.5, 2, size=(80, 300))
+        pa, pb = binding.rl_f8_pack(rows(a, torch.float32), "e5m2"), binding.rl_f8_pack(rows(b, torch.float32))
+        for t in (torch.float32, torch.bfloat16):
+            y = f64(binding.rl_f8_matmul(pa, pb, t))
+            assert np.array_equal(y[6], np.inf * np.sign(b[:, 0])) and np.array_equal(y[4], -np.inf * np.sign(b[:, 299]))
+            y[[4, 6]] = 0
+            assert np.isfinite(y).all()
+
+
+def test_matmul_at_the_ends_of_the_scales():
+    # single products of powers of two, the factors near the ends of the scale bytes' range, the product inside f32's
+    for M in (5, 40, 300):
+        a, b = np.zeros((M, 256)), np.zeros((64, 256))
+        a[:, 3], b[:, 3] = 2.0 ** -120, 2.0 ** 110
+        a[1, 3], b[1, 3] = 2.0 ** -126, 2.0 ** 126
+        a[:, 200], b[::2, 3] = 0, 0
+        b[::2, 200] = 2.0 ** -118
+        a[2, 200] = 2.0 ** 100
+        pa, pb = binding.rl_f8_pack(rows(a, torch.float32)), binding.rl_f8_pack(rows(b, torch.float32))
+        for t in (torch.float32, torch.bfloat16):
+            assert np.array_equal(f64(binding.rl_f8_matmul(pa, pb, t)), a @ b.T), (M, t)
+
+
 # ------------------------------------------------------------------ the linear layer
 LINEAR = [(1, 1, 1), (1, 100, 300), (3, 17, 129), (16, 40, 256), (17, 40, 256), (127, 72, 130), (128, 64, 128), (129, 1157, 70), (300, 130, 517), (700, 264, 264), (1300, 300, 515)]
 
