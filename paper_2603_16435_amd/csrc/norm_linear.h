@@ -95,15 +95,15 @@ static void run_norm_backward(NormBwd<T> j, hipStream_t s) {
 // ------------------------------------------------------------------ products
 // Tile and cut along K of a product.  A workgroup takes `start` us and `one` us a slab, `two` where a CU has two of them (measured, in rounds that fill the chip or part of it;
 // bf16 outputs and f32 ones, whose MFMAs run at half the rate); a cut product takes a second launch and a pass over the slices.  The cheapest by that account is
-// taken: within 10 % of the fastest of all tiles and cuts measured over 8 to 4000 rows and seven weights of 300 x 5000 to 14336 x 3584 (us, by tiles of 32 x 32 / 64 x 64 /
-// 64 x 128 / 128 x 128 / 256 x 256: 48 rows, 4096 x 2048 5.9 / 7.8 / - / - / -; 250, 14336 x 3584 53.7 / 27.4 / 23.0 / 24.5 / 35.1; 1000, 3584 x 3584 - / 27.8 / 22.2 / 24.9 / 35.3;
-// 2000, 3584 x 3584 - / 53.4 / 42.5 / 33.6 / 36.1; 4000 - / 117 / 79 / 63.5 / 37.1).
+// taken: 1 % behind the fastest of all tiles and cuts in the mean of 91 products of 48 to 4000 rows and seven weights of 300 x 5000 to 14336 x 3584, at most 15 % behind but for one
+// of 8 us (us, by tiles of 32 x 32 / 64 x 64 / 64 x 128 / 128 x 128 / 256 x 256, each with its best cut, 3584 columns and rows of w: 48 rows 7.9 / 8.4 / - / - / -;
+// 250 16.7 / 11.7 / 15.3 / 18.2 / 32.5; 1000 - / 27.1 / 23.0 / 26.7 / 35.2; 2000 - / 53.0 / 43.4 / 31.3 / 36.1; 4000 - / - / - / 61.9 / 37.0).
 struct F8Tile { int bm, bn; float start[2], one[2], two[2]; };
 constexpr F8Tile kF8Tiles[] = {
-    {32, 32, {2.6f, 2.6f}, {0.205f, 0.275f}, {0.25f, 0.36f}},
-    {64, 64, {3.0f, 3.2f}, {0.32f, 0.43f}, {0.45f, 0.70f}},
-    {64, 128, {3.4f, 3.8f}, {0.465f, 0.79f}, {0.69f, 1.18f}},
-    {128, 128, {4.3f, 5.0f}, {0.68f, 1.15f}, {1.05f, 1.82f}},
+    {32, 32, {2.7f, 3.2f}, {0.17f, 0.23f}, {0.20f, 0.31f}},
+    {64, 64, {3.2f, 3.4f}, {0.28f, 0.47f}, {0.39f, 0.65f}},
+    {64, 128, {3.9f, 4.4f}, {0.43f, 0.70f}, {0.67f, 1.06f}},
+    {128, 128, {4.4f, 4.7f}, {0.68f, 1.15f}, {0.95f, 1.69f}},
     {256, 256, {7.0f, 0.f}, {1.15f, 0.f}, {0.f, 0.f}},               // hot kernel: bf16 outputs, one workgroup a CU, not cut
 };
 constexpr int kF8Hot = 4;
