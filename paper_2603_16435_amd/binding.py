@@ -578,7 +578,7 @@ def rl_layer_norm_forward(x, gamma, beta=None, eps=1e-5, checkpoint=None, out=No
 
 def rl_layer_norm_backward(dy, x, stats, gamma, want_beta=True, out=None):
     """(dx, dgamma, dbeta) from dy [R, H], x or its checkpoint (F8Rows), and the statistics of the forward pass; dgamma, dbeta float32.
-    out: where dx goes, dy itself for instance."""
+    out: where dx goes, dy or x itself for instance."""
     R, H = dy.shape
     dev = dy.device
     pdy, lddy, dt = _rows(dy, "dy")

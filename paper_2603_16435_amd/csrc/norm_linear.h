@@ -77,6 +77,15 @@ static NormTeams norm_teams(int64_t R, int H, bool ck) {
 }
 static size_t norm_part_bytes(int64_t R, int H) { return up256((size_t)norm_teams(R, H, true).teams * 2 * norm_pitch(H) * 4); }
 
+// dx has bytes of dy or of x
+template <class T>
+static bool norm_in_place(const NormBwd<T>& j) {
+  auto meet = [&](const T* p, int64_t ld) {
+    return p && j.R && p < j.dx + (j.R - 1) * j.lddx + j.H && j.dx < p + (j.R - 1) * ld + j.H;
+  };
+  return meet(j.dy, j.lddy) || meet(j.x, j.ldx);
+}
+
 template <class T, bool CK>
 static void run_norm_backward(NormBwd<T> j, hipStream_t s) {
   const NormTeams t = norm_teams(j.R, j.H, CK);
@@ -86,8 +95,17 @@ static void run_norm_backward(NormBwd<T> j, hipStream_t s) {
       ln_backward_kernel<T, CK, TW, CH><<<t.blocks, NT, 0, s>>>(j);
       ln_sum_kernel<<<(2 * j.Hp + 63) / 64, 256, 0, s>>>(j.part, t.teams, j.Hp, j.H, j.dgamma, j.dbeta);
     } else {
-      j.row_blocks = (int)((j.R + TEAMS - 1) / TEAMS);
-      ln_backward_few_kernel<T, CK, TW, CH><<<j.row_blocks + f8_blocks(j.H), NT, 0, s>>>(j);
+      const int rows = (int)((j.R + TEAMS - 1) / TEAMS), columns = f8_blocks(j.H);
+      // the workgroups of a column read what those of a row may overwrite: then one after the other (the column's, of which there are always some, first)
+      if (!norm_in_place(j)) {
+        j.row_blocks = rows;
+        ln_backward_few_kernel<T, CK, TW, CH><<<rows + columns, NT, 0, s>>>(j);
+      } else {
+        j.row_blocks = 0;
+        ln_backward_few_kernel<T, CK, TW, CH><<<columns, NT, 0, s>>>(j);
+        j.row_blocks = rows;
+        if (rows) ln_backward_few_kernel<T, CK, TW, CH><<<rows, NT, 0, s>>>(j);
+      }
     }
   });
 }

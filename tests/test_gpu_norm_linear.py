@@ -94,6 +94,20 @@ def test_layer_norm(R, H, dtype, params, kept, pad):
         assert torch.all(x._base[:, H:] == 7) and torch.all(dy._base[:, H:] == 7)
 
 
+@pytest.mark.parametrize("R, H", [(1, 5), (200, 4096), (512, 1157), (512, 16384), (700, 1000)])
+@pytest.mark.parametrize("over", ["dy", "x", "kept"])
+def test_layer_norm_backward_in_place_keeps_the_sums(R, H, over):
+    """dx over dy (or x): the sums over the rows are those of dy and x as they came."""
+    rng = np.random.default_rng(R + H)
+    x, dy = rows(rng.normal(size=(R, H)), torch.bfloat16, 0), rows(rng.normal(size=(R, H)), torch.bfloat16, 0)
+    gamma = torch.from_numpy(rng.normal(size=H).astype(np.float32)).cuda()
+    _, stats, kept = binding.rl_layer_norm_forward(x, gamma, checkpoint="e4m3" if over == "kept" else None)
+    dx, dg, db = binding.rl_layer_norm_backward(dy, kept or x, stats, gamma)
+    out = x if over == "x" else dy
+    dx2, dg2, db2 = binding.rl_layer_norm_backward(dy, kept or x, stats, gamma, out=out)
+    assert dx2.data_ptr() == out.data_ptr() and torch.equal(dx, dx2) and torch.equal(dg, dg2) and torch.equal(db, db2)
+
+
 def test_layer_norm_without_beta_and_without_rows():
     x = torch.randn(3, 40, device="cuda")
     gamma = torch.randn(40, device="cuda")
