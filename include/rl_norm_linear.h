@@ -41,7 +41,7 @@ rl_status rl_layer_norm_forward(const void* x, int64_t ldx, int32_t dtype, int64
                                 int32_t format, void* stream);
 
 /* dx, dgamma [H] and dbeta [H] (f32, overwritten; dbeta may be NULL) from dy and either x or its checkpoint (x NULL, codes and scales given), with the
- * statistics of the forward pass.  dx may be dy, or x, with the same stride.  A row whose dy is zero contributes nothing and gets dx = 0. */
+ * statistics of the forward pass.  dx may be dy, or x, with the same stride.  A row whose dy is zero contributes nothing and gets dx = 0, whatever its x holds. */
 rl_status rl_layer_norm_backward_workspace_bytes(int64_t R, int32_t H, size_t* bytes);
 rl_status rl_layer_norm_backward(const void* dy, int64_t lddy, const void* x, int64_t ldx, const void* codes, const void* scales, int32_t format,
                                  int32_t dtype, int64_t R, int32_t H, const void* gamma, int32_t param_dtype, const float* stats,

@@ -23,6 +23,8 @@ __host__ __device__ inline int f8_scale_pitch(int K) { return (f8_blocks(K) + 3)
 
 // Eight consecutive values of a row as they lie in memory, at any alignment an element has (global accesses of this part need none).
 typedef unsigned u32x4_el2 __attribute__((ext_vector_type(4), aligned(2)));
+typedef unsigned u32x2_el2 __attribute__((ext_vector_type(2), aligned(2)));
+typedef unsigned u32_el2 __attribute__((aligned(2)));
 template <class T> struct Raw8;
 template <> struct Raw8<bf16_t> { u32x4_t v; };
 template <> struct Raw8<float> { u32x4_t v, w; };
@@ -39,14 +41,41 @@ template <class T> __device__ __attribute__((always_inline)) inline Raw8<T> raw_
   if constexpr (sizeof(T) == 4) r.w = *reinterpret_cast<const u32x4_el2*>(p + 4);
   return r;
 }
-template <class T> __device__ __attribute__((always_inline)) inline Raw8<T> raw_load_part(const T* p, int n) {       // the first n of 8
+// The first n of 8 (n < 8), by four, two and one.
+template <class T> __device__ __attribute__((always_inline)) inline Raw8<T> raw_load_part(const T* p, int n) {
   Raw8<T> r = raw_zero<T>();
-#pragma unroll
-  for (int i = 0; i < 7; ++i)
-    if (i < n) {
-      if constexpr (sizeof(T) == 4) { (i < 4 ? r.v : r.w)[i & 3] = __float_as_uint(p[i]); }
-      else r.v[i >> 1] |= (unsigned)reinterpret_cast<const uint16_t*>(p)[i] << ((i & 1) * 16);
-    }
+  const bool two = n & 2;
+  if constexpr (sizeof(T) == 4) {
+    u32x2_el2 b = {0, 0};
+    unsigned c = 0;
+    if (n & 4) r.v = *reinterpret_cast<const u32x4_el2*>(p);
+    if (n & 2) b = *reinterpret_cast<const u32x2_el2*>(p + (n & 4));
+    if (n & 1) c = *reinterpret_cast<const unsigned*>(p + (n & 6));
+    const u32x4_t rest = {two ? b[0] : c, two ? b[1] : 0u, two ? c : 0u, 0u};
+    if (n & 4) r.w = rest; else r.v = rest;
+  } else {
+    u32x2_el2 a = {0, 0};
+    unsigned b = 0, c = 0;
+    if (n & 4) a = *reinterpret_cast<const u32x2_el2*>(p);
+    if (n & 2) b = *reinterpret_cast<const u32_el2*>(p + (n & 4));
+    if (n & 1) c = *reinterpret_cast<const uint16_t*>(p + (n & 6));
+    const unsigned r0 = two ? b : c, r1 = two ? c : 0u;
+    r.v = n & 4 ? u32x4_t{a[0], a[1], r0, r1} : u32x4_t{r0, r1, 0u, 0u};
+  }
+  return r;
+}
+// r without its first d values (d < 8), zeros behind: by four, two and one.
+template <class T> __device__ __attribute__((always_inline)) inline Raw8<T> raw_skip(Raw8<T> r, int d) {
+  const bool four = d & 4, two = d & 2, one = d & 1;
+  if constexpr (sizeof(T) == 4) {
+    const u32x4_t a = four ? r.w : r.v, b = four ? u32x4_t{0, 0, 0, 0} : r.w;
+    const u32x4_t e = two ? u32x4_t{a[2], a[3], b[0], b[1]} : a, f = two ? u32x4_t{b[2], b[3], 0, 0} : b;
+    r.v = one ? u32x4_t{e[1], e[2], e[3], f[0]} : e;
+    r.w = one ? u32x4_t{f[1], f[2], f[3], 0} : f;
+  } else {
+    const u32x4_t a = four ? u32x4_t{r.v[2], r.v[3], 0, 0} : r.v, b = two ? u32x4_t{a[1], a[2], a[3], 0} : a;
+    r.v = one ? u32x4_t{b[0] >> 16 | b[1] << 16, b[1] >> 16 | b[2] << 16, b[2] >> 16 | b[3] << 16, b[3] >> 16} : b;
+  }
   return r;
 }
 // `left`: values that the row still has from p on (8 or more: all of them, none: zeros)
@@ -78,12 +107,18 @@ template <class T> __device__ __attribute__((always_inline)) inline void raw_sto
   if constexpr (sizeof(T) == 4) *reinterpret_cast<u32x4_el2*>(p + 4) = r.w;
 }
 template <class T> __device__ __attribute__((always_inline)) inline void raw_store_part(T* p, int n, const Raw8<T>& r) {
-#pragma unroll
-  for (int i = 0; i < 7; ++i)
-    if (i < n) {
-      if constexpr (sizeof(T) == 4) p[i] = __uint_as_float((i < 4 ? r.v : r.w)[i & 3]);
-      else reinterpret_cast<uint16_t*>(p)[i] = (uint16_t)(r.v[i >> 1] >> ((i & 1) * 16));
-    }
+  const bool four = n & 4, two = n & 2;
+  if constexpr (sizeof(T) == 4) {
+    const u32x4_t rest = four ? r.w : r.v;
+    if (n & 4) *reinterpret_cast<u32x4_el2*>(p) = r.v;
+    if (n & 2) *reinterpret_cast<u32x2_el2*>(p + (n & 4)) = u32x2_el2{rest[0], rest[1]};
+    if (n & 1) *reinterpret_cast<unsigned*>(p + (n & 6)) = two ? rest[2] : rest[0];
+  } else {
+    const unsigned r0 = four ? r.v[2] : r.v[0], r1 = four ? r.v[3] : r.v[1];
+    if (n & 4) *reinterpret_cast<u32x2_el2*>(p) = u32x2_el2{r.v[0], r.v[1]};
+    if (n & 2) *reinterpret_cast<u32_el2*>(p + (n & 4)) = r0;
+    if (n & 1) *reinterpret_cast<uint16_t*>(p + (n & 6)) = (uint16_t)(two ? r1 : r0);
+  }
 }
 template <class T> __device__ __attribute__((always_inline)) inline void raw_store(T* p, int left, const Raw8<T>& r) {
   if (left >= 8) raw_store8(p, r);

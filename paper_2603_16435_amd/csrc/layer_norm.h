@@ -10,6 +10,10 @@
 // Mean and variance: a wavefront's own values give its sum and the sum of squares about its own mean, which are joined exactly
 // (sum_w [q_w + n_w (mean_w - mean)^2]): no difference of large sums, and one exchange instead of two.
 //
+// A row of x that is not finite (a masked token's) has statistics that are not; where its dy is zero it counts as nothing and its dx is 0, because products
+// of zero are zeros here (asking once a row whether its statistics are finite: 32749 rows of 3584 and their checkpoint, both ways, 328 us
+// and 245).
+//
 // Backward: a team keeps its columns' sums of dgamma and dbeta in registers the whole way; they go to the workspace and ln_sum_kernel adds the teams' in
 // order (no atomics: same bits every run).  Few rows: one launch, in which further workgroups form those sums column by column out of a second read of x and dy.
 #pragma once
@@ -30,10 +34,11 @@ __device__ __attribute__((always_inline)) inline float wave_sum(float x) {
 }
 
 // Which columns of a row a lane holds: pieces of eight from c0 + c * TW * 512 on.  Where H is no multiple of eight, one lane of one wavefront has a piece
-// that is not whole; it is loaded and stored by element, apart from the others.
+// that is not whole: its load ends with the row and is shifted in registers (bf16, 10000 rows of 1157, forward 17.9 us, backward 26; by element 20.7 and 39).
 template <int TW, int CH> struct Pieces {
   int c0, H, part;                   // part: columns of the lane's piece that is not whole, 0 if it has none
   int part_c;                        // that piece
+  bool part_here;                    // it is in this wavefront (uniform)
   int held;                          // pieces of the wavefront that hold any column (uniform); the others are left out where that pays
   __device__ Pieces(int w, int lane, int H_) : c0((w * 64 + lane) * 8), H(H_) {
     const int p = H / 8;
@@ -42,6 +47,7 @@ template <int TW, int CH> struct Pieces {
     for (int c = 0; c < CH; ++c) held += (c * TW + w) * 512 < H ? 1 : 0;
     part_c = p / (TW * 64);
     part = p % (TW * 64) == w * 64 + lane ? H % 8 : 0;
+    part_here = H % 8 && p % (TW * 64) / 64 == w;
   }
   __device__ __attribute__((always_inline)) int col(int c) const { return c0 + c * TW * 512; }
   __device__ __attribute__((always_inline)) bool whole(int c) const { return col(c) + 8 <= H; }
@@ -49,15 +55,19 @@ template <int TW, int CH> struct Pieces {
   // a checkpoint 114 -> 128).
   __device__ __attribute__((always_inline)) bool has(int c) const { return TW < 8 || c < held; }
   template <class T> __device__ __attribute__((always_inline)) void load(const T* row, bool there, Raw8<T> (&r)[CH]) const {
+    if (H < 8) {                                     // (a row shorter than the load)
+#pragma unroll
+      for (int c = 0; c < CH; ++c) r[c] = c == 0 && there && part ? raw_load_part(row, part) : raw_zero<T>();
+      return;
+    }
 #pragma unroll
     for (int c = 0; c < CH; ++c) {
       r[c] = raw_zero<T>();
-      if (there && whole(c)) r[c] = raw_load8(row + col(c));
+      if (there && col(c) < H) r[c] = raw_load8(row + (whole(c) ? col(c) : H - 8));
     }
-    if (there && part) {
-      const Raw8<T> t = raw_load_part(row + col(part_c), part);
+    if (part_here) {
 #pragma unroll
-      for (int c = 0; c < CH; ++c) if (c == part_c) r[c] = t;
+      for (int c = 0; c < CH; ++c) if (c == part_c) r[c] = raw_skip(r[c], part ? 8 - part : 0);
     }
   }
   template <class T> __device__ __attribute__((always_inline)) void store(T* row, const Raw8<T> (&r)[CH]) const {
@@ -90,7 +100,7 @@ template <int TW, int CH> struct Pieces {
   }
 };
 
-constexpr int norm_threads(int tw) { return tw > 4 ? tw * 64 : 256; }
+constexpr int norm_threads(int tw) { return tw > 1 ? tw * 64 : 256; }
 
 struct NormParams { const void* gamma; const void* beta; int bf16; };
 template <class T> struct NormFwd {
@@ -148,7 +158,7 @@ __global__ __launch_bounds__(norm_threads(TW)) void ln_forward_kernel(NormFwd<T>
         for (int e = 0; e < 8; ++e) { const float d = raw_get(r[c], e) - m; t += d * d; }
         a += at.whole(c) ? t : 0.f;
       }
-    if (at.part) {
+    if (at.part_here) {
       Raw8<T> t = r[0];
 #pragma unroll
       for (int c = 1; c < CH; ++c) if (c == at.part_c) t = r[c];
@@ -193,13 +203,19 @@ template <class T> struct NormBwd {
   const T* dy; const T* x; T* dx; int64_t R, lddy, ldx, lddx; int H;
   const uint8_t *codes, *scales; int fmt, Kp, Ks;
   NormParams p; const float2* stats;
-  float* part; int Hp;            // [teams][2][Hp]: sums of dgamma and dbeta
+  float* part; int Hp;            // [workgroups][2][Hp]: sums of dgamma and dbeta
   float *dgamma, *dbeta; int row_blocks;          // few rows
 };
 
-// Team `team` of `teams`.  SUMS: dgamma, dbeta of its rows to the workspace.
+// a b, 0 where one of them is 0, whatever the other is (v_mul_legacy_f32).
+__device__ __attribute__((always_inline)) inline float mul_zero(float a, float b) {
+  float r;
+  asm("v_mul_legacy_f32 %0, %1, %2" : "=v"(r) : "v"(a), "v"(b));
+  return r;
+}
+// Team `team` of `teams`.  SUMS: dgamma, dbeta of its rows to sums [2][Hp].
 template <class T, bool CK, int TW, int CH, bool SUMS>
-__device__ __attribute__((always_inline)) inline void ln_backward_rows(const NormBwd<T>& j, int team, int teams, int w, int lane, float2 (&red)[2][TW]) {
+__device__ __attribute__((always_inline)) inline void ln_backward_rows(const NormBwd<T>& j, int team, int teams, int w, int lane, float2 (&red)[2][TW], float* sums) {
   const Pieces<TW, CH> at(w, lane, j.H);
   const float inv_h = 1.f / (float)j.H;
   float gamma[CH][8], dg[SUMS ? CH : 1][8], db[SUMS ? CH : 1][8];
@@ -244,8 +260,8 @@ __device__ __attribute__((always_inline)) inline void ln_backward_rows(const Nor
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
           const float d = raw_get(ry[c], e), g = d * gamma[c][e];
-          a += g; b += g * xh[e];
-          if constexpr (SUMS) { dg[c][e] += d * xh[e]; db[c][e] += d; }
+          a += g; b += mul_zero(g, xh[e]);
+          if constexpr (SUMS) { dg[c][e] += mul_zero(d, xh[e]); db[c][e] += d; }
         }
       }
     a = wave_sum(a); b = wave_sum(b);
@@ -265,7 +281,7 @@ __device__ __attribute__((always_inline)) inline void ln_backward_rows(const Nor
         float xh[8], v[8];
         normal(c, xh);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] = st.y * (raw_get(ry[c], e) * gamma[c][e] - ma - xh[e] * mb);
+        for (int e = 0; e < 8; ++e) v[e] = mul_zero(st.y, raw_get(ry[c], e) * gamma[c][e] - ma - mul_zero(xh[e], mb));
         out[c] = raw_make<T>(v);
       }
     at.store(j.dx + row * j.lddx, out);
@@ -275,7 +291,7 @@ __device__ __attribute__((always_inline)) inline void ln_backward_rows(const Nor
     for (int c = 0; c < CH; ++c) {
       const int col = at.col(c);
       if (col >= j.Hp) continue;
-      float* p = j.part + (int64_t)team * 2 * j.Hp + col;
+      float* p = sums + col;
 #pragma unroll
       for (int e = 0; e < 8; e += 4) {
         *reinterpret_cast<floatx4*>(p + e) = floatx4{dg[c][e], dg[c][e + 1], dg[c][e + 2], dg[c][e + 3]};
@@ -290,7 +306,19 @@ __global__ __launch_bounds__(norm_threads(TW)) void ln_backward_kernel(NormBwd<T
   constexpr int TEAMS = norm_threads(TW) / (TW * 64);
   __shared__ float2 red[2][TW];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  ln_backward_rows<T, CK, TW, CH, true>(j, blockIdx.x * TEAMS + wave / TW, gridDim.x * TEAMS, wave % TW, lane, red);
+  float* const out = j.part + (int64_t)blockIdx.x * 2 * j.Hp;
+  if constexpr (TEAMS == 1) ln_backward_rows<T, CK, TW, CH, true>(j, blockIdx.x, gridDim.x, wave, lane, red, out);
+  else {                                             // (5003 rows of 768, bf16, the teams' sums joined here 10.6 us with the sum, each to the workspace 16.0)
+    __shared__ __attribute__((aligned(16))) float sums[TEAMS][2 * TW * CH * 512];
+    ln_backward_rows<T, CK, TW, CH, true>(j, blockIdx.x * TEAMS + wave / TW, gridDim.x * TEAMS, wave % TW, lane, red, sums[wave / TW]);
+    __syncthreads();
+    for (int i = threadIdx.x * 4; i < 2 * j.Hp; i += 1024) {
+      floatx4 v = *reinterpret_cast<const floatx4*>(sums[0] + i);
+#pragma unroll
+      for (int t = 1; t < TEAMS; ++t) v += *reinterpret_cast<const floatx4*>(sums[t] + i);
+      *reinterpret_cast<floatx4*>(out + i) = v;
+    }
+  }
 }
 
 // dgamma, dbeta of 128 columns: sixteen lanes of eight columns, the rows dealt out among groups of such lanes.
@@ -323,7 +351,7 @@ __device__ __attribute__((always_inline)) inline void ln_backward_columns(const 
       for (int e = 0; e < 8; ++e) {
         if constexpr (!CK) xh[e] = raw_get(rx[u], e);
         const float d = raw_get(ry[u], e);
-        dg[e] += d * ((xh[e] - st[u].x) * st[u].y); db[e] += d;
+        dg[e] += mul_zero(d, (xh[e] - st[u].x) * st[u].y); db[e] += d;
       }
     }
   }
@@ -346,17 +374,17 @@ __global__ __launch_bounds__(norm_threads(TW)) void ln_backward_few_kernel(NormB
   __shared__ float sums[NT / 16][2][128];
   if ((int)blockIdx.x < j.row_blocks) {
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    ln_backward_rows<T, CK, TW, CH, false>(j, blockIdx.x * TEAMS + wave / TW, j.row_blocks * TEAMS, wave % TW, lane, red);
+    ln_backward_rows<T, CK, TW, CH, false>(j, blockIdx.x * TEAMS + wave / TW, j.row_blocks * TEAMS, wave % TW, lane, red, nullptr);
   } else ln_backward_columns<T, CK, NT>(j, (int)blockIdx.x - j.row_blocks, sums);
 }
 
-// Sums over the teams: a workgroup takes 64 columns of [teams][2 Hp], sixteen slices of the teams each.
-__global__ __launch_bounds__(256) void ln_sum_kernel(const float* part, int teams, int Hp, int H, float* dgamma, float* dbeta) {
-  __shared__ floatx4 lds[16][16];
-  const int q = threadIdx.x & 15, s = threadIdx.x >> 4, col = blockIdx.x * 64 + q * 4;
+// Sums over the workgroups: one takes 32 columns of [parts][2 Hp], a line of each part, in 32 slices of the parts.
+__global__ __launch_bounds__(256) void ln_sum_kernel(const float* part, int parts, int Hp, int H, float* dgamma, float* dbeta) {
+  __shared__ floatx4 lds[32][8];
+  const int q = threadIdx.x & 7, s = threadIdx.x >> 3, col = blockIdx.x * 32 + q * 4;
   floatx4 v = {0.f, 0.f, 0.f, 0.f};
   if (col < 2 * Hp) {
-    const int per = (teams + 15) / 16, end = (s + 1) * per < teams ? (s + 1) * per : teams;
+    const int per = (parts + 31) / 32, end = (s + 1) * per < parts ? (s + 1) * per : parts;
     int t = s * per;
     for (; t + 8 <= end; t += 8) {
       floatx4 x[8];
@@ -371,7 +399,7 @@ __global__ __launch_bounds__(256) void ln_sum_kernel(const float* part, int team
   __syncthreads();
   if (s > 0 || col >= 2 * Hp) return;
 #pragma unroll
-  for (int i = 1; i < 16; ++i) v += lds[i][q];
+  for (int i = 1; i < 32; ++i) v += lds[i][q];
   const bool second = col >= Hp;                     // (Hp is a multiple of 8: four columns are of one kind)
   float* o = second ? dbeta : dgamma;
   const int h = col - (second ? Hp : 0);

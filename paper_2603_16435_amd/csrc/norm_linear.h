@@ -58,24 +58,24 @@ static void run_norm_forward(const NormFwd<T>& j, hipStream_t s) {
 
 // Backward: one launch up to kNormFewRows rows.  us, 3584 columns, one launch / two: 128 rows 3.8 / 4.3 + 2.7, 256 5.6 / 5.3 + 3.0, 512 8.9 / 7.3 + 3.4, 1024 21.3 / 8.8 + 3.5;
 // 768 columns, 512 rows 8.0 / 3.9 + 3.4; the host takes 3.5 for a launch.
-// Beyond, the teams' sums cost 8 bytes a column and workgroup, twice, so there are only as many workgroups as keep the loads going: by the registers of a lane, four a CU up to 2048
-// columns (5003 rows of 1157, 512 / 768 / 1024 workgroups 24.9 / 20.6 / 17.7 us, from a checkpoint 20.3 / 16.9 / 15.2), two up to 4096 (32749 rows of 3584 125 / 134 / 138), three from a
-// checkpoint, whose loads are shorter (133 / 114 / 141), two up to 8192 (16000 rows of 5120 93 / 107 / 101 and 95 / 112 / 98), one beyond (6000 rows of 12000, 256 / 512 92 / 98); two where
-// a wavefront has a row to itself (20000 rows of 1000 22.4 / 23.3 / 24.4), with four rows each at least (2175 rows of 768, f32, 128 / 256 / 384 workgroups, with the sum 6.7 + 3.3 / 5.8 + 4.2 /
-// 6.1 + 5.2).
+// Beyond, the workgroups' sums cost 8 bytes a column and workgroup, twice: time goes as rows / workgroups and as workgroups, and is least at a multiple of the root of the rows,
+// 10 sqrt(R) (144 cases of 600 to 20000 rows of 768 to 3584 columns in both types, from x and from a checkpoint: 2 % behind the best of nine launches in the mean; 1000 rows of 2048: 11 us, a workgroup a row 18).
+// At most as many workgroups as keep the loads going: by the registers of a lane, four a CU up to 2048 columns, two up to 4096 (32749 rows of 3584, 512 / 768 / 1024 workgroups
+// 125 / 134 / 138 us), three from a checkpoint, whose loads are shorter (133 / 114 / 141), two up to 8192 (16000 rows of 5120 93 / 107 / 101 and 95 / 112 / 98), one beyond (6000 rows of
+// 12000, 256 / 512 92 / 98); two where a wavefront has a row to itself (20000 rows of 1000 22.4 / 23.3 / 24.4).
 constexpr int kNormFewRows = 512;
 static int norm_pitch(int H) { return (H + 7) / 8 * 8; }
-struct NormTeams { int blocks, teams; };
-static NormTeams norm_teams(int64_t R, int H, bool ck) {
-  NormTeams t{0, 0};
+// 0: one launch
+static int norm_blocks(int64_t R, int H, bool codes) {
+  int blocks = 0;
   if (R > kNormFewRows) with_team(H, [&](auto tw, auto ch) {
-    constexpr int TW = tw.value, TEAMS = norm_threads(TW) / (TW * 64), PER = TEAMS > 1 ? 4 * TEAMS : 1;
-    t.blocks = (int)blocks_of((R + PER - 1) / PER, TW == 16 ? 256 : TW != 4 ? 512 : ch.value == 1 ? 1024 : ck ? 768 : 512);
-    t.teams = t.blocks * TEAMS;
+    constexpr int TW = tw.value, TEAMS = norm_threads(TW) / (TW * 64), MOST = TW == 16 ? 256 : TW != 4 ? 512 : ch.value == 1 ? 1024 : 0;
+    const int64_t most = MOST ? MOST : codes ? 768 : 512, root = (int64_t)(10.f * sqrtf((float)R));
+    blocks = (int)blocks_of((R + TEAMS - 1) / TEAMS, root < most ? root : most);
   });
-  return t;
+  return blocks;
 }
-static size_t norm_part_bytes(int64_t R, int H) { return up256((size_t)norm_teams(R, H, true).teams * 2 * norm_pitch(H) * 4); }
+static size_t norm_part_bytes(int64_t R, int H) { return up256((size_t)norm_blocks(R, H, true) * 2 * norm_pitch(H) * 4); }
 
 // dx has bytes of dy or of x
 template <class T>
@@ -88,12 +88,12 @@ static bool norm_in_place(const NormBwd<T>& j) {
 
 template <class T, bool CK>
 static void run_norm_backward(NormBwd<T> j, hipStream_t s) {
-  const NormTeams t = norm_teams(j.R, j.H, CK);
+  const int blocks = norm_blocks(j.R, j.H, CK && sizeof(T) == 2);
   with_team(j.H, [&](auto tw, auto ch) {
     constexpr int TW = tw.value, CH = ch.value, NT = norm_threads(TW), TEAMS = NT / (TW * 64);
-    if (t.blocks) {
-      ln_backward_kernel<T, CK, TW, CH><<<t.blocks, NT, 0, s>>>(j);
-      ln_sum_kernel<<<(2 * j.Hp + 63) / 64, 256, 0, s>>>(j.part, t.teams, j.Hp, j.H, j.dgamma, j.dbeta);
+    if (blocks) {
+      ln_backward_kernel<T, CK, TW, CH><<<blocks, NT, 0, s>>>(j);
+      ln_sum_kernel<<<(2 * j.Hp + 31) / 32, 256, 0, s>>>(j.part, blocks, j.Hp, j.H, j.dgamma, j.dbeta);
     } else {
       const int rows = (int)((j.R + TEAMS - 1) / TEAMS), columns = f8_blocks(j.H);
       // the workgroups of a column read what those of a row may overwrite: then one after the other (the column's, of which there are always some, first)

@@ -139,6 +139,28 @@ def test_layer_norm_keeps_what_is_not_finite_in_its_row():
     assert torch.all(y.abs() <= 700 * U * 3 * 320) and torch.isfinite(stats).all()
 
 
+@pytest.mark.parametrize("R, H", [(1, 3), (5, 64), (40, 1157), (700, 1000), (600, 2304), (530, 5120)])
+@pytest.mark.parametrize("dtype, fmt", [("bf16", None), ("bf16", "e4m3"), ("f32", None), ("f32", "e5m2")])
+def test_layer_norm_rows_without_a_gradient_contribute_nothing(R, H, dtype, fmt):
+    """dy zero where x is infinite or no number: the gradients are those with such rows of x zero."""
+    rng = np.random.default_rng(R + H)
+    x, dy = rng.normal(size=(R, H)), rng.normal(size=(R, H))
+    bad = rng.random(R) < 0.3
+    bad[-1] = True
+    dy[bad] = 0
+    clean = x.copy()
+    clean[bad] = 0
+    x[bad, rng.integers(0, H, size=bad.sum())] = rng.choice([np.inf, -np.inf, np.nan], size=bad.sum())
+    gamma = torch.from_numpy(rng.normal(size=H).astype(np.float32)).cuda()
+    got = []
+    for v in (x, clean):
+        t, d = rows(v, DT[dtype]), rows(dy, DT[dtype])
+        _, stats, kept = binding.rl_layer_norm_forward(t, gamma, checkpoint=fmt)
+        got.append(binding.rl_layer_norm_backward(d, kept or t, stats, gamma))
+    for a, b in zip(*got):
+        assert torch.isfinite(a).all() and torch.equal(a, b)
+
+
 # ------------------------------------------------------------------ 8-bit rows
 @pytest.mark.parametrize("R, K", [(1, 1), (3, 127), (2, 128), (5, 129), (4, 512), (3, 513), (7, 1157), (2, 2048), (2, 2050), (6, 5120), (70, 300)])
 @pytest.mark.parametrize("dtype, fmt, pad", [("bf16", "e4m3", 0), ("bf16", "e5m2", 3), ("f32", "e4m3", 1), ("f32", "e5m2", 0)])
