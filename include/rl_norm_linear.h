@@ -61,7 +61,7 @@ rl_status rl_f8_matmul(const void* x_codes, const void* x_scales, int32_t x_form
                        int64_t M, int32_t N, int32_t K, void* y, int64_t ldy, int32_t dtype, void* workspace, size_t workspace_bytes, void* stream);
 
 /* The linear layer.  Forward: x [M, K] is packed into x_codes, x_scales (the checkpoint of the backward pass; both NULL: not kept) and multiplied with the packed
- * weight.  Workspace: with the packed x kept (keep != 0) or not. */
+ * weight; y must not overlap x.  Workspace: with the packed x kept (keep != 0) or not. */
 rl_status rl_f8_linear_forward_workspace_bytes(int64_t M, int32_t N, int32_t K, int32_t keep, size_t* bytes);
 rl_status rl_f8_linear_forward(const void* x, int64_t ldx, int32_t dtype, int64_t M, int32_t K, int32_t x_format, const void* w_codes,
                                const void* w_scales, int32_t w_format, int32_t N, void* y, int64_t ldy, void* x_codes, void* x_scales,
@@ -69,6 +69,7 @@ rl_status rl_f8_linear_forward(const void* x, int64_t ldx, int32_t dtype, int64_
 
 /* Backward, from dy [M, N]:  dx [M, K] (in `dtype`; NULL: not wanted) = pack(dy) W, with dy packed in dy_format and the packed transpose of W;
  * dW [N, K] f32 (NULL: not wanted), overwritten, or added to if accumulate is not 0, = dy^T x, with dy as it is and x from the checkpoint.
+ * dx and dW must not overlap dy.  A row whose dy is zero contributes nothing to dW, whatever its x holds.
  * (bf16 dy: where it holds infinities or NaN the rows of dW concerned are not finite, which of the two they hold is not specified.) */
 rl_status rl_f8_linear_backward_workspace_bytes(int64_t M, int32_t N, int32_t K, int32_t dtype, size_t* bytes);
 rl_status rl_f8_linear_backward(const void* dy, int64_t lddy, int32_t dtype, int64_t M, int32_t N, int32_t K, int32_t dy_format,

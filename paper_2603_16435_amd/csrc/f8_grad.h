@@ -23,6 +23,7 @@ template <class T> struct F8GradPrep {
   const T* chunk; int Np; bf16_t* terms;                                       // rows of dy of the chunk
 };
 
+// A token whose x is not finite counts as nothing where its dy is zero (a masked one): such values are restored as zeros.
 // x^T: a workgroup restores 64 tokens x 128 k and writes 128 rows of 64 tokens, whole lines.
 template <class T> __device__ __attribute__((always_inline)) inline void f8_restore_t(const F8GradPrep<T>& j, int block, bf16_t* lds) {
   constexpr int kPitch = 66;              // elements of a row in LDS
@@ -39,6 +40,23 @@ template <class T> __device__ __attribute__((always_inline)) inline void f8_rest
   for (int i = 0; i < 4; ++i) {
     float v[8];
     f8_restore8(code[i], s[i], j.fmt, v);
+    unsigned bad = 0;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) bad |= __builtin_isfinite(v[e]) ? 0u : 1u;
+    if (__any(bad)) {                     // sixteen lanes hold a token's values: they look through its dy
+      const int t = t0 + i * 16 + (tid >> 4);
+      bad = max_of_16(bad);
+      unsigned found = bad ^ 1u;
+      for (int n = c; __any(!found && n - c < j.N); n += 128) {
+        const Raw8<T> d = raw_load(j.chunk + (int64_t)t * j.lddy + n, t < j.tokens ? j.N - n : 0);
+        unsigned any = 0;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) any |= raw_get(d, e) == 0.f ? 0u : 1u;
+        found |= max_of_16(any);
+      }
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[e] = found ? v[e] : 0.f;
+    }
 #pragma unroll
     for (int e = 0; e < 8; ++e) lds[(c + e) * kPitch + i * 16 + (tid >> 4)] = (bf16_t)v[e];
   }

@@ -318,6 +318,26 @@ def test_matmul_keeps_what_is_not_finite_in_its_row():
         assert np.array_equal(np.isnan(y).all(1), bad) and np.isfinite(y[~bad]).all()
 
 
+@pytest.mark.parametrize("M, N, K", [(1, 5, 40), (9, 300, 130), (300, 1157, 259), (2100, 512, 256)])
+@pytest.mark.parametrize("dtype, fmt", [("bf16", "e4m3"), ("bf16", "e5m2"), ("f32", "e4m3")])
+def test_weight_gradient_of_rows_without_a_gradient(M, N, K, dtype, fmt):
+    """dy zero where x is infinite or no number: dW is that with such rows of x zero."""
+    rng = np.random.default_rng(M + N)
+    x, dy = rng.normal(size=(M, K)), rng.normal(size=(M, N))
+    bad = rng.random(M) < 0.3
+    bad[-1] = True
+    dy[bad] = 0
+    clean = x.copy()
+    clean[bad] = 0
+    x[bad, rng.integers(0, K, size=bad.sum())] = rng.choice([np.inf, -np.inf, np.nan], size=bad.sum())
+    w = binding.rl_f8_pack_weight(rows(rng.normal(size=(N, K)), torch.float32))
+    got = [binding.rl_f8_linear_backward(rows(dy, DT[dtype]), binding.rl_f8_pack(rows(v, DT[dtype]), fmt), w)[1] for v in (x, clean)]
+    assert torch.isfinite(got[0]).all() and torch.equal(*got)
+    dy[-1, N - 1] = 1                                                # with one value of dy it does count
+    dw = binding.rl_f8_linear_backward(rows(dy, DT[dtype]), binding.rl_f8_pack(rows(x, DT[dtype]), fmt), w)[1]
+    assert not torch.isfinite(dw[N - 1]).all()
+
+
 def test_matmul_keeps_infinities_of_e5m2():
     rng = np.random.default_rng(12)
     for M in (9, 33, 300):
