@@ -485,3 +485,29 @@ def test_a_captured_step_replays_with_new_inputs():
         graph.replay()
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(want, out)), seed
+
+
+def test_offsets_past_32_bits():
+    """The last rows of matrices of more than 2^32 bytes (codes: 2^31): what a call of those rows alone gives.  Small integers, whose sums are exact in any order."""
+    R, H, N, last = 520_000, 4200, 70, 100
+    g = torch.Generator(device="cuda").manual_seed(3)
+    x = torch.randint(-4, 5, (R, H), generator=g, device="cuda", dtype=torch.int8).to(torch.bfloat16)
+    gamma = torch.randn(H, generator=g, device="cuda")
+    w = binding.rl_f8_pack_weight(torch.randint(-2, 3, (N, H), generator=g, device="cuda").to(torch.bfloat16))
+    y, stats, kept = binding.rl_layer_norm_forward(x, gamma, checkpoint="e4m3")
+    ys, ss, ks = binding.rl_layer_norm_forward(x[-last:], gamma, checkpoint="e4m3")
+    assert torch.equal(y[-last:], ys) and torch.equal(stats[-last:], ss) and torch.equal(kept.codes[-last:], ks.codes) and torch.equal(kept.scales[-last:], ks.scales)
+    for v, k, small in ((x, None, x[-last:]), (x, kept, ks)):
+        dx = binding.rl_layer_norm_backward(y, k or v, stats, gamma)[0]
+        assert torch.equal(dx[-last:], binding.rl_layer_norm_backward(ys, small, ss, gamma)[0])
+        del dx
+    del y
+    assert torch.equal(binding.rl_f8_unpack(kept)[-last:], x[-last:])
+    out, kept = binding.rl_f8_linear_forward(x, w)
+    want, ks = binding.rl_f8_linear_forward(x[-last:], w)
+    assert torch.equal(out[-last:], want) and torch.equal(kept.codes[-last:], ks.codes)
+    dy = torch.zeros(R, N, device="cuda", dtype=torch.bfloat16)
+    dy[-last:] = torch.randint(-2, 3, (last, N), generator=g, device="cuda").to(torch.bfloat16)
+    dx, dw = binding.rl_f8_linear_backward(dy, kept, w)
+    dxs, dws = binding.rl_f8_linear_backward(dy[-last:], ks, w)
+    assert torch.equal(dx[-last:], dxs) and torch.equal(dw, dws) and torch.all(dx[:1000] == 0)
