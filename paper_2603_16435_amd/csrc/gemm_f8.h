@@ -209,7 +209,9 @@ __global__ __launch_bounds__(256) void f8_slices_kernel(const float* part, int s
 }
 
 // ------------------------------------------------------------------ hot kernel
-// 256 x 256 tile, four wavefronts of 128 x 128 (256 accumulators a lane, in AGPRs), y in bf16.  A slab's 64 MFMAs of 32 cycles are as long as those of a slab of the bf16
+// 256 x 256 tile, four wavefronts of 128 x 128 (256 accumulators a lane, in AGPRs), y in bf16.  32768 x 3584 x 3584: 316 to 330 us, 2.6 PFLOP/s (the vendor's product with one scale a
+// tensor 2.42); the MFMAs are busy 69 % of the clocks, at the 1.88 GHz that the power limit leaves (nothing but these MFMAs: 2.12 GHz, 4.2 PFLOP/s; without the loads 3.3 to 3.6; eight
+// wavefronts, other places for the loads, prefetches into the L2: no gain).  A slab's 64 MFMAs of 32 cycles are as long as those of a slab of the bf16
 // hot kernel (gemm_nt.h), on the same bytes, so it is built like that one: slabs go straight into two LDS stages, every MFMA is fenced, fragment reads, slab
 // loads are dealt out between them.  A slab is two phases: all eight blocks of x against blocks 0..3 of w, then against 4..7.  The
 // workgroup meets between them, when the last fragments of the slab have been read: the second phase runs from registers, covers the first fragment reads of the next slab (an
