@@ -78,6 +78,16 @@ template <class T> __device__ __attribute__((always_inline)) inline Raw8<T> raw_
   }
   return r;
 }
+// By word: a choice between two pieces of an array that is left to a branch puts the array into LDS.
+template <class T> __device__ __attribute__((always_inline)) inline Raw8<T> raw_pick(bool first, const Raw8<T>& a, const Raw8<T>& b) {
+  Raw8<T> o;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    o.v[i] = first ? a.v[i] : b.v[i];
+    if constexpr (sizeof(T) == 4) o.w[i] = first ? a.w[i] : b.w[i];
+  }
+  return o;
+}
 // `left`: values that the row still has from p on (8 or more: all of them, none: zeros)
 template <class T> __device__ __attribute__((always_inline)) inline Raw8<T> raw_load(const T* p, int left) {
   if (left >= 8) return raw_load8(p);

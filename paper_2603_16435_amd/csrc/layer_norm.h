@@ -4,7 +4,7 @@
 //   g = dy gamma,  dx = rstd (g - mean(g) - xh mean(g xh)),  dgamma = sum_rows dy xh,  dbeta = sum_rows dy
 //
 // Bound by HBM: forward x and y, backward x (or its codes), dy and dx, each once (32768 rows of 3584, bf16: 82 us, 5.7 TB/s, and 139, 5.1; with the checkpoint 114 and 125).  A row is held by a team of TW wavefronts, in registers, eight
-// consecutive values a lane and CH such pieces a lane (two at most: four made registers of 300, and 5120 columns ran at 3.9 TB/s); a team walks rows far apart with the
+// consecutive values a lane and CH such pieces a lane (three at most: four made registers of 300, and 5120 columns ran at 3.9 TB/s); a team walks rows far apart with the
 // parameters of its columns in registers.  Sums are f32.  (Two or four rows at a time: no faster, fewer wavefronts fit a CU.)
 //
 // Mean and variance: a wavefront's own values give its sum and the sum of squares about its own mean, which are joined exactly
@@ -34,7 +34,7 @@ __device__ __attribute__((always_inline)) inline float wave_sum(float x) {
 }
 
 // Which columns of a row a lane holds: pieces of eight from c0 + c * TW * 512 on.  Where H is no multiple of eight, one lane of one wavefront has a piece
-// that is not whole: its load ends with the row and is shifted in registers (bf16, 10000 rows of 1157, forward 17.9 us, backward 26; by element 20.7 and 39).
+// that is not whole: its load ends with the row and is shifted in registers (bf16, 10000 rows of 1157, four wavefronts a row, forward 17.9 us, backward 26; by element 20.7 and 39).
 template <int TW, int CH> struct Pieces {
   int c0, H, part;                   // part: columns of the lane's piece that is not whole, 0 if it has none
   int part_c;                        // that piece
@@ -66,18 +66,24 @@ template <int TW, int CH> struct Pieces {
       if (there && col(c) < H) r[c] = raw_load8(row + (whole(c) ? col(c) : H - 8));
     }
     if (part_here) {
+      const Raw8<T> t = raw_skip(last(r), part ? 8 - part : 0);
 #pragma unroll
-      for (int c = 0; c < CH; ++c) if (c == part_c) r[c] = raw_skip(r[c], part ? 8 - part : 0);
+      for (int c = 0; c < CH; ++c) r[c] = raw_pick(c == part_c, t, r[c]);
     }
+  }
+  // the wavefront's pieces that hold the one that is not whole
+  template <class T> __device__ __attribute__((always_inline)) Raw8<T> last(const Raw8<T> (&r)[CH]) const {
+    Raw8<T> t = r[0];
+#pragma unroll
+    for (int c = 1; c < CH; ++c) t = raw_pick(c == part_c, r[c], t);
+    return t;
   }
   template <class T> __device__ __attribute__((always_inline)) void store(T* row, const Raw8<T> (&r)[CH]) const {
 #pragma unroll
     for (int c = 0; c < CH; ++c) if (whole(c)) raw_store8(row + col(c), r[c]);
-    if (part) {
-      Raw8<T> t = r[0];
-#pragma unroll
-      for (int c = 1; c < CH; ++c) if (c == part_c) t = r[c];
-      raw_store_part(row + col(part_c), part, t);
+    if (part_here) {
+      const Raw8<T> t = last(r);
+      if (part) raw_store_part(row + col(part_c), part, t);
     }
   }
   // parameters of the lane's columns, zeros past the end
@@ -159,9 +165,7 @@ __global__ __launch_bounds__(norm_threads(TW)) void ln_forward_kernel(NormFwd<T>
         a += at.whole(c) ? t : 0.f;
       }
     if (at.part_here) {
-      Raw8<T> t = r[0];
-#pragma unroll
-      for (int c = 1; c < CH; ++c) if (c == at.part_c) t = r[c];
+      const Raw8<T> t = at.last(r);
 #pragma unroll
       for (int e = 0; e < 7; ++e) { const float d = raw_get(t, e) - m; a += e < at.part ? d * d : 0.f; }
     }

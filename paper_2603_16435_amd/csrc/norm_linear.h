@@ -33,11 +33,16 @@ static bool bad_product(int64_t M, int64_t N, int64_t K) {
 }
 
 // ------------------------------------------------------------------ layer norm
-// Calls f with the team of a row of H columns: wavefronts and pieces a lane as constants.
-template <class F> static void with_team(int H, F f) {
+// Calls f with the team of a row of H columns: wavefronts and pieces a lane as constants.  One wavefront exchanges nothing and takes its sums once, but is alone with the row's
+// latency: up to 1536 columns it has the row to itself, beyond 1024 of them only where there are rows enough (bf16, 1157 columns, one wavefront of three pieces / four of one, us: forward with the
+// checkpoint 64 rows 5.4 / 4.0, 1000 5.9 / 5.4, 5003 11.5 / 13.7, 20000 30.6 / 37.8; backward with its sum 600 9.5 / 9.3, 1000 9.8 / 10.5, 5003 15.2 / 18.3, 20000 32 / 37; f32: the same
+// or up to 10 % less).
+constexpr int kNormWideRows = 1024;
+template <class F> static void with_team(int64_t R, int H, F f) {
   typedef std::integral_constant<int, 1> I1; typedef std::integral_constant<int, 2> I2;
   if (H <= 512) f(I1(), I1());
   else if (H <= 1024) f(I1(), I2());
+  else if (H <= 1536 && R > kNormWideRows) f(I1(), std::integral_constant<int, 3>());
   else if (H <= 2048) f(std::integral_constant<int, 4>(), I1());
   else if (H <= 4096) f(std::integral_constant<int, 4>(), I2());
   else if (H <= 8192) f(std::integral_constant<int, 8>(), I2());
@@ -45,11 +50,11 @@ template <class F> static void with_team(int H, F f) {
 }
 
 // Workgroups: five a CU, each walking rows.  us, bf16, 768 / 1024 / 1280 workgroups: 32749 rows of 3584 89 / 88 / 87, with the checkpoint 124 / 117 / 118 (2048: 124, one a row: 162);
-// 5003 rows of 1157 13.6 / 12.5 / 11.5 and 17.0 / 15.2 / 14.6; 3000 rows of 3584 11.3 / 10.5 / 9.9 and 14.8 / 14.2 / 13.1; 16000 rows of 5120 66 / 65 / 65 and 102 / 94 / 98.
+// 5003 rows of 2048 at 512 / 1024 / 1280 13.2 / 10.9 / 10.8 and 17.4 / 14.1 / 14.1; 3000 rows of 3584 11.3 / 10.5 / 9.9 and 14.8 / 14.2 / 13.1; 16000 rows of 5120 66 / 65 / 65 and 102 / 94 / 98.
 constexpr int kNormBlocks = 1280;
 template <class T>
 static void run_norm_forward(const NormFwd<T>& j, hipStream_t s) {
-  with_team(j.H, [&](auto tw, auto ch) {
+  with_team(j.R, j.H, [&](auto tw, auto ch) {
     constexpr int TW = tw.value, CH = ch.value, NT = norm_threads(TW), TEAMS = NT / (TW * 64);
     const int64_t blocks = (j.R + TEAMS - 1) / TEAMS;
     ln_forward_kernel<T, TW, CH><<<blocks_of(blocks, kNormBlocks), NT, 0, s>>>(j);
@@ -68,7 +73,7 @@ static int norm_pitch(int H) { return (H + 7) / 8 * 8; }
 // 0: one launch
 static int norm_blocks(int64_t R, int H, bool codes) {
   int blocks = 0;
-  if (R > kNormFewRows) with_team(H, [&](auto tw, auto ch) {
+  if (R > kNormFewRows) with_team(R, H, [&](auto tw, auto ch) {
     constexpr int TW = tw.value, TEAMS = norm_threads(TW) / (TW * 64), MOST = TW == 16 ? 256 : TW != 4 ? 512 : ch.value == 1 ? 1024 : 0;
     const int64_t most = MOST ? MOST : codes ? 768 : 512, root = (int64_t)(10.f * sqrtf((float)R));
     blocks = (int)blocks_of((R + TEAMS - 1) / TEAMS, root < most ? root : most);
@@ -89,7 +94,7 @@ static bool norm_in_place(const NormBwd<T>& j) {
 template <class T, bool CK>
 static void run_norm_backward(NormBwd<T> j, hipStream_t s) {
   const int blocks = norm_blocks(j.R, j.H, CK && sizeof(T) == 2);
-  with_team(j.H, [&](auto tw, auto ch) {
+  with_team(j.R, j.H, [&](auto tw, auto ch) {
     constexpr int TW = tw.value, CH = ch.value, NT = norm_threads(TW), TEAMS = NT / (TW * 64);
     if (blocks) {
       ln_backward_kernel<T, CK, TW, CH><<<blocks, NT, 0, s>>>(j);

@@ -44,7 +44,7 @@ NORM = [(1, 1), (3, 7), (5, 64), (2, 127), (9, 128), (6, 130), (4, 512), (37, 51
         (3, 8192), (4, 8200), (2, 16384), (2100, 96), (2055, 1157), (2049, 2304), (2050, 4096)]
 
 
-@pytest.mark.parametrize("R, H", NORM)
+@pytest.mark.parametrize("R, H", NORM + [(1025, 1025), (1030, 1536), (1100, 1283)])
 @pytest.mark.parametrize("dtype, params, kept, pad", [("bf16", "f32", None, 0), ("bf16", "bf16", "e4m3", 5), ("f32", "f32", "e5m2", 0), ("f32", "bf16", None, 3)])
 def test_layer_norm(R, H, dtype, params, kept, pad):
     rng = np.random.default_rng(R * 31 + H)
@@ -94,7 +94,7 @@ def test_layer_norm(R, H, dtype, params, kept, pad):
         assert torch.all(x._base[:, H:] == 7) and torch.all(dy._base[:, H:] == 7)
 
 
-@pytest.mark.parametrize("R, H", [(1, 5), (200, 4096), (512, 1157), (512, 16384), (700, 1000)])
+@pytest.mark.parametrize("R, H", [(1, 5), (200, 4096), (512, 1157), (512, 16384), (700, 1000), (1300, 1157)])
 @pytest.mark.parametrize("over", ["dy", "x", "kept"])
 def test_layer_norm_backward_in_place_keeps_the_sums(R, H, over):
     """dx over dy (or x): the sums over the rows are those of dy and x as they came."""
@@ -139,7 +139,7 @@ def test_layer_norm_keeps_what_is_not_finite_in_its_row():
     assert torch.all(y.abs() <= 700 * U * 3 * 320) and torch.isfinite(stats).all()
 
 
-@pytest.mark.parametrize("R, H", [(1, 3), (5, 64), (40, 1157), (700, 1000), (600, 2304), (530, 5120)])
+@pytest.mark.parametrize("R, H", [(1, 3), (5, 64), (40, 1157), (700, 1000), (600, 2304), (530, 5120), (1500, 1283)])
 @pytest.mark.parametrize("dtype, fmt", [("bf16", None), ("bf16", "e4m3"), ("f32", None), ("f32", "e5m2")])
 def test_layer_norm_rows_without_a_gradient_contribute_nothing(R, H, dtype, fmt):
     """dy zero where x is infinite or no number: the gradients are those with such rows of x zero."""
