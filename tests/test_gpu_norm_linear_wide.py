@@ -65,3 +65,33 @@ def test_weight_gradient_over_several_chunks_of_tokens(M, N, K, dtype, pad, most
     into = torch.from_numpy(start).float().cuda()
     assert np.array_equal(base.f64(_gradient(t, kept, w, into)), want + start)
     assert np.array_equal(base.f64(binding.rl_f8_linear_backward(t, kept, w, want_dx=False, dw=into)[1]), want + start)
+
+
+# Few tokens and many tiles: tiles are not cut along the tokens, and whole ones leave in lines of 128 bytes where dW has its rows on them.
+@pytest.mark.parametrize("M, N, K, some", [(700, 520, 640, 0.5), (500, 1100, 1280, 0.5), (130, 256, 256, 0.5), (1, 640, 512, 1.0)])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_weight_gradient_in_whole_lines(M, N, K, some, dtype):
+    rng = np.random.default_rng(M + N)
+    x, dy = _whole(rng, M, N, K, 100, some)
+    want = dy.T @ x
+    t, kept = base.rows(dy, DT[dtype]), binding.rl_f8_pack(base.rows(x, DT[dtype]))
+    w = binding.rl_f8_pack_weight(torch.zeros(N, K, device="cuda"))
+    start = rng.integers(-1000, 1000, size=(N, K)).astype(np.float64)
+    into = torch.from_numpy(start).float().cuda()
+    for ld in (K, K + 2, K + 32):
+        assert np.array_equal(base.f64(_gradient(t, kept, w, ld=ld)), want), ld
+        assert np.array_equal(base.f64(_gradient(t, kept, w, into, ld=ld)), want + start), ld
+
+
+def test_weight_gradient_in_lines_and_in_halves_is_the_same():
+    """Ordinary values: the same bits, whichever way the tiles leave, and within the rounding of f32 sums."""
+    M, N, K = 700, 520, 640
+    rng = np.random.default_rng(1)
+    x, dy = rng.normal(size=(M, K)), rng.normal(size=(M, N)) * 1e-3
+    t, kept = base.rows(dy, torch.bfloat16), binding.rl_f8_pack(base.rows(x, torch.bfloat16))
+    w = binding.rl_f8_pack_weight(torch.zeros(N, K, device="cuda"))
+    got = _gradient(t, kept, w)
+    assert torch.equal(got, _gradient(t, kept, w, ld=K + 2))
+    vx, d = base.f64(binding.rl_f8_unpack(kept, torch.float32)), base.f64(t)
+    tol = 2 * (M + 32) * base.U * (np.abs(d).T @ np.abs(vx)) + 1e-38
+    assert np.all(np.abs(base.f64(got) - d.T @ vx) <= tol)
