@@ -27,7 +27,8 @@ static F8Operand f8_operand(const void* codes, const void* scales, int64_t rows,
   return F8Operand{(const uint8_t*)codes, (const uint8_t*)scales, (int)rows, f8_code_pitch(K), f8_scale_pitch(K)};
 }
 
-// (a launch has at most 2^32 threads; products of so many rows take tiles of 128 x 128 or more, 256 threads each)
+// A launch has less than 2^32 threads: that many workgroups of 256.  A product has at most half as many tiles of 128 x 128, and takes smaller ones only where they are not more (f8_plan).
+constexpr int64_t kMostBlocks = ((int64_t)1 << 24) - kXcds;
 static bool bad_product(int64_t M, int64_t N, int64_t K) {
   return M < 0 || M >= kMaxRows || N < 1 || N > kMaxCols || K < 1 || K > kMaxCols || ((M + 127) / 128) * ((N + 127) / 128) > (1 << 23);
 }
@@ -138,6 +139,7 @@ static F8Plan f8_plan(int64_t M, int N, int K, bool exact) {
   for (int t = 0; t <= kF8Hot - (exact ? 1 : 0); ++t) {
     const F8Tile& c = kF8Tiles[t];
     const int64_t tiles = ((M + c.bm - 1) / c.bm) * ((N + c.bn - 1) / c.bn);
+    if (tiles > kMostBlocks) continue;
     for (int slices = 1; slices <= 16 && slices <= (nk + 3) / 4; ++slices) {
       if (slices > 1 && (t == kF8Hot || tiles * slices > 512)) break;
       const int per = slices > 1 ? ((nk + slices - 1) / slices + 3) / 4 * 4 : whole;          // whole words of scales
@@ -218,6 +220,15 @@ template <class T> static void run_f8_pack(const T* x, int64_t ldx, int64_t R, i
 }
 
 // ------------------------------------------------------------------ backward of the linear layer
+// The launch that prepares the contractions has a workgroup for 64 tokens of a chunk and 128 k, and those that pack and copy dy; the weight gradient's one for 256 x 256 values
+// (with K's tiles rounded up to the XCDs).
+constexpr int kPackBlocks = 1 << 16, kCopyBlocks = 1 << 13;
+static bool bad_gradient(int64_t M, int64_t N, int64_t K) {
+  if (bad_product(M, N, K) || bad_product(M, K, N)) return true;
+  const int64_t tokens = M < kGradChunk ? (M + 127) / 128 * 128 : kGradChunk;
+  return tokens / 64 * f8_blocks((int)K) > kMostBlocks - kPackBlocks - kCopyBlocks || ((K + 255) / 256 + kXcds) * ((N + 255) / 256) > kMostBlocks;
+}
+
 struct F8GradPlan { size_t codes, scales, mm, xt, terms, part, total; int chunk, copies, Np; };
 static F8GradPlan f8_grad_plan(int64_t M, int N, int K, int32_t dtype) {
   F8GradPlan p{};
@@ -252,13 +263,13 @@ static void run_f8_backward(const T* dy, int64_t lddy, int64_t M, int N, int K, 
     const int tokens = (int)(M - t0 < p.chunk ? M - t0 : p.chunk), pad = (tokens + 127) / 128 * 128;
     F8GradPrep<T> j{};
     j.dy = dy; j.lddy = lddy; j.M = M; j.N = N; j.packed = f8_out(ws + p.codes, ws + p.scales, fdy, N);
-    if (dx && t0 == 0 && !raw) j.pack_blocks = (int)blocks_of((M * ((j.packed.Ks / 4 + kF8Steps - 1) / kF8Steps) + 3) / 4, 1 << 16);
+    if (dx && t0 == 0 && !raw) j.pack_blocks = (int)blocks_of((M * ((j.packed.Ks / 4 + kF8Steps - 1) / kF8Steps) + 3) / 4, kPackBlocks);
     int copy_blocks = 0;
     if (dW) {
       j.codes = x.codes + t0 * x.Kp; j.scales = x.scales + t0 * x.Ks; j.fmt = fx; j.tokens = tokens; j.Kp = x.Kp; j.Ks = x.Ks;
       j.xt = xt; j.pad = pad; j.copies = p.copies; j.restore_blocks = pad / 64 * f8_blocks(K);
       j.chunk = dy + t0 * lddy; j.Np = p.Np; j.terms = terms;
-      if (!direct) copy_blocks = (int)blocks_of(((int64_t)pad * p.Np / 8 + 255) / 256, 8192);
+      if (!direct) copy_blocks = (int)blocks_of(((int64_t)pad * p.Np / 8 + 255) / 256, kCopyBlocks);
     }
     const int blocks = j.pack_blocks + j.restore_blocks + copy_blocks;
     if (blocks) f8_grad_prep_kernel<T><<<blocks, 256, 0, s>>>(j);
@@ -435,7 +446,7 @@ rl_status rl_f8_linear_forward(const void* x, int64_t ldx, int32_t dtype, int64_
 rl_status rl_f8_linear_backward_workspace_bytes(int64_t M, int32_t N, int32_t K, int32_t dtype, size_t* bytes) {
   if (!bytes) return RL_ERR_NULL;
   if (!known(dtype)) return RL_ERR_DTYPE;
-  if (bad_product(M, N, K) || bad_product(M, K, N)) return RL_ERR_SHAPE;
+  if (bad_gradient(M, N, K)) return RL_ERR_SHAPE;
   *bytes = f8_grad_plan(M, N, K, dtype).total;
   return RL_OK;
 }
@@ -445,7 +456,7 @@ rl_status rl_f8_linear_backward(const void* dy, int64_t lddy, int32_t dtype, int
                                 void* dx, int64_t lddx, float* dW, int64_t lddw, int32_t accumulate, void* ws, size_t ws_bytes, void* stream) {
   if ((!dx && !dW && M != 0) || (M != 0 && !dy) || (dx && (!wt_codes || !wt_scales)) || (dW && M != 0 && (!x_codes || !x_scales))) return RL_ERR_NULL;
   if (!known(dtype) || (dx && (!known_f8(dy_format) || !known_f8(w_format))) || (dW && !known_f8(x_format))) return RL_ERR_DTYPE;
-  if (bad_product(M, N, K) || bad_product(M, K, N) || bad_rows(dy, lddy, dtype, M, N) || (dx && bad_rows(dx, lddx, dtype, M, K)) ||
+  if (bad_gradient(M, N, K) || bad_rows(dy, lddy, dtype, M, N) || (dx && bad_rows(dx, lddx, dtype, M, K)) ||
       (dW && (lddw < K || off(dW, 4))) || off(x_codes, 16) || off(x_scales, 16) || off(wt_codes, 16) || off(wt_scales, 16)) return RL_ERR_SHAPE;
   const F8GradPlan p = f8_grad_plan(M, N, K, dtype);
   if (bad_ws(ws, ws_bytes, p.total)) return RL_ERR_WORKSPACE;

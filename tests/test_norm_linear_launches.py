@@ -1,0 +1,66 @@
+"""The launches of the layers in front of the LM head, on the CPU (norm_linear_trace.cpp): what the entry points accept can be launched."""
+import os
+import shutil
+import subprocess
+
+import pytest
+
+from paper_2603_16435_amd import binding
+
+SOURCE = os.path.join(os.path.dirname(os.path.abspath(__file__)), "norm_linear_trace.cpp")
+pytestmark = pytest.mark.skipif(not os.path.exists(binding.LIB_PATH) or not shutil.which("g++"), reason="library not built, or no g++")
+OK, SHAPE = 0, 2
+
+
+@pytest.fixture(scope="module")
+def trace(tmp_path_factory):
+    """Calls to [(status, workspace bytes, [(workgroups, threads of each, kernel)])]."""
+    exe = str(tmp_path_factory.mktemp("trace") / "norm_linear_trace")
+    subprocess.run(["g++", "-std=c++17", "-O1", "-rdynamic", "-o", exe, SOURCE, "-ldl"], check=True)
+
+    def run(calls):
+        r = subprocess.run([exe, binding.LIB_PATH, *(str(x) for c in calls for x in c)], capture_output=True, text=True, timeout=100)
+        assert r.returncode == 0, r.stdout + r.stderr
+        out, launches = [], []
+        for line in r.stdout.splitlines():
+            w = line.split()
+            if w[0] == "status":
+                out.append((int(w[1]), int(w[3]), launches))
+                launches = []
+            else:
+                n = [int(v) for v in w[:6]]
+                launches.append(((n[0], n[1], n[2]), (n[3], n[4], n[5]), w[6]))
+        assert len(out) == len(calls)
+        return out
+    return run
+
+
+def _many():
+    """Calls with as many rows, or columns, as the entry points may be asked for."""
+    for M in (1 << 24, 1 << 27, (1 << 29) - 77, 1 << 29, (1 << 29) + 1, (1 << 30) - 300, (1 << 30) - 64, 1 << 30, (1 << 31) - (1 << 17)):
+        for N in (1, 16, 30, 32, 33, 64, 100, 128, 256, 300, 5000, 1 << 22):
+            for K in (1, 128, 700, 1700, 5000, 60_000, 1 << 22):
+                for dtype in (0, 1):
+                    yield "matmul", M, N, K, dtype
+                    yield "forward", M, N, K, dtype, 1
+    for M in (1, 20_000, 32_768, 100_000):
+        for N in (1, 64, 5000, 1 << 22):
+            for K in (1, 128, 60_000, 4_170_000, 1 << 22):
+                for dtype in (0, 1):
+                    yield "backward", M, N, K, dtype, 1, 1
+
+
+def test_what_is_accepted_can_be_launched(trace):
+    # a grid has less than 2^32 threads along each axis
+    calls = list(_many())
+    bad = [(c, l) for i in range(0, len(calls), 500) for c, (st, _, launches) in zip(calls[i:i + 500], trace(calls[i:i + 500])) for l in launches
+           if any(g * b >= 1 << 32 for g, b in zip(l[0], l[1]))]
+    assert not bad, (len(bad), bad[:5])
+
+
+def test_what_fits_the_card_is_accepted(trace):
+    # (288 GB of codes, scales, y and workspace)
+    calls = [("matmul", 400_000_000, 32, 512, 1), ("matmul", 1_000_000_000, 1, 128, 1), ("forward", 200_000_000, 64, 256, 1, 1), ("forward", 16_000_000, 3584, 3584, 1, 1),
+             ("backward", 16_000_000, 1024, 3584, 1, 1, 1), ("backward", 200_000, 100_000, 100_000, 1, 1, 1), ("forward", 1, 1 << 22, 1 << 14, 1, 0)]
+    for c, (st, _, launches) in zip(calls, trace(calls)):
+        assert st == OK and launches, c
