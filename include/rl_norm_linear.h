@@ -69,9 +69,12 @@ rl_status rl_f8_linear_forward(const void* x, int64_t ldx, int32_t dtype, int64_
 
 /* Backward, from dy [M, N]:  dx [M, K] (in `dtype`; NULL: not wanted) = pack(dy) W, with dy packed in dy_format and the packed transpose of W;
  * dW [N, K] f32 (NULL: not wanted), overwritten, or added to if accumulate is not 0, = dy^T x, with dy as it is and x from the checkpoint.
- * dx and dW must not overlap dy.  A row whose dy is zero contributes nothing to dW, whatever its x holds.
+ * Workspace: by the first query enough for any call of these sizes, by the second for the call at hand.  dx and dW must not overlap dy.  A row whose dy is zero contributes nothing to dW, whatever its x holds.
  * (bf16 dy: where it holds infinities or NaN the rows of dW concerned are not finite, which of the two they hold is not specified.) */
 rl_status rl_f8_linear_backward_workspace_bytes(int64_t M, int32_t N, int32_t K, int32_t dtype, size_t* bytes);
+/* What one call needs, at most that: dy_aligned: dy lies on 16 bytes (bf16 rows that all do are not copied); want_dx, want_dW: the output is not NULL. */
+rl_status rl_f8_linear_backward_workspace_bytes_for(int64_t M, int32_t N, int32_t K, int32_t dtype, int64_t lddy, int32_t dy_aligned, int32_t want_dx,
+                                                    int32_t want_dW, size_t* bytes);
 rl_status rl_f8_linear_backward(const void* dy, int64_t lddy, int32_t dtype, int64_t M, int32_t N, int32_t K, int32_t dy_format,
                                 const void* x_codes, const void* x_scales, int32_t x_format, const void* wt_codes, const void* wt_scales, int32_t w_format,
                                 void* dx, int64_t lddx, float* dW, int64_t lddw, int32_t accumulate, void* workspace, size_t workspace_bytes, void* stream);

@@ -142,6 +142,7 @@ def _declare_norm_linear(L):
             rl_f8_linear_forward_workspace_bytes=[l, i, i, i, nbytes],
             rl_f8_linear_forward=[p, l, i, l, i, i, p, p, i, i, p, l, p, p, p, z, p],
             rl_f8_linear_backward_workspace_bytes=[l, i, i, i, nbytes],
+            rl_f8_linear_backward_workspace_bytes_for=[l, i, i, i, l, i, i, i, nbytes],
             rl_f8_linear_backward=[p, l, i, l, i, i, i, p, p, i, p, p, i, p, l, p, l, i, p, z, p]).items():
         fn = getattr(L, name)
         fn.argtypes, fn.restype = args, C.c_int
@@ -686,7 +687,7 @@ def rl_f8_linear_backward(dy, kept: F8Rows, w: F8Weight, fmt="e5m2", want_dx=Tru
     if want_dw and (dw.shape != (N, K) or dw.dtype != torch.float32):
         raise ValueError(f"dw must be float32 [{N}, {K}]")
     pdw, lddw, _ = _rows(dw, "dw") if want_dw else (None, K, 0)
-    ws, pws, nws = _f8_workspace("rl_f8_linear_backward_workspace_bytes", dev, M, N, K, dt)
+    ws, pws, nws = _f8_workspace("rl_f8_linear_backward_workspace_bytes_for", dev, M, N, K, dt, lddy, int(pdy % 16 == 0), int(want_dx), int(want_dw))
     _check(lib().rl_f8_linear_backward(pdy, lddy, dt, M, N, K, F8_FORMATS[fmt], cx, sx, fx, ct, st, fw, dx.data_ptr() if want_dx else None, K,
                                        pdw, lddw, 1 if accumulate else 0, pws, nws, _stream_handle()))
     return dx, dw if want_dw else None

@@ -229,23 +229,36 @@ static bool bad_gradient(int64_t M, int64_t N, int64_t K) {
   return tokens / 64 * f8_blocks((int)K) > kMostBlocks - kPackBlocks - kCopyBlocks || ((K + 255) / 256 + kXcds) * ((N + 255) / 256) > kMostBlocks;
 }
 
-struct F8GradPlan { size_t codes, scales, mm, xt, terms, part, total; int chunk, copies, Np; };
-static F8GradPlan f8_grad_plan(int64_t M, int N, int K, int32_t dtype) {
+// bf16 rows of dy that lie on 16 bytes are read where they are, others and f32 go through the workspace.
+static bool f8_grad_direct(int32_t dtype, int N, int64_t lddy, bool aligned) { return dtype == RL_BF16 && N % 8 == 0 && lddy % 8 == 0 && aligned && lddy < (1 << 23); }
+// slices: of the weight gradient's contraction over a whole chunk, and over the tokens that are left
+struct F8GradPlan { size_t codes, scales, mm, xt, terms, part, total; int chunk, copies, Np; bool raw, direct; SplitK slices[2]; };
+// Only what a call for these outputs touches: at 32749 x 3584 x 3584, bf16, 354 MB, and 236 more where dy has to be copied; 119 for dx alone.
+static F8GradPlan f8_grad_plan(int64_t M, int N, int K, int32_t dtype, bool dx, bool dW, bool direct) {
   F8GradPlan p{};
   size_t o = 0;
   auto take = [&](size_t n) { const size_t at = o; o += up256(n); return at; };
-  p.codes = take((size_t)M * f8_code_pitch(N));
-  p.scales = take((size_t)M * f8_scale_pitch(N));
-  p.mm = take(f8_product_bytes(M, K, N));
+  p.raw = dx && f8_takes_raw(M, K, N);                             // (packed where it is multiplied)
+  p.direct = direct;
+  if (dx && !p.raw) {
+    p.codes = take((size_t)M * f8_code_pitch(N));
+    p.scales = take((size_t)M * f8_scale_pitch(N));
+    p.mm = take(f8_product_bytes(M, K, N));
+  }
   p.copies = dtype == RL_F32 ? kGradTerms : 1;
   const int most = kGradChunk / p.copies / 128 * 128;
   p.chunk = (int)(M < most ? (M + 127) / 128 * 128 : most);
   p.Np = (N + 7) / 8 * 8;
-  p.xt = take((size_t)p.copies * p.chunk * ((K + 255) / 256 * 256) * 2);
-  p.terms = take((size_t)p.copies * p.chunk * p.Np * 2);
-  const int tm = (K + kBM - 1) / kBM, tn = (p.Np + kBN - 1) / kBN;
-  const int64_t slices = (int64_t)tm * tn < 2 * kHotSlots ? 2 * kHotSlots / (tm * tn) : 1;
-  p.part = take(slices > 1 ? (size_t)(slices < kMaxSplit ? slices : kMaxSplit) * N * ((K + 3) / 4 * 4) * 4 : 0);
+  if (dW && M) {
+    p.xt = take((size_t)p.copies * p.chunk * ((K + 255) / 256 * 256) * 2);
+    if (!direct) p.terms = take((size_t)p.copies * p.chunk * p.Np * 2);
+    const int tiles = ((K + kBM - 1) / kBM) * ((p.Np + kBN - 1) / kBN);
+    auto cut = [&](int64_t tokens) { return split_k_host(tiles, (int)((tokens + 127) / 128) * p.copies, kHotSlots, 0); };
+    if (M >= p.chunk) p.slices[0] = cut(p.chunk);
+    if (M % p.chunk) p.slices[1] = cut(M % p.chunk);
+    const int slices = p.slices[0].slices > p.slices[1].slices ? p.slices[0].slices : p.slices[1].slices;
+    p.part = take(slices > 1 ? (size_t)slices * N * ((K + 3) / 4 * 4) * 4 : 0);
+  }
   p.total = o;
   return p;
 }
@@ -256,9 +269,7 @@ static void run_f8_backward(const T* dy, int64_t lddy, int64_t M, int N, int K, 
                             float* dW, int64_t lddw, bool accumulate, unsigned char* ws, const F8GradPlan& p, hipStream_t s) {
   bf16_t* xt = (bf16_t*)(ws + p.xt);
   bf16_t* terms = (bf16_t*)(ws + p.terms);
-  // bf16 rows that lie on 16 bytes are read where they are, others and f32 go through the workspace
-  const bool direct = sizeof(T) == 2 && N % 8 == 0 && lddy % 8 == 0 && !off(dy, 16) && lddy < (1 << 23);
-  const bool raw = dx && f8_takes_raw(M, K, N);                    // (packed where it is multiplied)
+  const bool direct = p.direct, raw = p.raw;
   for (int64_t t0 = 0; t0 < M; t0 += p.chunk) {
     const int tokens = (int)(M - t0 < p.chunk ? M - t0 : p.chunk), pad = (tokens + 127) / 128 * 128;
     F8GradPrep<T> j{};
@@ -280,7 +291,7 @@ static void run_f8_backward(const T* dy, int64_t lddy, int64_t M, int N, int K, 
     d.group_m = 8; d.split_slots = kHotSlots; d.b_k_rows = direct ? tokens : d.K;
     const bool add = accumulate || t0 > 0;
     const int tm = (d.M + kBM - 1) / kBM, tn = (d.N + kBN - 1) / kBN;
-    const SplitK sk = split_k_host(tm * tn, d.K / 64 / 2, kHotSlots, 0);
+    const SplitK sk = p.slices[tokens == p.chunk ? 0 : 1];          // (a step is 128 tokens, two slabs)
     const int64_t ldp = (K + 3) / 4 * 4;
     const EpiF8Grad e{dW, lddw, N, K, add, (float*)(ws + p.part), ldp};
     f8_grad_kernel<TuneDX><<<split_launch(tm, tn, kHotSlots), 256, 0, s>>>(xt, direct ? (const bf16_t*)(dy + t0 * lddy) : terms, d, e);
@@ -447,7 +458,15 @@ rl_status rl_f8_linear_backward_workspace_bytes(int64_t M, int32_t N, int32_t K,
   if (!bytes) return RL_ERR_NULL;
   if (!known(dtype)) return RL_ERR_DTYPE;
   if (bad_gradient(M, N, K)) return RL_ERR_SHAPE;
-  *bytes = f8_grad_plan(M, N, K, dtype).total;
+  *bytes = f8_grad_plan(M, N, K, dtype, true, true, false).total;
+  return RL_OK;
+}
+
+rl_status rl_f8_linear_backward_workspace_bytes_for(int64_t M, int32_t N, int32_t K, int32_t dtype, int64_t lddy, int32_t dy_aligned, int32_t want_dx, int32_t want_dW, size_t* bytes) {
+  if (!bytes) return RL_ERR_NULL;
+  if (!known(dtype)) return RL_ERR_DTYPE;
+  if (bad_gradient(M, N, K) || lddy < N) return RL_ERR_SHAPE;
+  *bytes = f8_grad_plan(M, N, K, dtype, want_dx != 0, want_dW != 0, f8_grad_direct(dtype, N, lddy, dy_aligned != 0)).total;
   return RL_OK;
 }
 
@@ -458,7 +477,7 @@ rl_status rl_f8_linear_backward(const void* dy, int64_t lddy, int32_t dtype, int
   if (!known(dtype) || (dx && (!known_f8(dy_format) || !known_f8(w_format))) || (dW && !known_f8(x_format))) return RL_ERR_DTYPE;
   if (bad_gradient(M, N, K) || bad_rows(dy, lddy, dtype, M, N) || (dx && bad_rows(dx, lddx, dtype, M, K)) ||
       (dW && (lddw < K || off(dW, 4))) || off(x_codes, 16) || off(x_scales, 16) || off(wt_codes, 16) || off(wt_scales, 16)) return RL_ERR_SHAPE;
-  const F8GradPlan p = f8_grad_plan(M, N, K, dtype);
+  const F8GradPlan p = f8_grad_plan(M, N, K, dtype, dx != nullptr, dW != nullptr, f8_grad_direct(dtype, N, lddy, !off(dy, 16)));
   if (bad_ws(ws, ws_bytes, p.total)) return RL_ERR_WORKSPACE;
   hipStream_t s = static_cast<hipStream_t>(stream);
   (void)hipGetLastError();
