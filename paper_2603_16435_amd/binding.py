@@ -570,8 +570,8 @@ def _output(out, x):
     return (out,) + _rows(out, "out")[:2]
 
 
-def rl_layer_norm_forward(x, gamma, beta=None, eps=1e-5, checkpoint=None, out=None):
-    """(y, stats, kept): y = (x - mean) rstd gamma + beta over the columns of x [R, H]; stats [R, 2] float32 (mean, rstd) for the backward pass;
+def rl_layer_norm_forward(x, gamma, beta=None, eps=1e-5, checkpoint=None, out=None, want_stats=True):
+    """(y, stats, kept): y = (x - mean) rstd gamma + beta over the columns of x [R, H]; stats [R, 2] float32 (mean, rstd) for the backward pass (want_stats=False: None);
     kept: x in 8-bit rows of the format `checkpoint` ("e4m3" | "e5m2"), or None.  gamma, beta [H]: float32 or bfloat16, one type.
     out: where y goes, x itself for instance."""
     R, H = x.shape
@@ -579,11 +579,11 @@ def rl_layer_norm_forward(x, gamma, beta=None, eps=1e-5, checkpoint=None, out=No
     if beta is not None and beta.dtype != gamma.dtype:
         raise ValueError("gamma and beta must have one dtype")
     y, py, ldy = _output(out, x)
-    stats = x.new_empty((R, 2), dtype=torch.float32)
+    stats = x.new_empty((R, 2), dtype=torch.float32) if want_stats else None
     kept = None if checkpoint is None else F8Rows.empty(R, H, checkpoint, x)
     codes, scales, fmt = (None, None, 0) if kept is None else kept._pointers("checkpoint")
     _check(lib().rl_layer_norm_forward(px, ldx, dt, R, H, _ptr(gamma, numel=H, name="gamma"), _ptr(beta, numel=H, name="beta"), _dtype_code(gamma), float(eps),
-                                       py, ldy, stats.data_ptr(), codes, scales, fmt, _stream_handle()))
+                                       py, ldy, stats.data_ptr() if want_stats else None, codes, scales, fmt, _stream_handle()))
     return y, stats, kept
 
 

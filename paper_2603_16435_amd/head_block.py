@@ -47,7 +47,7 @@ class HeadBlock:
 
     def hidden(self, x):
         """The LM head's input for x [R, H], nothing kept: scoring, or a decode step."""
-        y, _, _ = binding.rl_layer_norm_forward(x, self.gamma, self.beta, self.eps)
+        y = binding.rl_layer_norm_forward(x, self.gamma, self.beta, self.eps, want_stats=False)[0]
         return binding.rl_f8_linear_forward(y, self.packed, self.fmt, keep=False)[0]
 
     def forward(self, x, overwrite=False):
