@@ -84,7 +84,10 @@ template <class T> __device__ __attribute__((always_inline)) inline void f8_grad
     for (int e = 0; e < 8; ++e) v[e] = raw_get(r, e);
 #pragma unroll
     for (int k = TERMS - 1; k >= 0; --k) {
-      const Raw8<bf16_t> b = raw_make<bf16_t>(v);
+      float head[8];                                                // (a finite value's first term is finite: what lies between bf16's end and f32's goes to the second)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) head[e] = TERMS > 1 && k == TERMS - 1 && finite_bits(v[e]) > 0x7f7f0000u ? copysignf(__uint_as_float(0x7f7f0000u), v[e]) : v[e];
+      const Raw8<bf16_t> b = raw_make<bf16_t>(head);
       *reinterpret_cast<u32x4_t*>(j.terms + k * term + t * j.Np + n) = b.v;
       if constexpr (TERMS > 1) {
 #pragma unroll
