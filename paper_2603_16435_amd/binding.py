@@ -590,6 +590,8 @@ def rl_layer_norm_forward(x, gamma, beta=None, eps=1e-5, checkpoint=None, out=No
 def rl_layer_norm_backward(dy, x, stats, gamma, want_beta=True, out=None):
     """(dx, dgamma, dbeta) from dy [R, H], x or its checkpoint (F8Rows), and the statistics of the forward pass; dgamma, dbeta float32.
     out: where dx goes, dy or x itself for instance."""
+    if not isinstance(x, (torch.Tensor, F8Rows)):
+        raise ValueError("x must be the tensor of the forward pass or its checkpoint (F8Rows)")
     R, H = dy.shape
     dev = dy.device
     pdy, lddy, dt = _rows(dy, "dy")
@@ -670,14 +672,18 @@ def rl_f8_linear_forward(x, w: F8Weight, fmt="e4m3", keep=True):
 
 def rl_f8_linear_backward(dy, kept: F8Rows, w: F8Weight, fmt="e5m2", want_dx=True, want_dw=True, dw=None):
     """(dx, dw): dx = pack(dy) W in the dtype of dy, with dy packed in `fmt`; dw = dy^T x in float32 from the kept x, added to `dw` if that is given."""
+    if not want_dx and not want_dw:
+        raise ValueError("neither dx nor dw is wanted")
+    if want_dx and (w is None or w.cols is None):
+        raise ValueError("dx needs the packed transpose of the weight")
+    if want_dw and not isinstance(kept, F8Rows):
+        raise ValueError("dw needs the kept input of the forward pass (F8Rows)")
     M, N = dy.shape
-    K = kept.cols if kept is not None else w.rows.cols
+    K = kept.cols if want_dw else w.cols.rows
     dev = dy.device
     pdy, lddy, dt = _rows(dy, "dy")
     if fmt not in F8_FORMATS:
         raise ValueError(f"format must be one of {sorted(F8_FORMATS)}, got {fmt!r}")
-    if want_dx and (w is None or w.cols is None):
-        raise ValueError("dx needs the packed transpose of the weight")
     cx, sx, fx = _f8(kept, M, K, "kept") if want_dw else (None, None, 0)
     ct, st, fw = _f8(w.cols, K, N, "w.cols") if want_dx else (None, None, 0)
     dx = torch.empty((M, K), dtype=dy.dtype, device=dev) if want_dx else None
