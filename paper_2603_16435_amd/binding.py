@@ -643,7 +643,7 @@ def rl_f8_pack_weight(w, fmt="e4m3", transposed=True) -> F8Weight:
 
 
 def rl_f8_matmul(a: F8Rows, b: F8Rows, dtype=torch.bfloat16):
-    """a [M, K] times the transpose of b [N, K], both in 8-bit rows; sums in float32."""
+    """a [M, K] times the transpose of b [N, K], both in 8-bit rows; sums in float32 (dtype bfloat16: eight products at a time are cut at 2^-13 of the largest of them)."""
     M, N, K = a.rows, b.rows, a.cols
     ca, sa, fa = _f8(a, M, K, "a")
     cb, sb, fb = _f8(b, N, K, "b")

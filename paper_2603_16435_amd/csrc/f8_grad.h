@@ -4,7 +4,7 @@
 // significant bits times a power of two), so that the products of the bf16 MFMA are exact.  The checkpoint is restored, transposed, into the slab-tiled work buffer
 // that the hot kernel's A operand is read from (x^T [k][t], zeros past the last token), dy is its K-major B operand as it is stored:
 //     C[k, n] = sum_t x^T[k, t] dy[t, n] = dW[n, k],   a lane holding four consecutive k of one row of dW.
-// f32 dy goes as three bf16 terms, dy = d0 + d1 + d2 to 2^-24 of it, one contraction over three times the tokens, the smallest term first: each product is exact, and
+// f32 dy goes as three bf16 terms, dy = d0 + d1 + d2 to 2^-24 of it (and to 2^-133, where bf16 ends: dy below 2^-109), one contraction over three times the tokens, the smallest term first: each product is exact, and
 // three at the rate of the bf16 pipes take a third of the time of one on the f32 pipes.  (32749 tokens of 3584 x 3584 in bf16: 610 us, 1.38 PFLOP/s, and 122 to restore x and pack dy, 5.8 TB/s.)  (Three launches of a third each: 95 us where one takes a fraction, 3001 tokens of 1157 x 1163.)  Tokens are
 // taken a chunk at a time.
 #pragma once

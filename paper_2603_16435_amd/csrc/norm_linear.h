@@ -65,10 +65,11 @@ static void run_norm_forward(const NormFwd<T>& j, hipStream_t s) {
 // Backward: one launch up to kNormFewRows rows.  us, 3584 columns, one launch / two: 128 rows 3.8 / 4.3 + 2.7, 256 5.6 / 5.3 + 3.0, 512 8.9 / 7.3 + 3.4, 1024 21.3 / 8.8 + 3.5;
 // 768 columns, 512 rows 8.0 / 3.9 + 3.4; the host takes 3.5 for a launch.
 // Beyond, the workgroups' sums cost 8 bytes a column and workgroup, twice: time goes as rows / workgroups and as workgroups, and is least at a multiple of the root of the rows,
-// 10 sqrt(R) (144 cases of 600 to 20000 rows of 768 to 3584 columns in both types, from x and from a checkpoint: 2 % behind the best of nine launches in the mean; 1000 rows of 2048: 11 us, a workgroup a row 18).
+// 10 sqrt(R) (192 cases of 600 to 20000 rows of 768 to 3584 columns in both types, from x and from a checkpoint, with the sum: 5.5 % behind the best of nine launches in the mean, 22 % at worst: 2175
+// rows of 1024, f32, 466 workgroups 12.9, 256 10.5, a number that the sum's launch has no tail for; 1000 rows of 2048: 12.5 us, a workgroup a row 16.3).
 // At most as many workgroups as keep the loads going: by the registers of a lane, four a CU up to 2048 columns, two up to 4096 (32749 rows of 3584, 512 / 768 / 1024 workgroups
 // 125 / 134 / 138 us), three from a checkpoint, whose loads are shorter (133 / 114 / 141), two up to 8192 (16000 rows of 5120 93 / 107 / 101 and 95 / 112 / 98), one beyond (6000 rows of
-// 12000, 256 / 512 92 / 98); two where a wavefront has a row to itself (20000 rows of 1000 22.4 / 23.3 / 24.4).
+// 12000, 256 / 512 92 / 98); two where a wavefront has a row to itself (20000 rows of 1000 22.4 / 23.3 / 24.4, of 1157 32.0 / 38.2 / 35.5).
 constexpr int kNormFewRows = 512;
 static int norm_pitch(int H) { return (H + 7) / 8 * 8; }
 // 0: one launch
@@ -233,7 +234,7 @@ static bool bad_gradient(int64_t M, int64_t N, int64_t K) {
 static bool f8_grad_direct(int32_t dtype, int N, int64_t lddy, bool aligned) { return dtype == RL_BF16 && N % 8 == 0 && lddy % 8 == 0 && aligned && lddy < (1 << 23); }
 // slices: of the weight gradient's contraction over a whole chunk, and over the tokens that are left
 struct F8GradPlan { size_t codes, scales, mm, xt, terms, part, total; int chunk, copies, Np; bool raw, direct; SplitK slices[2]; };
-// Only what a call for these outputs touches: at 32749 x 3584 x 3584, bf16, 354 MB, and 236 more where dy has to be copied; 119 for dx alone.
+// Only what a call for these outputs touches: at 32749 x 3584 x 3584, bf16, 353 MB, and 235 more where dy has to be copied; 118 for dx alone (3001 x 1157 x 1163, f32: 97).
 static F8GradPlan f8_grad_plan(int64_t M, int N, int K, int32_t dtype, bool dx, bool dW, bool direct) {
   F8GradPlan p{};
   size_t o = 0;
