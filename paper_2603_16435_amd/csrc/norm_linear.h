@@ -101,7 +101,8 @@ static void run_norm_backward(NormBwd<T> j, hipStream_t s) {
     if (blocks) {
       ln_backward_kernel<T, CK, TW, CH><<<blocks, NT, 0, s>>>(j);
       ln_sum_kernel<<<(2 * j.Hp + 31) / 32, 256, 0, s>>>(j.part, blocks, j.Hp, j.H, j.dgamma, j.dbeta);
-    } else {
+    } else if constexpr (TW > 1 || CH < 3) {                        // (three pieces a lane: only with more rows)
+      static_assert(kNormFewRows <= kNormWideRows, "three pieces");
       const int rows = (int)((j.R + TEAMS - 1) / TEAMS), columns = f8_blocks(j.H);
       // the workgroups of a column read what those of a row may overwrite: then one after the other (the column's, of which there are always some, first)
       if (!norm_in_place(j)) {

@@ -1,5 +1,7 @@
-"""The launches of the layers in front of the LM head, on the CPU (norm_linear_trace.cpp): what the entry points accept can be launched."""
+"""The launches of the layers in front of the LM head, on the CPU (norm_linear_trace.cpp): what the entry points accept can be launched, and every kernel that the library
+holds is launched by some call."""
 import os
+import re
 import shutil
 import subprocess
 
@@ -30,8 +32,9 @@ def trace(tmp_path_factory):
             else:
                 n = [int(v) for v in w[:6]]
                 launches.append(((n[0], n[1], n[2]), (n[3], n[4], n[5]), w[6]))
-        assert len(out) == len(calls)
+        assert len(out) == sum(c[0] not in ("formats", "kernels") for c in calls)
         return out
+    run.kernels = {line.split()[1] for line in subprocess.run([exe, binding.LIB_PATH, "kernels"], capture_output=True, text=True, timeout=100).stdout.splitlines()}
     return run
 
 
@@ -64,3 +67,23 @@ def test_what_fits_the_card_is_accepted(trace):
              ("backward", 16_000_000, 1024, 3584, 1, 1, 1), ("backward", 200_000, 100_000, 100_000, 1, 1, 1), ("forward", 1, 1 << 22, 1 << 14, 1, 0)]
     for c, (st, _, launches) in zip(calls, trace(calls)):
         assert st == OK and launches, c
+
+
+def test_every_kernel_is_launched_by_some_call(trace):
+    own = {k for k in trace.kernels if re.search(r"rlk\d+(ln|f8)_\w+kernel", k)}
+    assert len(own) > 100
+    sizes = [(M, N, K) for M in (1, 8, 16, 17, 64, 200, 700, 2000, 4096, 9000) for N in (16, 264, 1157, 4096) for K in (100, 600, 1163, 4096)]
+    calls = []
+    for fx in (0, 1):
+        for fw in (0, 1):
+            calls.append(("formats", fx, fw))
+            for dtype in (0, 1):
+                for M, N, K in sizes:
+                    calls += [("matmul", M, N, K, dtype), ("forward", M, N, K, dtype, 1), ("backward", M, N, K, dtype, 1, 1)]
+                calls += [("norm", R, H, dtype, kept) for R in (3, 600, 1500) for H in (64, 600, 1300, 2000, 3000, 6000, 9000) for kept in (0, 1)]
+                calls += [("rows", 9, 300, dtype), ("weight", 300, 200, dtype), ("backward", 0, 40, 40, dtype, 1, 1)]
+    launched = set()
+    for i in range(0, len(calls), 300):                            # (the formats hold for a run of the program)
+        f = [c for c in calls[:i + 1] if c[0] == "formats"][-1:]
+        launched |= {l[2] for _, _, ls in trace(f + calls[i:i + 300]) for l in ls}
+    assert own <= launched, sorted(own - launched)
