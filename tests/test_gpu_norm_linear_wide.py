@@ -21,6 +21,13 @@ def test_layer_norm_of_wide_rows(R, H, dtype, params, kept, pad):
     base.test_layer_norm(R, H, dtype, params, kept, pad)
 
 
+# Four wavefronts of one piece a row: 1537 to 2048 columns, and 1025 to 1536 up to 1024 rows.
+@pytest.mark.parametrize("R, H", [(513, 1157), (1024, 1300), (700, 2048), (1500, 2001)])
+@pytest.mark.parametrize("dtype, params, kept, pad", [("bf16", "f32", None, 0), ("bf16", "bf16", "e4m3", 5), ("f32", "f32", "e5m2", 0), ("f32", "bf16", None, 3)])
+def test_layer_norm_of_four_wavefronts_a_row(R, H, dtype, params, kept, pad):
+    base.test_layer_norm(R, H, dtype, params, kept, pad)
+
+
 # ------------------------------------------------------------------ weight gradient
 def _gradient(dy, kept, w, into=None, ld=None):
     """dW alone, through the C entry: overwritten in rows of `ld` floats, or added to `into`."""
