@@ -8,6 +8,7 @@ import subprocess
 import pytest
 
 from paper_2603_16435_amd import binding
+from test_gpu_f8_tiles import TILES
 
 SOURCE = os.path.join(os.path.dirname(os.path.abspath(__file__)), "norm_linear_trace.cpp")
 pytestmark = pytest.mark.skipif(not os.path.exists(binding.LIB_PATH) or not shutil.which("g++"), reason="library not built, or no g++")
@@ -87,3 +88,11 @@ def test_every_kernel_is_launched_by_some_call(trace):
         f = [c for c in calls[:i + 1] if c[0] == "formats"][-1:]
         launched |= {l[2] for _, _, ls in trace(f + calls[i:i + 300]) for l in ls}
     assert own <= launched, sorted(own - launched)
+
+
+def test_the_tests_of_the_tiles_reach_them(trace):
+    got = trace([("matmul", M, N, K, 1 if dtype == "bf16" else 0) for _, _, dtype, M, N, K in TILES])
+    for (tile, pieces, dtype, *size), (_, _, launches) in zip(TILES, got):
+        kind = re.search(r"f8_gemm_kernelILi0ELi0E(f|DF16b)Li(\d+)ELi(\d+)", launches[0][2])
+        assert kind and (kind[2] + "x" + kind[3], "cut" if len(launches) > 1 else "whole", "f32" if kind[1] == "f" else "bf16") == (tile, pieces, dtype), (tile, size)
+    assert len({c[:3] for c in TILES}) == 15
