@@ -51,6 +51,24 @@ class rl_outputs(C.Structure):
                 ("target_logit", C.c_void_p)]
 
 
+class rl_top_params(C.Structure):
+    _fields_ = [("top_k", C.c_int32), ("chunk_rows", C.c_int32), ("temperature", C.c_float)]
+
+
+class rl_top_outputs(C.Structure):
+    _fields_ = [("logprob", C.c_void_p), ("lse", C.c_void_p), ("entropy", C.c_void_p), ("top_ids", C.c_void_p), ("top_logprob", C.c_void_p)]
+
+
+class rl_distill_params(C.Structure):
+    _fields_ = [("top_k", C.c_int32), ("rest", C.c_int32), ("aggregation", C.c_int32), ("chunk_rows", C.c_int32),
+                ("temperature", C.c_float), ("scale", C.c_float), ("d_weight_dtype", C.c_int32)]
+
+
+class rl_distill_outputs(C.Structure):
+    _fields_ = [("loss", C.c_void_p), ("row_loss", C.c_void_p), ("lse", C.c_void_p), ("d_hidden", C.c_void_p),
+                ("d_weight", C.c_void_p), ("stats", C.c_void_p)]
+
+
 PROF_CLASSES = ("prep", "gemm_fwd", "combine", "loss", "transpose", "gemm_ds", "gemm_dx", "gemm_dw", "gemm_bwd")
 
 
@@ -122,6 +140,7 @@ def lib() -> C.CDLL:
                                        C.POINTER(C.c_int32)]
         L.rl_debug_split_k.restype = C.c_int
         _declare_norm_linear(L)
+        _declare_distill(L)
         _lib = L
     return _lib
 
@@ -149,6 +168,20 @@ def _declare_norm_linear(L):
     for name in ("rl_f8_code_pitch", "rl_f8_scale_pitch"):
         fn = getattr(L, name)
         fn.argtypes, fn.restype = [i], l
+
+
+def _declare_distill(L):
+    """Signatures of include/rl_distill.h."""
+    p, z, nbytes, batch = C.c_void_p, C.c_size_t, C.POINTER(C.c_size_t), C.POINTER(rl_batch)
+    top, prm = C.POINTER(rl_top_params), C.POINTER(rl_distill_params)
+    for name, args in dict(
+            rl_token_top_logprobs_workspace_bytes=[batch, top, nbytes],
+            rl_token_top_logprobs=[batch, top, C.POINTER(rl_top_outputs), p, z, p],
+            rl_distill_workspace_bytes=[batch, prm, C.c_int32, nbytes],
+            rl_distill_loss_fwd_bwd=[batch, p, p, prm, C.POINTER(rl_distill_outputs), p, z, p],
+            rl_default_chunk_rows_distill=[]).items():
+        fn = getattr(L, name)
+        fn.argtypes, fn.restype = args, C.c_int
 
 
 def _check(st: int):
@@ -697,3 +730,106 @@ def rl_f8_linear_backward(dy, kept: F8Rows, w: F8Weight, fmt="e5m2", want_dx=Tru
     _check(lib().rl_f8_linear_backward(pdy, lddy, dt, M, N, K, F8_FORMATS[fmt], cx, sx, fx, ct, st, fw, dx.data_ptr() if want_dx else None, K,
                                        pdw, lddw, 1 if accumulate else 0, pws, nws, _stream_handle()))
     return dx, dw if want_dw else None
+
+
+# ------------------------------------------------------------------ scoring with top alternatives, distillation
+RESTS = {"bucket": 0, "renormalise": 1}
+DISTILL_STATS_FIELDS = ("n_tokens", "n_bad_entry", "n_empty_row", "n_bad_seq")
+
+
+@dataclass
+class TopLogprobs:
+    logprob: Optional[torch.Tensor]      # float32 [R]; None without token_ids
+    lse: torch.Tensor                    # float32 [R]
+    entropy: torch.Tensor                # float32 [R]
+    top_ids: torch.Tensor                # int32 [R, top_k], most probable first, -1 on rows that do not count
+    top_logprob: torch.Tensor            # float32 [R, top_k]
+
+
+@dataclass
+class DistillResult:
+    loss: torch.Tensor                   # float32 [1]
+    row_loss: torch.Tensor               # float32 [R]: divergence of each row
+    lse: torch.Tensor                    # float32 [R]
+    d_hidden: Optional[torch.Tensor]     # [R, H] in the dtype of hidden
+    d_weight: Optional[torch.Tensor]     # [V, H]
+    stats: torch.Tensor                  # int32[4]: see DISTILL_STATS_FIELDS
+
+    def stats_dict(self):
+        return dict(zip(DISTILL_STATS_FIELDS, self.stats.cpu().tolist()))
+
+
+def _head_batch(hidden, weight, token_ids, mask, cu_seqlens, *others):
+    """The batch of a call on the LM head, its tensors on one device (that of the call: the current stream is taken there)."""
+    if hidden.dim() != 2 or weight.dim() != 2:
+        raise ValueError("hidden must be [R, H] and weight [V, H]")
+    dev = hidden.device
+    for t in (weight, token_ids, mask, cu_seqlens, *others):
+        if t is not None and t.device != dev:
+            raise ValueError(f"all tensors must live on one device, got {dev} and {t.device}")
+    if cu_seqlens is None:
+        cu_seqlens = torch.zeros(2, dtype=torch.int32, device=dev)
+        cu_seqlens[1:] = hidden.shape[0]                   # (a fill: nothing is copied from the host)
+    return make_batch(hidden, weight, token_ids, mask, cu_seqlens), cu_seqlens
+
+
+def _given_workspace(ws, need, device):
+    if ws is None:
+        return _workspace(need, device)
+    if ws.device != device or ws.dtype != torch.uint8 or not ws.is_contiguous():
+        raise ValueError("workspace must be a contiguous uint8 tensor on the device of the call")
+    return ws
+
+
+def rl_token_top_logprobs(hidden, weight, token_ids, mask, top_k, temperature=1.0, cu_seqlens=None, chunk_rows=0, workspace=None) -> TopLogprobs:
+    """Log-probability of token_ids (may be None), logsumexp, entropy and the top_k most probable tokens of softmax(W x / temperature), ties to the
+    lower token.  Rows that do not count read 0, and -1 for tokens."""
+    b, cu_seqlens = _head_batch(hidden, weight, token_ids, mask, cu_seqlens)
+    with torch.cuda.device(hidden.device):
+        prm = rl_top_params(int(top_k), int(chunk_rows), float(temperature))
+        need = C.c_size_t(0)
+        _check(lib().rl_token_top_logprobs_workspace_bytes(C.byref(b), C.byref(prm), C.byref(need)))
+        f32 = dict(dtype=torch.float32, device=hidden.device)
+        R = hidden.shape[0]
+        r = TopLogprobs(torch.empty(R, **f32) if token_ids is not None else None, torch.empty(R, **f32), torch.empty(R, **f32),
+                        torch.empty((R, prm.top_k), dtype=torch.int32, device=hidden.device), torch.empty((R, prm.top_k), **f32))
+        out = rl_top_outputs(r.logprob.data_ptr() if r.logprob is not None else None, r.lse.data_ptr(), r.entropy.data_ptr(), r.top_ids.data_ptr(),
+                             r.top_logprob.data_ptr())
+        ws = _given_workspace(workspace, need.value, hidden.device)
+        _check(lib().rl_token_top_logprobs(C.byref(b), C.byref(prm), C.byref(out), ws.data_ptr(), ws.numel(), _stream_handle()))
+    return r
+
+
+def rl_distill_loss_fwd_bwd(hidden, weight, teacher_ids, teacher_logprob, mask, cu_seqlens=None, rest="bucket", temperature=1.0, aggregation="sequence",
+                            scale=1.0, chunk_rows=0, backward=True, d_weight_dtype=torch.float32, d_hidden=None, workspace=None) -> DistillResult:
+    """Divergence from a teacher's entries teacher_ids, teacher_logprob [R, K] (as rl_token_top_logprobs writes them; -1: no entry) to softmax(W x /
+    temperature), its loss over the batch and the gradients.  rest: "bucket" (what the entries leave is one entry for all other tokens) or
+    "renormalise"; aggregation: "sequence" or "token".  d_hidden: where that gradient goes (hidden itself will do), else a new tensor."""
+    if teacher_ids.dim() != 2:
+        raise ValueError("teacher_ids must be [R, K]")
+    b, cu_seqlens = _head_batch(hidden, weight, None, mask, cu_seqlens, teacher_ids, teacher_logprob, d_hidden)
+    (R, H), V, K = hidden.shape, weight.shape[0], teacher_ids.shape[1]
+    p_ids = _ptr(teacher_ids, torch.int32, R * K, "teacher_ids")
+    p_lp = _ptr(teacher_logprob, torch.float32, R * K, "teacher_logprob")
+    if d_weight_dtype not in _DTYPE_CODES:
+        raise ValueError(f"d_weight_dtype must be float32 or bfloat16, got {d_weight_dtype}")
+    with torch.cuda.device(hidden.device):
+        if float(scale) == 0.0:
+            raise ValueError("scale must not be 0")
+        prm = rl_distill_params(K, _enum(RESTS, rest), _enum(AGGREGATIONS, aggregation), int(chunk_rows), float(temperature), float(scale),
+                                _DTYPE_CODES[d_weight_dtype])
+        need = C.c_size_t(0)
+        _check(lib().rl_distill_workspace_bytes(C.byref(b), C.byref(prm), 1 if backward else 0, C.byref(need)))
+        f32 = dict(dtype=torch.float32, device=hidden.device)
+        if backward:
+            if d_hidden is None:
+                d_hidden = torch.empty_like(hidden)
+            _ptr(d_hidden, hidden.dtype, R * H, "d_hidden")
+        r = DistillResult(torch.empty(1, **f32), torch.empty(R, **f32), torch.empty(R, **f32), d_hidden if backward else None,
+                          torch.empty((V, H), dtype=d_weight_dtype, device=hidden.device) if backward else None,
+                          torch.empty(4, dtype=torch.int32, device=hidden.device))
+        out = rl_distill_outputs(r.loss.data_ptr(), r.row_loss.data_ptr(), r.lse.data_ptr(), r.d_hidden.data_ptr() if backward else None,
+                                 r.d_weight.data_ptr() if backward else None, r.stats.data_ptr())
+        ws = _given_workspace(workspace, need.value, hidden.device)
+        _check(lib().rl_distill_loss_fwd_bwd(C.byref(b), p_ids, p_lp, C.byref(prm), C.byref(out), ws.data_ptr(), ws.numel(), _stream_handle()))
+    return r

@@ -1,0 +1,935 @@
+// distill.h - scoring with top alternatives, and distillation from a teacher's top entries: kernels and C ABI of include/rl_distill.h.
+//
+// Both keep a chunk's logits in f32, and beside them a record of every 64 vocabulary entries of a token, made where the logits are in registers:
+// their maximum and softmax sums.  A record is 1/16 of what it stands for, and nearly everything after the contraction is answered from the records:
+//  * logsumexp and entropy are sums over them;
+//  * the K largest logits of a row lie in the K groups with the largest maxima (ties of maxima to the lower group: K maxima come before any element
+//    of another group, in the order by value, then by index), so K of V / 64 groups are read;
+//  * the sum over all tokens that a teacher's list does not name is the sum over the groups without a listed token, from their records, and over the
+//    others from the logits, with the listed ones left out: never a difference of two sums, which would have no digit left where the list has nearly
+//    all of the probability.
+// What is read of the logits once more is the whole chunk, by the backward, which turns it into dS in one pass.
+//
+// Sums: those of a group in f32, of groups in f64; each exponential is taken of a difference to the group's or the row's maximum (formed before it is
+// scaled), so that what carries the sum carries no error of the shift.
+#pragma once
+#include "../../include/rl_distill.h"
+
+namespace rlk {
+
+constexpr int kDefaultChunkRowsDistill = 16384;   // 10 GB of logits and 5 of dS at the 7B head
+constexpr int kMostChunkRows = 1 << 20;           // (launches of a chunk stay below 2^32 threads)
+constexpr int kGroup = 64;                        // vocabulary entries of a record
+
+// ------------------------------------------------------------------ logits and records
+// Record of 64 logits of a token, x largest (raw), y sum exp(zs (z - x)), z sum of those times (z - x); w unused.
+//
+// In what order the 64 are added: bf16 (kPermute, a lane holds eight consecutive entries of each half of the group): the sixteen of a lane in order, then lanes 16
+// apart, then 32.  f32, by quads of four consecutive entries Q = 0 .. 15: over bits 2 and 3 of Q in order, then bit 1, then bit 0, which both
+// block shapes of the f32 kernels can do: a token's sums do not depend on the tile it is in.
+template <class T>
+struct EpiScore {
+  typedef NoPre Pre;
+  template <class L> __device__ Pre preload(const TileCtx&, const GemmDims&) const { return Pre(); }
+  static constexpr bool kSwap = false;
+  static constexpr bool kSplit = false;
+  static constexpr bool kPermute = true;
+  static constexpr bool kGatherB = true;
+  __device__ void keep_alive() const { z[0] = 0.f; }
+  float* z; int64_t ldz;      // logits, slab-tiled like the bf16 work buffers: a tile of 256 x 256 is one piece of memory
+  float4* rec; int ldr;       // [vocabulary / 64][chunk rows]
+  int V;
+  float zs;                   // inverse temperature
+
+  // sixteen logits of a lane (entries (r / 8) 32 + g 8 + r % 8 of the group), of its token n; even and odd lanes have neighbouring tokens
+  template <bool PAD>
+  __device__ __attribute__((always_inline)) float4 group16(const float (&v)[16], int g, int vleft) const {
+    const float NEG = -__builtin_inff(), c = zs * kLog2e;
+    auto in = [&](int r) __attribute__((always_inline)) { return !PAD || (r >> 3) * 32 + g * 8 + (r & 7) < vleft; };
+    float mx = NEG, a, b;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) mx = fmaxf(mx, in(r) ? v[r] : NEG);
+    lane_pair<16>(mx, a, b); mx = fmaxf(a, b);
+    lane_pair<32>(mx, a, b); mx = fmaxf(a, b);
+    const float ms = mx == NEG ? 0.f : mx;
+    float s = 0.f, u = 0.f;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      const float d = v[r] - ms, e = in(r) ? __builtin_amdgcn_exp2f(d * c) : 0.f;
+      s += e;
+      u = in(r) ? __builtin_fmaf(e, d, u) : u;
+    }
+    lane_pair<16>(s, a, b); s = a + b;
+    lane_pair<32>(s, a, b); s = a + b;
+    lane_pair<16>(u, a, b); u = a + b;
+    lane_pair<32>(u, a, b); u = a + b;
+    return make_float4(mx, s, u, 0.f);
+  }
+
+  // MB = 8 block rows (128 permuted rows) of NB columns; COL: token of column bj
+  template <int MB, int NB, bool AGPR, class COL>
+  __device__ __attribute__((always_inline)) void permuted(floatx4 (&acc)[MB][NB], const TileCtx& c, COL col) const {
+    static_assert(MB == 8, "128 rows");
+    const int g = c.lane >> 4, p = c.lane & 1;
+    const int vleft = V - c.m0;
+#pragma unroll
+    for (int j = 0; j < 2; ++j)
+#pragma unroll
+      for (int bj = 0; bj < NB; ++bj) {
+        float v[16];
+#pragma unroll
+        for (int r = 0; r < 16; ++r) v[r] = acc_read<AGPR>(acc[4 * j + (r >> 2)][bj], r & 3);
+        const int n = col(bj, c.lane);
+        const float4 q = vleft < j * 64 + 64 ? group16<true>(v, g, vleft - j * 64) : group16<false>(v, g, 64);
+        if (g == (NB >= 4 ? bj / (NB / 4) : bj) && n < c.Nv) rec[(int64_t)(c.m0 / kGroup + j) * ldr + n] = q;
+        // lane pairs swap quads, so that a store writes whole lines of 128 bytes
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          floatx4 even, odd;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const float lo = v[h * 8 + e], hi = v[h * 8 + 4 + e];
+            const float got = __uint_as_float((unsigned)__builtin_amdgcn_mov_dpp((int)__float_as_uint(p ? lo : hi), 0xB1, 0xF, 0xF, true));
+            even[e] = p ? got : lo; odd[e] = p ? hi : got;
+          }
+          const int ne = col(bj, c.lane & ~1), no = col(bj, c.lane | 1), at = c.m0 + j * 64 + h * 32 + g * 8 + p * 4;
+          if (ne < c.Nv) __builtin_nontemporal_store(even, reinterpret_cast<floatx4*>(z + tiled_index(ne, at, ldz)));
+          if (no < c.Nv) __builtin_nontemporal_store(odd, reinterpret_cast<floatx4*>(z + tiled_index(no, at, ldz)));
+        }
+      }
+  }
+
+  // general and f32 kernels: rows in their natural order
+  template <class L, int MB, int NB>
+  __device__ __attribute__((always_inline)) void natural(typename L::acc_t (&acc)[MB][NB], const TileCtx& c) const {
+    constexpr int PER = kGroup / L::kBlk;                        // blocks of a group
+    static_assert(MB % PER == 0, "a wavefront has whole groups");
+    const float NEG = -__builtin_inff(), cs = zs * kLog2e;
+#pragma unroll
+    for (int bj = 0; bj < NB; ++bj) {
+      const int n = c.n0 + L::col(bj, c.lane);
+#pragma unroll
+      for (int k = 0; k < MB / PER; ++k) {
+        const int vleft = V - c.m0 - k * kGroup;
+        float mx = NEG, a, b;
+        auto in = [&](int bi, int i) __attribute__((always_inline)) { return L::row(bi, i, c.lane) < vleft; };
+#pragma unroll
+        for (int bi = 0; bi < PER; ++bi)
+#pragma unroll
+          for (int i = 0; i < L::kRegs; ++i) mx = fmaxf(mx, in(bi, i) ? acc[k * PER + bi][bj][i] : NEG);
+        lane_pair<32>(mx, a, b); mx = fmaxf(a, b);
+        if constexpr (L::kBlk == 16) { lane_pair<16>(mx, a, b); mx = fmaxf(a, b); }
+        const float ms = mx == NEG ? 0.f : mx;
+        float s[2] = {0.f, 0.f}, u[2] = {0.f, 0.f};              // (32 x 32 blocks: by bit 1 of the quad)
+#pragma unroll
+        for (int bi = 0; bi < PER; ++bi)
+#pragma unroll
+          for (int i = 0; i < L::kRegs; ++i) {
+            const int w = L::kBlk == 32 ? (i >> 2) & 1 : 0;
+            const float d = acc[k * PER + bi][bj][i] - ms, e = in(bi, i) ? __builtin_amdgcn_exp2f(d * cs) : 0.f;
+            s[w] += e;
+            u[w] = in(bi, i) ? __builtin_fmaf(e, d, u[w]) : u[w];
+          }
+        auto join = [&](float (&x)[2]) __attribute__((always_inline)) {
+          float r;
+          if constexpr (L::kBlk == 32) { r = x[0] + x[1]; lane_pair<32>(r, a, b); r = a + b; }
+          else { lane_pair<32>(x[0], a, b); r = a + b; lane_pair<16>(r, a, b); r = a + b; }
+          return r;
+        };
+        const float S = join(s), U = join(u);
+        if (n < c.Nv) {
+          if (c.lane < L::kBlk) rec[(int64_t)(c.m0 / kGroup + k) * ldr + n] = make_float4(mx, S, U, 0.f);
+#pragma unroll
+          for (int bi = 0; bi < PER; ++bi)
+#pragma unroll
+            for (int i = 0; i < L::kRegs; i += 4) {
+              floatx4 o;
+#pragma unroll
+              for (int e = 0; e < 4; ++e) o[e] = acc[k * PER + bi][bj][i + e];
+              *reinterpret_cast<floatx4*>(z + tiled_index(n, c.m0 + k * kGroup + L::row(bi, i, c.lane), ldz)) = o;
+            }
+        }
+      }
+    }
+  }
+
+  template <class L, int MB, int NB>
+  __device__ __attribute__((always_inline)) void half_tile(typename L::acc_t (&acc)[MB][NB], const TileCtx& c, const int (&)[NB]) const {
+    permuted<MB, NB, false>(acc, c, [&](int bj, int lane) { return c.n0 + L::col(bj, lane); });
+  }
+  template <class L, int MB, int NB, int BM, int BN, int WAVES_M, int WAVES_N, bool AGPR>
+  __device__ __attribute__((always_inline)) void run(typename L::acc_t (&acc)[MB][NB], const TileCtx& c, unsigned char*, const GemmDims&, const Pre&) const {
+    if constexpr (AGPR) permuted<MB, NB, true>(acc, c, [&](int bj, int lane) { return c.n0 + perm_col(bj, lane & 15); });
+    else natural<L, MB, NB>(acc, c);
+  }
+};
+
+template <int BN, bool NT>
+__global__ __launch_bounds__(256, 1)
+void score_few_kernel(const bf16_t* __restrict__ W, const bf16_t* __restrict__ X, GemmDims d, EpiScore<bf16_t> epi, const int* ids_c) {
+  __shared__ __attribute__((aligned(1024))) unsigned char smem[few_lds_bytes<BN>()];
+  const int left = *d.n_real;
+  logits_few_tile<BN, NT>(W, X, d, epi, blockIdx.x, left < d.N ? left : d.N, d.b_rows, ids_c, smem);
+}
+
+// ------------------------------------------------------------------ a row, by a wavefront
+// What a lane wrote to LDS is there for the wavefront's other lanes.
+__device__ __attribute__((always_inline)) inline void wave_sync() {
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
+__device__ inline float wave_max(float v) { for (int o = 32; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor(v, o)); return v; }
+
+// Order of logits as unsigned numbers: -0 is 0, what is no number comes before everything.
+__device__ inline unsigned order_key(float z) {
+  const unsigned u = __float_as_uint(z + 0.f);
+  return z != z ? 0u : u ^ ((unsigned)((int)u >> 31) | 0x80000000u);
+}
+__device__ inline float key_value(unsigned k) { return __uint_as_float(k & 0x80000000u ? k ^ 0x80000000u : ~k); }
+
+// Sums under a running maximum (raw units, c = log2(e) / temperature).  Not-a-numbers stay in s.
+struct Online {
+  float m = -__builtin_inff();
+  double s = 0.0, u = 0.0;
+  __device__ __attribute__((always_inline)) void raise(float mm, float c) {
+    if (!(mm > m)) return;
+    if (m != -__builtin_inff()) {
+      const double f = (double)__builtin_amdgcn_exp2f((m - mm) * c);
+      u = f * (u + (double)(m - mm) * s);
+      s *= f;
+    }
+    m = mm;
+  }
+  __device__ __attribute__((always_inline)) void add(const float4& q, float c) {       // a record with a maximum of at most m
+    if (q.x > -__builtin_inff()) {
+      const float d = q.x - m, f = __builtin_amdgcn_exp2f(d * c);
+      s += (double)f * (double)q.y;
+      u += (double)f * ((double)q.z + (double)d * (double)q.y);
+    } else if (q.y != q.y) s = __builtin_nan("");
+  }
+  __device__ void join_lanes(float c) {
+    raise(wave_max(m), c);
+    s = wave_sum(s); u = wave_sum(u);
+  }
+};
+
+// The records of row t, group after group to the lanes: f(group, record), after the maxima of eight have been given to r(maximum).
+template <class RAISE, class F>
+__device__ __attribute__((always_inline)) inline void walk_records(const float4* rec, int ldr, int groups, int t, int lane, RAISE r, F f) {
+  for (int b0 = lane; b0 < groups; b0 += 8 * 64) {
+    float4 q[8];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      const int b = b0 + 64 * k;
+      q[k] = make_float4(-__builtin_inff(), 0.f, 0.f, 0.f);
+      if (b < groups) q[k] = rec[(int64_t)b * ldr + t];
+    }
+    r(q, b0);
+#pragma unroll
+    for (int k = 0; k < 8; ++k) if (b0 + 64 * k < groups) f(b0 + 64 * k, q[k]);
+  }
+}
+
+constexpr int kRowWaves = 4;            // most wavefronts, and rows, of a workgroup of the two kernels below
+constexpr int kTopList = 512;           // candidates held at a time
+
+struct TopJob {
+  const float* z; int64_t ldz; const float4* rec; int ldr, groups, V, K;
+  float zs;
+  const int *row_map, *ids_c, *cpos;
+  const Ctrl* ctrl;
+  int chunk_start, chunk_rows;
+  int64_t R;
+  int row_blocks;                       // workgroups with rows; the rest write what rows that do not count read
+  float *logprob, *lse, *entropy; int32_t* ids; float* lp;
+};
+__host__ __device__ inline int top_lds_words(int groups) { return groups + 2 * kTopList + RL_TOP_MAX_K; }       // of a wavefront
+// as many as 64 KiB hold, which is one at least (RL_TOP_MAX_V)
+static int top_waves(int groups) { const int n = (64 << 10) / (4 * top_lds_words(groups)); return n < kRowWaves ? n : kRowWaves; }
+static_assert(4 * (RL_TOP_MAX_V / kGroup + 2 * kTopList + RL_TOP_MAX_K) <= (64 << 10), "a row's keys fit");
+
+// The K-th largest of n keys, of which lane l has key(i) at i 64 + l: x, with `at_least` keys >= x, K of them or, where more equal the K-th, more.  n >= K.
+// (Bit by bit from the top; done when a prefix parts K from the rest.)
+template <class KEY>
+__device__ __attribute__((always_inline)) inline unsigned kth_key(int n, int K, int lane, KEY key, int& at_least) {
+  unsigned x = 0;
+  at_least = n;
+  for (int bit = 31; bit >= 0 && at_least != K; --bit) {
+    const unsigned cand = x | 1u << bit;
+    int c = 0;
+    for (int i = 0; i * 64 < n; ++i) c += __popcll(__ballot(i * 64 + lane < n && key(i) >= cand));
+    if (c >= K) { x = cand; at_least = c; }
+  }
+  return x;
+}
+// Whether a key is among the K best, keys given in order of index: calls in order, wavefront-uniform.  Equals of the K-th go in while there is room.
+struct BestOf {
+  unsigned x; int room; bool exact;
+  template <class KEY>
+  __device__ __attribute__((always_inline)) BestOf(int n, int K, int lane, KEY key) {
+    int at_least;
+    x = kth_key(n, K, lane, key, at_least);
+    exact = at_least == K;
+    room = K;
+    if (!exact) for (int i = 0; i * 64 < n; ++i) room -= __popcll(__ballot(i * 64 + lane < n && key(i) > x));
+  }
+  __device__ __attribute__((always_inline)) unsigned long long take(unsigned k, bool there, int lane) {
+    if (exact) return __ballot(there && k >= x);
+    const unsigned long long eq = __ballot(there && k == x);
+    const bool in = there && (k > x || (k == x && (int)__popcll(eq & ((1ull << lane) - 1ull)) < room));
+    room -= __popcll(eq);
+    return __ballot(in);
+  }
+};
+
+__global__ __launch_bounds__(kRowWaves * 64) void top_kernel(TopJob j) {
+  extern __shared__ unsigned lds[];
+  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, waves = blockDim.x >> 6;
+  if ((int)blockIdx.x >= j.row_blocks) {
+    const int64_t step = (int64_t)(gridDim.x - j.row_blocks) * waves;
+    for (int64_t r = (int64_t)(blockIdx.x - j.row_blocks) * waves + w; r < j.R; r += step) {
+      if (j.cpos[r] >= 0) continue;
+      for (int k = lane; k < j.K; k += 64) {
+        if (j.ids) j.ids[r * j.K + k] = -1;
+        if (j.lp) j.lp[r * j.K + k] = 0.f;
+      }
+    }
+    return;
+  }
+  int left = j.ctrl->n_real - j.chunk_start;
+  left = left < j.chunk_rows ? left : j.chunk_rows;
+  const int t = (int)blockIdx.x * waves + w;
+  if (t >= left) return;                                          // (no barrier below: a wavefront is on its own)
+  unsigned* keys = lds + w * top_lds_words(j.groups);
+  unsigned* lk = keys + j.groups;                                 // candidates: key, token, in order of tokens
+  unsigned* lv = lk + kTopList;
+  unsigned* sel = lv + kTopList;                                  // groups taken
+  const float c = j.zs * kLog2e;
+  const int tg = j.chunk_start + t, row = j.row_map[tg];
+
+  Online o;
+  walk_records(j.rec, j.ldr, j.groups, t, lane,
+               [&](const float4 (&q)[8], int) { float mm = o.m; for (int k = 0; k < 8; ++k) mm = fmaxf(mm, q[k].x); o.raise(mm, c); },
+               [&](int b, const float4& q) { o.add(q, c); keys[b] = order_key(q.x); });
+  o.join_lanes(c);
+  const double ln = log(o.s), lse = (double)j.zs * (double)o.m + ln;
+  if (lane == 0) {
+    if (j.lse) j.lse[row] = (float)lse;
+    if (j.logprob) j.logprob[row] = (float)((double)j.zs * ((double)j.z[tiled_index(t, j.ids_c[tg], j.ldz)] - (double)o.m) - ln);
+    if (j.entropy) { const double h = ln - (double)j.zs * o.u / o.s; j.entropy[row] = (float)(h < 0.0 ? 0.0 : h); }
+  }
+  if (!j.ids && !j.lp) return;
+  wave_sync();
+
+  // the groups that hold them
+  const int K = j.K;
+  int n_sel = 0;
+  unsigned least = 0;                                             // keys below it are not among the K best
+  if (j.groups <= K) {
+    for (int b = lane; b < j.groups; b += 64) sel[b] = b;
+    n_sel = j.groups;
+  } else {
+    BestOf best(j.groups, K, lane, [&](int i) { return keys[i * 64 + lane]; });
+    least = best.x;
+    for (int b0 = 0; b0 < j.groups; b0 += 64) {
+      const bool there = b0 + lane < j.groups;
+      const unsigned long long in = best.take(there ? keys[b0 + lane] : 0u, there, lane);
+      if (in >> lane & 1) sel[n_sel + __popcll(in & ((1ull << lane) - 1ull))] = b0 + lane;
+      n_sel += __popcll(in);
+    }
+  }
+  wave_sync();
+
+  // the best K of those listed so far, in place; a later token has to be larger than the K-th to come in
+  int n = 0;
+  auto keep_best = [&]() {
+    unsigned k[kTopList / 64], v[kTopList / 64];
+#pragma unroll
+    for (int i = 0; i < kTopList / 64; ++i) { k[i] = lk[i * 64 + lane]; v[i] = lv[i * 64 + lane]; }
+    wave_sync();
+    BestOf best(n, K, lane, [&](int i) { return lk[i * 64 + lane]; });
+    int m = 0;
+    wave_sync();
+#pragma unroll
+    for (int i = 0; i < kTopList / 64; ++i) {
+      const unsigned long long in = best.take(k[i], i * 64 + lane < n, lane);
+      if (in >> lane & 1) { const int at = m + __popcll(in & ((1ull << lane) - 1ull)); lk[at] = k[i]; lv[at] = v[i]; }
+      m += __popcll(in);
+    }
+    wave_sync();
+    n = m;
+    least = best.x + 1;
+  };
+  for (int s0 = 0; s0 < n_sel; s0 += 8) {
+    float z[8];
+    int at[8];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      at[k] = (int)sel[s0 + k < n_sel ? s0 + k : s0] * kGroup + lane;
+      z[k] = j.z[tiled_index(t, at[k], j.ldz)];
+    }
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      const unsigned key = order_key(z[k]);
+      const unsigned long long in = __ballot(s0 + k < n_sel && at[k] < j.V && z[k] == z[k] && key >= least);
+      if (!in) continue;
+      if (in >> lane & 1) { const int i = n + __popcll(in & ((1ull << lane) - 1ull)); lk[i] = key; lv[i] = at[k]; }
+      n += __popcll(in);
+      wave_sync();
+      if (n > kTopList - 64) { if (n > K) keep_best(); }
+    }
+  }
+  if (n > K) keep_best();
+
+  // in order: each counts those before it
+  for (int i0 = 0; i0 < K; i0 += 64) {
+    const int i = i0 + lane;
+    const unsigned mine = i < n ? lk[i] : 0u, tok = i < n ? lv[i] : 0u;
+    int rank = 0;
+    for (int q = 0; q < n; ++q) { const unsigned k = lk[q]; rank += k > mine || (k == mine && q < i); }
+    if (i >= K) continue;
+    if (i >= n) rank = i;                                         // (fewer numbers than K in the row)
+    if (j.ids) j.ids[(int64_t)row * K + rank] = i < n ? (int)tok : -1;
+    if (j.lp) j.lp[(int64_t)row * K + rank] = i < n ? (float)((double)j.zs * ((double)key_value(mine) - (double)o.m) - ln) : __builtin_nanf("");
+  }
+}
+
+// ------------------------------------------------------------------ distillation, a row by a wavefront
+// What the backward needs of a row: dS = f exp(zs (z - m) - l) at tokens that the list does not name, in log2 units.
+struct DistillRow { float m, l2, f, pad; };
+struct DistillJob {
+  const float* z; int64_t ldz; const float4* rec; int ldr, groups, V, K;
+  float zs;
+  const int *row_map, *cstart;
+  const Ctrl* ctrl;
+  int chunk_start, chunk_rows, B;
+  const int32_t* t_ids; const float* t_lp;
+  int rest, token_mean;
+  float scale;
+  float *row_loss, *lse;
+  double* term;                         // [compact row] this row's part of the loss
+  int* info;                            // [compact row] entries left out, bit 30: empty
+  DistillRow* rows; int* p_ids; float* p_val;          // [chunk row], [chunk row][K]: the tokens that are listed and their dS (-1: none); NULL without backward
+};
+__host__ __device__ inline size_t distill_lds_bytes(int groups) { return (size_t)kRowWaves * 4 * ((groups + 31) / 32 + 2 * RL_TOP_MAX_K + 4); }
+
+// Sequence of compact row t: the last i with cstart[i] <= t, 64 at a time.
+__device__ inline int sequence_of(const int* cstart, int B, int t, int lane) {
+  int lo = 0, n = B;                    // among [lo, lo + n)
+  while (n > 1) {
+    const int step = (n + 63) / 64, i = lane * step;
+    const int c = __popcll(__ballot(i < n && cstart[lo + i] <= t)) - 1;
+    lo += c * step;
+    n = n - c * step < step ? n - c * step : step;
+  }
+  return lo;
+}
+
+__global__ __launch_bounds__(kRowWaves * 64) void distill_row_kernel(DistillJob j) {
+  extern __shared__ unsigned lds[];
+  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+  int left = j.ctrl->n_real - j.chunk_start;
+  left = left < j.chunk_rows ? left : j.chunk_rows;
+  const int t = (int)blockIdx.x * kRowWaves + w;
+  if (t >= left) return;                                          // (a wavefront is on its own)
+  const int words = (j.groups + 31) / 32, K = j.K;
+  unsigned* bits = lds + w * (words + 2 * RL_TOP_MAX_K + 4);      // groups with a listed token
+  int* ids = (int*)(bits + words);
+  unsigned* sel = (unsigned*)(ids + RL_TOP_MAX_K);
+  unsigned* mask = sel + RL_TOP_MAX_K;                            // tokens listed of two groups in turn
+  const float c = j.zs * kLog2e;
+  const int tg = j.chunk_start + t, row = j.row_map[tg];
+  const float NEG = -__builtin_inff();
+
+  // the list: entry lane and lane + 64
+  int id[2]; float lp[2]; bool in[2];
+  int left_out = 0;
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    const int i = h * 64 + lane;
+    id[h] = -1; lp[h] = NEG;
+    if (i < K) { id[h] = j.t_ids[(int64_t)row * K + i]; lp[h] = j.t_lp[(int64_t)row * K + i]; }
+    in[h] = id[h] >= 0 && id[h] < j.V;
+    left_out += __popcll(__ballot(id[h] != -1 && !in[h]));
+    ids[i] = in[h] ? id[h] : -1;
+  }
+  for (int b = lane; b < words; b += 64) bits[b] = 0u;
+  wave_sync();
+  bool again[2] = {false, false};
+  for (int i = 0; i < K; ++i) {
+    const int o = ids[i];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) again[h] |= in[h] && o == id[h] && i < h * 64 + lane;
+  }
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    left_out += __popcll(__ballot(again[h]));
+    in[h] = in[h] && !again[h];
+    if (in[h]) atomicOr(&bits[id[h] / kGroup >> 5], 1u << (id[h] / kGroup & 31));
+  }
+  wave_sync();
+
+  // all tokens, and those of groups without a listed one
+  Online o, r;
+  auto plain = [&](int b) { return !(bits[b >> 5] >> (b & 31) & 1u); };
+  walk_records(j.rec, j.ldr, j.groups, t, lane,
+               [&](const float4 (&q)[8], int b0) {
+                 float mm = o.m, mr = r.m;
+                 for (int k = 0; k < 8; ++k) {
+                   mm = fmaxf(mm, q[k].x);
+                   if (b0 + 64 * k < j.groups && plain(b0 + 64 * k)) mr = fmaxf(mr, q[k].x);
+                 }
+                 o.raise(mm, c); r.raise(mr, c);
+               },
+               [&](int b, const float4& q) { o.add(q, c); if (plain(b)) r.add(q, c); });
+  o.join_lanes(c);
+  const double ln = log(o.s);
+  if (lane == 0 && j.lse) j.lse[row] = (float)((double)j.zs * (double)o.m + ln);
+
+  double P = 0.0, pr = 0.0, kl = 0.0, lnr = 0.0;
+  double p[2], lq[2];
+  bool any = false;
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    lq[h] = in[h] ? (double)j.zs * ((double)j.z[tiled_index(t, id[h], j.ldz)] - (double)o.m) - ln : 0.0;
+    any |= in[h];
+  }
+  const bool empty = !__ballot(any);
+  if (j.rest == RL_REST_BUCKET) {
+    // ... and the others of groups with one
+    int n_sel = 0;
+    for (int b0 = 0; b0 < words; ++b0)
+      for (unsigned m = bits[b0]; m; m &= m - 1) { if (lane == 0) sel[n_sel] = b0 * 32 + __builtin_ctz(m); ++n_sel; }
+    wave_sync();
+    for (int s0 = 0; s0 < n_sel; s0 += 8) {
+      float z[8];
+      int gr[8];
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {
+        gr[k] = (int)sel[s0 + k < n_sel ? s0 + k : s0];
+        z[k] = j.z[tiled_index(t, gr[k] * kGroup + lane, j.ldz)];
+      }
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {
+        if (s0 + k >= n_sel) continue;
+        unsigned* mk = mask + (k & 1) * 2;
+        if (lane < 2) mk[lane] = 0u;
+        wave_sync();
+#pragma unroll
+        for (int h = 0; h < 2; ++h) if (in[h] && id[h] / kGroup == gr[k]) atomicOr(&mk[(id[h] & 63) >> 5], 1u << (id[h] & 31));
+        wave_sync();
+        if (gr[k] * kGroup + lane < j.V && !(mk[lane >> 5] >> (lane & 31) & 1u)) {
+          r.raise(z[k], c);
+          r.add(make_float4(z[k], 1.f, 0.f, 0.f), c);
+        }
+        if (z[k] != z[k] && gr[k] * kGroup + lane < j.V) r.s = __builtin_nan("");
+      }
+    }
+    r.join_lanes(c);
+    double sum = 0.0;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) { p[h] = in[h] ? exp((double)lp[h]) : 0.0; sum += p[h]; }
+    sum = wave_sum(sum);
+    pr = 1.0 - sum; pr = pr < 0.0 ? 0.0 : pr;
+    if (r.m == NEG && r.s == 0.0) pr = 0.0;                       // (the list names all tokens)
+    if (empty) pr = 1.0;
+    P = sum + pr;
+    lnr = log(r.s);
+    if (pr > 0.0 && !empty) kl += pr * (log(pr) - ((double)j.zs * ((double)r.m - (double)o.m) + lnr - ln));
+  } else {
+    const float m = wave_max(fmaxf(in[0] ? lp[0] : NEG, in[1] ? lp[1] : NEG));
+    const float ms = m == NEG ? 0.f : m;
+    double sum = 0.0;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) { p[h] = in[h] ? exp((double)lp[h] - (double)ms) : 0.0; sum += p[h]; }
+    sum = wave_sum(sum);
+#pragma unroll
+    for (int h = 0; h < 2; ++h) p[h] = sum == 0.0 ? 0.0 : p[h] / sum;
+    P = sum == 0.0 ? 0.0 : 1.0;
+  }
+  double part = 0.0;
+#pragma unroll
+  for (int h = 0; h < 2; ++h) if (p[h] > 0.0 || p[h] != p[h]) part += p[h] * (log(p[h]) - lq[h]);
+  kl += wave_sum(part);
+  const bool nothing = empty || P == 0.0;
+  if (nothing) kl = 0.0;
+
+  const double share = j.token_mean ? 1.0 / (double)j.ctrl->n_real : [&]() {
+    const int i = sequence_of(j.cstart, j.B, tg, lane);
+    return 1.0 / ((double)j.B * (double)(j.cstart[i + 1] - j.cstart[i]));
+  }();
+  const double coef = (double)j.scale * share;
+  if (lane == 0) {
+    if (j.row_loss) j.row_loss[row] = (float)kl;
+    j.term[tg] = coef * kl;
+    j.info[tg] = left_out | (nothing ? 1 << 30 : 0);
+  }
+  if (!j.rows) return;
+  // dS at the others, coef zs q (P - pr / q_r).  With a bucket relative to their own sum, q / q_r (P q_r - pr): nothing overflows where q_r is small
+  const double f = coef * (double)j.zs;
+  if (lane == 0) {
+    DistillRow d{o.m, (float)(ln * 1.4426950408889634), nothing ? 0.f : (float)(f * P), 0.f};
+    if (j.rest == RL_REST_BUCKET && pr > 0.0 && !nothing) {
+      const double lqr = (double)j.zs * ((double)r.m - (double)o.m) + lnr - ln;
+      d.m = r.m; d.l2 = (float)(lnr * 1.4426950408889634); d.f = (float)(f * (P * exp(lqr) - pr));
+    }
+    j.rows[t] = d;
+  }
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    const int i = h * 64 + lane;
+    if (i >= K) continue;
+    j.p_ids[(int64_t)t * K + i] = in[h] && !nothing ? id[h] : -1;
+    j.p_val[(int64_t)t * K + i] = (float)(f * (P * exp(lq[h]) - p[h]));
+  }
+}
+
+// ------------------------------------------------------------------ dS
+__device__ __attribute__((always_inline)) inline float ds_entry(float z, const DistillRow& d, float c) {
+  return d.f == 0.f ? 0.f : d.f * __builtin_amdgcn_exp2f((z - d.m) * c - d.l2);
+}
+
+// bf16: logits and dS are both slab-tiled, a pass over memory in order; a workgroup takes a slab (256 rows, 64 vocabulary entries).  Rows of a slab without a token become 0,
+// as does the padding of the vocabulary.
+__global__ __launch_bounds__(256) void distill_ds_kernel(const float* z, int64_t ldz, const DistillRow* rows, const Ctrl* ctrl, int chunk_start, int V, float zs, bf16_t* dS) {
+  const int slabs = (int)(ldz / 64), tile = (int)(blockIdx.x / slabs), slab = (int)(blockIdx.x % slabs);
+  const int left = ctrl->n_real - chunk_start - tile * 256;
+  if (left <= 0) return;
+  const int64_t at = ((int64_t)tile * slabs + slab) * 16384;
+  const int e0 = (threadIdx.x & 7) * 8, v0 = slab * 64 + e0;
+  const float c = zs * kLog2e;
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    floatx4 x[4][2];
+    DistillRow d[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const int n = (h * 4 + k) * 32 + (threadIdx.x >> 3);
+      d[k].f = 0.f;
+      x[k][0] = x[k][1] = floatx4{0.f, 0.f, 0.f, 0.f};
+      if (n < left) {
+        d[k] = rows[tile * 256 + n];
+        const floatx4* p = reinterpret_cast<const floatx4*>(z + at + n * 64 + e0);
+        x[k][0] = __builtin_nontemporal_load(p); x[k][1] = __builtin_nontemporal_load(p + 1);
+      }
+    }
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const int n = (h * 4 + k) * 32 + (threadIdx.x >> 3);
+      bf16x8 o;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) o[e] = (bf16_t)(v0 + e < V ? ds_entry(x[k][e >> 2][e & 3], d[k], c) : 0.f);
+      store_stream(dS + at + n * 64 + e0, o);
+    }
+  }
+}
+
+// f32: dS (NULL: not wanted) and dS^T, row-major; 64 rows x 64 vocabulary entries of a workgroup.  Rows up to the next multiple of 64 become 0.
+__global__ __launch_bounds__(256) void distill_ds_f32_kernel(const float* z, int64_t ldz, const DistillRow* rows, const Ctrl* ctrl, int chunk_start, int V, float zs,
+                                                             float* dS, int64_t ld_ds, float* dST, int64_t ld_dst) {
+  __shared__ float tile[64][65];
+  const int vb = (int)(ldz / 64), n0 = (int)(blockIdx.x / vb) * 64, m0 = (int)(blockIdx.x % vb) * 64;
+  const int left = ctrl->n_real - chunk_start;
+  if (n0 >= left) return;
+  const int tx = threadIdx.x & 63, ty = threadIdx.x >> 6;
+  const float c = zs * kLog2e;
+#pragma unroll
+  for (int k = 0; k < 16; ++k) {
+    const int n = n0 + ty + 4 * k;
+    float o = 0.f;
+    if (n < left && m0 + tx < V) o = ds_entry(z[tiled_index(n, m0 + tx, ldz)], rows[n], c);
+    if (dS) dS[(int64_t)n * ld_ds + m0 + tx] = o;
+    tile[ty + 4 * k][tx] = o;
+  }
+  __syncthreads();
+#pragma unroll
+  for (int k = 0; k < 16; ++k) dST[(int64_t)(m0 + ty + 4 * k) * ld_dst + n0 + tx] = tile[tx][ty + 4 * k];
+}
+
+// dS of the listed tokens over what the pass wrote there
+template <class T>
+__global__ __launch_bounds__(256) void distill_patch_kernel(const int* ids, const float* val, int K, const Ctrl* ctrl, int chunk_start, int chunk_rows, T* dS, int64_t ld_ds,
+                                                            T* dST, int64_t ld_dst) {
+  int left = ctrl->n_real - chunk_start;
+  left = left < chunk_rows ? left : chunk_rows;
+  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  if (i >= (int64_t)left * K) return;
+  const int v = ids[i], t = (int)(i / K);
+  if (v < 0) return;
+  if (dS) dS[operand_index(sizeof(T) == 2, t, v, ld_ds)] = (T)val[i];
+  if (sizeof(T) == 4) dST[(int64_t)v * ld_dst + t] = (T)val[i];
+}
+
+// loss, and the counts: one workgroup, each thread its rows in order
+__global__ __launch_bounds__(1024) void distill_finish_kernel(const double* term, const int* info, const Ctrl* ctrl, const rl_stats* st, float* loss, rl_distill_stats* out) {
+  __shared__ double sh[16];
+  __shared__ int cnt[2];
+  if (threadIdx.x < 2) cnt[threadIdx.x] = 0;
+  __syncthreads();
+  const int n = ctrl->n_real;
+  double s = 0.0;
+  int bad = 0, empty = 0;
+  for (int i = threadIdx.x; i < n; i += 1024) { s += term[i]; bad += info[i] & 0xffff; empty += info[i] >> 30; }
+  s = block_sum(s, sh);
+  atomicAdd(&cnt[0], bad); atomicAdd(&cnt[1], empty);
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    loss[0] = (float)s;
+    if (out) *out = rl_distill_stats{n, cnt[0], cnt[1], st->n_bad_seq};
+  }
+}
+
+// d_weight from the f32 sums, rounded once; eight values a thread, of any alignment
+__global__ __launch_bounds__(256) void distill_round_kernel(const float* x, bf16_t* y, int64_t n) {
+  typedef bf16_t bf16x8_any __attribute__((ext_vector_type(8), aligned(2)));
+  for (int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 8; i < n; i += (int64_t)gridDim.x * 2048) {       // (n is a multiple of 8)
+    const floatx4 a = __builtin_nontemporal_load(reinterpret_cast<const floatx4*>(x + i)), b = __builtin_nontemporal_load(reinterpret_cast<const floatx4*>(x + i + 4));
+    bf16x8 o;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) { o[e] = (bf16_t)a[e]; o[4 + e] = (bf16_t)b[e]; }
+    *reinterpret_cast<bf16x8_any*>(y + i) = o;
+  }
+}
+
+// ------------------------------------------------------------------ host side
+struct HeadPlan {
+  Plan p;
+  int K, groups;
+  size_t off_z, off_rec, off_stats, off_term, off_info, off_rows, off_pids, off_pval, off_dw, total;
+};
+
+static bool good_temperature(float t) { return t == 0.f || (t > 0.f && t <= 3.0e38f); }
+
+static rl_status head_plan(const rl_batch* b, int K, int chunk_rows, float temperature, bool bwd, bool distill, bool round_dw, HeadPlan& h) {
+  if (!b) return RL_ERR_NULL;
+  if (!good_temperature(temperature)) return RL_ERR_RANGE;
+  if (chunk_rows < 0) return RL_ERR_SHAPE;
+  rl_batch one = *b;
+  one.P = 1;
+  rl_params prm{};
+  prm.chunk_rows = !chunk_rows ? kDefaultChunkRowsDistill : chunk_rows < kMostChunkRows ? chunk_rows : kMostChunkRows;
+  prm.temperature = temperature;
+  prm.backward_mode = RL_BWD_RECOMPUTE;
+  const rl_status st = make_plan(&one, &prm, bwd, h.p);
+  if (st != RL_OK) return st;
+  if (K < 1 || K > RL_TOP_MAX_K || b->V > RL_TOP_MAX_V) return RL_ERR_SHAPE;
+  Plan& p = h.p;
+  p.keep = false; p.small_grads = false;
+  h.K = K; h.groups = p.Vp / kGroup;
+  size_t o = p.total;
+  auto take = [&](size_t bytes) { size_t at = o; o += up256(bytes); return at; };
+  const size_t tc = (size_t)p.Tc, R = (size_t)p.R;
+  h.off_z = take(4 * tc * (size_t)p.Vp);
+  h.off_rec = take(sizeof(float4) * tc * (size_t)h.groups);
+  h.off_stats = h.off_term = h.off_info = h.off_rows = h.off_pids = h.off_pval = h.off_dw = 0;
+  if (distill) {
+    h.off_stats = take(sizeof(rl_stats));
+    h.off_term = take(8 * R); h.off_info = take(4 * R);
+    if (bwd) {
+      h.off_rows = take(sizeof(DistillRow) * tc);
+      h.off_pids = take(4 * tc * (size_t)K); h.off_pval = take(4 * tc * (size_t)K);
+      if (round_dw) h.off_dw = take(4 * (size_t)p.V * (size_t)p.H);
+    }
+  }
+  h.total = o;
+  return RL_OK;
+}
+
+// Outputs that meet an input or one another.
+struct Span { const void* p; size_t n; };
+static bool overlap(const Span* out, int n_out, const Span* in, int n_in) {
+  for (int i = 0; i < n_out; ++i) {
+    for (int k = 0; k < n_in; ++k) if (meets(out[i].p, out[i].n, in[k].p, in[k].n)) return true;
+    for (int k = 0; k < i; ++k) if (meets(out[i].p, out[i].n, out[k].p, out[k].n)) return true;
+  }
+  return false;
+}
+
+static void head_prep(const rl_batch* b, const Plan& p, const Ptrs& q, const rl_outputs& out, hipStream_t s) {
+  PrepJob job;
+  run_prep(b, p, q, nullptr, out, AdvJob{}, job, s);
+  if (job.on) prep_small_kernel<<<1, 1024, 0, s>>>(job.s, job.f, job.adv);        // (no launch of these logits prepares)
+}
+
+template <class T>
+static void score_chunk(const rl_batch* b, const HeadPlan& h, const Ptrs& q, int c0, float* z, float4* rec, hipStream_t s) {
+  const Plan& p = h.p;
+  const T* X = static_cast<const T*>(b->hidden);
+  const T* W = static_cast<const T*>(b->weight);
+  GemmDims d{};
+  d.M = p.V; d.N = p.Tc; d.K = p.H; d.lda = p.H; d.ldb = p.H;
+  d.b_rows = q.row_map + c0; d.b_span = p.R; d.n_real = &q.ctrl->n_real; d.chunk_start = c0; d.dyn = 2; d.group_m = TuneLogits::kBand;
+  const EpiScore<T> e{z, p.Vp, rec, p.Tc, p.V, p.inv_tau};
+  ProfScope ps(RL_PROF_GEMM_FWD, s);
+  if constexpr (sizeof(T) == 2)
+    if (few_tokens(b, p)) {
+      auto kern = few_streams_w(b, p) ? (p.R <= 64 ? score_few_kernel<64, true> : score_few_kernel<128, true>) : (p.R <= 64 ? score_few_kernel<64, false> : score_few_kernel<128, false>);
+      kern<<<2 * p.tiles_v, 256, 0, s>>>(W, X, d, e, q.ids_c);
+      return;
+    }
+  launch_gemm<TuneLogits>(W, X, d, e, s);
+}
+
+static int64_t chunk_bound(const Plan& p, int c0) { return p.R - c0 < p.Tc ? p.R - c0 : p.Tc; }      // rows of the chunk, at most
+
+template <class T>
+static void run_distill(const rl_batch* b, const HeadPlan& h, const Ptrs& q, unsigned char* w, const int32_t* t_ids, const float* t_lp, const rl_distill_params* prm,
+                        const rl_distill_outputs* out, bool bwd, hipStream_t s) {
+  const Plan& p = h.p;
+  float* z = (float*)(w + h.off_z);
+  float4* rec = (float4*)(w + h.off_rec);
+  const T* X = static_cast<const T*>(b->hidden);
+  const T* W = static_cast<const T*>(b->weight);
+  T* dS = static_cast<T*>(q.ds); T* dST = static_cast<T*>(q.dst);
+  float* dw = h.off_dw ? (float*)(w + h.off_dw) : static_cast<float*>(out->d_weight);
+  DistillRow* rows = bwd ? (DistillRow*)(w + h.off_rows) : nullptr;
+  int* p_ids = (int*)(w + h.off_pids);
+  float* p_val = (float*)(w + h.off_pval);
+  if (bwd) {
+    ProfScope ps(RL_PROF_TRANSPOSE, s);
+    for (int64_t r0 = 0; r0 < p.R; r0 += 1 << 25) {               // (64 threads a row)
+      const int64_t n = p.R - r0 < (1 << 25) ? p.R - r0 : 1 << 25;
+      zero_masked_rows_kernel<T><<<(unsigned)((n + 3) / 4), 256, 0, s>>>(q.cpos + r0, static_cast<T*>(out->d_hidden) + r0 * p.H, n, p.H);
+    }
+    if (!p.k_major_w) launch_transpose<T>(dim3((p.Vp + 63) / 64, (p.H + 63) / 64), s, W, p.H, p.V, p.H, nullptr, q.ctrl, 0, 0, nullptr, nullptr, static_cast<T*>(q.wt), p.Vp, p.Vp, p.tiled);
+  }
+  for (int ch = 0; ch < p.n_chunks; ++ch) {
+    const int c0 = ch * p.Tc;
+    const int64_t n = chunk_bound(p, c0);
+    score_chunk<T>(b, h, q, c0, z, rec, s);
+    {
+      ProfScope ps(RL_PROF_COMBINE, s);
+      const DistillJob j{z, p.Vp, rec, p.Tc, h.groups, p.V, h.K, p.inv_tau, q.row_map, q.cstart, q.ctrl, c0, p.Tc, p.B, t_ids, t_lp, prm->rest,
+                         prm->aggregation == RL_AGG_TOKEN, prm->scale == 0.f ? 1.f : prm->scale, out->row_loss, out->lse,
+                         (double*)(w + h.off_term), (int*)(w + h.off_info), rows, p_ids, p_val};
+      distill_row_kernel<<<(unsigned)((n + kRowWaves - 1) / kRowWaves), kRowWaves * 64, distill_lds_bytes(h.groups), s>>>(j);
+    }
+    if (!bwd) continue;
+    {
+      ProfScope ps(RL_PROF_GEMM_DS, s);
+      if constexpr (sizeof(T) == 2) distill_ds_kernel<<<(unsigned)((n + 255) / 256 * (p.Vp / 64)), 256, 0, s>>>(z, p.Vp, rows, q.ctrl, c0, p.V, p.inv_tau, dS);
+      else distill_ds_f32_kernel<<<(unsigned)((n + 63) / 64 * (p.Vp / 64)), 256, 0, s>>>(z, p.Vp, rows, q.ctrl, c0, p.V, p.inv_tau, p.k_major_w ? nullptr : dS, p.Vp, dST, p.Tc);
+      distill_patch_kernel<T><<<(unsigned)((n * h.K + 255) / 256), 256, 0, s>>>(p_ids, p_val, h.K, q.ctrl, c0, p.Tc, sizeof(T) == 4 && p.k_major_w ? nullptr : dS, p.Vp, dST, p.Tc);
+    }
+    {  // X^T chunk [H][Tc], gathered through row_map, zero beyond the valid rows
+      ProfScope ps(RL_PROF_TRANSPOSE, s);
+      launch_transpose<T>(dim3((p.Tc + 63) / 64, (p.H + 63) / 64), s, X, p.H, p.Tc, p.H, q.row_map, q.ctrl, c0, 1, nullptr, nullptr, static_cast<T*>(q.xt), p.Tc, p.Tc, p.tiled);
+    }
+    contract_grads<T>(b, p, q, ch, out->d_hidden, dw, s);
+  }
+  ProfScope ps(RL_PROF_LOSS, s);
+  distill_finish_kernel<<<1, 1024, 0, s>>>((const double*)(w + h.off_term), (const int*)(w + h.off_info), q.ctrl, (const rl_stats*)(w + h.off_stats), out->loss, out->stats);
+  if (bwd && h.off_dw) distill_round_kernel<<<2048, 256, 0, s>>>(dw, static_cast<bf16_t*>(out->d_weight), (int64_t)p.V * p.H);
+}
+
+}  // namespace rlk
+
+using namespace rlk;
+
+extern "C" {
+
+int32_t rl_default_chunk_rows_distill(void) { return kDefaultChunkRowsDistill; }
+
+static rl_status top_plan(const rl_batch* b, const rl_top_params* prm, HeadPlan& h) {
+  if (!b || !prm) return RL_ERR_NULL;
+  const rl_status st = head_plan(b, prm->top_k, prm->chunk_rows, prm->temperature, false, false, false, h);
+  if (st != RL_OK) return st;
+  return prm->top_k > b->V ? RL_ERR_SHAPE : RL_OK;
+}
+
+rl_status rl_token_top_logprobs_workspace_bytes(const rl_batch* b, const rl_top_params* prm, size_t* bytes) {
+  if (!bytes) return RL_ERR_NULL;
+  HeadPlan h;
+  const rl_status st = top_plan(b, prm, h);
+  if (st == RL_OK) *bytes = h.total;
+  return st;
+}
+
+rl_status rl_token_top_logprobs(const rl_batch* b, const rl_top_params* prm, const rl_top_outputs* out, void* ws, size_t ws_bytes, void* stream) {
+  if (!b || !prm || !out) return RL_ERR_NULL;
+  if (!b->hidden || !b->weight || !b->mask || !b->cu_seqlens || (out->logprob && !b->token_ids)) return RL_ERR_NULL;
+  if (!out->logprob && !out->lse && !out->entropy && !out->top_ids && !out->top_logprob) return RL_ERR_NULL;
+  HeadPlan h;
+  const rl_status st = top_plan(b, prm, h);
+  if (st != RL_OK) return st;
+  const Plan& p = h.p;
+  const size_t R = (size_t)p.R;
+  const Span in[] = {{b->hidden, p.esz * R * p.H}, {b->weight, p.esz * (size_t)p.V * p.H}, {b->token_ids, 4 * R}, {b->mask, R}, {b->cu_seqlens, 4 * ((size_t)p.B + 1)}};
+  const Span outs[] = {{out->logprob, 4 * R}, {out->lse, 4 * R}, {out->entropy, 4 * R}, {out->top_ids, 4 * R * h.K}, {out->top_logprob, 4 * R * h.K}};
+  if (overlap(outs, 5, in, 5)) return RL_ERR_RANGE;
+  if (!ws || (reinterpret_cast<uintptr_t>(ws) & 255) || ws_bytes < h.total) return RL_ERR_WORKSPACE;
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  (void)hipGetLastError();
+  const Ptrs q = carve(ws, p);
+  unsigned char* w = static_cast<unsigned char*>(ws);
+  float* z = (float*)(w + h.off_z);
+  float4* rec = (float4*)(w + h.off_rec);
+  rl_outputs cleared{};
+  cleared.logprob = out->logprob; cleared.lse = out->lse; cleared.entropy = out->entropy;
+  head_prep(b, p, q, cleared, s);
+  for (int ch = 0; ch < p.n_chunks; ++ch) {
+    const int c0 = ch * p.Tc;
+    if (p.dtype == RL_BF16) score_chunk<bf16_t>(b, h, q, c0, z, rec, s);
+    else score_chunk<float>(b, h, q, c0, z, rec, s);
+    ProfScope ps(RL_PROF_COMBINE, s);
+    const int waves = top_waves(h.groups);
+    const unsigned blocks = (unsigned)((chunk_bound(p, c0) + waves - 1) / waves);
+    const int64_t all = (p.R + waves - 1) / waves;
+    const unsigned fill = ch == 0 && (out->top_ids || out->top_logprob) ? (unsigned)(all < 4096 ? all : 4096) : 0;
+    const TopJob j{z, p.Vp, rec, p.Tc, h.groups, p.V, h.K, p.inv_tau, q.row_map, q.ids_c, q.cpos, q.ctrl, c0, p.Tc, p.R, (int)blocks,
+                   out->logprob, out->lse, out->entropy, out->top_ids, out->top_logprob};
+    top_kernel<<<blocks + fill, waves * 64, (size_t)waves * 4 * top_lds_words(h.groups), s>>>(j);
+  }
+  return hipGetLastError() == hipSuccess ? RL_OK : RL_ERR_HIP;
+}
+
+static rl_status distill_plan(const rl_batch* b, const rl_distill_params* prm, bool bwd, HeadPlan& h) {
+  if (!b || !prm) return RL_ERR_NULL;
+  if (prm->d_weight_dtype != RL_F32 && !(prm->d_weight_dtype == RL_BF16 && b->dtype == RL_BF16)) return RL_ERR_DTYPE;
+  if (prm->rest != RL_REST_BUCKET && prm->rest != RL_REST_RENORMALISE) return RL_ERR_RANGE;
+  if (prm->aggregation != RL_AGG_SEQUENCE && prm->aggregation != RL_AGG_TOKEN) return RL_ERR_RANGE;
+  if (!(prm->scale >= -3.0e38f && prm->scale <= 3.0e38f)) return RL_ERR_RANGE;
+  return head_plan(b, prm->top_k, prm->chunk_rows, prm->temperature, bwd, true, prm->d_weight_dtype == RL_BF16, h);
+}
+
+rl_status rl_distill_workspace_bytes(const rl_batch* b, const rl_distill_params* prm, int32_t want_backward, size_t* bytes) {
+  if (!bytes) return RL_ERR_NULL;
+  HeadPlan h;
+  const rl_status st = distill_plan(b, prm, want_backward != 0, h);
+  if (st == RL_OK) *bytes = h.total;
+  return st;
+}
+
+rl_status rl_distill_loss_fwd_bwd(const rl_batch* b, const int32_t* t_ids, const float* t_lp, const rl_distill_params* prm, const rl_distill_outputs* out,
+                                  void* ws, size_t ws_bytes, void* stream) {
+  if (!b || !prm || !out) return RL_ERR_NULL;
+  if (!b->hidden || !b->weight || !b->mask || !b->cu_seqlens || !t_ids || !t_lp || !out->loss) return RL_ERR_NULL;
+  const bool bwd = out->d_hidden || out->d_weight;
+  if (bwd && (!out->d_hidden || !out->d_weight)) return RL_ERR_NULL;
+  HeadPlan h;
+  const rl_status st = distill_plan(b, prm, bwd, h);
+  if (st != RL_OK) return st;
+  const Plan& p = h.p;
+  const size_t R = (size_t)p.R, K = (size_t)h.K, xb = p.esz * R * p.H;
+  const Span in[] = {{b->weight, p.esz * (size_t)p.V * p.H}, {b->mask, R}, {b->cu_seqlens, 4 * ((size_t)p.B + 1)}, {t_ids, 4 * R * K}, {t_lp, 4 * R * K},
+                     {b->hidden, xb}};
+  const Span outs[] = {{out->loss, 4}, {out->row_loss, 4 * R}, {out->lse, 4 * R}, {out->stats, sizeof(rl_distill_stats)},
+                       {out->d_weight, (size_t)(prm->d_weight_dtype == RL_BF16 ? 2 : 4) * p.V * p.H}, {out->d_hidden, xb}};
+  if (overlap(outs, 5, in, 6) || overlap(&outs[5], 1, in, out->d_hidden == b->hidden ? 5 : 6) || overlap(outs, 6, in, 0)) return RL_ERR_RANGE;
+  if (!ws || (reinterpret_cast<uintptr_t>(ws) & 255) || ws_bytes < h.total) return RL_ERR_WORKSPACE;
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  (void)hipGetLastError();
+  const Ptrs q = carve(ws, p);
+  unsigned char* w = static_cast<unsigned char*>(ws);
+  rl_batch no_ids = *b;
+  no_ids.token_ids = nullptr;
+  rl_outputs cleared{};
+  cleared.logprob = out->row_loss; cleared.lse = out->lse; cleared.stats = (rl_stats*)(w + h.off_stats);
+  head_prep(&no_ids, p, q, cleared, s);
+  if (p.dtype == RL_BF16) run_distill<bf16_t>(b, h, q, w, t_ids, t_lp, prm, out, bwd, s);
+  else run_distill<float>(b, h, q, w, t_ids, t_lp, prm, out, bwd, s);
+  return hipGetLastError() == hipSuccess ? RL_OK : RL_ERR_HIP;
+}
+
+}  // extern "C"

@@ -18,8 +18,9 @@ template <int BN> constexpr int few_lds_bytes() { return kFewStages * (128 + BN)
 // The work of workgroup `tile` of the launch, N tokens whose rows of X are in `rows`, their sampled tokens in `ids`.  BN: tokens per workgroup, 64 or 128.
 // NT: W in non-temporal loads.  They stream faster (7.2 TB/s of a large array instead of 6.1), and leave nothing behind for a next call: for a W that the memory-side
 // cache does not hold (few_streams_w).
-template <int BN, bool NT>
-__device__ __attribute__((always_inline)) inline void logits_few_tile(const bf16_t* __restrict__ W, const bf16_t* __restrict__ X, const GemmDims& d, const EpiFwd<bf16_t>& epi,
+// Epilogues with kPermute have the 128 vocabulary rows in the order of the hot kernel's (perm_row).
+template <int BN, bool NT, class Epi>
+__device__ __attribute__((always_inline)) inline void logits_few_tile(const bf16_t* __restrict__ W, const bf16_t* __restrict__ X, const GemmDims& d, const Epi& epi,
                                                                       int tile, int N, const int* rows, const int* ids, unsigned char* smem) {
   constexpr int BM = 128, BK = 64, MB = 8, NB = BN / 64, STAGES = kFewStages;
   constexpr int A_BYTES = BM * kSlabBytes, STAGE = A_BYTES + BN * kSlabBytes, LA = BM / 32, LB = BN / 32, LOADS = LA + LB;   // loads per slab and wavefront
@@ -35,7 +36,7 @@ __device__ __attribute__((always_inline)) inline void logits_few_tile(const bf16
     const int lr = (j < LA ? wave * (BM / 4) + j * 8 : wave * (BN / 4) + (j - LA) * 8) + (lane >> 3);
     chunk[j] = (lane & 7) ^ ((lr >> 1) & 7);
     int r;
-    if (j < LA) { const int last = (m0 < d.M ? d.M - m0 : d.M) - 1; r = lr < last ? lr : last; }
+    if (j < LA) { const int last = (m0 < d.M ? d.M - m0 : d.M) - 1, at = Epi::kPermute ? perm_lds_row_a(lr) : lr; r = at < last ? at : last; }
     else r = rows[lr < N ? lr : N - 1];
     off[j] = (unsigned)(((int64_t)r * (j < LA ? d.lda : d.ldb) + chunk[j] * 8) * 2);      // (128 rows of X: far below 4 GiB)
   }
@@ -96,7 +97,7 @@ __device__ __attribute__((always_inline)) inline void logits_few_tile(const bf16
           acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, fa[s][i]), __builtin_bit_cast(bf16x8, fb[s][j]), acc[i][j], 0, 0, 0);
   }
   __builtin_amdgcn_s_waitcnt(0x0F70);       // no load into LDS may be in flight when the workgroup gives its LDS back
-  epi.half_tile<Layout16, MB, NB>(acc, c, y);
+  epi.template half_tile<Layout16, MB, NB>(acc, c, y);
 }
 
 }  // namespace rlk

@@ -228,7 +228,7 @@ __global__ __launch_bounds__(kInitThreads) void prep_init_kernel(const int32_t* 
 }
 __global__ __launch_bounds__(kInitThreads) void row_fill_kernel(int64_t R, RowFill f) { fill_rows(f, R, blockIdx.x, gridDim.x); }
 
-// One workgroup per sequence: validate its row range and group index, count rows that count.
+// One workgroup per sequence: validate its row range and group index, count rows that count.  (ids, here and in the two kernels below, may be NULL: every row's token is then 0.)
 __global__ void seq_count_kernel(const uint8_t* mask, const int32_t* ids, const int32_t* cu, const int32_t* cu_hi,
                                  const int32_t* group_idx, int64_t R, int V, int P,
                                  int32_t* seq_len, rl_stats* stats) {
@@ -243,7 +243,7 @@ __global__ void seq_count_kernel(const uint8_t* mask, const int32_t* ids, const 
   if (seq_ok && grp_ok) {
     for (int64_t r = a + threadIdx.x; r < b; r += blockDim.x) {
       if (mask[r]) {
-        const int y = ids[r];
+        const int y = ids ? ids[r] : 0;
         if (y >= 0 && y < V) ++cnt; else ++bad;
       }
     }
@@ -358,7 +358,7 @@ __global__ __launch_bounds__(1024) void compact_kernel(const uint8_t* mask, cons
     const int64_t r = base + threadIdx.x;
     int y = 0;
     bool f = false;
-    if (r < b && mask[r]) { y = ids[r]; f = (y >= 0 && y < V); }
+    if (r < b && mask[r]) { y = ids ? ids[r] : 0; f = (y >= 0 && y < V); }
     int tot;
     const int pre = wave_prefix_count(f, lane, tot);
     if (lane == 0) wsum[w] = tot;
@@ -407,7 +407,7 @@ __device__ inline void prep_small(const SmallPrep& s, const RowFill& f, const Ad
   for (int k = 0; k < kPer; ++k) {                             // (all loads in flight together)
     const int r = k * NT + t;
     on[k] = false; y[k] = -1;
-    if (r < s.R) { on[k] = s.mask[r]; y[k] = s.ids[r]; }
+    if (r < s.R) { on[k] = s.mask[r]; y[k] = s.ids ? s.ids[r] : 0; }
   }
   if (t <= s.B) sh_cu[t] = s.cu[t];
   if (t < s.B) {
@@ -546,10 +546,10 @@ void logits_few_kernel(const bf16_t* __restrict__ W, const bf16_t* __restrict__ 
     if (blockIdx.x == 0) { prep_small<256, kFewTokens>(s, f, adv); return; }
     __shared__ LocalRows<kFewTokens> l;
     local_rows<256>(s, l);
-    logits_few_tile<BN, NT>(W, X, d, epi, (int)blockIdx.x - 1, l.n, l.rows, l.ids, smem);
+    logits_few_tile<BN, NT, EpiFwd<bf16_t>>(W, X, d, epi, (int)blockIdx.x - 1, l.n, l.rows, l.ids, smem);
   } else {
     const int left = *d.n_real;
-    logits_few_tile<BN, NT>(W, X, d, epi, blockIdx.x, left < d.N ? left : d.N, d.b_rows, epi.ids_c, smem);
+    logits_few_tile<BN, NT, EpiFwd<bf16_t>>(W, X, d, epi, blockIdx.x, left < d.N ? left : d.N, d.b_rows, epi.ids_c, smem);
   }
 }
 
@@ -1616,6 +1616,49 @@ static void run_forward(const rl_batch* b, const Plan& p, const Ptrs& q, float* 
   }
 }
 
+// dX and dW (+)= of chunk ch, out of its dS (and dS^T for f32 inputs), X^T and W or W^T.
+template <class T>
+static void contract_grads(const rl_batch* b, const Plan& p, const Ptrs& q, int ch, void* d_hidden, float* d_weight, hipStream_t s) {
+  const T* W = static_cast<const T*>(b->weight);
+  T* WT = static_cast<T*>(q.wt); T* XT = static_cast<T*>(q.xt);
+  T* dS = static_cast<T*>(q.ds); T* dST = static_cast<T*>(q.dst);
+  T* dX = static_cast<T*>(d_hidden);
+  const int c0 = ch * p.Tc;
+  // dX = dS W: A = dS [Tc][Vp], B = W^T [H][Vp]
+  GemmDims dx{};
+  dx.M = p.Tc; dx.N = p.H; dx.K = p.Vp; dx.lda = p.Vp; dx.ldb = p.Vp;
+  dx.n_real = &q.ctrl->n_real; dx.chunk_start = c0; dx.dyn = 1; dx.group_m = TuneDX::kBand;
+  EpiDX<T> ex{q.row_map, dX, p.H, p.H, nullptr, q.split};
+  // dW (+)= dS^T X: B = X^T [H][Tc]; A = dS^T, for bf16 read out of dS itself as a K-major operand (K = Tc is a multiple of 256
+  // and the workspace is aligned: always the hot kernel), for f32 the stored copy [Vp][Tc]
+  GemmDims dw{};
+  dw.M = p.V; dw.N = p.H; dw.K = p.Tc; dw.lda = p.tiled ? p.Vp : p.Tc; dw.ldb = p.Tc;
+  dw.n_real = &q.ctrl->n_real; dw.chunk_start = c0; dw.dyn = 3; dw.k_round = p.tiled ? 256 : kF32SmallBN; dw.group_m = TuneDW::kBand;
+  dw.zero_if_empty = (ch == 0);
+  EpiDW ew{d_weight, p.H, p.V, p.H, ch > 0 ? 1 : 0};
+  if constexpr (sizeof(T) == 2) {
+    ProfScope ps(RL_PROF_GEMM_BWD, s);
+    launch_dx_dw(dS, W, p.k_major_w ? nullptr : WT, dx, ex, XT, dw, ew, s);
+  } else {
+    dx.split_slots = kF32Slots;
+    if (p.small_pair) {
+      ProfScope ps(RL_PROF_GEMM_BWD, s);
+      const int n1 = split_launch((dx.M + 63) / 64, (dx.N + kF32SmallBN - 1) / kF32SmallBN, kF32Slots);
+      gemm_nt_small_pair_kernel<<<n1 + launch_tiles((dw.M + 63) / 64, (dw.N + kF32SmallBN - 1) / kF32SmallBN), 1024, 0, s>>>(dS, WT, dx, ex, n1, dST, XT, dw, ew);
+      splitk_reduce_kernel<T><<<512, 256, 0, s>>>(dx, ex, 64, kF32SmallBN, 128);
+      return;
+    }
+    {
+      ProfScope ps(RL_PROF_GEMM_DX, s);
+      if (p.k_major_w) { dx.lda = p.Tc; dx.ldb = p.H; dx.b_k_rows = p.V; }
+      launch_gemm<TuneDX>(p.k_major_w ? dST : dS, p.k_major_w ? W : WT, dx, ex, s);
+      splitk_reduce_kernel<T><<<512, 256, 0, s>>>(dx, ex, kBM, f32_tile_n(dx.M, dx.N, dx.K, true), 32);
+    }
+    ProfScope ps(RL_PROF_GEMM_DW, s);
+    launch_gemm<TuneDW>(dST, XT, dw, ew, s);
+  }
+}
+
 template <class T>
 static void run_backward(const rl_batch* b, const Plan& p, const Ptrs& q, void* d_hidden, float* d_weight, bool xt_done, const LossJob& loss, hipStream_t s) {
   const T* X = static_cast<const T*>(b->hidden);
@@ -1661,39 +1704,7 @@ static void run_backward(const rl_batch* b, const Plan& p, const Ptrs& q, void* 
       ProfScope ps(RL_PROF_GEMM_DS, s);
       launch_gemm<TuneLogits>(W, X, d, e, s);
     }
-    // dX = dS W: A = dS [Tc][Vp], B = W^T [H][Vp]
-    GemmDims dx{};
-    dx.M = p.Tc; dx.N = p.H; dx.K = p.Vp; dx.lda = p.Vp; dx.ldb = p.Vp;
-    dx.n_real = &q.ctrl->n_real; dx.chunk_start = c0; dx.dyn = 1; dx.group_m = TuneDX::kBand;
-    EpiDX<T> ex{q.row_map, dX, p.H, p.H, nullptr, q.split};
-    // dW (+)= dS^T X: B = X^T [H][Tc]; A = dS^T, for bf16 read out of dS itself as a K-major operand (K = Tc is a multiple of 256
-    // and the workspace is aligned: always the hot kernel), for f32 the stored copy [Vp][Tc]
-    GemmDims dw{};
-    dw.M = p.V; dw.N = p.H; dw.K = p.Tc; dw.lda = p.tiled ? p.Vp : p.Tc; dw.ldb = p.Tc;
-    dw.n_real = &q.ctrl->n_real; dw.chunk_start = c0; dw.dyn = 3; dw.k_round = p.tiled ? 256 : kF32SmallBN; dw.group_m = TuneDW::kBand;
-    dw.zero_if_empty = (ch == 0);
-    EpiDW ew{d_weight, p.H, p.V, p.H, ch > 0 ? 1 : 0};
-    if constexpr (sizeof(T) == 2) {
-      ProfScope ps(RL_PROF_GEMM_BWD, s);
-      launch_dx_dw(dS, W, p.k_major_w ? nullptr : WT, dx, ex, XT, dw, ew, s);
-    } else {
-      dx.split_slots = kF32Slots;
-      if (p.small_pair) {
-        ProfScope ps(RL_PROF_GEMM_BWD, s);
-        const int n1 = split_launch((dx.M + 63) / 64, (dx.N + kF32SmallBN - 1) / kF32SmallBN, kF32Slots);
-        gemm_nt_small_pair_kernel<<<n1 + launch_tiles((dw.M + 63) / 64, (dw.N + kF32SmallBN - 1) / kF32SmallBN), 1024, 0, s>>>(dS, WT, dx, ex, n1, dST, XT, dw, ew);
-        splitk_reduce_kernel<T><<<512, 256, 0, s>>>(dx, ex, 64, kF32SmallBN, 128);
-        continue;
-      }
-      {
-        ProfScope ps(RL_PROF_GEMM_DX, s);
-        if (p.k_major_w) { dx.lda = p.Tc; dx.ldb = p.H; dx.b_k_rows = p.V; }
-        launch_gemm<TuneDX>(p.k_major_w ? dST : dS, p.k_major_w ? W : WT, dx, ex, s);
-        splitk_reduce_kernel<T><<<512, 256, 0, s>>>(dx, ex, kBM, f32_tile_n(dx.M, dx.N, dx.K, true), 32);
-      }
-      ProfScope ps(RL_PROF_GEMM_DW, s);
-      launch_gemm<TuneDW>(dST, XT, dw, ew, s);
-    }
+    contract_grads<T>(b, p, q, ch, d_hidden, d_weight, s);
   }
 }
 
@@ -2195,3 +2206,4 @@ rl_status rl_rvq_encode_counted(const void* vectors, const void* codebooks, cons
 }  // extern "C"
 
 #include "norm_linear.h"
+#include "distill.h"

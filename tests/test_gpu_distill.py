@@ -1,0 +1,152 @@
+"""Scoring with top alternatives and distillation through the C ABI, against the float64 oracle.
+
+Inputs lie on grids of powers of two on which every logit is a sum without rounding, so that the order of the alternatives is that of the oracle to the bit, and what is
+left in the tolerances is what follows the logits.  With u = 2^-24 (half a step of f32, relative):
+  * an exponential: the difference to the maximum and its scaling round once each, which changes e = exp(-d) by 2 u d e, summed at most 2 u sum d e; exp2 itself 2 u.
+    A group's 64 are added in chains of 18 at most: 18 u.  Groups are added in f64, their weights are exponentials of the same kind: 2 u d + 2 u.  d e^-d <= 0.37,
+    so a sum is off by less than 26 u of itself, its logarithm by 26 u.  SUM = 32 u.
+  * lse and log-probabilities: SUM, and their own rounding.   * entropy: ln S (SUM) and sum e d / S, off by 32 u (1 + D) D with D = its value: SUM (2 + 2 D).
+  * dS: exponentials of the row's maximum, SUM more from the sum: (32 + 2 d) u of each magnitude that it is the difference of, d < 60 here: 2^-16.  Then one rounding, 2^-8 in bf16.
+  * contractions of n terms: n u of the sum of magnitudes; one rounding at the end (2^-8 in bf16, u in f32)."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import distill_oracle as orc
+from paper_2603_16435_amd import binding
+
+pytestmark = pytest.mark.gpu
+U = 2.0 ** -24
+SUM = 32 * U
+DTYPES = {"f32": torch.float32, "bf16": torch.bfloat16}
+
+
+def off_grid(t, elements):
+    """The same values in a tensor that starts `elements` behind a 16-byte boundary."""
+    buf = torch.empty(t.numel() + elements, dtype=t.dtype, device=t.device)
+    buf[elements:].copy_(t.flatten())
+    return buf[elements:].view(t.shape)
+
+
+class Batch:
+    def __init__(self, R, H, V, dtype, seed=0, B=3, w_levels=31, x_levels=60, masked=0.25, cu=None):
+        g = torch.Generator().manual_seed(seed)
+        sw = 2.0 ** round(np.log2(1.2 / np.sqrt(H) / (w_levels / 3)))
+        self.weight = ((torch.randn(V, H, generator=g) * 1.2 / np.sqrt(H) / sw).round().clamp(-w_levels, w_levels) * sw).to(DTYPES[dtype]).cuda()
+        x = torch.randn(R, H, generator=g) + (torch.rand(R, 1, generator=g) * 12) * self.weight.float().cpu()[torch.randint(V, (R,), generator=g)]
+        self.hidden = ((x * 16).round().clamp(-x_levels, x_levels) / 16).to(DTYPES[dtype]).cuda()
+        self.ids = torch.randint(V, (R,), generator=g, dtype=torch.int32).cuda()
+        self.mask = (torch.rand(R, generator=g) >= masked).to(torch.uint8)
+        if R == 1:
+            self.mask[0] = 1
+        self.mask = self.mask.cuda()
+        cuts = sorted(torch.randint(R + 1, (B - 1,), generator=g).tolist())
+        self.cu = torch.tensor([0, *cuts, R] if cu is None else cu, dtype=torch.int32, device="cuda")
+        self.R, self.H, self.V, self.dtype, self.g = R, H, V, dtype, g
+
+    def teacher(self, K, spread=1.5, wild=True):
+        """Lists out of a perturbed student, some short or empty; wild: tokens named twice or out of range, log-probabilities of -inf, and anything where nothing counts."""
+        z = (self.hidden.double() @ self.weight.double().t()).cpu() + spread * torch.randn(self.R, self.V, generator=self.g, dtype=torch.float64)
+        top = z.topk(min(K, self.V), 1)
+        ids = torch.full((self.R, K), -1, dtype=torch.int32)
+        lp = torch.zeros(self.R, K)
+        ids[:, :top.indices.shape[1]] = top.indices.int()
+        lp[:, :top.indices.shape[1]] = (top.values - torch.logsumexp(z, 1, keepdim=True)).float()
+        have = torch.where(torch.rand(self.R, generator=self.g) < 0.3, torch.randint(K + 1, (self.R,), generator=self.g), K)
+        gone = torch.arange(K)[None] >= have[:, None]
+        ids[gone], lp[gone] = -1, float("nan")
+        if wild:
+            for r in range(0, self.R, 5):
+                a, b = torch.randint(K, (2,), generator=self.g).tolist()
+                if a < b and ids[r, a] >= 0 and ids[r, b] >= 0:
+                    ids[r, b] = ids[r, a]
+            for r, bad in ((1, self.V), (2, -2), (3, 2 ** 31 - 1), (4, -2 ** 31)):
+                if r < self.R:
+                    ids[r, K // 2] = bad
+            if self.R > 6 and ids[6, 0] >= 0:
+                lp[6, 0] = -float("inf")
+            hide = self.mask.cpu() == 0
+            ids[hide], lp[hide] = 7 * self.V, float("nan")
+        return ids.cuda(), lp.cuda()
+
+    def score(self, K, tau=1.0, **kw):
+        return binding.rl_token_top_logprobs(self.hidden, self.weight, kw.pop("ids", self.ids), self.mask, K, temperature=tau, cu_seqlens=self.cu, **kw)
+
+    def distill(self, ids, lp, **kw):
+        return binding.rl_distill_loss_fwd_bwd(self.hidden, self.weight, ids, lp, self.mask, self.cu, **kw)
+
+
+def host(t):
+    return t.float().cpu().numpy() if t.is_floating_point() else t.cpu().numpy()
+
+
+def near(got, want, tol, what):
+    got = host(got).astype(np.float64)
+    bad = ~(np.abs(got - want) <= tol)
+    assert not bad.any(), (what, int(bad.sum()), got[bad][:4], want[bad][:4], np.broadcast_to(tol, want.shape)[bad][:4])
+
+
+def check_score(b, r, K, tau):
+    want = orc.top_logprobs(host(b.hidden), host(b.weight), host(b.ids), host(b.mask), host(b.cu), K, tau)
+    assert np.array_equal(host(r.top_ids), want["top_ids"])
+    for f in ("lse", "logprob", "top_logprob"):
+        near(getattr(r, f), want[f], SUM + 2 * U * np.abs(want[f]) + 2 * U * 60, f)
+    near(r.entropy, want["entropy"], SUM * (2 + 2 * 60), "entropy")
+
+
+def check_distill(b, r, ids, lp, rest, tau, aggregation, scale=1.0):
+    want = orc.distill(host(b.hidden), host(b.weight), host(ids), host(lp), host(b.mask), host(b.cu), rest, tau, aggregation, scale)
+    assert r.stats_dict() == want["stats"]
+    near(r.lse, want["lse"], SUM + 4 * U * 60, "lse")
+    # each log p - log q is off by SUM and its own roundings, and the p add up to one
+    row = 2 * SUM + 4 * U * 60 + U * np.abs(want["row_loss"])
+    near(r.row_loss, want["row_loss"], row, "row_loss")
+    near(r.loss, np.array([want["loss"]]), abs(scale) * row.max() + U * abs(want["loss"]), "loss")
+    if r.d_hidden is None:
+        return
+    bf = b.dtype == "bf16"
+    ds, x, w = np.abs(want["dS"]), np.abs(host(b.hidden).astype(np.float64)), np.abs(host(b.weight).astype(np.float64))
+    err = 2.0 ** -16 * want["gross"] + (2.0 ** -8 * ds if bf else U * ds) + 1e-37
+    for got, ref, e, gross, n in ((r.d_hidden, want["d_hidden"], err @ w, ds @ w, b.V), (r.d_weight, want["d_weight"], err.T @ x, ds.T @ x, b.R)):
+        half = 2.0 ** -8 if got.dtype == torch.bfloat16 else U
+        near(got, ref, e + (n + 64) * U * gross + half * (np.abs(ref) + e) + 1e-37, "gradient")
+
+
+# bf16: few tokens (64, 128), the hot kernel (H on the grid of 128, off it), whole and partial tiles, one group, several chunks; f32: narrow tiles, 256 x 64, a K tail
+SCORE = [(1, 64, 300, "bf16", 1, 0), (1, 512, 20000, "bf16", 20, 0), (63, 128, 129, "bf16", 128, 0), (65, 136, 5000, "bf16", 7, 0), (128, 456, 65537, "bf16", 5, 0),
+         (129, 128, 1000, "bf16", 128, 0), (300, 256, 50257, "bf16", 33, 0), (700, 264, 4097, "bf16", 64, 256), (530, 128, 64, "bf16", 64, 512),
+         (1, 4, 5, "f32", 5, 0), (40, 68, 777, "f32", 9, 0), (300, 128, 8200, "f32", 128, 256), (1100, 100, 20011, "f32", 11, 0), (2, 64, 130000, "f32", 100, 0)]
+
+
+@pytest.mark.parametrize("R,H,V,dtype,K,chunk", SCORE)
+@pytest.mark.parametrize("tau", [1.0, 0.7])
+def test_score(R, H, V, dtype, K, chunk, tau):
+    b = Batch(R, H, V, dtype, seed=R + V)
+    check_score(b, b.score(K, tau, chunk_rows=chunk), K, tau)
+
+
+# ties: a few values only, all equal, more equal at the K-th place than there is room for
+@pytest.mark.parametrize("R,H,V,dtype,K", [(70, 64, 3000, "bf16", 128), (200, 64, 20000, "bf16", 100), (300, 64, 70000, "f32", 5), (90, 16, 8192, "f32", 128)])
+@pytest.mark.parametrize("kind", ["few", "equal", "blocks"])
+def test_ties_go_to_the_lower_token(R, H, V, dtype, K, kind):
+    b = Batch(R, H, V, dtype, seed=5, w_levels=1, x_levels=16)
+    if kind == "equal":
+        b.weight.zero_()
+    if kind == "blocks":                                       # the same logits over and over, the largest last
+        b.weight = b.weight[:97].repeat(V // 97 + 1, 1)[:V].contiguous()
+        b.weight[V - 3:] = b.weight[V - 3]
+    check_score(b, b.score(K), K, 1.0)
+
+
+# distillation: the routes of the forward as above, and of the backward (f32: small tiles in one launch, dX out of dS^T and W, several chunks; bf16: W as it is, W^T)
+DISTILL = [(1, 64, 300, "bf16", 1, 0), (61, 128, 3000, "bf16", 8, 0), (128, 136, 5000, "bf16", 100, 0), (300, 256, 1025, "bf16", 128, 0), (700, 264, 4097, "bf16", 30, 256),
+           (1, 4, 5, "f32", 5, 0), (50, 68, 777, "f32", 9, 0), (600, 128, 1500, "f32", 128, 256), (900, 100, 6001, "f32", 21, 0), (1100, 260, 3000, "f32", 16, 0)]
+
+
+@pytest.mark.parametrize("R,H,V,dtype,K,chunk", DISTILL)
+@pytest.mark.parametrize("rest,tau,aggregation", [("bucket", 1.0, "sequence"), ("renormalise", 1.7, "token"), ("bucket", 0.6, "token")])
+def test_distill(R, H, V, dtype, K, chunk, rest, tau, aggregation):
+    b = Batch(R, H, V, dtype, seed=R + V + 1)
+    ids, lp = b.teacher(K)
+    r = b.distill(ids, lp, rest=rest, temperature=tau, aggregation=aggregation, chunk_rows=chunk, d_weight_dtype=DTYPES[dtype])
+    check_distill(b, r, ids, lp, rest, tau, aggregation)
