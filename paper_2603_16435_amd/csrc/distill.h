@@ -231,8 +231,10 @@ __device__ __attribute__((always_inline)) inline void walk_records(const float4*
   }
 }
 
-constexpr int kRowWaves = 4;            // most wavefronts, and rows, of a workgroup of the two kernels below
-constexpr int kTopList = 512;           // candidates held at a time
+// ------------------------------------------------------------------ the best of a row, by a workgroup
+constexpr int kTopThreads = 256, kTopWaves = kTopThreads / 64;
+constexpr int kTopBatch = 16;           // groups looked at between two looks at how full the list is
+constexpr int kTopList = 2048, kTopRoom = kTopList - kTopBatch * kGroup;
 
 struct TopJob {
   const float* z; int64_t ldz; const float4* rec; int ldr, groups, V, K;
@@ -244,51 +246,47 @@ struct TopJob {
   int row_blocks;                       // workgroups with rows; the rest write what rows that do not count read
   float *logprob, *lse, *entropy; int32_t* ids; float* lp;
 };
-__host__ __device__ inline int top_lds_words(int groups) { return groups + 2 * kTopList + RL_TOP_MAX_K; }       // of a wavefront
-// as many as 64 KiB hold, which is one at least (RL_TOP_MAX_V)
-static int top_waves(int groups) { const int n = (64 << 10) / (4 * top_lds_words(groups)); return n < kRowWaves ? n : kRowWaves; }
-static_assert(4 * (RL_TOP_MAX_V / kGroup + 2 * kTopList + RL_TOP_MAX_K) <= (64 << 10), "a row's keys fit");
 
-// The K-th largest of n keys, of which lane l has key(i) at i 64 + l: x, with `at_least` keys >= x, K of them or, where more equal the K-th, more.  n >= K.
-// (Bit by bit from the top; done when a prefix parts K from the rest.)
-template <class KEY>
-__device__ __attribute__((always_inline)) inline unsigned kth_key(int n, int K, int lane, KEY key, int& at_least) {
-  unsigned x = 0;
-  at_least = n;
-  for (int bit = 31; bit >= 0 && at_least != K; --bit) {
-    const unsigned cand = x | 1u << bit;
+// Sums over a workgroup, each with one barrier: the next one writes the other half of its words.
+struct BlockSum {
+  int (*words)[kTopWaves]; int lane, w, flip;
+  __device__ __attribute__((always_inline)) int operator()(int of_wave) {
+    flip ^= 1;
+    if (lane == 0) words[flip][w] = of_wave;
+    __syncthreads();
     int c = 0;
-    for (int i = 0; i * 64 < n; ++i) c += __popcll(__ballot(i * 64 + lane < n && key(i) >= cand));
-    if (c >= K) { x = cand; at_least = c; }
+#pragma unroll
+    for (int i = 0; i < kTopWaves; ++i) c += words[flip][i];
+    return c;
+  }
+};
+// The largest x of which `count` says that at least K are no smaller, from its bit `bit` down; done early where exactly K are.  c: how many.
+template <class X, class COUNT>
+__device__ __attribute__((always_inline)) inline X least_of_best(int bit, int K, int& c, COUNT count) {
+  X x = 0;
+  for (; bit >= 0 && c != K; --bit) {
+    const X cand = x | (X)1 << bit;
+    const int n = count(cand);
+    if (n >= K) { x = cand; c = n; }
   }
   return x;
 }
-// Whether a key is among the K best, keys given in order of index: calls in order, wavefront-uniform.  Equals of the K-th go in while there is room.
-struct BestOf {
-  unsigned x; int room; bool exact;
-  template <class KEY>
-  __device__ __attribute__((always_inline)) BestOf(int n, int K, int lane, KEY key) {
-    int at_least;
-    x = kth_key(n, K, lane, key, at_least);
-    exact = at_least == K;
-    room = K;
-    if (!exact) for (int i = 0; i * 64 < n; ++i) room -= __popcll(__ballot(i * 64 + lane < n && key(i) > x));
-  }
-  __device__ __attribute__((always_inline)) unsigned long long take(unsigned k, bool there, int lane) {
-    if (exact) return __ballot(there && k >= x);
-    const unsigned long long eq = __ballot(there && k == x);
-    const bool in = there && (k > x || (k == x && (int)__popcll(eq & ((1ull << lane) - 1ull)) < room));
-    room -= __popcll(eq);
-    return __ballot(in);
-  }
-};
 
-__global__ __launch_bounds__(kRowWaves * 64) void top_kernel(TopJob j) {
-  extern __shared__ unsigned lds[];
-  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, waves = blockDim.x >> 6;
+// A row by a workgroup of 256: every thread holds up to REG records.  Bound by the latency of a chain of short steps, so a row is spread over a
+// workgroup and its records are read once; neighbouring rows, which share the records' lines, go to one XCD.  Where maxima or logits are equal the lower index is
+// the better one: a second search, over the index, parts the groups, and candidates are pairs (key, token) that are all different.
+template <int REG>
+__global__ __launch_bounds__(kTopThreads) void top_kernel(TopJob j) {
+  __shared__ float red_m[kTopWaves];
+  __shared__ double red_s[kTopWaves], red_u[kTopWaves];
+  __shared__ int words[2][kTopWaves];
+  __shared__ int n_sel, n_list;
+  __shared__ int sel[RL_TOP_MAX_K];
+  __shared__ unsigned long long list[kTopList];
+  const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
   if ((int)blockIdx.x >= j.row_blocks) {
-    const int64_t step = (int64_t)(gridDim.x - j.row_blocks) * waves;
-    for (int64_t r = (int64_t)(blockIdx.x - j.row_blocks) * waves + w; r < j.R; r += step) {
+    const int64_t step = (int64_t)(gridDim.x - j.row_blocks) * kTopWaves;
+    for (int64_t r = (int64_t)(blockIdx.x - j.row_blocks) * kTopWaves + w; r < j.R; r += step) {
       if (j.cpos[r] >= 0) continue;
       for (int k = lane; k < j.K; k += 64) {
         if (j.ids) j.ids[r * j.K + k] = -1;
@@ -297,107 +295,155 @@ __global__ __launch_bounds__(kRowWaves * 64) void top_kernel(TopJob j) {
     }
     return;
   }
-  int left = j.ctrl->n_real - j.chunk_start;
+  int left = j.ctrl->n_real - j.chunk_start, t;
   left = left < j.chunk_rows ? left : j.chunk_rows;
-  const int t = (int)blockIdx.x * waves + w;
-  if (t >= left) return;                                          // (no barrier below: a wavefront is on its own)
-  unsigned* keys = lds + w * top_lds_words(j.groups);
-  unsigned* lk = keys + j.groups;                                 // candidates: key, token, in order of tokens
-  unsigned* lv = lk + kTopList;
-  unsigned* sel = lv + kTopList;                                  // groups taken
-  const float c = j.zs * kLog2e;
-  const int tg = j.chunk_start + t, row = j.row_map[tg];
+  if (left <= 0 || !run_of_block(blockIdx.x, left, t)) return;
+  const float c = j.zs * kLog2e, NEG = -__builtin_inff();
+  const int tg = j.chunk_start + t, row = j.row_map[tg], K = j.K;
+  const float zy = j.logprob ? j.z[tiled_index(t, j.ids_c[tg], j.ldz)] : 0.f;
 
-  Online o;
-  walk_records(j.rec, j.ldr, j.groups, t, lane,
-               [&](const float4 (&q)[8], int) { float mm = o.m; for (int k = 0; k < 8; ++k) mm = fmaxf(mm, q[k].x); o.raise(mm, c); },
-               [&](int b, const float4& q) { o.add(q, c); keys[b] = order_key(q.x); });
-  o.join_lanes(c);
-  const double ln = log(o.s), lse = (double)j.zs * (double)o.m + ln;
-  if (lane == 0) {
-    if (j.lse) j.lse[row] = (float)lse;
-    if (j.logprob) j.logprob[row] = (float)((double)j.zs * ((double)j.z[tiled_index(t, j.ids_c[tg], j.ldz)] - (double)o.m) - ln);
-    if (j.entropy) { const double h = ln - (double)j.zs * o.u / o.s; j.entropy[row] = (float)(h < 0.0 ? 0.0 : h); }
+  float4 q[REG];
+  float m = NEG;
+#pragma unroll
+  for (int i = 0; i < REG; ++i) {
+    const int b = i * kTopThreads + tid;
+    q[i] = make_float4(NEG, 0.f, 0.f, 0.f);
+    if (b < j.groups) q[i] = j.rec[(int64_t)b * j.ldr + t];
+  }
+#pragma unroll
+  for (int i = 0; i < REG; ++i) m = fmaxf(m, q[i].x);
+  m = wave_max(m);
+  if (lane == 0) red_m[w] = m;
+  if (tid == 0) { n_sel = 0; n_list = 0; }
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < kTopWaves; ++i) m = fmaxf(m, red_m[i]);
+  double s = 0.0, u = 0.0;
+#pragma unroll
+  for (int i = 0; i < REG; ++i) {
+    if (q[i].x > NEG) {
+      const float d = q[i].x - m, f = __builtin_amdgcn_exp2f(d * c);
+      s += (double)f * (double)q[i].y;
+      u += (double)f * ((double)q[i].z + (double)d * (double)q[i].y);
+    } else if (q[i].y != q[i].y) s = __builtin_nan("");
+  }
+  s = wave_sum(s); u = wave_sum(u);
+  if (lane == 0) { red_s[w] = s; red_u[w] = u; }
+  __syncthreads();
+  s = red_s[0]; u = red_u[0];
+#pragma unroll
+  for (int i = 1; i < kTopWaves; ++i) { s += red_s[i]; u += red_u[i]; }
+  const double ln = log(s);
+  if (tid == 0) {
+    if (j.lse) j.lse[row] = (float)((double)j.zs * (double)m + ln);
+    if (j.logprob) j.logprob[row] = (float)((double)j.zs * ((double)zy - (double)m) - ln);
+    if (j.entropy) { const double h = ln - (double)j.zs * u / s; j.entropy[row] = (float)(h < 0.0 ? 0.0 : h); }
   }
   if (!j.ids && !j.lp) return;
-  wave_sync();
 
   // the groups that hold them
-  const int K = j.K;
-  int n_sel = 0;
-  unsigned least = 0;                                             // keys below it are not among the K best
-  if (j.groups <= K) {
-    for (int b = lane; b < j.groups; b += 64) sel[b] = b;
-    n_sel = j.groups;
-  } else {
-    BestOf best(j.groups, K, lane, [&](int i) { return keys[i * 64 + lane]; });
-    least = best.x;
-    for (int b0 = 0; b0 < j.groups; b0 += 64) {
-      const bool there = b0 + lane < j.groups;
-      const unsigned long long in = best.take(there ? keys[b0 + lane] : 0u, there, lane);
-      if (in >> lane & 1) sel[n_sel + __popcll(in & ((1ull << lane) - 1ull))] = b0 + lane;
-      n_sel += __popcll(in);
-    }
-  }
-  wave_sync();
-
-  // the best K of those listed so far, in place; a later token has to be larger than the K-th to come in
-  int n = 0;
-  auto keep_best = [&]() {
-    unsigned k[kTopList / 64], v[kTopList / 64];
+  BlockSum sum{words, lane, w, 0};
+  unsigned key[REG];
 #pragma unroll
-    for (int i = 0; i < kTopList / 64; ++i) { k[i] = lk[i * 64 + lane]; v[i] = lv[i * 64 + lane]; }
-    wave_sync();
-    BestOf best(n, K, lane, [&](int i) { return lk[i * 64 + lane]; });
-    int m = 0;
-    wave_sync();
+  for (int i = 0; i < REG; ++i) key[i] = order_key(q[i].x);
+  auto count = [&](auto f) __attribute__((always_inline)) {
+    int n = 0;
 #pragma unroll
-    for (int i = 0; i < kTopList / 64; ++i) {
-      const unsigned long long in = best.take(k[i], i * 64 + lane < n, lane);
-      if (in >> lane & 1) { const int at = m + __popcll(in & ((1ull << lane) - 1ull)); lk[at] = k[i]; lv[at] = v[i]; }
-      m += __popcll(in);
-    }
-    wave_sync();
-    n = m;
-    least = best.x + 1;
+    for (int i = 0; i < REG; ++i) n += (int)__popcll(__ballot(i * kTopThreads + tid < j.groups && f(key[i], i * kTopThreads + tid)));
+    return sum(n);
   };
-  for (int s0 = 0; s0 < n_sel; s0 += 8) {
-    float z[8];
-    int at[8];
-#pragma unroll
-    for (int k = 0; k < 8; ++k) {
-      at[k] = (int)sel[s0 + k < n_sel ? s0 + k : s0] * kGroup + lane;
-      z[k] = j.z[tiled_index(t, at[k], j.ldz)];
+  unsigned long long least = 0;                                   // pairs below it are not among the K best
+  unsigned x = 0;
+  int last = j.groups;                                            // of the groups with x itself, those below this one
+  if (j.groups > K) {
+    int n = j.groups;
+    x = least_of_best<unsigned>(31, K, n, [&](unsigned cand) { return count([&](unsigned k, int) { return k >= cand; }); });
+    if (n != K) {                                                 // more equal the K-th than there is room for
+      const int room = K - count([&](unsigned k, int) { return k > x; });
+      last = 0;                                                   // the largest bound with at most `room` below it
+      for (int bit = 30 - __builtin_clz(RL_TOP_MAX_V / kGroup); bit >= 0; --bit) {
+        const int cand = last | 1 << bit;
+        if (count([&](unsigned k, int b) { return k == x && b < cand; }) <= room) last = cand;
+      }
     }
-#pragma unroll
-    for (int k = 0; k < 8; ++k) {
-      const unsigned key = order_key(z[k]);
-      const unsigned long long in = __ballot(s0 + k < n_sel && at[k] < j.V && z[k] == z[k] && key >= least);
-      if (!in) continue;
-      if (in >> lane & 1) { const int i = n + __popcll(in & ((1ull << lane) - 1ull)); lk[i] = key; lv[i] = at[k]; }
-      n += __popcll(in);
-      wave_sync();
-      if (n > kTopList - 64) { if (n > K) keep_best(); }
-    }
+    least = (unsigned long long)x << 32;
   }
-  if (n > K) keep_best();
+#pragma unroll
+  for (int i = 0; i < REG; ++i) {
+    const int b = i * kTopThreads + tid;
+    if (b < j.groups && (key[i] > x || (key[i] == x && b < last))) sel[atomicAdd(&n_sel, 1)] = b;
+  }
+  __syncthreads();
+  const int ns = n_sel;
+
+  auto keep_best = [&](int n) {                                   // the best K of n > K pairs, anywhere in the list
+    unsigned long long p[kTopList / kTopThreads];
+#pragma unroll
+    for (int i = 0; i < kTopList / kTopThreads; ++i) p[i] = i * kTopThreads + tid < n ? list[i * kTopThreads + tid] : 0ull;
+    least = least_of_best<unsigned long long>(63, K, n, [&](unsigned long long cand) {
+      int k = 0;
+#pragma unroll
+      for (int i = 0; i < kTopList / kTopThreads; ++i) k += (int)__popcll(__ballot(p[i] >= cand));
+      return sum(k);
+    });
+    __syncthreads();
+    if (tid == 0) n_list = 0;
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < kTopList / kTopThreads; ++i) if (p[i] >= least) list[atomicAdd(&n_list, 1)] = p[i];
+    __syncthreads();
+  };
+  int n = 0;
+  for (int s0 = 0; s0 < ns; s0 += kTopBatch) {
+    float z[kTopBatch / kTopWaves];
+    int at[kTopBatch / kTopWaves];
+#pragma unroll
+    for (int k = 0; k < kTopBatch / kTopWaves; ++k) {
+      const int i = s0 + k * kTopWaves + w;
+      at[k] = sel[i < ns ? i : s0] * kGroup + lane;
+      z[k] = j.z[tiled_index(t, at[k], j.ldz)];
+      if (i >= ns || at[k] >= j.V) z[k] = __builtin_nanf("");     // (none)
+    }
+#pragma unroll
+    for (int k = 0; k < kTopBatch / kTopWaves; ++k) {
+      const unsigned long long p = (unsigned long long)order_key(z[k]) << 32 | (0xffffffffu - (unsigned)at[k]);
+      const unsigned long long in = __ballot(z[k] == z[k] && p >= least);
+      int base = 0;
+      if (lane == 0 && in) base = atomicAdd(&n_list, (int)__popcll(in));
+      base = __shfl(base, 0);
+      if (in >> lane & 1) list[base + (int)__popcll(in & ((1ull << lane) - 1ull))] = p;
+    }
+    __syncthreads();
+    n = n_list;
+    if (n > kTopRoom || (s0 + kTopBatch >= ns && n > 2 * kTopThreads)) { keep_best(n); n = n_list; }
+    __syncthreads();
+  }
 
   // in order: each counts those before it
-  for (int i0 = 0; i0 < K; i0 += 64) {
-    const int i = i0 + lane;
-    const unsigned mine = i < n ? lk[i] : 0u, tok = i < n ? lv[i] : 0u;
+  for (int i = tid; i < n; i += kTopThreads) {
+    const unsigned long long p = list[i];
     int rank = 0;
-    for (int q = 0; q < n; ++q) { const unsigned k = lk[q]; rank += k > mine || (k == mine && q < i); }
-    if (i >= K) continue;
-    if (i >= n) rank = i;                                         // (fewer numbers than K in the row)
-    if (j.ids) j.ids[(int64_t)row * K + rank] = i < n ? (int)tok : -1;
-    if (j.lp) j.lp[(int64_t)row * K + rank] = i < n ? (float)((double)j.zs * ((double)key_value(mine) - (double)o.m) - ln) : __builtin_nanf("");
+    for (int k = 0; k < n; ++k) rank += list[k] > p;
+    if (rank >= K) continue;
+    if (j.ids) j.ids[(int64_t)row * K + rank] = (int)(0xffffffffu - (unsigned)p);
+    if (j.lp) j.lp[(int64_t)row * K + rank] = (float)((double)j.zs * ((double)key_value((unsigned)(p >> 32)) - (double)m) - ln);
   }
+  for (int i = n + tid; i < K; i += kTopThreads) {                // (fewer numbers than K in the row)
+    if (j.ids) j.ids[(int64_t)row * K + i] = -1;
+    if (j.lp) j.lp[(int64_t)row * K + i] = __builtin_nanf("");
+  }
+}
+static void launch_top(const TopJob& j, unsigned blocks, hipStream_t s) {
+  static_assert(RL_TOP_MAX_V <= 32 * kTopThreads * kGroup, "the largest vocabulary's records fit the registers");
+  const int reg = (j.groups + kTopThreads - 1) / kTopThreads;
+  auto kern = reg <= 2 ? top_kernel<2> : reg <= 4 ? top_kernel<4> : reg <= 10 ? top_kernel<10> : top_kernel<32>;
+  kern<<<blocks, kTopThreads, 0, s>>>(j);
 }
 
 // ------------------------------------------------------------------ distillation, a row by a wavefront
 // What the backward needs of a row: dS = f exp(zs (z - m) - l) at tokens that the list does not name, in log2 units.
 struct DistillRow { float m, l2, f, pad; };
+constexpr int kRowWaves = 4;            // wavefronts, and rows, of a workgroup
 struct DistillJob {
   const float* z; int64_t ldz; const float4* rec; int ldr, groups, V, K;
   float zs;
@@ -873,13 +919,12 @@ rl_status rl_token_top_logprobs(const rl_batch* b, const rl_top_params* prm, con
     if (p.dtype == RL_BF16) score_chunk<bf16_t>(b, h, q, c0, z, rec, s);
     else score_chunk<float>(b, h, q, c0, z, rec, s);
     ProfScope ps(RL_PROF_COMBINE, s);
-    const int waves = top_waves(h.groups);
-    const unsigned blocks = (unsigned)((chunk_bound(p, c0) + waves - 1) / waves);
-    const int64_t all = (p.R + waves - 1) / waves;
+    const unsigned blocks = (unsigned)((chunk_bound(p, c0) + kXcds - 1) / kXcds * kXcds);
+    const int64_t all = (p.R + kTopWaves - 1) / kTopWaves;
     const unsigned fill = ch == 0 && (out->top_ids || out->top_logprob) ? (unsigned)(all < 4096 ? all : 4096) : 0;
     const TopJob j{z, p.Vp, rec, p.Tc, h.groups, p.V, h.K, p.inv_tau, q.row_map, q.ids_c, q.cpos, q.ctrl, c0, p.Tc, p.R, (int)blocks,
                    out->logprob, out->lse, out->entropy, out->top_ids, out->top_logprob};
-    top_kernel<<<blocks + fill, waves * 64, (size_t)waves * 4 * top_lds_words(h.groups), s>>>(j);
+    launch_top(j, blocks + fill, s);
   }
   return hipGetLastError() == hipSuccess ? RL_OK : RL_ERR_HIP;
 }
