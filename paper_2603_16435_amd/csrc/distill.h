@@ -172,13 +172,7 @@ void score_few_kernel(const bf16_t* __restrict__ W, const bf16_t* __restrict__ X
   logits_few_tile<BN, NT>(W, X, d, epi, blockIdx.x, left < d.N ? left : d.N, d.b_rows, ids_c, smem);
 }
 
-// ------------------------------------------------------------------ a row, by a wavefront
-// What a lane wrote to LDS is there for the wavefront's other lanes.
-__device__ __attribute__((always_inline)) inline void wave_sync() {
-  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-  __builtin_amdgcn_wave_barrier();
-  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
-}
+// ------------------------------------------------------------------ a row, by a workgroup
 __device__ inline float wave_max(float v) { for (int o = 32; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor(v, o)); return v; }
 
 // Order of logits as unsigned numbers: -0 is 0, what is no number comes before everything.
@@ -208,30 +202,8 @@ struct Online {
       u += (double)f * ((double)q.z + (double)d * (double)q.y);
     } else if (q.y != q.y) s = __builtin_nan("");
   }
-  __device__ void join_lanes(float c) {
-    raise(wave_max(m), c);
-    s = wave_sum(s); u = wave_sum(u);
-  }
 };
 
-// The records of row t, group after group to the lanes: f(group, record), after the maxima of eight have been given to r(maximum).
-template <class RAISE, class F>
-__device__ __attribute__((always_inline)) inline void walk_records(const float4* rec, int ldr, int groups, int t, int lane, RAISE r, F f) {
-  for (int b0 = lane; b0 < groups; b0 += 8 * 64) {
-    float4 q[8];
-#pragma unroll
-    for (int k = 0; k < 8; ++k) {
-      const int b = b0 + 64 * k;
-      q[k] = make_float4(-__builtin_inff(), 0.f, 0.f, 0.f);
-      if (b < groups) q[k] = rec[(int64_t)b * ldr + t];
-    }
-    r(q, b0);
-#pragma unroll
-    for (int k = 0; k < 8; ++k) if (b0 + 64 * k < groups) f(b0 + 64 * k, q[k]);
-  }
-}
-
-// ------------------------------------------------------------------ the best of a row, by a workgroup
 constexpr int kTopThreads = 256, kTopWaves = kTopThreads / 64;
 constexpr int kTopBatch = 16;           // groups looked at between two looks at how full the list is
 constexpr int kTopList = 2048, kTopRoom = kTopList - kTopBatch * kGroup;
@@ -440,10 +412,9 @@ static void launch_top(const TopJob& j, unsigned blocks, hipStream_t s) {
   kern<<<blocks, kTopThreads, 0, s>>>(j);
 }
 
-// ------------------------------------------------------------------ distillation, a row by a wavefront
+// ------------------------------------------------------------------ distillation, a row
 // What the backward needs of a row: dS = f exp(zs (z - m) - l) at tokens that the list does not name, in log2 units.
 struct DistillRow { float m, l2, f, pad; };
-constexpr int kRowWaves = 4;            // wavefronts, and rows, of a workgroup
 struct DistillJob {
   const float* z; int64_t ldz; const float4* rec; int ldr, groups, V, K;
   float zs;
@@ -458,8 +429,6 @@ struct DistillJob {
   int* info;                            // [compact row] entries left out, bit 30: empty
   DistillRow* rows; int* p_ids; float* p_val;          // [chunk row], [chunk row][K]: the tokens that are listed and their dS (-1: none); NULL without backward
 };
-__host__ __device__ inline size_t distill_lds_bytes(int groups) { return (size_t)kRowWaves * 4 * ((groups + 31) / 32 + 2 * RL_TOP_MAX_K + 4); }
-
 // Sequence of compact row t: the last i with cstart[i] <= t, 64 at a time.
 __device__ inline int sequence_of(const int* cstart, int B, int t, int lane) {
   int lo = 0, n = B;                    // among [lo, lo + n)
@@ -472,163 +441,179 @@ __device__ inline int sequence_of(const int* cstart, int B, int t, int lane) {
   return lo;
 }
 
-__global__ __launch_bounds__(kRowWaves * 64) void distill_row_kernel(DistillJob j) {
-  extern __shared__ unsigned lds[];
-  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
-  int left = j.ctrl->n_real - j.chunk_start;
+// A row by a workgroup, as in top_kernel; thread i < K has entry i of the list.
+template <int REG>
+__global__ __launch_bounds__(kTopThreads) void distill_row_kernel(DistillJob j) {
+  constexpr int kWords = RL_TOP_MAX_V / kGroup / 32;
+  __shared__ unsigned bits[kWords];                               // groups with a listed token
+  __shared__ int ids[RL_TOP_MAX_K], sel[RL_TOP_MAX_K];            // tokens (-1: none); groups with one, by their first entry
+  __shared__ int words[2][kTopWaves];
+  __shared__ float red_m[3][kTopWaves];
+  __shared__ double red[2][4][kTopWaves];
+  const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
+  int left = j.ctrl->n_real - j.chunk_start, t;
   left = left < j.chunk_rows ? left : j.chunk_rows;
-  const int t = (int)blockIdx.x * kRowWaves + w;
-  if (t >= left) return;                                          // (a wavefront is on its own)
-  const int words = (j.groups + 31) / 32, K = j.K;
-  unsigned* bits = lds + w * (words + 2 * RL_TOP_MAX_K + 4);      // groups with a listed token
-  int* ids = (int*)(bits + words);
-  unsigned* sel = (unsigned*)(ids + RL_TOP_MAX_K);
-  unsigned* mask = sel + RL_TOP_MAX_K;                            // tokens listed of two groups in turn
-  const float c = j.zs * kLog2e;
-  const int tg = j.chunk_start + t, row = j.row_map[tg];
-  const float NEG = -__builtin_inff();
+  if (left <= 0 || !run_of_block(blockIdx.x, left, t)) return;
+  const int tg = j.chunk_start + t, row = j.row_map[tg], K = j.K;
+  const float c = j.zs * kLog2e, NEG = -__builtin_inff();
+  const bool bucket = j.rest == RL_REST_BUCKET;
 
-  // the list: entry lane and lane + 64
-  int id[2]; float lp[2]; bool in[2];
-  int left_out = 0;
+  float4 q[REG];
 #pragma unroll
-  for (int h = 0; h < 2; ++h) {
-    const int i = h * 64 + lane;
-    id[h] = -1; lp[h] = NEG;
-    if (i < K) { id[h] = j.t_ids[(int64_t)row * K + i]; lp[h] = j.t_lp[(int64_t)row * K + i]; }
-    in[h] = id[h] >= 0 && id[h] < j.V;
-    left_out += __popcll(__ballot(id[h] != -1 && !in[h]));
-    ids[i] = in[h] ? id[h] : -1;
+  for (int i = 0; i < REG; ++i) {
+    const int b = i * kTopThreads + tid;
+    q[i] = make_float4(NEG, 0.f, 0.f, 0.f);
+    if (b < j.groups) q[i] = j.rec[(int64_t)b * j.ldr + t];
   }
-  for (int b = lane; b < words; b += 64) bits[b] = 0u;
-  wave_sync();
-  bool again[2] = {false, false};
-  for (int i = 0; i < K; ++i) {
-    const int o = ids[i];
-#pragma unroll
-    for (int h = 0; h < 2; ++h) again[h] |= in[h] && o == id[h] && i < h * 64 + lane;
-  }
-#pragma unroll
-  for (int h = 0; h < 2; ++h) {
-    left_out += __popcll(__ballot(again[h]));
-    in[h] = in[h] && !again[h];
-    if (in[h]) atomicOr(&bits[id[h] / kGroup >> 5], 1u << (id[h] / kGroup & 31));
-  }
-  wave_sync();
-
-  // all tokens, and those of groups without a listed one
-  Online o, r;
-  auto plain = [&](int b) { return !(bits[b >> 5] >> (b & 31) & 1u); };
-  walk_records(j.rec, j.ldr, j.groups, t, lane,
-               [&](const float4 (&q)[8], int b0) {
-                 float mm = o.m, mr = r.m;
-                 for (int k = 0; k < 8; ++k) {
-                   mm = fmaxf(mm, q[k].x);
-                   if (b0 + 64 * k < j.groups && plain(b0 + 64 * k)) mr = fmaxf(mr, q[k].x);
-                 }
-                 o.raise(mm, c); r.raise(mr, c);
-               },
-               [&](int b, const float4& q) { o.add(q, c); if (plain(b)) r.add(q, c); });
-  o.join_lanes(c);
-  const double ln = log(o.s);
-  if (lane == 0 && j.lse) j.lse[row] = (float)((double)j.zs * (double)o.m + ln);
-
-  double P = 0.0, pr = 0.0, kl = 0.0, lnr = 0.0;
-  double p[2], lq[2];
-  bool any = false;
-#pragma unroll
-  for (int h = 0; h < 2; ++h) {
-    lq[h] = in[h] ? (double)j.zs * ((double)j.z[tiled_index(t, id[h], j.ldz)] - (double)o.m) - ln : 0.0;
-    any |= in[h];
-  }
-  const bool empty = !__ballot(any);
-  if (j.rest == RL_REST_BUCKET) {
-    // ... and the others of groups with one
-    int n_sel = 0;
-    for (int b0 = 0; b0 < words; ++b0)
-      for (unsigned m = bits[b0]; m; m &= m - 1) { if (lane == 0) sel[n_sel] = b0 * 32 + __builtin_ctz(m); ++n_sel; }
-    wave_sync();
-    for (int s0 = 0; s0 < n_sel; s0 += 8) {
-      float z[8];
-      int gr[8];
-#pragma unroll
-      for (int k = 0; k < 8; ++k) {
-        gr[k] = (int)sel[s0 + k < n_sel ? s0 + k : s0];
-        z[k] = j.z[tiled_index(t, gr[k] * kGroup + lane, j.ldz)];
-      }
-#pragma unroll
-      for (int k = 0; k < 8; ++k) {
-        if (s0 + k >= n_sel) continue;
-        unsigned* mk = mask + (k & 1) * 2;
-        if (lane < 2) mk[lane] = 0u;
-        wave_sync();
-#pragma unroll
-        for (int h = 0; h < 2; ++h) if (in[h] && id[h] / kGroup == gr[k]) atomicOr(&mk[(id[h] & 63) >> 5], 1u << (id[h] & 31));
-        wave_sync();
-        if (gr[k] * kGroup + lane < j.V && !(mk[lane >> 5] >> (lane & 31) & 1u)) {
-          r.raise(z[k], c);
-          r.add(make_float4(z[k], 1.f, 0.f, 0.f), c);
-        }
-        if (z[k] != z[k] && gr[k] * kGroup + lane < j.V) r.s = __builtin_nan("");
+  int id = -1;
+  float lp = NEG;
+  if (tid < K) { id = j.t_ids[(int64_t)row * K + tid]; lp = j.t_lp[(int64_t)row * K + tid]; }
+  bool in = id >= 0 && id < j.V;
+  bool out = id != -1 && !in;                                     // left out
+  if (tid < RL_TOP_MAX_K) ids[tid] = in ? id : -1;
+  for (int b = tid; b < (j.groups + 31) / 32; b += kTopThreads) bits[b] = 0u;
+  const float zi = in ? j.z[tiled_index(t, id, j.ldz)] : 0.f;
+  __syncthreads();
+  bool head = in;                                                 // first of its group
+  if (w < 2)
+    for (int i = 0; i < K; ++i) {
+      const int o = ids[i];
+      if (i < tid && o >= 0) {
+        if (o == id) { out |= in; in = false; }
+        if (o / kGroup == id / kGroup) head = false;
       }
     }
-    r.join_lanes(c);
-    double sum = 0.0;
-#pragma unroll
-    for (int h = 0; h < 2; ++h) { p[h] = in[h] ? exp((double)lp[h]) : 0.0; sum += p[h]; }
-    sum = wave_sum(sum);
-    pr = 1.0 - sum; pr = pr < 0.0 ? 0.0 : pr;
-    if (r.m == NEG && r.s == 0.0) pr = 0.0;                       // (the list names all tokens)
-    if (empty) pr = 1.0;
-    P = sum + pr;
-    lnr = log(r.s);
-    if (pr > 0.0 && !empty) kl += pr * (log(pr) - ((double)j.zs * ((double)r.m - (double)o.m) + lnr - ln));
-  } else {
-    const float m = wave_max(fmaxf(in[0] ? lp[0] : NEG, in[1] ? lp[1] : NEG));
-    const float ms = m == NEG ? 0.f : m;
-    double sum = 0.0;
-#pragma unroll
-    for (int h = 0; h < 2; ++h) { p[h] = in[h] ? exp((double)lp[h] - (double)ms) : 0.0; sum += p[h]; }
-    sum = wave_sum(sum);
-#pragma unroll
-    for (int h = 0; h < 2; ++h) p[h] = sum == 0.0 ? 0.0 : p[h] / sum;
-    P = sum == 0.0 ? 0.0 : 1.0;
+  BlockSum count{words, lane, w, 0};
+  const unsigned long long heads = __ballot(head);
+  // (a word each: entries left out, entries, heads of the first wavefront)
+  const int tally = count((int)__popcll(__ballot(out)) | (int)__popcll(__ballot(in)) << 8 | (int)__popcll(heads) << 16);
+  const int left_out = tally & 255, ns = tally >> 16;
+  const bool empty = (tally >> 8 & 255) == 0;
+  if (head) {
+    const int at = (int)__popcll(heads & ((1ull << lane) - 1ull)) + (w == 1 ? words[count.flip][0] >> 16 : 0);
+    sel[at] = id / kGroup;
+    atomicOr(&bits[id / kGroup >> 5], 1u << (id / kGroup & 31));
   }
-  double part = 0.0;
+  __syncthreads();
+
+  // tokens that are not listed, of groups with a listed one: each lane its own running sum
+  Online r;
+  if (bucket)
+    for (int s0 = w; s0 < ns; s0 += 4 * kTopWaves) {
+      float z[4];
+      int g[4];
 #pragma unroll
-  for (int h = 0; h < 2; ++h) if (p[h] > 0.0 || p[h] != p[h]) part += p[h] * (log(p[h]) - lq[h]);
-  kl += wave_sum(part);
+      for (int k = 0; k < 4; ++k) {
+        const int i = s0 + k * kTopWaves;
+        g[k] = sel[i < ns ? i : s0];
+        z[k] = j.z[tiled_index(t, g[k] * kGroup + lane, j.ldz)];
+      }
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        if (s0 + k * kTopWaves >= ns) continue;
+        unsigned long long named = 0;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const int o = ids[h * 64 + lane];
+          for (unsigned long long m = __ballot(o >= 0 && o / kGroup == g[k]); m; m &= m - 1) named |= 1ull << (ids[h * 64 + __builtin_ctzll(m)] & 63);
+        }
+        if (g[k] * kGroup + lane >= j.V || (named >> lane & 1)) continue;
+        if (z[k] != z[k]) r.s = __builtin_nan("");
+        r.raise(z[k], c);
+        r.add(make_float4(z[k], 1.f, 0.f, 0.f), c);
+      }
+    }
+  // and of the others, by their records; all tokens
+  bool plain[REG];
+  float m = NEG, mr = r.m, ml = wave_max(in ? lp : NEG);
+#pragma unroll
+  for (int i = 0; i < REG; ++i) {
+    const int b = i * kTopThreads + tid;
+    plain[i] = bucket && b < j.groups && !(bits[b >> 5] >> (b & 31) & 1u);
+    m = fmaxf(m, q[i].x);
+    if (plain[i]) mr = fmaxf(mr, q[i].x);
+  }
+  m = wave_max(m); mr = wave_max(mr);
+  if (lane == 0) { red_m[0][w] = m; red_m[1][w] = mr; red_m[2][w] = ml; }
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < kTopWaves; ++i) { m = fmaxf(m, red_m[0][i]); mr = fmaxf(mr, red_m[1][i]); ml = fmaxf(ml, red_m[2][i]); }
+  Online o;
+  o.m = m;
+  r.raise(mr, c);
+#pragma unroll
+  for (int i = 0; i < REG; ++i) {
+    if (i * kTopThreads + tid >= j.groups) continue;
+    o.add(q[i], c);
+    if (plain[i]) r.add(q[i], c);
+  }
+  auto sum4 = [&](int half, double (&v)[4]) __attribute__((always_inline)) {
+#pragma unroll
+    for (int k = 0; k < 4; ++k) v[k] = wave_sum(v[k]);
+    if (lane == 0) {
+#pragma unroll
+      for (int k = 0; k < 4; ++k) red[half][k][w] = v[k];
+    }
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      v[k] = red[half][k][0];
+#pragma unroll
+      for (int i = 1; i < kTopWaves; ++i) v[k] += red[half][k][i];
+    }
+  };
+  if (ml == NEG) ml = 0.f;
+  double p = in ? exp(bucket ? (double)lp : (double)lp - (double)ml) : 0.0;
+  double v[4] = {o.s, r.s, p, 0.0};
+  sum4(0, v);
+  const double ln = log(v[0]), lnr = log(v[1]);
+  const double lq = in ? (double)j.zs * ((double)zi - (double)m) - ln : 0.0;
+  const double lqr = (double)j.zs * ((double)mr - (double)m) + lnr - ln;       // log of the others' probability
+  double P, pr = 0.0;
+  if (bucket) {
+    pr = 1.0 - v[2]; pr = pr < 0.0 ? 0.0 : pr;
+    if (mr == NEG && v[1] == 0.0) pr = 0.0;                       // (the list names all tokens)
+    P = v[2] + pr;
+  } else {
+    p = v[2] == 0.0 ? 0.0 : p / v[2];
+    P = v[2] == 0.0 ? 0.0 : 1.0;
+  }
+  double part[4] = {p > 0.0 || p != p ? p * (log(p) - lq) : 0.0, 0.0, 0.0, 0.0};
+  sum4(1, part);
   const bool nothing = empty || P == 0.0;
+  double kl = part[0];
+  if (pr > 0.0) kl += pr * (log(pr) - lqr);
   if (nothing) kl = 0.0;
 
-  const double share = j.token_mean ? 1.0 / (double)j.ctrl->n_real : [&]() {
+  double share;
+  if (j.token_mean) share = 1.0 / (double)j.ctrl->n_real;
+  else {
     const int i = sequence_of(j.cstart, j.B, tg, lane);
-    return 1.0 / ((double)j.B * (double)(j.cstart[i + 1] - j.cstart[i]));
-  }();
-  const double coef = (double)j.scale * share;
-  if (lane == 0) {
+    share = 1.0 / ((double)j.B * (double)(j.cstart[i + 1] - j.cstart[i]));
+  }
+  const double coef = (double)j.scale * share, f = coef * (double)j.zs;
+  if (tid == 0) {
+    if (j.lse) j.lse[row] = (float)((double)j.zs * (double)m + ln);
     if (j.row_loss) j.row_loss[row] = (float)kl;
     j.term[tg] = coef * kl;
     j.info[tg] = left_out | (nothing ? 1 << 30 : 0);
   }
   if (!j.rows) return;
   // dS at the others, coef zs q (P - pr / q_r).  With a bucket relative to their own sum, q / q_r (P q_r - pr): nothing overflows where q_r is small
-  const double f = coef * (double)j.zs;
-  if (lane == 0) {
-    DistillRow d{o.m, (float)(ln * 1.4426950408889634), nothing ? 0.f : (float)(f * P), 0.f};
-    if (j.rest == RL_REST_BUCKET && pr > 0.0 && !nothing) {
-      const double lqr = (double)j.zs * ((double)r.m - (double)o.m) + lnr - ln;
-      d.m = r.m; d.l2 = (float)(lnr * 1.4426950408889634); d.f = (float)(f * (P * exp(lqr) - pr));
-    }
+  if (tid == 0) {
+    DistillRow d{m, (float)(ln * 1.4426950408889634), nothing ? 0.f : (float)(f * P), 0.f};
+    if (pr > 0.0 && !nothing) { d.m = mr; d.l2 = (float)(lnr * 1.4426950408889634); d.f = (float)(f * (P * exp(lqr) - pr)); }
     j.rows[t] = d;
   }
-#pragma unroll
-  for (int h = 0; h < 2; ++h) {
-    const int i = h * 64 + lane;
-    if (i >= K) continue;
-    j.p_ids[(int64_t)t * K + i] = in[h] && !nothing ? id[h] : -1;
-    j.p_val[(int64_t)t * K + i] = (float)(f * (P * exp(lq[h]) - p[h]));
+  if (tid < K) {
+    j.p_ids[(int64_t)t * K + tid] = in && !nothing ? id : -1;
+    j.p_val[(int64_t)t * K + tid] = (float)(f * (P * exp(lq) - p));
   }
+}
+static void launch_distill_rows(const DistillJob& j, int64_t rows, hipStream_t s) {
+  const int reg = (j.groups + kTopThreads - 1) / kTopThreads;
+  auto kern = reg <= 2 ? distill_row_kernel<2> : reg <= 4 ? distill_row_kernel<4> : reg <= 10 ? distill_row_kernel<10> : distill_row_kernel<32>;
+  kern<<<(unsigned)((rows + kXcds - 1) / kXcds * kXcds), kTopThreads, 0, s>>>(j);
 }
 
 // ------------------------------------------------------------------ dS
@@ -636,15 +621,17 @@ __device__ __attribute__((always_inline)) inline float ds_entry(float z, const D
   return d.f == 0.f ? 0.f : d.f * __builtin_amdgcn_exp2f((z - d.m) * c - d.l2);
 }
 
+struct DsJob { const float* z; int64_t ldz; const DistillRow* rows; const Ctrl* ctrl; int chunk_start, V; float zs; };
+
 // bf16: logits and dS are both slab-tiled, a pass over memory in order; a workgroup takes a slab (256 rows, 64 vocabulary entries).  Rows of a slab without a token become 0,
 // as does the padding of the vocabulary.
-__global__ __launch_bounds__(256) void distill_ds_kernel(const float* z, int64_t ldz, const DistillRow* rows, const Ctrl* ctrl, int chunk_start, int V, float zs, bf16_t* dS) {
-  const int slabs = (int)(ldz / 64), tile = (int)(blockIdx.x / slabs), slab = (int)(blockIdx.x % slabs);
-  const int left = ctrl->n_real - chunk_start - tile * 256;
+__device__ __attribute__((always_inline)) inline void ds_block(int block, const DsJob& j, bf16_t* dS) {
+  const int slabs = (int)(j.ldz / 64), tile = block / slabs, slab = block % slabs;
+  const int left = j.ctrl->n_real - j.chunk_start - tile * 256;
   if (left <= 0) return;
   const int64_t at = ((int64_t)tile * slabs + slab) * 16384;
   const int e0 = (threadIdx.x & 7) * 8, v0 = slab * 64 + e0;
-  const float c = zs * kLog2e;
+  const float c = j.zs * kLog2e;
 #pragma unroll
   for (int h = 0; h < 2; ++h) {
     floatx4 x[4][2];
@@ -655,8 +642,8 @@ __global__ __launch_bounds__(256) void distill_ds_kernel(const float* z, int64_t
       d[k].f = 0.f;
       x[k][0] = x[k][1] = floatx4{0.f, 0.f, 0.f, 0.f};
       if (n < left) {
-        d[k] = rows[tile * 256 + n];
-        const floatx4* p = reinterpret_cast<const floatx4*>(z + at + n * 64 + e0);
+        d[k] = j.rows[tile * 256 + n];
+        const floatx4* p = reinterpret_cast<const floatx4*>(j.z + at + n * 64 + e0);
         x[k][0] = __builtin_nontemporal_load(p); x[k][1] = __builtin_nontemporal_load(p + 1);
       }
     }
@@ -665,77 +652,114 @@ __global__ __launch_bounds__(256) void distill_ds_kernel(const float* z, int64_t
       const int n = (h * 4 + k) * 32 + (threadIdx.x >> 3);
       bf16x8 o;
 #pragma unroll
-      for (int e = 0; e < 8; ++e) o[e] = (bf16_t)(v0 + e < V ? ds_entry(x[k][e >> 2][e & 3], d[k], c) : 0.f);
+      for (int e = 0; e < 8; ++e) o[e] = (bf16_t)(v0 + e < j.V ? ds_entry(x[k][e >> 2][e & 3], d[k], c) : 0.f);
       store_stream(dS + at + n * 64 + e0, o);
     }
   }
 }
 
-// f32: dS (NULL: not wanted) and dS^T, row-major; 64 rows x 64 vocabulary entries of a workgroup.  Rows up to the next multiple of 64 become 0.
-__global__ __launch_bounds__(256) void distill_ds_f32_kernel(const float* z, int64_t ldz, const DistillRow* rows, const Ctrl* ctrl, int chunk_start, int V, float zs,
-                                                             float* dS, int64_t ld_ds, float* dST, int64_t ld_dst) {
-  __shared__ float tile[64][65];
-  const int vb = (int)(ldz / 64), n0 = (int)(blockIdx.x / vb) * 64, m0 = (int)(blockIdx.x % vb) * 64;
-  const int left = ctrl->n_real - chunk_start;
+// f32: dS (NULL: not wanted) and dS^T, row-major; 64 rows x 64 vocabulary entries of a workgroup, 16 bytes a lane both ways.  Rows up to the next multiple of 64 become 0.
+__device__ __attribute__((always_inline)) inline void ds_f32_block(int block, const DsJob& j, float* dS, int64_t ld_ds, float* dST, int64_t ld_dst, float (&tile)[64][65]) {
+  const int vb = (int)(j.ldz / 64), n0 = block / vb * 64, m0 = block % vb * 64;
+  const int left = j.ctrl->n_real - j.chunk_start;
   if (n0 >= left) return;
-  const int tx = threadIdx.x & 63, ty = threadIdx.x >> 6;
-  const float c = zs * kLog2e;
+  const int q = threadIdx.x & 15, ty = threadIdx.x >> 4;
+  const float c = j.zs * kLog2e;
+  floatx4 x[4];
 #pragma unroll
-  for (int k = 0; k < 16; ++k) {
-    const int n = n0 + ty + 4 * k;
-    float o = 0.f;
-    if (n < left && m0 + tx < V) o = ds_entry(z[tiled_index(n, m0 + tx, ldz)], rows[n], c);
-    if (dS) dS[(int64_t)n * ld_ds + m0 + tx] = o;
-    tile[ty + 4 * k][tx] = o;
+  for (int k = 0; k < 4; ++k) {
+    const int n = n0 + ty + 16 * k;
+    x[k] = floatx4{0.f, 0.f, 0.f, 0.f};
+    if (n < left) x[k] = *reinterpret_cast<const floatx4*>(j.z + tiled_index(n, m0 + q * 4, j.ldz));
+  }
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    const int r = ty + 16 * k, n = n0 + r;
+    DistillRow d{0.f, 0.f, 0.f, 0.f};
+    if (n < left) d = j.rows[n];
+    floatx4 o;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) { o[e] = m0 + q * 4 + e < j.V ? ds_entry(x[k][e], d, c) : 0.f; tile[r][q * 4 + e] = o[e]; }
+    if (dS) *reinterpret_cast<floatx4*>(dS + (int64_t)n * ld_ds + m0 + q * 4) = o;
   }
   __syncthreads();
 #pragma unroll
-  for (int k = 0; k < 16; ++k) dST[(int64_t)(m0 + ty + 4 * k) * ld_dst + n0 + tx] = tile[tx][ty + 4 * k];
+  for (int k = 0; k < 4; ++k) {
+    const int v = ty + 16 * k;
+    floatx4 o;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) o[e] = tile[q * 4 + e][v];
+    *reinterpret_cast<floatx4*>(dST + (int64_t)(m0 + v) * ld_dst + n0 + q * 4) = o;
+  }
 }
 
-// dS of the listed tokens over what the pass wrote there
+// dS of a chunk, and beside it what else the contractions want: X^T, and, in the first chunk's launch, the rows of dX that do not count as 0.  Workgroups [0, n_ds), n_xt, and the rest.
+struct XtJob { const void* x; int64_t R; int H, cols, n_ds, n_xt, fast; const int *row_map, *cpos; void *xt, *dX; int tc; };
 template <class T>
-__global__ __launch_bounds__(256) void distill_patch_kernel(const int* ids, const float* val, int K, const Ctrl* ctrl, int chunk_start, int chunk_rows, T* dS, int64_t ld_ds,
-                                                            T* dST, int64_t ld_dst) {
+__global__ __launch_bounds__(256) void distill_ds_kernel(DsJob j, T* dS, int64_t ld_ds, T* dST, int64_t ld_dst, XtJob x) {
+  __shared__ union { float f[64][65]; unsigned b[64][33]; bf16_t h[64][65]; } tile;
+  int b = blockIdx.x;
+  if (b < x.n_ds) {
+    if constexpr (sizeof(T) == 2) ds_block(b, j, dS); else ds_f32_block(b, j, dS, ld_ds, dST, ld_dst, tile.f);
+    return;
+  }
+  b -= x.n_ds;
+  const T* X = static_cast<const T*>(x.x);
+  T* XT = static_cast<T*>(x.xt);
+  if (b < x.n_xt) {
+    const int bx = b % x.cols, by = b / x.cols;
+    if constexpr (sizeof(T) == 2) {
+      if (x.fast) transpose_bf16_block(bx, by, tile.b, X, x.H, x.tc, x.H, x.row_map, j.ctrl, j.chunk_start, 1, nullptr, nullptr, XT, x.tc, x.tc);
+      else transpose_block(TransposeJob<T>{X, x.H, x.tc, x.H, x.row_map, j.ctrl, j.chunk_start, 1, nullptr, nullptr, XT, x.tc, x.tc, true}, bx, by, tile.h);
+    } else transpose_block(TransposeJob<T>{X, x.H, x.tc, x.H, x.row_map, j.ctrl, j.chunk_start, 1, nullptr, nullptr, XT, x.tc, x.tc, false}, bx, by, tile.f);
+    return;
+  }
+  b -= x.n_xt;
+  const int64_t step = (int64_t)((int)gridDim.x - x.n_ds - x.n_xt) * 4;
+  for (int64_t r = (int64_t)b * 4 + (threadIdx.x >> 6); r < x.R; r += step) zero_masked_row(r, x.cpos, static_cast<T*>(x.dX), x.R, x.H);
+}
+
+// loss, and the counts: a workgroup, each thread its rows in order
+struct FinishJob { const double* term; const int* info; const Ctrl* ctrl; const rl_stats* st; float* loss; rl_distill_stats* out; };
+__device__ inline void distill_finish(const FinishJob& j) {
+  __shared__ double sh[16];
+  __shared__ int cnt[2];
+  if (threadIdx.x < 2) cnt[threadIdx.x] = 0;
+  __syncthreads();
+  const int n = j.ctrl->n_real, step = blockDim.x;
+  double s = 0.0;
+  int bad = 0, empty = 0;
+  for (int i0 = threadIdx.x; i0 < n; i0 += 8 * step) {            // (eight loads in flight)
+    double t[8];
+    int f[8];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) { const int i = i0 + k * step; t[k] = i < n ? j.term[i] : 0.0; f[k] = i < n ? j.info[i] : 0; }
+#pragma unroll
+    for (int k = 0; k < 8; ++k) { s += t[k]; bad += f[k] & 0xffff; empty += f[k] >> 30; }
+  }
+  s = block_sum(s, sh);
+  atomicAdd(&cnt[0], bad); atomicAdd(&cnt[1], empty);
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    j.loss[0] = (float)s;
+    if (j.out) *j.out = rl_distill_stats{n, cnt[0], cnt[1], j.st->n_bad_seq};
+  }
+}
+__global__ __launch_bounds__(1024) void distill_finish_kernel(FinishJob j) { distill_finish(j); }
+
+// dS of the listed tokens over what the pass wrote there; the last chunk's launch has one workgroup more, for the loss (term != NULL)
+template <class T>
+__global__ __launch_bounds__(1024) void distill_patch_kernel(const int* ids, const float* val, int K, const Ctrl* ctrl, int chunk_start, int chunk_rows, T* dS, int64_t ld_ds,
+                                                             T* dST, int64_t ld_dst, FinishJob fin) {
+  if (fin.term && blockIdx.x == 0) { distill_finish(fin); return; }
   int left = ctrl->n_real - chunk_start;
   left = left < chunk_rows ? left : chunk_rows;
-  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  const int64_t i = (int64_t)(blockIdx.x - (fin.term ? 1 : 0)) * 1024 + threadIdx.x;
   if (i >= (int64_t)left * K) return;
   const int v = ids[i], t = (int)(i / K);
   if (v < 0) return;
   if (dS) dS[operand_index(sizeof(T) == 2, t, v, ld_ds)] = (T)val[i];
   if (sizeof(T) == 4) dST[(int64_t)v * ld_dst + t] = (T)val[i];
-}
-
-// loss, and the counts: one workgroup, each thread its rows in order
-__global__ __launch_bounds__(1024) void distill_finish_kernel(const double* term, const int* info, const Ctrl* ctrl, const rl_stats* st, float* loss, rl_distill_stats* out) {
-  __shared__ double sh[16];
-  __shared__ int cnt[2];
-  if (threadIdx.x < 2) cnt[threadIdx.x] = 0;
-  __syncthreads();
-  const int n = ctrl->n_real;
-  double s = 0.0;
-  int bad = 0, empty = 0;
-  for (int i = threadIdx.x; i < n; i += 1024) { s += term[i]; bad += info[i] & 0xffff; empty += info[i] >> 30; }
-  s = block_sum(s, sh);
-  atomicAdd(&cnt[0], bad); atomicAdd(&cnt[1], empty);
-  __syncthreads();
-  if (threadIdx.x == 0) {
-    loss[0] = (float)s;
-    if (out) *out = rl_distill_stats{n, cnt[0], cnt[1], st->n_bad_seq};
-  }
-}
-
-// d_weight from the f32 sums, rounded once; eight values a thread, of any alignment
-__global__ __launch_bounds__(256) void distill_round_kernel(const float* x, bf16_t* y, int64_t n) {
-  typedef bf16_t bf16x8_any __attribute__((ext_vector_type(8), aligned(2)));
-  for (int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 8; i < n; i += (int64_t)gridDim.x * 2048) {       // (n is a multiple of 8)
-    const floatx4 a = __builtin_nontemporal_load(reinterpret_cast<const floatx4*>(x + i)), b = __builtin_nontemporal_load(reinterpret_cast<const floatx4*>(x + i + 4));
-    bf16x8 o;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) { o[e] = (bf16_t)a[e]; o[4 + e] = (bf16_t)b[e]; }
-    *reinterpret_cast<bf16x8_any*>(y + i) = o;
-  }
 }
 
 // ------------------------------------------------------------------ host side
@@ -775,7 +799,7 @@ static rl_status head_plan(const rl_batch* b, int K, int chunk_rows, float tempe
     if (bwd) {
       h.off_rows = take(sizeof(DistillRow) * tc);
       h.off_pids = take(4 * tc * (size_t)K); h.off_pval = take(4 * tc * (size_t)K);
-      if (round_dw) h.off_dw = take(4 * (size_t)p.V * (size_t)p.H);
+      if (round_dw && p.n_chunks > 1) h.off_dw = take(4 * (size_t)p.V * (size_t)p.H);
     }
   }
   h.total = o;
@@ -828,17 +852,15 @@ static void run_distill(const rl_batch* b, const HeadPlan& h, const Ptrs& q, uns
   const T* X = static_cast<const T*>(b->hidden);
   const T* W = static_cast<const T*>(b->weight);
   T* dS = static_cast<T*>(q.ds); T* dST = static_cast<T*>(q.dst);
-  float* dw = h.off_dw ? (float*)(w + h.off_dw) : static_cast<float*>(out->d_weight);
+  const bool round = prm->d_weight_dtype == RL_BF16;
+  float* dw = !round ? static_cast<float*>(out->d_weight) : h.off_dw ? (float*)(w + h.off_dw) : nullptr;
   DistillRow* rows = bwd ? (DistillRow*)(w + h.off_rows) : nullptr;
   int* p_ids = (int*)(w + h.off_pids);
   float* p_val = (float*)(w + h.off_pval);
-  if (bwd) {
+  const FinishJob fin{(const double*)(w + h.off_term), (const int*)(w + h.off_info), q.ctrl, (const rl_stats*)(w + h.off_stats), out->loss, out->stats};
+  if (bwd && !p.k_major_w) {
     ProfScope ps(RL_PROF_TRANSPOSE, s);
-    for (int64_t r0 = 0; r0 < p.R; r0 += 1 << 25) {               // (64 threads a row)
-      const int64_t n = p.R - r0 < (1 << 25) ? p.R - r0 : 1 << 25;
-      zero_masked_rows_kernel<T><<<(unsigned)((n + 3) / 4), 256, 0, s>>>(q.cpos + r0, static_cast<T*>(out->d_hidden) + r0 * p.H, n, p.H);
-    }
-    if (!p.k_major_w) launch_transpose<T>(dim3((p.Vp + 63) / 64, (p.H + 63) / 64), s, W, p.H, p.V, p.H, nullptr, q.ctrl, 0, 0, nullptr, nullptr, static_cast<T*>(q.wt), p.Vp, p.Vp, p.tiled);
+    launch_transpose<T>(dim3((p.Vp + 63) / 64, (p.H + 63) / 64), s, W, p.H, p.V, p.H, nullptr, q.ctrl, 0, 0, nullptr, nullptr, static_cast<T*>(q.wt), p.Vp, p.Vp, p.tiled);
   }
   for (int ch = 0; ch < p.n_chunks; ++ch) {
     const int c0 = ch * p.Tc;
@@ -846,27 +868,28 @@ static void run_distill(const rl_batch* b, const HeadPlan& h, const Ptrs& q, uns
     score_chunk<T>(b, h, q, c0, z, rec, s);
     {
       ProfScope ps(RL_PROF_COMBINE, s);
-      const DistillJob j{z, p.Vp, rec, p.Tc, h.groups, p.V, h.K, p.inv_tau, q.row_map, q.cstart, q.ctrl, c0, p.Tc, p.B, t_ids, t_lp, prm->rest,
-                         prm->aggregation == RL_AGG_TOKEN, prm->scale == 0.f ? 1.f : prm->scale, out->row_loss, out->lse,
-                         (double*)(w + h.off_term), (int*)(w + h.off_info), rows, p_ids, p_val};
-      distill_row_kernel<<<(unsigned)((n + kRowWaves - 1) / kRowWaves), kRowWaves * 64, distill_lds_bytes(h.groups), s>>>(j);
+      launch_distill_rows(DistillJob{z, p.Vp, rec, p.Tc, h.groups, p.V, h.K, p.inv_tau, q.row_map, q.cstart, q.ctrl, c0, p.Tc, p.B, t_ids, t_lp, prm->rest,
+                                     prm->aggregation == RL_AGG_TOKEN, prm->scale == 0.f ? 1.f : prm->scale, out->row_loss, out->lse,
+                                     (double*)(w + h.off_term), (int*)(w + h.off_info), rows, p_ids, p_val}, n, s);
     }
     if (!bwd) continue;
     {
       ProfScope ps(RL_PROF_GEMM_DS, s);
-      if constexpr (sizeof(T) == 2) distill_ds_kernel<<<(unsigned)((n + 255) / 256 * (p.Vp / 64)), 256, 0, s>>>(z, p.Vp, rows, q.ctrl, c0, p.V, p.inv_tau, dS);
-      else distill_ds_f32_kernel<<<(unsigned)((n + 63) / 64 * (p.Vp / 64)), 256, 0, s>>>(z, p.Vp, rows, q.ctrl, c0, p.V, p.inv_tau, p.k_major_w ? nullptr : dS, p.Vp, dST, p.Tc);
-      distill_patch_kernel<T><<<(unsigned)((n * h.K + 255) / 256), 256, 0, s>>>(p_ids, p_val, h.K, q.ctrl, c0, p.Tc, sizeof(T) == 4 && p.k_major_w ? nullptr : dS, p.Vp, dST, p.Tc);
+      const int tile = sizeof(T) == 2 ? 256 : 64, cols = (int)((n + 255) / 256 * 4);
+      const int n_ds = (int)((n + tile - 1) / tile * (p.Vp / 64)), n_xt = cols * ((p.H + 63) / 64);
+      const int64_t zero = ch ? 0 : (p.R + 3) / 4;
+      T* plain = sizeof(T) == 4 && p.k_major_w ? nullptr : dS;
+      distill_ds_kernel<T><<<(unsigned)(n_ds + n_xt + (zero < 16384 ? zero : 16384)), 256, 0, s>>>(
+          DsJob{z, p.Vp, rows, q.ctrl, c0, p.V, p.inv_tau}, plain, p.Vp, dST, p.Tc,
+          XtJob{X, p.R, p.H, cols, n_ds, n_xt, reinterpret_cast<uintptr_t>(X) % 16 == 0, q.row_map, q.cpos, q.xt, out->d_hidden, p.Tc});
+      const bool last = ch + 1 == p.n_chunks;
+      distill_patch_kernel<T><<<(unsigned)((n * h.K + 1023) / 1024 + last), 1024, 0, s>>>(p_ids, p_val, h.K, q.ctrl, c0, p.Tc, plain, p.Vp, dST, p.Tc, last ? fin : FinishJob{});
     }
-    {  // X^T chunk [H][Tc], gathered through row_map, zero beyond the valid rows
-      ProfScope ps(RL_PROF_TRANSPOSE, s);
-      launch_transpose<T>(dim3((p.Tc + 63) / 64, (p.H + 63) / 64), s, X, p.H, p.Tc, p.H, q.row_map, q.ctrl, c0, 1, nullptr, nullptr, static_cast<T*>(q.xt), p.Tc, p.Tc, p.tiled);
-    }
-    contract_grads<T>(b, p, q, ch, out->d_hidden, dw, s);
+    contract_grads<T>(b, p, q, ch, out->d_hidden, dw, s, round ? static_cast<bf16_t*>(out->d_weight) : nullptr);
   }
+  if (bwd) return;
   ProfScope ps(RL_PROF_LOSS, s);
-  distill_finish_kernel<<<1, 1024, 0, s>>>((const double*)(w + h.off_term), (const int*)(w + h.off_info), q.ctrl, (const rl_stats*)(w + h.off_stats), out->loss, out->stats);
-  if (bwd && h.off_dw) distill_round_kernel<<<2048, 256, 0, s>>>(dw, static_cast<bf16_t*>(out->d_weight), (int64_t)p.V * p.H);
+  distill_finish_kernel<<<1, 1024, 0, s>>>(fin);
 }
 
 }  // namespace rlk

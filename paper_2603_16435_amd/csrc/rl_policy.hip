@@ -1097,11 +1097,9 @@ __global__ __launch_bounds__(kGradWaves * 64, U == 1 ? 8 : 4) void small_grads_k
 // The same for bf16 with 16-byte accesses on both sides (cols % 8 == 0, 16-byte aligned rows; rows_padded % 8 == 0, tiled
 // destination): a thread loads two 16-byte pieces of source rows and stores two 16-byte pieces of destination rows, each
 // gathered from eight consecutive source rows of one column in LDS (row stride 33 dwords: the gather is conflict-free).
-__global__ __launch_bounds__(256)
-void transpose_bf16_kernel(const bf16_t* src, int64_t ld_src, int rows, int cols, const int32_t* row_idx,
+__device__ __attribute__((always_inline)) inline void transpose_bf16_block(int bx, int by, unsigned (&tile)[64][33], const bf16_t* src, int64_t ld_src, int rows, int cols, const int32_t* row_idx,
                            const Ctrl* ctrl, int chunk_start, int dyn_rows, const ChunkDesc* desc, const float* row_scale,
                            bf16_t* dst, int64_t ld_dst, int rows_padded) {
-  __shared__ unsigned tile[64][33];
   int rv = rows;
   if (dyn_rows) {
     int left;
@@ -1109,7 +1107,7 @@ void transpose_bf16_kernel(const bf16_t* src, int64_t ld_src, int rows, int cols
     if (left <= 0) return;
     rv = left < rows ? left : rows;
   }
-  const int r0 = blockIdx.x * 64, c0 = blockIdx.y * 64;
+  const int r0 = bx * 64, c0 = by * 64;
   if (dyn_rows && r0 >= ((rv + 255) & ~255)) return;
   const int ch = threadIdx.x & 7, k0 = threadIdx.x >> 3;
 #pragma unroll
@@ -1142,6 +1140,13 @@ void transpose_bf16_kernel(const bf16_t* src, int64_t ld_src, int rows, int cols
       *reinterpret_cast<uint4*>(dst + tiled_index(c, r, ld_dst)) = make_uint4(w[0], w[1], w[2], w[3]);
     }
   }
+}
+__global__ __launch_bounds__(256)
+void transpose_bf16_kernel(const bf16_t* src, int64_t ld_src, int rows, int cols, const int32_t* row_idx,
+                           const Ctrl* ctrl, int chunk_start, int dyn_rows, const ChunkDesc* desc, const float* row_scale,
+                           bf16_t* dst, int64_t ld_dst, int rows_padded) {
+  __shared__ unsigned tile[64][33];
+  transpose_bf16_block(blockIdx.x, blockIdx.y, tile, src, ld_src, rows, cols, row_idx, ctrl, chunk_start, dyn_rows, desc, row_scale, dst, ld_dst, rows_padded);
 }
 
 // Host side: the 16-byte kernel where its conditions hold (always, for the library's own bf16 buffers and 16-byte aligned inputs).
@@ -1458,19 +1463,20 @@ static void launch_gemm(const float* A, const float* B, const GemmDims& d, const
 // dX = diag(f) dS W  (A = dS or E' [Tc][Vp], B = W^T [H][Vp]) and dW (+)= dS^T (diag(f) X)  (A = the same array read as a K-major
 // operand, B = X^T [H][Tc]) of a bf16 chunk in one launch: dX alone has few (long) tiles, whose last round would leave CUs
 // idle; the dW tiles fill them.  dX is cut along K where its tiles are fewer still.
+template <class EDW>
 static void launch_dx_dw(const bf16_t* E, const bf16_t* W, const bf16_t* WT, GemmDims dx, EpiDX<bf16_t> ex, const bf16_t* XT, const GemmDims& dw,
-                         const EpiDW& ew, hipStream_t s) {
+                         const EDW& ew, hipStream_t s) {
   const int tn = (dx.N + kBN - 1) / kBN;
   dx.split_slots = kHotSlots; dx.fill_tiles = (dw.M + kBM - 1) / kBM * tn;
   const int n1 = split_launch((dx.M + kBM - 1) / kBM, tn, kHotSlots);
   const int n2 = launch_tiles((dw.M + kBM - 1) / kBM, tn);
   if (WT) {
     const bool both = step_prefetch(dx.M, tn, dx.fill_tiles);
-    gemm_nt_bf16_pair_kernel<EpiDX<bf16_t>, TuneDX, EpiDW, TuneDW, false><<<n1 + n2, 256, 0, s>>>(E, WT, dx, ex, n1, E, XT, dw, ew, 0, both ? kStepRows : 0);
-    if (both) gemm_nt_bf16_pair_kernel<EpiDX<bf16_t>, TuneDXStep, EpiDW, TuneDWStep, false><<<n1 + n2, 256, 0, s>>>(E, WT, dx, ex, n1, E, XT, dw, ew, kStepRows, 0);
+    gemm_nt_bf16_pair_kernel<EpiDX<bf16_t>, TuneDX, EDW, TuneDW, false><<<n1 + n2, 256, 0, s>>>(E, WT, dx, ex, n1, E, XT, dw, ew, 0, both ? kStepRows : 0);
+    if (both) gemm_nt_bf16_pair_kernel<EpiDX<bf16_t>, TuneDXStep, EDW, TuneDWStep, false><<<n1 + n2, 256, 0, s>>>(E, WT, dx, ex, n1, E, XT, dw, ew, kStepRows, 0);
   } else {
     dx.ldb = dx.N; dx.b_k_rows = dw.M;
-    gemm_nt_bf16_pair_kernel<EpiDX<bf16_t>, TuneDX, EpiDW, TuneDW, true><<<n1 + n2, 256, 0, s>>>(E, W, dx, ex, n1, E, XT, dw, ew, 0, 0);
+    gemm_nt_bf16_pair_kernel<EpiDX<bf16_t>, TuneDX, EDW, TuneDW, true><<<n1 + n2, 256, 0, s>>>(E, W, dx, ex, n1, E, XT, dw, ew, 0, 0);
   }
   splitk_reduce_kernel<bf16_t><<<512, 256, 0, s>>>(dx, ex, kBM, kBN, kHotStep);
 }
@@ -1616,9 +1622,9 @@ static void run_forward(const rl_batch* b, const Plan& p, const Ptrs& q, float* 
   }
 }
 
-// dX and dW (+)= of chunk ch, out of its dS (and dS^T for f32 inputs), X^T and W or W^T.
+// dX and dW (+)= of chunk ch, out of its dS (and dS^T for f32 inputs), X^T and W or W^T.  rounded (bf16): where the last chunk's dW goes, d_weight having the sums of the others.
 template <class T>
-static void contract_grads(const rl_batch* b, const Plan& p, const Ptrs& q, int ch, void* d_hidden, float* d_weight, hipStream_t s) {
+static void contract_grads(const rl_batch* b, const Plan& p, const Ptrs& q, int ch, void* d_hidden, float* d_weight, hipStream_t s, bf16_t* rounded = nullptr) {
   const T* W = static_cast<const T*>(b->weight);
   T* WT = static_cast<T*>(q.wt); T* XT = static_cast<T*>(q.xt);
   T* dS = static_cast<T*>(q.ds); T* dST = static_cast<T*>(q.dst);
@@ -1638,7 +1644,10 @@ static void contract_grads(const rl_batch* b, const Plan& p, const Ptrs& q, int 
   EpiDW ew{d_weight, p.H, p.V, p.H, ch > 0 ? 1 : 0};
   if constexpr (sizeof(T) == 2) {
     ProfScope ps(RL_PROF_GEMM_BWD, s);
-    launch_dx_dw(dS, W, p.k_major_w ? nullptr : WT, dx, ex, XT, dw, ew, s);
+    if (rounded && ch + 1 == p.n_chunks) {
+      dw.zero_if_empty = true;
+      launch_dx_dw(dS, W, p.k_major_w ? nullptr : WT, dx, ex, XT, dw, EpiDWRounded{rounded, p.H, p.V, p.H, ch > 0 ? d_weight : nullptr}, s);
+    } else launch_dx_dw(dS, W, p.k_major_w ? nullptr : WT, dx, ex, XT, dw, ew, s);
   } else {
     dx.split_slots = kF32Slots;
     if (p.small_pair) {
