@@ -27,6 +27,10 @@ constexpr int kGroup = 64;                        // vocabulary entries of a rec
 // In what order the 64 are added: bf16 (kPermute, a lane holds eight consecutive entries of each half of the group): the sixteen of a lane in order, then lanes 16
 // apart, then 32.  f32, by quads of four consecutive entries Q = 0 .. 15: over bits 2 and 3 of Q in order, then bit 1, then bit 0, which both
 // block shapes of the f32 kernels can do: a token's sums do not depend on the tile it is in.
+//
+// Where the record of group g and token t lies: those of four groups, a tile's 256 entries, are neighbours, so that a row's records are pieces of 64 bytes (a row by
+// itself takes a whole line for each piece; with one record a piece the row kernels waited for L2: 4.5 k rows of V 152064 126 us), and a tile's are one piece of memory.
+__device__ inline int64_t rec_index(int g, int t, int ldr) { return ((int64_t)(g >> 2) * ldr + t) * 4 + (g & 3); }
 template <class T>
 struct EpiScore {
   typedef NoPre Pre;
@@ -37,7 +41,7 @@ struct EpiScore {
   static constexpr bool kGatherB = true;
   __device__ void keep_alive() const { z[0] = 0.f; }
   float* z; int64_t ldz;      // logits, slab-tiled like the bf16 work buffers: a tile of 256 x 256 is one piece of memory
-  float4* rec; int ldr;       // [vocabulary / 64][chunk rows]
+  float4* rec; int ldr;       // [vocabulary / 256][chunk rows][4]
   int V;
   float zs;                   // inverse temperature
 
@@ -81,7 +85,7 @@ struct EpiScore {
         for (int r = 0; r < 16; ++r) v[r] = acc_read<AGPR>(acc[4 * j + (r >> 2)][bj], r & 3);
         const int n = col(bj, c.lane);
         const float4 q = vleft < j * 64 + 64 ? group16<true>(v, g, vleft - j * 64) : group16<false>(v, g, 64);
-        if (g == (NB >= 4 ? bj / (NB / 4) : bj) && n < c.Nv) rec[(int64_t)(c.m0 / kGroup + j) * ldr + n] = q;
+        if (g == (NB >= 4 ? bj / (NB / 4) : bj) && n < c.Nv) rec[rec_index(c.m0 / kGroup + j, n, ldr)] = q;
         // lane pairs swap quads, so that a store writes whole lines of 128 bytes
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
@@ -138,7 +142,7 @@ struct EpiScore {
         };
         const float S = join(s), U = join(u);
         if (n < c.Nv) {
-          if (c.lane < L::kBlk) rec[(int64_t)(c.m0 / kGroup + k) * ldr + n] = make_float4(mx, S, U, 0.f);
+          if (c.lane < L::kBlk) rec[rec_index(c.m0 / kGroup + k, n, ldr)] = make_float4(mx, S, U, 0.f);
 #pragma unroll
           for (int bi = 0; bi < PER; ++bi)
 #pragma unroll
@@ -174,6 +178,12 @@ void score_few_kernel(const bf16_t* __restrict__ W, const bf16_t* __restrict__ X
 
 // ------------------------------------------------------------------ a row, by a workgroup
 __device__ inline float wave_max(float v) { for (int o = 32; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor(v, o)); return v; }
+
+// e^x, to 2^-23 of itself: the hardware's exponential of what is left of x beside a power of two
+__device__ inline double exp_near(double x) {
+  const double v = x * 1.4426950408889634, n = rint(v);
+  return v < -1000.0 ? 0.0 : ldexp((double)__builtin_amdgcn_exp2f((float)(v - n)), (int)n);
+}
 
 // Order of logits as unsigned numbers: -0 is 0, what is no number comes before everything.
 __device__ inline unsigned order_key(float z) {
@@ -280,7 +290,7 @@ __global__ __launch_bounds__(kTopThreads) void top_kernel(TopJob j) {
   for (int i = 0; i < REG; ++i) {
     const int b = i * kTopThreads + tid;
     q[i] = make_float4(NEG, 0.f, 0.f, 0.f);
-    if (b < j.groups) q[i] = j.rec[(int64_t)b * j.ldr + t];
+    if (b < j.groups) q[i] = j.rec[rec_index(b, t, j.ldr)];
   }
 #pragma unroll
   for (int i = 0; i < REG; ++i) m = fmaxf(m, q[i].x);
@@ -463,7 +473,15 @@ __global__ __launch_bounds__(kTopThreads) void distill_row_kernel(DistillJob j) 
   for (int i = 0; i < REG; ++i) {
     const int b = i * kTopThreads + tid;
     q[i] = make_float4(NEG, 0.f, 0.f, 0.f);
-    if (b < j.groups) q[i] = j.rec[(int64_t)b * j.ldr + t];
+    if (b < j.groups) q[i] = j.rec[rec_index(b, t, j.ldr)];
+  }
+  double share = 0.0;                                             // (wavefronts 0 and 1, as all that is asked of entries)
+  if (w < 2) {
+    if (j.token_mean) share = 1.0 / (double)j.ctrl->n_real;
+    else {
+      const int i = sequence_of(j.cstart, j.B, tg, lane);
+      share = 1.0 / ((double)j.B * (double)(j.cstart[i + 1] - j.cstart[i]));
+    }
   }
   int id = -1;
   float lp = NEG;
@@ -475,14 +493,17 @@ __global__ __launch_bounds__(kTopThreads) void distill_row_kernel(DistillJob j) 
   const float zi = in ? j.z[tiled_index(t, id, j.ldz)] : 0.f;
   __syncthreads();
   bool head = in;                                                 // first of its group
-  if (w < 2)
-    for (int i = 0; i < K; ++i) {
-      const int o = ids[i];
-      if (i < tid && o >= 0) {
-        if (o == id) { out |= in; in = false; }
-        if (o / kGroup == id / kGroup) head = false;
-      }
+  auto before = [&](int o, bool earlier) __attribute__((always_inline)) {
+    if (earlier && o >= 0) {
+      if (o == id) { out |= in; in = false; }
+      if (o / kGroup == id / kGroup) head = false;
     }
+  };
+  if (w < 2) {
+    const int first = ids[lane], own = w == 0 ? first : ids[64 + lane];
+    if (w == 1) for (int i = 0; i < 64; ++i) before(__builtin_amdgcn_readlane(first, i), true);
+    for (int i = 0; i < K - w * 64 && i < 64; ++i) before(__builtin_amdgcn_readlane(own, i), i < lane);
+  }
   BlockSum count{words, lane, w, 0};
   const unsigned long long heads = __ballot(head);
   // (a word each: entries left out, entries, heads of the first wavefront)
@@ -563,34 +584,34 @@ __global__ __launch_bounds__(kTopThreads) void distill_row_kernel(DistillJob j) 
     }
   };
   if (ml == NEG) ml = 0.f;
-  double p = in ? exp(bucket ? (double)lp : (double)lp - (double)ml) : 0.0;
+  const double lt = bucket ? (double)lp : (double)lp - (double)ml;
+  double p = in ? exp(lt) : 0.0;                                  // (exact: 1 - sum p may be small)
   double v[4] = {o.s, r.s, p, 0.0};
   sum4(0, v);
-  const double ln = log(v[0]), lnr = log(v[1]);
-  const double lq = in ? (double)j.zs * ((double)zi - (double)m) - ln : 0.0;
-  const double lqr = (double)j.zs * ((double)mr - (double)m) + lnr - ln;       // log of the others' probability
-  double P, pr = 0.0;
-  if (bucket) {
-    pr = 1.0 - v[2]; pr = pr < 0.0 ? 0.0 : pr;
-    if (mr == NEG && v[1] == 0.0) pr = 0.0;                       // (the list names all tokens)
-    P = v[2] + pr;
-  } else {
-    p = v[2] == 0.0 ? 0.0 : p / v[2];
-    P = v[2] == 0.0 ? 0.0 : 1.0;
+  double ln = 0.0, lnr = 0.0, lq = 0.0, lqr = 0.0, P = 0.0, pr = 0.0, part[4] = {0.0, 0.0, 0.0, 0.0};
+  if (w < 2) {
+    ln = log(v[0]);
+    if (in) lq = (double)j.zs * ((double)zi - (double)m) - ln;
+    double lnp = 0.0;
+    if (bucket) {
+      lnr = log(v[1]);
+      lqr = (double)j.zs * ((double)mr - (double)m) + lnr - ln;   // log of the others' probability
+      pr = 1.0 - v[2]; pr = pr < 0.0 ? 0.0 : pr;
+      if (mr == NEG && v[1] == 0.0) pr = 0.0;                     // (the list names all tokens)
+      P = v[2] + pr;
+    } else if (v[2] != 0.0) {
+      lnp = log(v[2]);
+      p /= v[2];
+      P = 1.0;
+    }
+    if (p > 0.0 || p != p) part[0] = p * (lt - lnp - lq);
   }
-  double part[4] = {p > 0.0 || p != p ? p * (log(p) - lq) : 0.0, 0.0, 0.0, 0.0};
   sum4(1, part);
+  if (w >= 2) return;
   const bool nothing = empty || P == 0.0;
   double kl = part[0];
   if (pr > 0.0) kl += pr * (log(pr) - lqr);
   if (nothing) kl = 0.0;
-
-  double share;
-  if (j.token_mean) share = 1.0 / (double)j.ctrl->n_real;
-  else {
-    const int i = sequence_of(j.cstart, j.B, tg, lane);
-    share = 1.0 / ((double)j.B * (double)(j.cstart[i + 1] - j.cstart[i]));
-  }
   const double coef = (double)j.scale * share, f = coef * (double)j.zs;
   if (tid == 0) {
     if (j.lse) j.lse[row] = (float)((double)j.zs * (double)m + ln);
@@ -602,12 +623,12 @@ __global__ __launch_bounds__(kTopThreads) void distill_row_kernel(DistillJob j) 
   // dS at the others, coef zs q (P - pr / q_r).  With a bucket relative to their own sum, q / q_r (P q_r - pr): nothing overflows where q_r is small
   if (tid == 0) {
     DistillRow d{m, (float)(ln * 1.4426950408889634), nothing ? 0.f : (float)(f * P), 0.f};
-    if (pr > 0.0 && !nothing) { d.m = mr; d.l2 = (float)(lnr * 1.4426950408889634); d.f = (float)(f * (P * exp(lqr) - pr)); }
+    if (pr > 0.0 && !nothing) { d.m = mr; d.l2 = (float)(lnr * 1.4426950408889634); d.f = (float)(f * (P * exp_near(lqr) - pr)); }
     j.rows[t] = d;
   }
   if (tid < K) {
     j.p_ids[(int64_t)t * K + tid] = in && !nothing ? id : -1;
-    j.p_val[(int64_t)t * K + tid] = (float)(f * (P * exp(lq) - p));
+    j.p_val[(int64_t)t * K + tid] = (float)(f * (P * exp_near(lq) - p));
   }
 }
 static void launch_distill_rows(const DistillJob& j, int64_t rows, hipStream_t s) {
@@ -693,32 +714,6 @@ __device__ __attribute__((always_inline)) inline void ds_f32_block(int block, co
   }
 }
 
-// dS of a chunk, and beside it what else the contractions want: X^T, and, in the first chunk's launch, the rows of dX that do not count as 0.  Workgroups [0, n_ds), n_xt, and the rest.
-struct XtJob { const void* x; int64_t R; int H, cols, n_ds, n_xt, fast; const int *row_map, *cpos; void *xt, *dX; int tc; };
-template <class T>
-__global__ __launch_bounds__(256) void distill_ds_kernel(DsJob j, T* dS, int64_t ld_ds, T* dST, int64_t ld_dst, XtJob x) {
-  __shared__ union { float f[64][65]; unsigned b[64][33]; bf16_t h[64][65]; } tile;
-  int b = blockIdx.x;
-  if (b < x.n_ds) {
-    if constexpr (sizeof(T) == 2) ds_block(b, j, dS); else ds_f32_block(b, j, dS, ld_ds, dST, ld_dst, tile.f);
-    return;
-  }
-  b -= x.n_ds;
-  const T* X = static_cast<const T*>(x.x);
-  T* XT = static_cast<T*>(x.xt);
-  if (b < x.n_xt) {
-    const int bx = b % x.cols, by = b / x.cols;
-    if constexpr (sizeof(T) == 2) {
-      if (x.fast) transpose_bf16_block(bx, by, tile.b, X, x.H, x.tc, x.H, x.row_map, j.ctrl, j.chunk_start, 1, nullptr, nullptr, XT, x.tc, x.tc);
-      else transpose_block(TransposeJob<T>{X, x.H, x.tc, x.H, x.row_map, j.ctrl, j.chunk_start, 1, nullptr, nullptr, XT, x.tc, x.tc, true}, bx, by, tile.h);
-    } else transpose_block(TransposeJob<T>{X, x.H, x.tc, x.H, x.row_map, j.ctrl, j.chunk_start, 1, nullptr, nullptr, XT, x.tc, x.tc, false}, bx, by, tile.f);
-    return;
-  }
-  b -= x.n_xt;
-  const int64_t step = (int64_t)((int)gridDim.x - x.n_ds - x.n_xt) * 4;
-  for (int64_t r = (int64_t)b * 4 + (threadIdx.x >> 6); r < x.R; r += step) zero_masked_row(r, x.cpos, static_cast<T*>(x.dX), x.R, x.H);
-}
-
 // loss, and the counts: a workgroup, each thread its rows in order
 struct FinishJob { const double* term; const int* info; const Ctrl* ctrl; const rl_stats* st; float* loss; rl_distill_stats* out; };
 __device__ inline void distill_finish(const FinishJob& j) {
@@ -747,14 +742,44 @@ __device__ inline void distill_finish(const FinishJob& j) {
 }
 __global__ __launch_bounds__(1024) void distill_finish_kernel(FinishJob j) { distill_finish(j); }
 
-// dS of the listed tokens over what the pass wrote there; the last chunk's launch has one workgroup more, for the loss (term != NULL)
+// dS of a chunk, and beside it what else is wanted by then: X^T, in the first chunk's launch the rows of dX that do not count as 0, in the last one's the loss (term != NULL).  Workgroups, in
+// this order: the loss, n_ds, n_xt, and the rest.
+struct XtJob { const void* x; int64_t R; int H, cols, n_ds, n_xt, fast; const int *row_map, *cpos; void *xt, *dX; int tc; };
 template <class T>
-__global__ __launch_bounds__(1024) void distill_patch_kernel(const int* ids, const float* val, int K, const Ctrl* ctrl, int chunk_start, int chunk_rows, T* dS, int64_t ld_ds,
-                                                             T* dST, int64_t ld_dst, FinishJob fin) {
-  if (fin.term && blockIdx.x == 0) { distill_finish(fin); return; }
+__global__ __launch_bounds__(256) void distill_ds_kernel(DsJob j, T* dS, int64_t ld_ds, T* dST, int64_t ld_dst, XtJob x, FinishJob fin) {
+  __shared__ union { float f[64][65]; unsigned b[64][33]; bf16_t h[64][65]; } tile;
+  int b = blockIdx.x;
+  if (fin.term) {
+    if (b == 0) { distill_finish(fin); return; }
+    --b;
+  }
+  if (b < x.n_ds) {
+    if constexpr (sizeof(T) == 2) ds_block(b, j, dS); else ds_f32_block(b, j, dS, ld_ds, dST, ld_dst, tile.f);
+    return;
+  }
+  b -= x.n_ds;
+  const T* X = static_cast<const T*>(x.x);
+  T* XT = static_cast<T*>(x.xt);
+  if (b < x.n_xt) {
+    const int bx = b % x.cols, by = b / x.cols;
+    if constexpr (sizeof(T) == 2) {
+      if (x.fast) transpose_bf16_block(bx, by, tile.b, X, x.H, x.tc, x.H, x.row_map, j.ctrl, j.chunk_start, 1, nullptr, nullptr, XT, x.tc, x.tc);
+      else transpose_block(TransposeJob<T>{X, x.H, x.tc, x.H, x.row_map, j.ctrl, j.chunk_start, 1, nullptr, nullptr, XT, x.tc, x.tc, true}, bx, by, tile.h);
+    } else transpose_block(TransposeJob<T>{X, x.H, x.tc, x.H, x.row_map, j.ctrl, j.chunk_start, 1, nullptr, nullptr, XT, x.tc, x.tc, false}, bx, by, tile.f);
+    return;
+  }
+  b -= x.n_xt;
+  const int64_t step = (int64_t)((int)gridDim.x - (fin.term ? 1 : 0) - x.n_ds - x.n_xt) * 4;
+  for (int64_t r = (int64_t)b * 4 + (threadIdx.x >> 6); r < x.R; r += step) zero_masked_row(r, x.cpos, static_cast<T*>(x.dX), x.R, x.H);
+}
+
+// dS of the listed tokens over what the pass wrote there
+template <class T>
+__global__ __launch_bounds__(256) void distill_patch_kernel(const int* ids, const float* val, int K, const Ctrl* ctrl, int chunk_start, int chunk_rows, T* dS, int64_t ld_ds,
+                                                            T* dST, int64_t ld_dst) {
   int left = ctrl->n_real - chunk_start;
   left = left < chunk_rows ? left : chunk_rows;
-  const int64_t i = (int64_t)(blockIdx.x - (fin.term ? 1 : 0)) * 1024 + threadIdx.x;
+  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
   if (i >= (int64_t)left * K) return;
   const int v = ids[i], t = (int)(i / K);
   if (v < 0) return;
@@ -879,11 +904,11 @@ static void run_distill(const rl_batch* b, const HeadPlan& h, const Ptrs& q, uns
       const int n_ds = (int)((n + tile - 1) / tile * (p.Vp / 64)), n_xt = cols * ((p.H + 63) / 64);
       const int64_t zero = ch ? 0 : (p.R + 3) / 4;
       T* plain = sizeof(T) == 4 && p.k_major_w ? nullptr : dS;
-      distill_ds_kernel<T><<<(unsigned)(n_ds + n_xt + (zero < 16384 ? zero : 16384)), 256, 0, s>>>(
-          DsJob{z, p.Vp, rows, q.ctrl, c0, p.V, p.inv_tau}, plain, p.Vp, dST, p.Tc,
-          XtJob{X, p.R, p.H, cols, n_ds, n_xt, reinterpret_cast<uintptr_t>(X) % 16 == 0, q.row_map, q.cpos, q.xt, out->d_hidden, p.Tc});
       const bool last = ch + 1 == p.n_chunks;
-      distill_patch_kernel<T><<<(unsigned)((n * h.K + 1023) / 1024 + last), 1024, 0, s>>>(p_ids, p_val, h.K, q.ctrl, c0, p.Tc, plain, p.Vp, dST, p.Tc, last ? fin : FinishJob{});
+      distill_ds_kernel<T><<<(unsigned)(last + n_ds + n_xt + (zero < 16384 ? zero : 16384)), 256, 0, s>>>(
+          DsJob{z, p.Vp, rows, q.ctrl, c0, p.V, p.inv_tau}, plain, p.Vp, dST, p.Tc,
+          XtJob{X, p.R, p.H, cols, n_ds, n_xt, reinterpret_cast<uintptr_t>(X) % 16 == 0, q.row_map, q.cpos, q.xt, out->d_hidden, p.Tc}, last ? fin : FinishJob{});
+      distill_patch_kernel<T><<<(unsigned)((n * h.K + 255) / 256), 256, 0, s>>>(p_ids, p_val, h.K, q.ctrl, c0, p.Tc, plain, p.Vp, dST, p.Tc);
     }
     contract_grads<T>(b, p, q, ch, out->d_hidden, dw, s, round ? static_cast<bf16_t*>(out->d_weight) : nullptr);
   }
