@@ -14,6 +14,7 @@
 // scaled), so that what carries the sum carries no error of the shift.
 #pragma once
 #include "../../include/rl_distill.h"
+#include "few_grads.h"
 
 namespace rlk {
 
@@ -773,6 +774,62 @@ __global__ __launch_bounds__(256) void distill_ds_kernel(DsJob j, T* dS, int64_t
   for (int64_t r = (int64_t)b * 4 + (threadIdx.x >> 6); r < x.R; r += step) zero_masked_row(r, x.cpos, static_cast<T*>(x.dX), x.R, x.H);
 }
 
+// The same for few rows (few_grads.h): `tokens` rows in two copies, those without a token 0; 64 vocabulary entries of a workgroup.
+template <class T>
+__global__ __launch_bounds__(256) void few_ds_kernel(DsJob j, int tokens, int pitch, T* ds1, T* ds2, XtJob x, FinishJob fin) {
+  constexpr int STEP = few_step<T>(), PER = 16 / sizeof(T);
+  __shared__ T tile[sizeof(T) == 2 ? kFewGradRows : kFewGradRowsF32][64 + 16 / sizeof(T) / 4];
+  int b = blockIdx.x;
+  if (fin.term) {
+    if (b == 0) { distill_finish(fin); return; }
+    --b;
+  }
+  if (b >= x.n_ds) {
+    const int64_t step = (int64_t)((int)gridDim.x - (fin.term ? 1 : 0) - x.n_ds) * 4;
+    for (int64_t r = (int64_t)(b - x.n_ds) * 4 + (threadIdx.x >> 6); r < x.R; r += step) zero_masked_row(r, x.cpos, static_cast<T*>(x.dX), x.R, x.H);
+    return;
+  }
+  const int left = j.ctrl->n_real, m = threadIdx.x & 63, v = b * 64 + m;
+  const float c = j.zs * kLog2e;
+  for (int t0 = threadIdx.x >> 6; t0 < pitch; t0 += 16) {              // (pitch is a multiple of 16; four loads in flight)
+    float z[4];
+    DistillRow d[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const int t = t0 + 4 * k;
+      z[k] = 0.f; d[k].f = 0.f;
+      if (t < left) { z[k] = j.z[tiled_index(t, v, j.ldz)]; d[k] = j.rows[t]; }
+    }
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const int t = t0 + 4 * k;
+      const T o = (T)(v < j.V ? ds_entry(z[k], d[k], c) : 0.f);
+      tile[t][m] = o;
+      if (t < tokens) ds1[((int64_t)(v / STEP) * tokens + t) * STEP + v % STEP] = o;
+    }
+  }
+  __syncthreads();
+  typedef T piece __attribute__((ext_vector_type(16 / sizeof(T))));
+  const int cols = pitch / PER;
+  for (int e = threadIdx.x; e < 64 * cols; e += 256) {
+    const int r = e / cols, t0 = e % cols * PER;
+    piece o;
+#pragma unroll
+    for (int i = 0; i < PER; ++i) o[i] = tile[t0 + i][r];
+    *reinterpret_cast<piece*>(ds2 + (int64_t)(b * 64 + r) * pitch + t0) = o;
+  }
+}
+template <class T>
+__global__ __launch_bounds__(256) void few_patch_kernel(const int* ids, const float* val, int K, const Ctrl* ctrl, int tokens, int pitch, T* ds1, T* ds2) {
+  constexpr int STEP = few_step<T>();
+  const int i = blockIdx.x * 256 + threadIdx.x;
+  if (i >= ctrl->n_real * K) return;
+  const int v = ids[i], t = i / K;
+  if (v < 0) return;
+  ds1[((int64_t)(v / STEP) * tokens + t) * STEP + v % STEP] = (T)val[i];
+  ds2[(int64_t)v * pitch + t] = (T)val[i];
+}
+
 // dS of the listed tokens over what the pass wrote there
 template <class T>
 __global__ __launch_bounds__(256) void distill_patch_kernel(const int* ids, const float* val, int K, const Ctrl* ctrl, int chunk_start, int chunk_rows, T* dS, int64_t ld_ds,
@@ -791,8 +848,26 @@ __global__ __launch_bounds__(256) void distill_patch_kernel(const int* ids, cons
 struct HeadPlan {
   Plan p;
   int K, groups;
-  size_t off_z, off_rec, off_stats, off_term, off_info, off_rows, off_pids, off_pval, off_dw, total;
+  int few_nt, few_splits, few_steps;        // few rows (few_grads.h): blocks of 16 tokens (0: not few), runs of the vocabulary, steps of a wavefront
+  size_t off_z, off_rec, off_stats, off_term, off_info, off_rows, off_pids, off_pval, off_dw, off_few, total;
 };
+
+static int few_cols(int dtype) { return dtype == RL_BF16 ? 128 : 64; }       // of a wavefront
+// Batches of so few rows that both gradients are one pass over the weight, and their launch: a wavefront on each SIMD (us with 768, 1024, 1536, 2048 wavefronts: 36 rows, H 5120,
+// V 50257 266 233 269 242; 3 rows, H 3584, V 126849 368 355 409 358; 61 rows, H 2048, V 32000 69 67 85 85).
+static void few_plan(HeadPlan& h) {
+  const Plan& p = h.p;
+  h.few_nt = 0;
+  if (p.R > (p.dtype == RL_BF16 ? kFewGradRows : kFewGradRowsF32)) return;
+  const int nt = p.R <= 16 ? 1 : p.R <= 32 ? 2 : 4;
+  const int cols = few_cols(p.dtype), step = p.dtype == RL_BF16 ? 32 : 16;
+  const int hs = (p.H + cols - 1) / cols, all = (p.V + step - 1) / step;
+  int splits = 4 * kHotSlots / hs;
+  splits = splits < 1 ? 1 : splits > kFewSplits ? kFewSplits : splits;
+  h.few_steps = (all + splits - 1) / splits;
+  h.few_splits = (all + h.few_steps - 1) / h.few_steps;
+  h.few_nt = nt;
+}
 
 static bool good_temperature(float t) { return t == 0.f || (t > 0.f && t <= 3.0e38f); }
 
@@ -817,13 +892,16 @@ static rl_status head_plan(const rl_batch* b, int K, int chunk_rows, float tempe
   const size_t tc = (size_t)p.Tc, R = (size_t)p.R;
   h.off_z = take(4 * tc * (size_t)p.Vp);
   h.off_rec = take(sizeof(float4) * tc * (size_t)h.groups);
-  h.off_stats = h.off_term = h.off_info = h.off_rows = h.off_pids = h.off_pval = h.off_dw = 0;
+  h.off_stats = h.off_term = h.off_info = h.off_rows = h.off_pids = h.off_pval = h.off_dw = h.off_few = 0;
+  h.few_nt = 0;
   if (distill) {
     h.off_stats = take(sizeof(rl_stats));
     h.off_term = take(8 * R); h.off_info = take(4 * R);
     if (bwd) {
       h.off_rows = take(sizeof(DistillRow) * tc);
       h.off_pids = take(4 * tc * (size_t)K); h.off_pval = take(4 * tc * (size_t)K);
+      few_plan(h);
+      if (h.few_nt) h.off_few = take(4 * (size_t)h.few_splits * (size_t)h.few_nt * 16 * (size_t)p.H);
       if (round_dw && p.n_chunks > 1) h.off_dw = take(4 * (size_t)p.V * (size_t)p.H);
     }
   }
@@ -868,6 +946,31 @@ static void score_chunk(const rl_batch* b, const HeadPlan& h, const Ptrs& q, int
 
 static int64_t chunk_bound(const Plan& p, int c0) { return p.R - c0 < p.Tc ? p.R - c0 : p.Tc; }      // rows of the chunk, at most
 
+template <class TO> static auto few_grads_kernel(int nt) { return nt == 1 ? few_grads_bf16_kernel<1, TO> : nt == 2 ? few_grads_bf16_kernel<2, TO> : few_grads_bf16_kernel<4, TO>; }
+// dS, then both gradients, of a batch of few rows; beside dS the loss and the rows of dX that do not count
+template <class T>
+static void run_few_grads(const rl_batch* b, const HeadPlan& h, const Ptrs& q, unsigned char* w, const DsJob& ds, const FinishJob& fin, const rl_distill_outputs* out, bool round, hipStream_t s) {
+  const Plan& p = h.p;
+  const int tokens = 16 * h.few_nt, pitch = few_pitch<T>(h.few_nt);
+  T* ds1 = static_cast<T*>(q.ds);
+  T* ds2 = sizeof(T) == 2 ? ds1 + (int64_t)kFewGradRows * p.Vp : static_cast<T*>(q.dst);          // (room for 256 rows)
+  float* part = (float*)(w + h.off_few);
+  const int n_ds = p.Vp / 64, zero = (int)((p.R + 3) / 4);
+  {
+    ProfScope ps(RL_PROF_GEMM_DS, s);
+    few_ds_kernel<T><<<1 + n_ds + zero, 256, 0, s>>>(ds, tokens, pitch, ds1, ds2, XtJob{nullptr, p.R, p.H, 0, n_ds, 0, 0, q.row_map, q.cpos, nullptr, out->d_hidden, p.Tc}, fin);
+    few_patch_kernel<T><<<(unsigned)((p.R * h.K + 255) / 256), 256, 0, s>>>((const int*)(w + h.off_pids), (const float*)(w + h.off_pval), h.K, q.ctrl, tokens, pitch, ds1, ds2);
+  }
+  ProfScope ps(RL_PROF_GEMM_BWD, s);
+  const FewGrads j{b->weight, b->hidden, p.V, p.H, q.row_map, &q.ctrl->n_real, ds1, ds2, out->d_weight, part, h.few_splits, h.few_steps};
+  const int cols = few_cols(p.dtype), hs = (p.H + cols - 1) / cols, waves = hs < 4 ? hs : 4, blocks = (hs + waves - 1) / waves * h.few_splits;
+  if constexpr (sizeof(T) == 2) {
+    auto kern = round ? few_grads_kernel<bf16_t>(h.few_nt) : few_grads_kernel<float>(h.few_nt);
+    kern<<<blocks, 64 * waves, 0, s>>>(j);
+  } else (h.few_nt == 1 ? few_grads_f32_kernel<1> : few_grads_f32_kernel<2>)<<<blocks, 64 * waves, 0, s>>>(j);
+  few_dx_kernel<T><<<(unsigned)(p.R * ((p.H + 63) / 64)), 256, 0, s>>>(part, h.few_splits, tokens, q.row_map, &q.ctrl->n_real, p.H, static_cast<T*>(out->d_hidden));
+}
+
 template <class T>
 static void run_distill(const rl_batch* b, const HeadPlan& h, const Ptrs& q, unsigned char* w, const int32_t* t_ids, const float* t_lp, const rl_distill_params* prm,
                         const rl_distill_outputs* out, bool bwd, hipStream_t s) {
@@ -883,7 +986,8 @@ static void run_distill(const rl_batch* b, const HeadPlan& h, const Ptrs& q, uns
   int* p_ids = (int*)(w + h.off_pids);
   float* p_val = (float*)(w + h.off_pval);
   const FinishJob fin{(const double*)(w + h.off_term), (const int*)(w + h.off_info), q.ctrl, (const rl_stats*)(w + h.off_stats), out->loss, out->stats};
-  if (bwd && !p.k_major_w) {
+  const bool few = bwd && h.few_nt && reinterpret_cast<uintptr_t>(W) % 16 == 0;
+  if (bwd && !few && !p.k_major_w) {
     ProfScope ps(RL_PROF_TRANSPOSE, s);
     launch_transpose<T>(dim3((p.Vp + 63) / 64, (p.H + 63) / 64), s, W, p.H, p.V, p.H, nullptr, q.ctrl, 0, 0, nullptr, nullptr, static_cast<T*>(q.wt), p.Vp, p.Vp, p.tiled);
   }
@@ -898,6 +1002,10 @@ static void run_distill(const rl_batch* b, const HeadPlan& h, const Ptrs& q, uns
                                      (double*)(w + h.off_term), (int*)(w + h.off_info), rows, p_ids, p_val}, n, s);
     }
     if (!bwd) continue;
+    if (few) {
+      run_few_grads<T>(b, h, q, w, DsJob{z, p.Vp, rows, q.ctrl, c0, p.V, p.inv_tau}, fin, out, round, s);
+      continue;
+    }
     {
       ProfScope ps(RL_PROF_GEMM_DS, s);
       const int tile = sizeof(T) == 2 ? 256 : 64, cols = (int)((n + 255) / 256 * 4);

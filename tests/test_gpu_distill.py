@@ -150,3 +150,18 @@ def test_distill(R, H, V, dtype, K, chunk, rest, tau, aggregation):
     ids, lp = b.teacher(K)
     r = b.distill(ids, lp, rest=rest, temperature=tau, aggregation=aggregation, chunk_rows=chunk, d_weight_dtype=DTYPES[dtype])
     check_distill(b, r, ids, lp, rest, tau, aggregation)
+
+
+# few rows, whose gradients are one pass over the weight: every number of token blocks, columns inside a wavefront's, at its border and past it, vocabularies inside a step, past the
+# last whole one, in one run and in many; a weight off the 16-byte grid takes the other route
+@pytest.mark.parametrize("R,H,V,dtype", [(1, 8, 33, "bf16"), (16, 128, 64, "bf16"), (17, 136, 1000, "bf16"), (32, 264, 4001, "bf16"), (33, 120, 300, "bf16"), (64, 1160, 9000, "bf16"),
+                                         (65, 64, 700, "bf16"), (100, 200, 5001, "bf16"), (128, 1032, 3000, "bf16"), (3, 4, 17, "f32"), (16, 64, 48, "f32"), (17, 68, 1001, "f32"),
+                                         (32, 516, 9003, "f32"), (33, 60, 500, "f32")])
+@pytest.mark.parametrize("dw,off", [("own", 0), ("f32", 0), ("own", 1)])
+def test_few_rows(R, H, V, dtype, dw, off):
+    b = Batch(R, H, V, dtype, seed=R + H)
+    ids, lp = b.teacher(7)
+    if off:
+        b.weight, b.hidden = off_grid(b.weight, off), off_grid(b.hidden, off)
+    r = b.distill(ids, lp, aggregation="token", d_weight_dtype=DTYPES[dtype] if dw == "own" else torch.float32)
+    check_distill(b, r, ids, lp, "bucket", 1.0, "token")
