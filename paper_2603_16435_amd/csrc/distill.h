@@ -177,6 +177,115 @@ void score_few_kernel(const bf16_t* __restrict__ W, const bf16_t* __restrict__ X
   logits_few_tile<BN, NT>(W, X, d, epi, blockIdx.x, left < d.N ? left : d.N, d.b_rows, ids_c, smem);
 }
 
+// f32 logits of a few tokens, up to 64.  Bound by reading the weight once, which the tiles of gemm_f32.h, 64 tokens wide, and the narrow ones, which leave most CUs without work where the
+// vocabulary is small, are far from (us, TB/s of W: 4 tokens, H 2048, V 152064 366, 3.4; 2 tokens, H 5120, V 32000 216, 3.0; 3 tokens, V 5726 169, 0.7).  A workgroup takes a group of
+// 64 vocabulary entries; KS sets of four wavefronts share K, each wavefront 16 entries.  Slabs of 32 k go straight into LDS, as whole lines (loaded into the operands' registers, 64 bytes of a row by
+// four lanes, L1 bounds it: 325 us for the first of the three), two ahead of the one computed on; five workgroups fit a CU.  v_mfma_f32_16x16x4, lane group g with k = 16 s + 4 g + e of a slab in its
+// k-step (s, e).  What the sets found is added in order in LDS, and the record made there.  (The order of a logit's sum is not that of the other f32 kernels: scored with more than 64
+// rows, a token's last bit may be another.)
+constexpr int kFewF32Stages = 3;
+template <int NT, int KS> constexpr int few_f32_lds_bytes() {
+  constexpr int stages = KS * kFewF32Stages * (kGroup + 16 * NT) * kSlabBytes, part = KS * kGroup * (16 * NT + 1) * 4;
+  return stages > part ? stages : part;
+}
+template <int NT, int KS, bool STREAM>
+__global__ __launch_bounds__(256 * KS) void score_few_f32_kernel(const float* __restrict__ W, const float* __restrict__ X, GemmDims d, EpiScore<float> epi) {
+  constexpr int T = 16 * NT, P = T + 1, BK = 32, STAGES = kFewF32Stages, A_BYTES = kGroup * kSlabBytes, STAGE = A_BYTES + T * kSlabBytes, XL = NT < 2 ? 1 : NT / 2, LOADS = 2 + XL;
+  __shared__ __attribute__((aligned(1024))) unsigned char smem[few_f32_lds_bytes<NT, KS>()];
+  float (*part)[kGroup][P] = reinterpret_cast<float (*)[kGroup][P]>(smem);       // (when the slabs are done with)
+  const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = w & 3, set = w >> 2;
+  const int rows = *d.n_real, K = d.K, v0 = (int)blockIdx.x * kGroup;
+  if (rows <= 0) return;
+  unsigned char* mine = smem + set * STAGES * STAGE;
+  // loads of a slab, eight rows each: sixteen rows of W by a wavefront, a quarter of X's (of 16: by wavefronts 0 and 2, 1 and 3 alike)
+  const float* src[LOADS];
+  int chunk[LOADS], at[LOADS];
+#pragma unroll
+  for (int j = 0; j < LOADS; ++j) {
+    const int to = j < 2 ? r * 16 + j * 8 : (NT == 1 ? r & 1 : r * XL + j - 2) * 8, lr = to + (lane >> 3);
+    chunk[j] = (lane & 7) ^ ((lr >> 1) & 7);
+    const float* row;
+    if (j < 2) row = W + (int64_t)(v0 + lr < d.M ? v0 + lr : d.M - 1) * d.lda;
+    else row = X + (int64_t)d.b_rows[lr < rows ? lr : rows - 1] * d.ldb;
+    src[j] = row + chunk[j] * 4;
+    at[j] = (j < 2 ? 0 : A_BYTES) + to * kSlabBytes;
+  }
+  const int steps = (K + BK - 1) / BK, per = (steps + KS - 1) / KS, first = set * per, last = first + per < steps ? first + per : steps;
+  auto issue = [&](int i) __attribute__((always_inline)) {               // the i-th slab of the set
+    const int k = (first + i < steps ? first + i : steps - 1) * BK;       // past the end: a harmless re-load keeps the count of loads
+    unsigned char* stage = mine + i % STAGES * STAGE;
+#pragma unroll
+    for (int j = 0; j < LOADS; ++j) {
+      const void* p = k + chunk[j] * 4 < K ? (const void*)(src[j] + k) : (const void*)&kZeroChunk;       // (K % 4 == 0)
+      const unsigned to = (unsigned)(size_t)(lds_ptr_t)(stage + at[j]);
+      if (STREAM && j < 2) asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off nt" :: "v"(p), "s"(to) : "memory");
+      else load16_to_lds_lanes(p, stage + at[j]);
+    }
+  };
+  floatx4 acc[NT];
+#pragma unroll
+  for (int b = 0; b < NT; ++b) acc[b] = floatx4{0.f, 0.f, 0.f, 0.f};
+  const int frow = lane & 15, fq = lane >> 4, swz = (frow >> 1) & 7;
+  __builtin_amdgcn_s_waitcnt(0x0F70);       // vmcnt(0): what was fetched above is not among the loads counted below
+#pragma unroll
+  for (int i = 0; i < STAGES - 1; ++i) issue(i);
+  constexpr int PEND = (STAGES - 2) * LOADS;
+  for (int i = 0; i < per; ++i) {
+    __builtin_amdgcn_s_waitcnt(0x0070 | (PEND & 15) | (PEND >> 4) << 14);       // all but the slab behind this one; lgkmcnt(0)
+    __syncthreads();                        // ... in every wavefront, and the stage filled next has been read
+    issue(i + STAGES - 1);
+    const unsigned char* stage = mine + i % STAGES * STAGE;
+    if (first + i < last) {
+#pragma unroll
+      for (int s = 0; s < 2; ++s) {
+        const int slot = ((s * 4 + fq) ^ swz) << 4;
+        const floatx4 a = *reinterpret_cast<const floatx4*>(stage + (r * 16 + frow) * kSlabBytes + slot);
+        floatx4 x[NT];
+#pragma unroll
+        for (int b = 0; b < NT; ++b) x[b] = *reinterpret_cast<const floatx4*>(stage + A_BYTES + (b * 16 + frow) * kSlabBytes + slot);
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+#pragma unroll
+          for (int b = 0; b < NT; ++b) acc[b] = __builtin_amdgcn_mfma_f32_16x16x4f32(a[e], x[b][e], acc[b], 0, 0, 0);
+      }
+    }
+  }
+  __builtin_amdgcn_s_waitcnt(0x0070);       // no load into LDS may be in flight when it gets another use
+  __syncthreads();
+#pragma unroll
+  for (int b = 0; b < NT; ++b)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) part[set][r * 16 + fq * 4 + i][b * 16 + frow] = acc[b][i];
+  __syncthreads();
+  // logits to memory, a token's 64 in a row; the sums stay in the first set's place
+  for (int e = threadIdx.x; e < kGroup * T; e += 256 * KS) {
+    const int t = e / kGroup, i = e % kGroup;
+    float z = part[0][i][t];
+#pragma unroll
+    for (int k = 1; k < KS; ++k) z += part[k][i][t];
+    part[0][i][t] = z;
+    if (t < rows) epi.z[tiled_index(t, v0 + i, epi.ldz)] = z;
+  }
+  __syncthreads();
+  // record: four lanes of a token, sixteen entries each
+  const int t = (int)threadIdx.x >> 2, q = threadIdx.x & 3, vleft = epi.V - v0;
+  if (t >= rows || t >= T) return;
+  const float NEG = -__builtin_inff(), c = epi.zs * kLog2e;
+  float z[16], mx = NEG, s = 0.f, u = 0.f;
+#pragma unroll
+  for (int i = 0; i < 16; ++i) { z[i] = part[0][q * 16 + i][t]; mx = fmaxf(mx, q * 16 + i < vleft ? z[i] : NEG); }
+  mx = fmaxf(mx, __shfl_xor(mx, 1)); mx = fmaxf(mx, __shfl_xor(mx, 2));
+  const float ms = mx == NEG ? 0.f : mx;
+#pragma unroll
+  for (int i = 0; i < 16; ++i) {
+    const float dd = z[i] - ms, e = __builtin_amdgcn_exp2f(dd * c);
+    if (q * 16 + i < vleft) { s += e; u = __builtin_fmaf(e, dd, u); }
+  }
+  s += __shfl_xor(s, 1); s += __shfl_xor(s, 2);
+  u += __shfl_xor(u, 1); u += __shfl_xor(u, 2);
+  if (q == 0) epi.rec[rec_index((int)blockIdx.x, t, epi.ldr)] = make_float4(mx, s, u, 0.f);
+}
+
 // ------------------------------------------------------------------ a row, by a workgroup
 __device__ inline float wave_max(float v) { for (int o = 32; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor(v, o)); return v; }
 
@@ -925,6 +1034,14 @@ static void head_prep(const rl_batch* b, const Plan& p, const Ptrs& q, const rl_
   if (job.on) prep_small_kernel<<<1, 1024, 0, s>>>(job.s, job.f, job.adv);        // (no launch of these logits prepares)
 }
 
+constexpr int kFewScoreF32 = 64;
+// Sets of wavefronts of score_few_f32_kernel that share K, where the groups alone do not fill the chip.  us with 1, 2, 4 sets: 3 tokens, H 5120, V 5726 (90 groups) 62 47 44, V 32000 (500) 111 99 104;
+// 30 tokens, H 768, V 50257 (786) 45 47 56; 2 tokens, H 216, V 152064 34 41 56; 7 tokens, H 768, V 5462 13.9 12.7 11.7.
+static int few_f32_sets(int blocks, int H) { return blocks >= 640 || H < 256 ? 1 : blocks >= 256 || H < 512 ? 2 : 4; }
+template <int NT> static auto few_f32_kernel(int ks, bool stream) {
+  return stream ? (ks == 1 ? score_few_f32_kernel<NT, 1, true> : ks == 2 ? score_few_f32_kernel<NT, 2, true> : score_few_f32_kernel<NT, 4, true>)
+                : (ks == 1 ? score_few_f32_kernel<NT, 1, false> : ks == 2 ? score_few_f32_kernel<NT, 2, false> : score_few_f32_kernel<NT, 4, false>);
+}
 template <class T>
 static void score_chunk(const rl_batch* b, const HeadPlan& h, const Ptrs& q, int c0, float* z, float4* rec, hipStream_t s) {
   const Plan& p = h.p;
@@ -935,12 +1052,24 @@ static void score_chunk(const rl_batch* b, const HeadPlan& h, const Ptrs& q, int
   d.b_rows = q.row_map + c0; d.b_span = p.R; d.n_real = &q.ctrl->n_real; d.chunk_start = c0; d.dyn = 2; d.group_m = TuneLogits::kBand;
   const EpiScore<T> e{z, p.Vp, rec, p.Tc, p.V, p.inv_tau};
   ProfScope ps(RL_PROF_GEMM_FWD, s);
-  if constexpr (sizeof(T) == 2)
-    if (few_tokens(b, p)) {
-      auto kern = few_streams_w(b, p) ? (p.R <= 64 ? score_few_kernel<64, true> : score_few_kernel<128, true>) : (p.R <= 64 ? score_few_kernel<64, false> : score_few_kernel<128, false>);
-      kern<<<2 * p.tiles_v, 256, 0, s>>>(W, X, d, e, q.ids_c);
+  if ((reinterpret_cast<uintptr_t>(W) | reinterpret_cast<uintptr_t>(X)) % 16 == 0) {
+    const bool stream = (int64_t)p.V * p.H * sizeof(T) > (int64_t)256 << 20;                  // (more than the memory-side cache holds, see few_streams_w)
+    if constexpr (sizeof(T) == 2) {
+      // up to 64 tokens always, up to 128 where the hot kernel's tiles fill the chip worse (few_tokens).  us of the hot kernel and here: 3 tokens, H 3584, V 126849 227 and 177, 40 tokens 215
+      // and 165, 100 tokens 216 and 217; 3 tokens, H 5120, V 50257 137 and 106; 60, H 2048, V 100000 130 and 119; 1, H 1024, V 60000 38 and 30.  (Same bits.)
+      if (p.R <= 64 || (p.R <= kFewTokens && (p.tiles_v + 127) / 128 % 2)) {
+        const bool nt = stream && p.H % 64 == 0 && reinterpret_cast<uintptr_t>(W) % 128 == 0;
+        auto kern = nt ? (p.R <= 64 ? score_few_kernel<64, true> : score_few_kernel<128, true>) : (p.R <= 64 ? score_few_kernel<64, false> : score_few_kernel<128, false>);
+        kern<<<2 * p.tiles_v, 256, 0, s>>>(W, X, d, e, q.ids_c);
+        return;
+      }
+    } else if (p.R <= kFewScoreF32) {
+      const int blocks = p.Vp / kGroup, sets = few_f32_sets(blocks, p.H), ks = p.R > 32 && sets > 2 ? 2 : sets;        // (LDS holds two sets of 64 tokens)
+      auto kern = p.R <= 16 ? few_f32_kernel<1>(ks, stream) : p.R <= 32 ? few_f32_kernel<2>(ks, stream) : ks == 1 ? (stream ? score_few_f32_kernel<4, 1, true> : score_few_f32_kernel<4, 1, false>) : (stream ? score_few_f32_kernel<4, 2, true> : score_few_f32_kernel<4, 2, false>);
+      kern<<<blocks, 256 * ks, 0, s>>>(W, X, d, e);
       return;
     }
+  }
   launch_gemm<TuneLogits>(W, X, d, e, s);
 }
 

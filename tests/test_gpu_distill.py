@@ -115,7 +115,8 @@ def check_distill(b, r, ids, lp, rest, tau, aggregation, scale=1.0):
 # bf16: few tokens (64, 128), the hot kernel (H on the grid of 128, off it), whole and partial tiles, one group, several chunks; f32: narrow tiles, 256 x 64, a K tail
 SCORE = [(1, 64, 300, "bf16", 1, 0), (1, 512, 20000, "bf16", 20, 0), (63, 128, 129, "bf16", 128, 0), (65, 136, 5000, "bf16", 7, 0), (128, 456, 65537, "bf16", 5, 0),
          (129, 128, 1000, "bf16", 128, 0), (300, 256, 50257, "bf16", 33, 0), (700, 264, 4097, "bf16", 64, 256), (530, 128, 64, "bf16", 64, 512),
-         (1, 4, 5, "f32", 5, 0), (40, 68, 777, "f32", 9, 0), (300, 128, 8200, "f32", 128, 256), (1100, 100, 20011, "f32", 11, 0), (2, 64, 130000, "f32", 100, 0)]
+         (1, 4, 5, "f32", 5, 0), (16, 36, 64, "f32", 9, 0), (17, 260, 20000, "f32", 3, 0), (33, 516, 3000, "f32", 20, 0), (64, 520, 41000, "f32", 2, 0), (31, 1028, 2000, "f32", 33, 0),
+         (65, 68, 777, "f32", 9, 0), (300, 128, 8200, "f32", 128, 256), (1100, 100, 20011, "f32", 11, 0), (2, 64, 130000, "f32", 100, 0)]
 
 
 @pytest.mark.parametrize("R,H,V,dtype,K,chunk", SCORE)
