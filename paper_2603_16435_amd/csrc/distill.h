@@ -39,6 +39,7 @@ struct EpiScore {
   static constexpr bool kSwap = false;
   static constexpr bool kSplit = false;
   static constexpr bool kPermute = true;
+  static constexpr bool kNaturalB = true;
   static constexpr bool kGatherB = true;
   __device__ void keep_alive() const { z[0] = 0.f; }
   float* z; int64_t ldz;      // logits, slab-tiled like the bf16 work buffers: a tile of 256 x 256 is one piece of memory
@@ -71,11 +72,13 @@ struct EpiScore {
     return make_float4(mx, s, u, 0.f);
   }
 
-  // MB = 8 block rows (128 permuted rows) of NB columns; COL: token of column bj
-  template <int MB, int NB, bool AGPR, class COL>
-  __device__ __attribute__((always_inline)) void permuted(floatx4 (&acc)[MB][NB], const TileCtx& c, COL col) const {
+  // MB = 8 block rows (128 permuted rows) of NB columns.  A lane has eight consecutive entries of its token, two quads; lanes eight apart exchange one each, so that a store writes whole lines
+  // of 128 bytes, those of eight neighbouring tokens.  (Tokens eight and more apart, as with permuted columns, lie 2 KiB and more apart and meet the same memory channels:
+  // 16 k rows at the 7B head 13.33 ms.)
+  template <int MB, int NB, bool AGPR>
+  __device__ __attribute__((always_inline)) void permuted(floatx4 (&acc)[MB][NB], const TileCtx& c) const {
     static_assert(MB == 8, "128 rows");
-    const int g = c.lane >> 4, p = c.lane & 1;
+    const int g = c.lane >> 4, p = (c.lane >> 3) & 1;
     const int vleft = V - c.m0;
 #pragma unroll
     for (int j = 0; j < 2; ++j)
@@ -84,22 +87,21 @@ struct EpiScore {
         float v[16];
 #pragma unroll
         for (int r = 0; r < 16; ++r) v[r] = acc_read<AGPR>(acc[4 * j + (r >> 2)][bj], r & 3);
-        const int n = col(bj, c.lane);
+        const int n = c.n0 + bj * 16 + (c.lane & 15), lo = n - 8 * p, hi = lo + 8;
         const float4 q = vleft < j * 64 + 64 ? group16<true>(v, g, vleft - j * 64) : group16<false>(v, g, 64);
         if (g == (NB >= 4 ? bj / (NB / 4) : bj) && n < c.Nv) rec[rec_index(c.m0 / kGroup + j, n, ldr)] = q;
-        // lane pairs swap quads, so that a store writes whole lines of 128 bytes
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-          floatx4 even, odd;
+          floatx4 a, b;                                             // the lower lane's token, the upper lane's
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
-            const float lo = v[h * 8 + e], hi = v[h * 8 + 4 + e];
-            const float got = __uint_as_float((unsigned)__builtin_amdgcn_mov_dpp((int)__float_as_uint(p ? lo : hi), 0xB1, 0xF, 0xF, true));
-            even[e] = p ? got : lo; odd[e] = p ? hi : got;
+            const int x = (int)__float_as_uint(v[h * 8 + e]), y = (int)__float_as_uint(v[h * 8 + 4 + e]);
+            a[e] = __uint_as_float((unsigned)__builtin_amdgcn_update_dpp(x, y, 0x128, 0xF, 0xC, false));       // upper lanes: the lower's second quad
+            b[e] = __uint_as_float((unsigned)__builtin_amdgcn_update_dpp(y, x, 0x128, 0xF, 0x3, false));       // lower lanes: the upper's first
           }
-          const int ne = col(bj, c.lane & ~1), no = col(bj, c.lane | 1), at = c.m0 + j * 64 + h * 32 + g * 8 + p * 4;
-          if (ne < c.Nv) __builtin_nontemporal_store(even, reinterpret_cast<floatx4*>(z + tiled_index(ne, at, ldz)));
-          if (no < c.Nv) __builtin_nontemporal_store(odd, reinterpret_cast<floatx4*>(z + tiled_index(no, at, ldz)));
+          const int at = c.m0 + j * 64 + h * 32 + g * 8 + p * 4;
+          if (lo < c.Nv) __builtin_nontemporal_store(a, reinterpret_cast<floatx4*>(z + tiled_index(lo, at, ldz)));
+          if (hi < c.Nv) __builtin_nontemporal_store(b, reinterpret_cast<floatx4*>(z + tiled_index(hi, at, ldz)));
         }
       }
   }
@@ -160,11 +162,11 @@ struct EpiScore {
 
   template <class L, int MB, int NB>
   __device__ __attribute__((always_inline)) void half_tile(typename L::acc_t (&acc)[MB][NB], const TileCtx& c, const int (&)[NB]) const {
-    permuted<MB, NB, false>(acc, c, [&](int bj, int lane) { return c.n0 + L::col(bj, lane); });
+    permuted<MB, NB, false>(acc, c);
   }
   template <class L, int MB, int NB, int BM, int BN, int WAVES_M, int WAVES_N, bool AGPR>
   __device__ __attribute__((always_inline)) void run(typename L::acc_t (&acc)[MB][NB], const TileCtx& c, unsigned char*, const GemmDims&, const Pre&) const {
-    if constexpr (AGPR) permuted<MB, NB, true>(acc, c, [&](int bj, int lane) { return c.n0 + perm_col(bj, lane & 15); });
+    if constexpr (AGPR) permuted<MB, NB, true>(acc, c);
     else natural<L, MB, NB>(acc, c);
   }
 };

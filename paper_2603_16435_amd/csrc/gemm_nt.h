@@ -509,6 +509,9 @@ template <class P> __device__ inline P* uniform_ptr(P* p) {
 // Inside each 128-row half of the tile, LDS row 16*b + 4*g + e (block b, lane group g, register e)
 // holds matrix row 32*(b/2) + 8*g + 4*(b%2) + e, and LDS column-row 16*b + c holds matrix column
 // 8*c + b: a lane (g, c) then owns runs of eight consecutive rows and of eight consecutive columns.
+// (kNaturalB: its rows only, the columns stay as they are.)
+template <class Epi, class = void> struct PermuteB { static constexpr bool value = Epi::kPermute; };
+template <class Epi> struct PermuteB<Epi, decltype((void)Epi::kNaturalB)> { static constexpr bool value = false; };
 __device__ inline int perm_row(int b, int g, int e) { return ((b >> 1) << 5) + (g << 3) + ((b & 1) << 2) + e; }
 __device__ inline int perm_col(int b, int c) { return (c << 3) + b; }
 __device__ inline int perm_lds_row_a(int lr) { return (lr & 128) + perm_row((lr >> 4) & 7, (lr >> 2) & 3, lr & 3); }
@@ -630,7 +633,7 @@ __device__ __attribute__((always_inline)) inline void gemm_nt_bf16_tile(const bf
   pf_row = pf_row < N ? pf_row : N - 1;
 #pragma unroll
   for (int j = 0; j < 8; ++j) {
-    const int lr = wave * 64 + j * 8 + (lane >> 3), r = tn * BN + (Epi::kPermute ? perm_lds_row_b(lr) : lr);
+    const int lr = wave * 64 + j * 8 + (lane >> 3), r = tn * BN + (PermuteB<Epi>::value ? perm_lds_row_b(lr) : lr);
     brow_of[j] = r < N ? r : N - 1;
     if constexpr (GB) brow_of[j] = d.b_rows[brow_of[j]];
   }

@@ -1,6 +1,6 @@
-"""The block in front of the LM head, trained together with it: final layer norm, a projection on 8-bit operands, then the policy loss.
+"""The block in front of the LM head, trained together with it: final layer norm, a projection on 8-bit operands, then the policy loss, or a loss of distillation.
 
-    y = layer_norm(x) gamma + beta,   hidden = pack(y) W^T,   loss = policy loss of (hidden, LM head)
+    y = layer_norm(x) gamma + beta,   hidden = pack(y) W^T,   loss = policy loss of (hidden, LM head), or its divergence from a teacher's lists
 
 What the forward pass keeps for the backward pass is in 8 bits: x for the norm, y for the weight gradient (a byte and 1/128 a value each instead of two or
 four), so that x may be overwritten.  Every step runs in the HIP library; this module only holds the pieces together."""
@@ -30,7 +30,7 @@ class HeadGrads:
     dgamma: torch.Tensor                     # float32, as the two below
     dbeta: torch.Tensor
     dweight: torch.Tensor                    # [N, H]
-    dlm_head: torch.Tensor                   # [V, N]
+    dlm_head: torch.Tensor                   # [V, N] (distill_step: in the type that its options name)
 
 
 class HeadBlock:
@@ -66,5 +66,16 @@ class HeadBlock:
         """One pass over a batch of rollouts whose last block left x [R, H]: (LossResult, HeadGrads).  options: those of rl_policy_loss_fwd_bwd."""
         hidden, kept = self.forward(x, overwrite)
         res = binding.rl_policy_loss_fwd_bwd(objective, hidden, self.lm_head, token_ids, mask, cu_seqlens, group_idx, rewards, old_logprob, ref_logprob, log_z, P, **options)
+        dx, dgamma, dbeta, dweight = self.backward(res.d_hidden, kept)
+        return res, HeadGrads(dx, dgamma, dbeta, dweight, res.d_weight)
+
+    def top_logprobs(self, x, token_ids, mask, top_k, **options):
+        """TopLogprobs of x [R, H] under this model: what its lists are for a student.  options: those of rl_token_top_logprobs."""
+        return binding.rl_token_top_logprobs(self.hidden(x), self.lm_head, token_ids, mask, top_k, **options)
+
+    def distill_step(self, x, teacher_ids, teacher_logprob, mask, cu_seqlens=None, overwrite=False, **options):
+        """One pass over a batch that a teacher has scored: (DistillResult, HeadGrads).  options: those of rl_distill_loss_fwd_bwd."""
+        hidden, kept = self.forward(x, overwrite)
+        res = binding.rl_distill_loss_fwd_bwd(hidden, self.lm_head, teacher_ids, teacher_logprob, mask, cu_seqlens, d_hidden=hidden, **options)
         dx, dgamma, dbeta, dweight = self.backward(res.d_hidden, kept)
         return res, HeadGrads(dx, dgamma, dbeta, dweight, res.d_weight)
