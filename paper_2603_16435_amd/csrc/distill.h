@@ -171,12 +171,20 @@ struct EpiScore {
   }
 };
 
-template <int BN, bool NT>
+// PREP: with the preparation, by workgroup 0; the others work out which rows count for themselves (local_rows).
+template <int BN, bool NT, bool PREP>
 __global__ __launch_bounds__(256, 1)
-void score_few_kernel(const bf16_t* __restrict__ W, const bf16_t* __restrict__ X, GemmDims d, EpiScore<bf16_t> epi, const int* ids_c) {
+void score_few_kernel(const bf16_t* __restrict__ W, const bf16_t* __restrict__ X, GemmDims d, EpiScore<bf16_t> epi, const int* ids_c, SmallPrep s, RowFill f) {
   __shared__ __attribute__((aligned(1024))) unsigned char smem[few_lds_bytes<BN>()];
-  const int left = *d.n_real;
-  logits_few_tile<BN, NT>(W, X, d, epi, blockIdx.x, left < d.N ? left : d.N, d.b_rows, ids_c, smem);
+  if constexpr (PREP) {
+    if (blockIdx.x == 0) { prep_small<256, kFewTokens>(s, f, AdvJob{}); return; }
+    __shared__ LocalRows<kFewTokens> l;
+    local_rows<256>(s, l);
+    logits_few_tile<BN, NT>(W, X, d, epi, (int)blockIdx.x - 1, l.n, l.rows, l.ids, smem);
+  } else {
+    const int left = *d.n_real;
+    logits_few_tile<BN, NT>(W, X, d, epi, blockIdx.x, left < d.N ? left : d.N, d.b_rows, ids_c, smem);
+  }
 }
 
 // f32 logits of a few tokens, up to 64.  Bound by reading the weight once, which the tiles of gemm_f32.h, 64 tokens wide, and the narrow ones, which leave most CUs without work where the
@@ -190,13 +198,21 @@ template <int NT, int KS> constexpr int few_f32_lds_bytes() {
   constexpr int stages = KS * kFewF32Stages * (kGroup + 16 * NT) * kSlabBytes, part = KS * kGroup * (16 * NT + 1) * 4;
   return stages > part ? stages : part;
 }
-template <int NT, int KS, bool STREAM>
-__global__ __launch_bounds__(256 * KS) void score_few_f32_kernel(const float* __restrict__ W, const float* __restrict__ X, GemmDims d, EpiScore<float> epi) {
+template <int NT, int KS, bool STREAM, bool PREP>
+__global__ __launch_bounds__(256 * KS) void score_few_f32_kernel(const float* __restrict__ W, const float* __restrict__ X, GemmDims d, EpiScore<float> epi, SmallPrep sp, RowFill f) {
   constexpr int T = 16 * NT, P = T + 1, BK = 32, STAGES = kFewF32Stages, A_BYTES = kGroup * kSlabBytes, STAGE = A_BYTES + T * kSlabBytes, XL = NT < 2 ? 1 : NT / 2, LOADS = 2 + XL;
   __shared__ __attribute__((aligned(1024))) unsigned char smem[few_f32_lds_bytes<NT, KS>()];
   float (*part)[kGroup][P] = reinterpret_cast<float (*)[kGroup][P]>(smem);       // (when the slabs are done with)
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = w & 3, set = w >> 2;
-  const int rows = *d.n_real, K = d.K, v0 = (int)blockIdx.x * kGroup;
+  int rows, group = blockIdx.x;
+  if constexpr (PREP) {
+    if (blockIdx.x == 0) { prep_small<256 * KS, kFewTokens>(sp, f, AdvJob{}); return; }
+    __shared__ LocalRows<kFewTokens> l;
+    local_rows<256 * KS>(sp, l);
+    rows = l.n; --group;
+    d.b_rows = l.rows;
+  } else rows = *d.n_real;
+  const int K = d.K, v0 = group * kGroup;
   if (rows <= 0) return;
   unsigned char* mine = smem + set * STAGES * STAGE;
   // loads of a slab, eight rows each: sixteen rows of W by a wavefront, a quarter of X's (of 16: by wavefronts 0 and 2, 1 and 3 alike)
@@ -285,7 +301,7 @@ __global__ __launch_bounds__(256 * KS) void score_few_f32_kernel(const float* __
   }
   s += __shfl_xor(s, 1); s += __shfl_xor(s, 2);
   u += __shfl_xor(u, 1); u += __shfl_xor(u, 2);
-  if (q == 0) epi.rec[rec_index((int)blockIdx.x, t, epi.ldr)] = make_float4(mx, s, u, 0.f);
+  if (q == 0) epi.rec[rec_index(group, t, epi.ldr)] = make_float4(mx, s, u, 0.f);
 }
 
 // ------------------------------------------------------------------ a row, by a workgroup
@@ -885,9 +901,9 @@ __global__ __launch_bounds__(256) void distill_ds_kernel(DsJob j, T* dS, int64_t
   for (int64_t r = (int64_t)b * 4 + (threadIdx.x >> 6); r < x.R; r += step) zero_masked_row(r, x.cpos, static_cast<T*>(x.dX), x.R, x.H);
 }
 
-// The same for few rows (few_grads.h): `tokens` rows in two copies, those without a token 0; 64 vocabulary entries of a workgroup.
+// The same for few rows (few_grads.h): `tokens` rows in two copies, those without a token 0; 64 vocabulary entries of a workgroup, which looks through the rows' lists for them itself (p_ids, p_val, K).
 template <class T>
-__global__ __launch_bounds__(256) void few_ds_kernel(DsJob j, int tokens, int pitch, T* ds1, T* ds2, XtJob x, FinishJob fin) {
+__global__ __launch_bounds__(256) void few_ds_kernel(DsJob j, const int* p_ids, const float* p_val, int K, int tokens, int pitch, T* ds1, T* ds2, XtJob x, FinishJob fin) {
   constexpr int STEP = few_step<T>(), PER = 16 / sizeof(T);
   __shared__ T tile[sizeof(T) == 2 ? kFewGradRows : kFewGradRowsF32][64 + 16 / sizeof(T) / 4];
   int b = blockIdx.x;
@@ -912,12 +928,16 @@ __global__ __launch_bounds__(256) void few_ds_kernel(DsJob j, int tokens, int pi
       if (t < left) { z[k] = j.z[tiled_index(t, v, j.ldz)]; d[k] = j.rows[t]; }
     }
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
-      const int t = t0 + 4 * k;
-      const T o = (T)(v < j.V ? ds_entry(z[k], d[k], c) : 0.f);
-      tile[t][m] = o;
-      if (t < tokens) ds1[((int64_t)(v / STEP) * tokens + t) * STEP + v % STEP] = o;
-    }
+    for (int k = 0; k < 4; ++k) tile[t0 + 4 * k][m] = (T)(v < j.V ? ds_entry(z[k], d[k], c) : 0.f);
+  }
+  __syncthreads();
+  const int n = (left < tokens ? left : tokens) * K;
+  for (int i0 = threadIdx.x; i0 < n; i0 += 8 * 256) {
+    int id[8];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) id[k] = i0 + 256 * k < n ? p_ids[i0 + 256 * k] : -1;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) if (id[k] >= 0 && id[k] >> 6 == b) tile[(i0 + 256 * k) / K][id[k] & 63] = (T)p_val[i0 + 256 * k];
   }
   __syncthreads();
   typedef T piece __attribute__((ext_vector_type(16 / sizeof(T))));
@@ -929,16 +949,13 @@ __global__ __launch_bounds__(256) void few_ds_kernel(DsJob j, int tokens, int pi
     for (int i = 0; i < PER; ++i) o[i] = tile[t0 + i][r];
     *reinterpret_cast<piece*>(ds2 + (int64_t)(b * 64 + r) * pitch + t0) = o;
   }
-}
-template <class T>
-__global__ __launch_bounds__(256) void few_patch_kernel(const int* ids, const float* val, int K, const Ctrl* ctrl, int tokens, int pitch, T* ds1, T* ds2) {
-  constexpr int STEP = few_step<T>();
-  const int i = blockIdx.x * 256 + threadIdx.x;
-  if (i >= ctrl->n_real * K) return;
-  const int v = ids[i], t = i / K;
-  if (v < 0) return;
-  ds1[((int64_t)(v / STEP) * tokens + t) * STEP + v % STEP] = (T)val[i];
-  ds2[(int64_t)v * pitch + t] = (T)val[i];
+  for (int e = threadIdx.x; e < tokens * (64 / PER); e += 256) {         // pieces of 64 bytes a token and step
+    const int t = e / (64 / PER), m0 = e % (64 / PER) * PER, v0 = b * 64 + m0;
+    piece o;
+#pragma unroll
+    for (int i = 0; i < PER; ++i) o[i] = tile[t][m0 + i];
+    *reinterpret_cast<piece*>(ds1 + ((int64_t)(v0 / STEP) * tokens + t) * STEP + v0 % STEP) = o;
+  }
 }
 
 // dS of the listed tokens over what the pass wrote there
@@ -1030,22 +1047,35 @@ static bool overlap(const Span* out, int n_out, const Span* in, int n_in) {
   return false;
 }
 
-static void head_prep(const rl_batch* b, const Plan& p, const Ptrs& q, const rl_outputs& out, hipStream_t s) {
-  PrepJob job;
-  run_prep(b, p, q, nullptr, out, AdvJob{}, job, s);
-  if (job.on) prep_small_kernel<<<1, 1024, 0, s>>>(job.s, job.f, job.adv);        // (no launch of these logits prepares)
+// Whether the logits come from a kernel for few tokens, and whether that does the preparation as well: up to three rounds of workgroups, as few_prepare says.
+constexpr int kFewScoreF32 = 64;
+static bool few_scores(const rl_batch* b, const Plan& p) {
+  if ((reinterpret_cast<uintptr_t>(b->weight) | reinterpret_cast<uintptr_t>(b->hidden)) % 16) return false;
+  // bf16: up to 64 tokens always, up to 128 where the hot kernel's tiles fill the chip worse (few_tokens).  us of the hot kernel and here: 3 tokens, H 3584, V 126849 227 and 177, 40 tokens
+  // 215 and 165, 100 tokens 216 and 217; 3 tokens, H 5120, V 50257 137 and 106; 60, H 2048, V 100000 130 and 119; 1, H 1024, V 60000 38 and 30.  (Same bits.)
+  if (p.dtype == RL_BF16) return p.R <= 64 || (p.R <= kFewTokens && (p.tiles_v + 127) / 128 % 2);
+  return p.R <= kFewScoreF32;
+}
+static PrepJob head_prep(const rl_batch* b, const Plan& p, const Ptrs& q, const rl_outputs& out, hipStream_t s) {
+  PrepJob job{};
+  run_prep(b, p, q, nullptr, out, AdvJob{}, job, s, few_scores(b, p) && few_prepare(p));
+  return job;
 }
 
-constexpr int kFewScoreF32 = 64;
 // Sets of wavefronts of score_few_f32_kernel that share K, where the groups alone do not fill the chip.  us with 1, 2, 4 sets: 3 tokens, H 5120, V 5726 (90 groups) 62 47 44, V 32000 (500) 111 99 104;
 // 30 tokens, H 768, V 50257 (786) 45 47 56; 2 tokens, H 216, V 152064 34 41 56; 7 tokens, H 768, V 5462 13.9 12.7 11.7.
 static int few_f32_sets(int blocks, int H) { return blocks >= 640 || H < 256 ? 1 : blocks >= 256 || H < 512 ? 2 : 4; }
-template <int NT> static auto few_f32_kernel(int ks, bool stream) {
-  return stream ? (ks == 1 ? score_few_f32_kernel<NT, 1, true> : ks == 2 ? score_few_f32_kernel<NT, 2, true> : score_few_f32_kernel<NT, 4, true>)
-                : (ks == 1 ? score_few_f32_kernel<NT, 1, false> : ks == 2 ? score_few_f32_kernel<NT, 2, false> : score_few_f32_kernel<NT, 4, false>);
+template <int NT, bool STREAM, bool PREP> static auto few_f32_sets_kernel(int ks) {
+  if constexpr (NT == 4) return ks == 1 ? score_few_f32_kernel<NT, 1, STREAM, PREP> : score_few_f32_kernel<NT, 2, STREAM, PREP>;            // (LDS holds two sets of 64 tokens)
+  else return ks == 1 ? score_few_f32_kernel<NT, 1, STREAM, PREP> : ks == 2 ? score_few_f32_kernel<NT, 2, STREAM, PREP> : score_few_f32_kernel<NT, 4, STREAM, PREP>;
 }
+template <bool STREAM, bool PREP> static auto few_f32_kernel(int64_t rows, int ks) {
+  return rows <= 16 ? few_f32_sets_kernel<1, STREAM, PREP>(ks) : rows <= 32 ? few_f32_sets_kernel<2, STREAM, PREP>(ks) : few_f32_sets_kernel<4, STREAM, PREP>(ks);
+}
+template <bool NT, bool PREP> static auto few_bf16_kernel(int64_t rows) { return rows <= 64 ? score_few_kernel<64, NT, PREP> : score_few_kernel<128, NT, PREP>; }
+
 template <class T>
-static void score_chunk(const rl_batch* b, const HeadPlan& h, const Ptrs& q, int c0, float* z, float4* rec, hipStream_t s) {
+static void score_chunk(const rl_batch* b, const HeadPlan& h, const Ptrs& q, int c0, float* z, float4* rec, const PrepJob& prep, hipStream_t s) {
   const Plan& p = h.p;
   const T* X = static_cast<const T*>(b->hidden);
   const T* W = static_cast<const T*>(b->weight);
@@ -1054,23 +1084,18 @@ static void score_chunk(const rl_batch* b, const HeadPlan& h, const Ptrs& q, int
   d.b_rows = q.row_map + c0; d.b_span = p.R; d.n_real = &q.ctrl->n_real; d.chunk_start = c0; d.dyn = 2; d.group_m = TuneLogits::kBand;
   const EpiScore<T> e{z, p.Vp, rec, p.Tc, p.V, p.inv_tau};
   ProfScope ps(RL_PROF_GEMM_FWD, s);
-  if ((reinterpret_cast<uintptr_t>(W) | reinterpret_cast<uintptr_t>(X)) % 16 == 0) {
-    const bool stream = (int64_t)p.V * p.H * sizeof(T) > (int64_t)256 << 20;                  // (more than the memory-side cache holds, see few_streams_w)
+  if (few_scores(b, p)) {
+    const bool large = (int64_t)p.V * p.H * sizeof(T) > (int64_t)256 << 20;                  // (more than the memory-side cache holds, see few_streams_w)
     if constexpr (sizeof(T) == 2) {
-      // up to 64 tokens always, up to 128 where the hot kernel's tiles fill the chip worse (few_tokens).  us of the hot kernel and here: 3 tokens, H 3584, V 126849 227 and 177, 40 tokens 215
-      // and 165, 100 tokens 216 and 217; 3 tokens, H 5120, V 50257 137 and 106; 60, H 2048, V 100000 130 and 119; 1, H 1024, V 60000 38 and 30.  (Same bits.)
-      if (p.R <= 64 || (p.R <= kFewTokens && (p.tiles_v + 127) / 128 % 2)) {
-        const bool nt = stream && p.H % 64 == 0 && reinterpret_cast<uintptr_t>(W) % 128 == 0;
-        auto kern = nt ? (p.R <= 64 ? score_few_kernel<64, true> : score_few_kernel<128, true>) : (p.R <= 64 ? score_few_kernel<64, false> : score_few_kernel<128, false>);
-        kern<<<2 * p.tiles_v, 256, 0, s>>>(W, X, d, e, q.ids_c);
-        return;
-      }
-    } else if (p.R <= kFewScoreF32) {
-      const int blocks = p.Vp / kGroup, sets = few_f32_sets(blocks, p.H), ks = p.R > 32 && sets > 2 ? 2 : sets;        // (LDS holds two sets of 64 tokens)
-      auto kern = p.R <= 16 ? few_f32_kernel<1>(ks, stream) : p.R <= 32 ? few_f32_kernel<2>(ks, stream) : ks == 1 ? (stream ? score_few_f32_kernel<4, 1, true> : score_few_f32_kernel<4, 1, false>) : (stream ? score_few_f32_kernel<4, 2, true> : score_few_f32_kernel<4, 2, false>);
-      kern<<<blocks, 256 * ks, 0, s>>>(W, X, d, e);
-      return;
+      const bool nt = large && p.H % 64 == 0 && reinterpret_cast<uintptr_t>(W) % 128 == 0;
+      auto kern = prep.on ? (nt ? few_bf16_kernel<true, true>(p.R) : few_bf16_kernel<false, true>(p.R)) : (nt ? few_bf16_kernel<true, false>(p.R) : few_bf16_kernel<false, false>(p.R));
+      kern<<<2 * p.tiles_v + prep.on, 256, 0, s>>>(W, X, d, e, q.ids_c, prep.s, prep.f);
+    } else {
+      const int blocks = p.Vp / kGroup, sets = few_f32_sets(blocks, p.H), ks = p.R > 32 && sets > 2 ? 2 : sets;
+      auto kern = prep.on ? (large ? few_f32_kernel<true, true>(p.R, ks) : few_f32_kernel<false, true>(p.R, ks)) : (large ? few_f32_kernel<true, false>(p.R, ks) : few_f32_kernel<false, false>(p.R, ks));
+      kern<<<blocks + prep.on, 256 * ks, 0, s>>>(W, X, d, e, prep.s, prep.f);
     }
+    return;
   }
   launch_gemm<TuneLogits>(W, X, d, e, s);
 }
@@ -1089,8 +1114,8 @@ static void run_few_grads(const rl_batch* b, const HeadPlan& h, const Ptrs& q, u
   const int n_ds = p.Vp / 64, zero = (int)((p.R + 3) / 4);
   {
     ProfScope ps(RL_PROF_GEMM_DS, s);
-    few_ds_kernel<T><<<1 + n_ds + zero, 256, 0, s>>>(ds, tokens, pitch, ds1, ds2, XtJob{nullptr, p.R, p.H, 0, n_ds, 0, 0, q.row_map, q.cpos, nullptr, out->d_hidden, p.Tc}, fin);
-    few_patch_kernel<T><<<(unsigned)((p.R * h.K + 255) / 256), 256, 0, s>>>((const int*)(w + h.off_pids), (const float*)(w + h.off_pval), h.K, q.ctrl, tokens, pitch, ds1, ds2);
+    few_ds_kernel<T><<<1 + n_ds + zero, 256, 0, s>>>(ds, (const int*)(w + h.off_pids), (const float*)(w + h.off_pval), h.K, tokens, pitch, ds1, ds2,
+                                                     XtJob{nullptr, p.R, p.H, 0, n_ds, 0, 0, q.row_map, q.cpos, nullptr, out->d_hidden, p.Tc}, fin);
   }
   ProfScope ps(RL_PROF_GEMM_BWD, s);
   const FewGrads j{b->weight, b->hidden, p.V, p.H, q.row_map, &q.ctrl->n_real, ds1, ds2, out->d_weight, part, h.few_splits, h.few_steps};
@@ -1104,7 +1129,7 @@ static void run_few_grads(const rl_batch* b, const HeadPlan& h, const Ptrs& q, u
 
 template <class T>
 static void run_distill(const rl_batch* b, const HeadPlan& h, const Ptrs& q, unsigned char* w, const int32_t* t_ids, const float* t_lp, const rl_distill_params* prm,
-                        const rl_distill_outputs* out, bool bwd, hipStream_t s) {
+                        const rl_distill_outputs* out, bool bwd, const PrepJob& prep, hipStream_t s) {
   const Plan& p = h.p;
   float* z = (float*)(w + h.off_z);
   float4* rec = (float4*)(w + h.off_rec);
@@ -1125,7 +1150,7 @@ static void run_distill(const rl_batch* b, const HeadPlan& h, const Ptrs& q, uns
   for (int ch = 0; ch < p.n_chunks; ++ch) {
     const int c0 = ch * p.Tc;
     const int64_t n = chunk_bound(p, c0);
-    score_chunk<T>(b, h, q, c0, z, rec, s);
+    score_chunk<T>(b, h, q, c0, z, rec, prep, s);
     {
       ProfScope ps(RL_PROF_COMBINE, s);
       launch_distill_rows(DistillJob{z, p.Vp, rec, p.Tc, h.groups, p.V, h.K, p.inv_tau, q.row_map, q.cstart, q.ctrl, c0, p.Tc, p.B, t_ids, t_lp, prm->rest,
@@ -1200,11 +1225,11 @@ rl_status rl_token_top_logprobs(const rl_batch* b, const rl_top_params* prm, con
   float4* rec = (float4*)(w + h.off_rec);
   rl_outputs cleared{};
   cleared.logprob = out->logprob; cleared.lse = out->lse; cleared.entropy = out->entropy;
-  head_prep(b, p, q, cleared, s);
+  const PrepJob prep = head_prep(b, p, q, cleared, s);
   for (int ch = 0; ch < p.n_chunks; ++ch) {
     const int c0 = ch * p.Tc;
-    if (p.dtype == RL_BF16) score_chunk<bf16_t>(b, h, q, c0, z, rec, s);
-    else score_chunk<float>(b, h, q, c0, z, rec, s);
+    if (p.dtype == RL_BF16) score_chunk<bf16_t>(b, h, q, c0, z, rec, prep, s);
+    else score_chunk<float>(b, h, q, c0, z, rec, prep, s);
     ProfScope ps(RL_PROF_COMBINE, s);
     const unsigned blocks = (unsigned)((chunk_bound(p, c0) + kXcds - 1) / kXcds * kXcds);
     const int64_t all = (p.R + kTopWaves - 1) / kTopWaves;
@@ -1258,9 +1283,9 @@ rl_status rl_distill_loss_fwd_bwd(const rl_batch* b, const int32_t* t_ids, const
   no_ids.token_ids = nullptr;
   rl_outputs cleared{};
   cleared.logprob = out->row_loss; cleared.lse = out->lse; cleared.stats = (rl_stats*)(w + h.off_stats);
-  head_prep(&no_ids, p, q, cleared, s);
-  if (p.dtype == RL_BF16) run_distill<bf16_t>(b, h, q, w, t_ids, t_lp, prm, out, bwd, s);
-  else run_distill<float>(b, h, q, w, t_ids, t_lp, prm, out, bwd, s);
+  const PrepJob prep = head_prep(&no_ids, p, q, cleared, s);
+  if (p.dtype == RL_BF16) run_distill<bf16_t>(b, h, q, w, t_ids, t_lp, prm, out, bwd, prep, s);
+  else run_distill<float>(b, h, q, w, t_ids, t_lp, prm, out, bwd, prep, s);
   return hipGetLastError() == hipSuccess ? RL_OK : RL_ERR_HIP;
 }
 

@@ -504,7 +504,7 @@ __device__ inline void local_rows(const SmallPrep& s, LocalRows<ROWS>& l) {
   for (int k = 0; k < kPer; ++k) {
     const int r = k * NT + t;
     on[k] = false; y[k] = -1;
-    if (r < s.R) { on[k] = s.mask[r]; y[k] = s.ids[r]; }
+    if (r < s.R) { on[k] = s.mask[r]; y[k] = s.ids ? s.ids[r] : 0; }
   }
   // A lane of every wavefront has a sequence (as there: a valid range at or behind every earlier offset, of a valid prompt), and the lanes put together which of
   // the wavefront's 64 rows are in one: no barrier, and no walk over the sequences (60 of them, 947 rows, V 114 in f32 25.6 us that way).
@@ -1540,9 +1540,12 @@ template <bool NT> static auto few_kernel(int64_t rows, bool prep) {
 }
 static bool small_logits(const Plan& p) { return p.dtype == RL_F32 && p.n_chunks == 1 && p.R <= kLocalRows && few_forward_tiles(p.V, p.Tc, p.H); }
 
+static bool logits_prepare(const rl_batch* b, const Plan& p) { return small_logits(p) || (few_tokens(b, p) && few_prepare(p)); }
+
 // prep: row outputs cleared (rows that do not count read 0 / -1), advantages, counts, compaction, chunk records
+// (inside: whether the launch of the logits can do it, if the batch is small enough)
 static void run_prep(const rl_batch* b, const Plan& p, const Ptrs& q, const int32_t* group_idx, const rl_outputs& out, const AdvJob& adv,
-                     PrepJob& job, hipStream_t s) {
+                     PrepJob& job, hipStream_t s, bool inside) {
   ProfScope ps(RL_PROF_PREP, s);
   job.on = false;
   RowFill f{};
@@ -1556,7 +1559,7 @@ static void run_prep(const rl_batch* b, const Plan& p, const Ptrs& q, const int3
   clear(out.logprob, 0); clear(out.lse, 0); clear(out.coeff, 0);
   if (!late) clear_last();
   if (!late && p.R <= kSmallRows && p.B <= kSmallSeqs && (!adv.blocks || p.P <= kSmallPrompts)) {
-    job = PrepJob{small_logits(p) || (few_tokens(b, p) && few_prepare(p)),
+    job = PrepJob{inside,
                   SmallPrep{b->mask, b->token_ids, b->cu_seqlens, group_idx, (int)p.R, p.V, p.P, p.B, q.seq_len, q.cstart, q.row_map, q.ids_c, q.cpos, out.row_map, q.ctrl,
                             ChunkJob{p.stash ? q.desc : nullptr, p.n_desc, p.Tc, p.max_len}, out.stats}, f, adv};
     // (there, outputs are cleared while other workgroups still read the inputs: with one in the place of another the preparation goes first)
@@ -1951,7 +1954,7 @@ rl_status rl_token_logprob_tempered(const rl_batch* b, float temperature, float*
   rl_outputs out{};
   out.logprob = logprob; out.lse = lse;
   PrepJob prep;
-  run_prep(b, p, q, nullptr, out, AdvJob{}, prep, s);
+  run_prep(b, p, q, nullptr, out, AdvJob{}, prep, s, logits_prepare(b, p));
   if (p.dtype == RL_BF16) run_forward<bf16_t>(b, p, q, logprob, lse, nullptr, nullptr, nullptr, false, prep, s);
   else run_forward<float>(b, p, q, logprob, lse, nullptr, nullptr, nullptr, false, prep, s);
   return hipGetLastError() == hipSuccess ? RL_OK : RL_ERR_HIP;
@@ -1987,7 +1990,7 @@ rl_status rl_policy_loss_fwd_bwd(const rl_batch* b, const rl_params* prm, int32_
 
   const AdvJob adv{(p.P + kInitThreads / 64 - 1) / (kInitThreads / 64), b->rewards, b->group_idx, p.P, prm->adv_eps, prm->adv_std_ddof, q.adv, out->group_count};
   PrepJob prep;
-  run_prep(b, p, q, b->group_idx, *out, adv, prep, s);
+  run_prep(b, p, q, b->group_idx, *out, adv, prep, s, logits_prepare(b, p));
 
   if (p.stash) {
     run_fused(b, prm, objective, p, q, out, s);
@@ -2067,7 +2070,7 @@ rl_status rl_token_logprob_static(const rl_batch* b, float temperature, float* l
   rl_outputs out{};
   out.logprob = logprob; out.lse = lse;
   PrepJob prep;
-  run_prep(b, p, q, nullptr, out, AdvJob{}, prep, s);
+  run_prep(b, p, q, nullptr, out, AdvJob{}, prep, s, logits_prepare(b, p));
   if (p.dtype == RL_BF16) run_forward<bf16_t>(b, p, q, logprob, lse, nullptr, nullptr, nullptr, false, prep, s);
   else run_forward<float>(b, p, q, logprob, lse, nullptr, nullptr, nullptr, false, prep, s);
   return hipGetLastError() == hipSuccess ? RL_OK : RL_ERR_HIP;
