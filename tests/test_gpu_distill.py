@@ -2,11 +2,13 @@
 
 Inputs lie on grids of powers of two on which every logit is a sum without rounding, so that the order of the alternatives is that of the oracle to the bit, and what is
 left in the tolerances is what follows the logits.  With u = 2^-24 (half a step of f32, relative):
-  * an exponential: the difference to the maximum and its scaling round once each, which changes e = exp(-d) by 2 u d e, summed at most 2 u sum d e; exp2 itself 2 u.
-    A group's 64 are added in chains of 18 at most: 18 u.  Groups are added in f64, their weights are exponentials of the same kind: 2 u d + 2 u.  d e^-d <= 0.37,
-    so a sum is off by less than 26 u of itself, its logarithm by 26 u.  SUM = 32 u.
-  * lse and log-probabilities: SUM, and their own rounding.   * entropy: ln S (SUM) and sum e d / S, off by 32 u (1 + D) D with D = its value: SUM (2 + 2 D).
-  * dS: exponentials of the row's maximum, SUM more from the sum: (32 + 2 d) u of each magnitude that it is the difference of, d < 60 here: 2^-16.  Then one rounding, 2^-8 in bf16.
+  * c = log2(e) / temperature in f32: two roundings of its own and that of the temperature, 1.3 u at those used here (arithmetic; 0.5 u at 0.6).  It acts as another temperature:
+    lse moves by that share of the mean logit / temperature (below 40 here), a log-probability by that share of itself.
+  * an exponential 2^(z c - k): one rounding of the exponent, which changes e^-d by u d e^-d, <= 0.37 u summed; exp2 itself 2 u.  A group's 64 are added in chains of
+    18 at most: 18 u.  Groups differ by powers of two, exact, and are added in f64.  So a sum is off by less than 24 u of itself, its logarithm by 24 u.  SUM = 32 u.
+  * lse and log-probabilities: SUM, c, their own rounding.   * entropy: ln S (SUM) and sum e d / S, off by 32 u (1 + D) D with D = its value: SUM (2 + 2 D).
+  * dS: SUM from the sum, and for an entry d below the sum c, the exponent's rounding and that of the sum's logarithm: (32 + 3.3 d) u of each magnitude that it is the difference of,
+    d < 50 here: 2^-16.  Then one rounding, 2^-8 in bf16.
   * contractions of n terms: n u of the sum of magnitudes; one rounding at the end (2^-8 in bf16, u in f32)."""
 import numpy as np
 import pytest
