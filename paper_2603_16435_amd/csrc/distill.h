@@ -10,8 +10,8 @@
 //    all of the probability.
 // What is read of the logits once more is the whole chunk, by the backward, which turns it into dS in one pass.
 //
-// Sums: those of a group in f32, of groups in f64.  With c = log2(e) / temperature in f32, every exponential is 2^(z c - k) for a whole number k next to the group's
-// or the row's largest z c: one fused multiply-add, whose rounding is relative to what is left, and sums of different groups differ by exact powers of two.
+// Sums: those of a group in f32, of groups in f64; each exponential is taken of a difference to the group's or the row's maximum (formed before it is
+// scaled), so that what carries the sum carries no error of the shift.
 #pragma once
 #include "../../include/rl_distill.h"
 #include "few_grads.h"
@@ -20,11 +20,10 @@ namespace rlk {
 
 constexpr int kDefaultChunkRowsDistill = 16384;   // 10 GB of logits and 5 of dS at the 7B head
 constexpr int kMostChunkRows = 1 << 20;           // (launches of a chunk stay below 2^32 threads)
-constexpr double kLn2 = 0.69314718055994530942;
 constexpr int kGroup = 64;                        // vocabulary entries of a record
 
 // ------------------------------------------------------------------ logits and records
-// Record of 64 logits of a token: x the largest (raw), w = k the whole number next to x c (-inf: no number), y the sum of e = 2^(z c - k), z the sum of e (z c - k).
+// Record of 64 logits of a token, x largest (raw), y sum exp(zs (z - x)), z sum of those times (z - x); w unused.
 //
 // In what order the 64 are added: bf16 (kPermute, a lane holds eight consecutive entries of each half of the group): the sixteen of a lane in order, then lanes 16
 // apart, then 32.  f32, by quads of four consecutive entries Q = 0 .. 15: over bits 2 and 3 of Q in order, then bit 1, then bit 0, which both
@@ -55,14 +54,14 @@ struct EpiScore {
     auto in = [&](int r) __attribute__((always_inline)) { return !PAD || (r >> 3) * 32 + g * 8 + (r & 7) < vleft; };
     float mx = NEG, a, b;
 #pragma unroll
-    for (int r = 0; r < 16; r += 2) mx = fmaxf(fmaxf(mx, in(r) ? v[r] : NEG), in(r + 1) ? v[r + 1] : NEG);
+    for (int r = 0; r < 16; ++r) mx = fmaxf(mx, in(r) ? v[r] : NEG);
     lane_pair<16>(mx, a, b); mx = fmaxf(a, b);
     lane_pair<32>(mx, a, b); mx = fmaxf(a, b);
-    const float k = mx == NEG ? 0.f : __builtin_rintf(mx * c);
+    const float ms = mx == NEG ? 0.f : mx;
     float s = 0.f, u = 0.f;
 #pragma unroll
     for (int r = 0; r < 16; ++r) {
-      const float d = __builtin_fmaf(v[r], c, -k), e = in(r) ? __builtin_amdgcn_exp2f(d) : 0.f;
+      const float d = v[r] - ms, e = in(r) ? __builtin_amdgcn_exp2f(d * c) : 0.f;
       s += e;
       u = in(r) ? __builtin_fmaf(e, d, u) : u;
     }
@@ -70,7 +69,7 @@ struct EpiScore {
     lane_pair<32>(s, a, b); s = a + b;
     lane_pair<16>(u, a, b); u = a + b;
     lane_pair<32>(u, a, b); u = a + b;
-    return make_float4(mx, s, u, mx == NEG ? NEG : k);
+    return make_float4(mx, s, u, 0.f);
   }
 
   // MB = 8 block rows (128 permuted rows) of NB columns.  A lane has eight consecutive entries of its token, two quads; lanes eight apart exchange one each, so that a store writes whole lines
@@ -127,14 +126,14 @@ struct EpiScore {
           for (int i = 0; i < L::kRegs; ++i) mx = fmaxf(mx, in(bi, i) ? acc[k * PER + bi][bj][i] : NEG);
         lane_pair<32>(mx, a, b); mx = fmaxf(a, b);
         if constexpr (L::kBlk == 16) { lane_pair<16>(mx, a, b); mx = fmaxf(a, b); }
-        const float sh = mx == NEG ? 0.f : __builtin_rintf(mx * cs);
+        const float ms = mx == NEG ? 0.f : mx;
         float s[2] = {0.f, 0.f}, u[2] = {0.f, 0.f};              // (32 x 32 blocks: by bit 1 of the quad)
 #pragma unroll
         for (int bi = 0; bi < PER; ++bi)
 #pragma unroll
           for (int i = 0; i < L::kRegs; ++i) {
             const int w = L::kBlk == 32 ? (i >> 2) & 1 : 0;
-            const float d = __builtin_fmaf(acc[k * PER + bi][bj][i], cs, -sh), e = in(bi, i) ? __builtin_amdgcn_exp2f(d) : 0.f;
+            const float d = acc[k * PER + bi][bj][i] - ms, e = in(bi, i) ? __builtin_amdgcn_exp2f(d * cs) : 0.f;
             s[w] += e;
             u[w] = in(bi, i) ? __builtin_fmaf(e, d, u[w]) : u[w];
           }
@@ -146,7 +145,7 @@ struct EpiScore {
         };
         const float S = join(s), U = join(u);
         if (n < c.Nv) {
-          if (c.lane < L::kBlk) rec[rec_index(c.m0 / kGroup + k, n, ldr)] = make_float4(mx, S, U, mx == NEG ? NEG : sh);
+          if (c.lane < L::kBlk) rec[rec_index(c.m0 / kGroup + k, n, ldr)] = make_float4(mx, S, U, 0.f);
 #pragma unroll
           for (int bi = 0; bi < PER; ++bi)
 #pragma unroll
@@ -294,15 +293,15 @@ __global__ __launch_bounds__(256 * KS) void score_few_f32_kernel(const float* __
 #pragma unroll
   for (int i = 0; i < 16; ++i) { z[i] = part[0][q * 16 + i][t]; mx = fmaxf(mx, q * 16 + i < vleft ? z[i] : NEG); }
   mx = fmaxf(mx, __shfl_xor(mx, 1)); mx = fmaxf(mx, __shfl_xor(mx, 2));
-  const float sh = mx == NEG ? 0.f : __builtin_rintf(mx * c);
+  const float ms = mx == NEG ? 0.f : mx;
 #pragma unroll
   for (int i = 0; i < 16; ++i) {
-    const float dd = __builtin_fmaf(z[i], c, -sh), e = __builtin_amdgcn_exp2f(dd);
+    const float dd = z[i] - ms, e = __builtin_amdgcn_exp2f(dd * c);
     if (q * 16 + i < vleft) { s += e; u = __builtin_fmaf(e, dd, u); }
   }
   s += __shfl_xor(s, 1); s += __shfl_xor(s, 2);
   u += __shfl_xor(u, 1); u += __shfl_xor(u, 2);
-  if (q == 0) epi.rec[rec_index(group, t, epi.ldr)] = make_float4(mx, s, u, mx == NEG ? NEG : sh);
+  if (q == 0) epi.rec[rec_index(group, t, epi.ldr)] = make_float4(mx, s, u, 0.f);
 }
 
 // ------------------------------------------------------------------ a row, by a workgroup
@@ -321,25 +320,24 @@ __device__ inline unsigned order_key(float z) {
 }
 __device__ inline float key_value(unsigned k) { return __uint_as_float(k & 0x80000000u ? k ^ 0x80000000u : ~k); }
 
-// Sums of 2^(z c - k) (s), and of those times z c - k (u), under a running whole number k.  Not-a-numbers stay in s.
+// Sums under a running maximum (raw units, c = log2(e) / temperature).  Not-a-numbers stay in s.
 struct Online {
-  float k = -__builtin_inff();
+  float m = -__builtin_inff();
   double s = 0.0, u = 0.0;
-  __device__ __attribute__((always_inline)) void raise(float kk) {
-    if (!(kk > k)) return;
-    if (k != -__builtin_inff()) {
-      const double f = (double)__builtin_amdgcn_exp2f(k - kk);                           // (exact, or nothing is left)
-      u = f * (u + (double)(k - kk) * s);
+  __device__ __attribute__((always_inline)) void raise(float mm, float c) {
+    if (!(mm > m)) return;
+    if (m != -__builtin_inff()) {
+      const double f = (double)__builtin_amdgcn_exp2f((m - mm) * c);
+      u = f * (u + (double)(m - mm) * s);
       s *= f;
     }
-    k = kk;
+    m = mm;
   }
-  __device__ __attribute__((always_inline)) void add(const float4& q) {                // a record with a w of at most k
-    if (q.w > -__builtin_inff()) {
-      const float d = q.w - k;
-      const int n = d < -1000.f ? -1000 : (int)d;                                       // (a power of two: exact; below 2^-149 nothing is left)
-      s += (double)ldexpf(q.y, n);
-      u += (double)ldexpf(__builtin_fmaf(d, q.y, q.z), n);
+  __device__ __attribute__((always_inline)) void add(const float4& q, float c) {       // a record with a maximum of at most m
+    if (q.x > -__builtin_inff()) {
+      const float d = q.x - m, f = __builtin_amdgcn_exp2f(d * c);
+      s += (double)f * (double)q.y;
+      u += (double)f * ((double)q.z + (double)d * (double)q.y);
     } else if (q.y != q.y) s = __builtin_nan("");
   }
 };
@@ -415,37 +413,41 @@ __global__ __launch_bounds__(kTopThreads) void top_kernel(TopJob j) {
   const float zy = j.logprob ? j.z[tiled_index(t, j.ids_c[tg], j.ldz)] : 0.f;
 
   float4 q[REG];
-  float m = NEG;                                                  // the largest w
+  float m = NEG;
 #pragma unroll
   for (int i = 0; i < REG; ++i) {
     const int b = i * kTopThreads + tid;
-    q[i] = make_float4(NEG, 0.f, 0.f, NEG);
+    q[i] = make_float4(NEG, 0.f, 0.f, 0.f);
     if (b < j.groups) q[i] = j.rec[rec_index(b, t, j.ldr)];
   }
 #pragma unroll
-  for (int i = 0; i < REG; ++i) m = fmaxf(m, q[i].w);
+  for (int i = 0; i < REG; ++i) m = fmaxf(m, q[i].x);
   m = wave_max(m);
   if (lane == 0) red_m[w] = m;
   if (tid == 0) { n_sel = 0; n_list = 0; }
   __syncthreads();
 #pragma unroll
   for (int i = 0; i < kTopWaves; ++i) m = fmaxf(m, red_m[i]);
-  Online o;
-  o.k = m;
+  double s = 0.0, u = 0.0;
 #pragma unroll
-  for (int i = 0; i < REG; ++i) if (i * kTopThreads + tid < j.groups) o.add(q[i]);
-  double s = wave_sum(o.s), u = wave_sum(o.u);
+  for (int i = 0; i < REG; ++i) {
+    if (q[i].x > NEG) {
+      const float d = q[i].x - m, f = __builtin_amdgcn_exp2f(d * c);
+      s += (double)f * (double)q[i].y;
+      u += (double)f * ((double)q[i].z + (double)d * (double)q[i].y);
+    } else if (q[i].y != q[i].y) s = __builtin_nan("");
+  }
+  s = wave_sum(s); u = wave_sum(u);
   if (lane == 0) { red_s[w] = s; red_u[w] = u; }
   __syncthreads();
   s = red_s[0]; u = red_u[0];
 #pragma unroll
   for (int i = 1; i < kTopWaves; ++i) { s += red_s[i]; u += red_u[i]; }
   const double ln = log(s);
-  auto log_prob = [&](float z) __attribute__((always_inline)) { return (float)(((double)z * (double)c - (double)m) * kLn2 - ln); };
   if (tid == 0) {
-    if (j.lse) j.lse[row] = (float)((double)m * kLn2 + ln);
-    if (j.logprob) j.logprob[row] = log_prob(zy);
-    if (j.entropy) { const double h = ln - kLn2 * u / s; j.entropy[row] = (float)(h < 0.0 ? 0.0 : h); }
+    if (j.lse) j.lse[row] = (float)((double)j.zs * (double)m + ln);
+    if (j.logprob) j.logprob[row] = (float)((double)j.zs * ((double)zy - (double)m) - ln);
+    if (j.entropy) { const double h = ln - (double)j.zs * u / s; j.entropy[row] = (float)(h < 0.0 ? 0.0 : h); }
   }
   if (!j.ids && !j.lp) return;
 
@@ -534,7 +536,7 @@ __global__ __launch_bounds__(kTopThreads) void top_kernel(TopJob j) {
     for (int k = 0; k < n; ++k) rank += list[k] > p;
     if (rank >= K) continue;
     if (j.ids) j.ids[(int64_t)row * K + rank] = (int)(0xffffffffu - (unsigned)p);
-    if (j.lp) j.lp[(int64_t)row * K + rank] = log_prob(key_value((unsigned)(p >> 32)));
+    if (j.lp) j.lp[(int64_t)row * K + rank] = (float)((double)j.zs * ((double)key_value((unsigned)(p >> 32)) - (double)m) - ln);
   }
   for (int i = n + tid; i < K; i += kTopThreads) {                // (fewer numbers than K in the row)
     if (j.ids) j.ids[(int64_t)row * K + i] = -1;
@@ -549,8 +551,8 @@ static void launch_top(const TopJob& j, unsigned blocks, hipStream_t s) {
 }
 
 // ------------------------------------------------------------------ distillation, a row
-// What the backward needs of a row: dS = f 2^(z c - k - l2) at tokens that the list does not name (k a whole number).
-struct DistillRow { float k, l2, f, pad; };
+// What the backward needs of a row: dS = f exp(zs (z - m) - l) at tokens that the list does not name, in log2 units.
+struct DistillRow { float m, l2, f, pad; };
 struct DistillJob {
   const float* z; int64_t ldz; const float4* rec; int ldr, groups, V, K;
   float zs;
@@ -598,7 +600,7 @@ __global__ __launch_bounds__(kTopThreads) void distill_row_kernel(DistillJob j) 
 #pragma unroll
   for (int i = 0; i < REG; ++i) {
     const int b = i * kTopThreads + tid;
-    q[i] = make_float4(NEG, 0.f, 0.f, NEG);
+    q[i] = make_float4(NEG, 0.f, 0.f, 0.f);
     if (b < j.groups) q[i] = j.rec[rec_index(b, t, j.ldr)];
   }
   double share = 0.0;                                             // (wavefronts 0 and 1, as all that is asked of entries)
@@ -666,21 +668,19 @@ __global__ __launch_bounds__(kTopThreads) void distill_row_kernel(DistillJob j) 
         }
         if (g[k] * kGroup + lane >= j.V || (named >> lane & 1)) continue;
         if (z[k] != z[k]) r.s = __builtin_nan("");
-        if (!(z[k] > NEG)) continue;
-        const float kk = __builtin_rintf(z[k] * c);
-        r.raise(kk);
-        r.add(make_float4(z[k], __builtin_amdgcn_exp2f(__builtin_fmaf(z[k], c, -kk)), 0.f, kk));
+        r.raise(z[k], c);
+        r.add(make_float4(z[k], 1.f, 0.f, 0.f), c);
       }
     }
   // and of the others, by their records; all tokens
   bool plain[REG];
-  float m = NEG, mr = r.k, ml = wave_max(in ? lp : NEG);             // the largest w of all, of those that are not listed
+  float m = NEG, mr = r.m, ml = wave_max(in ? lp : NEG);
 #pragma unroll
   for (int i = 0; i < REG; ++i) {
     const int b = i * kTopThreads + tid;
     plain[i] = bucket && b < j.groups && !(bits[b >> 5] >> (b & 31) & 1u);
-    m = fmaxf(m, q[i].w);
-    if (plain[i]) mr = fmaxf(mr, q[i].w);
+    m = fmaxf(m, q[i].x);
+    if (plain[i]) mr = fmaxf(mr, q[i].x);
   }
   m = wave_max(m); mr = wave_max(mr);
   if (lane == 0) { red_m[0][w] = m; red_m[1][w] = mr; red_m[2][w] = ml; }
@@ -688,13 +688,13 @@ __global__ __launch_bounds__(kTopThreads) void distill_row_kernel(DistillJob j) 
 #pragma unroll
   for (int i = 0; i < kTopWaves; ++i) { m = fmaxf(m, red_m[0][i]); mr = fmaxf(mr, red_m[1][i]); ml = fmaxf(ml, red_m[2][i]); }
   Online o;
-  o.k = m;
-  r.raise(mr);
+  o.m = m;
+  r.raise(mr, c);
 #pragma unroll
   for (int i = 0; i < REG; ++i) {
     if (i * kTopThreads + tid >= j.groups) continue;
-    o.add(q[i]);
-    if (plain[i]) r.add(q[i]);
+    o.add(q[i], c);
+    if (plain[i]) r.add(q[i], c);
   }
   auto sum4 = [&](int half, double (&v)[4]) __attribute__((always_inline)) {
 #pragma unroll
@@ -719,11 +719,11 @@ __global__ __launch_bounds__(kTopThreads) void distill_row_kernel(DistillJob j) 
   double ln = 0.0, lnr = 0.0, lq = 0.0, lqr = 0.0, P = 0.0, pr = 0.0, part[4] = {0.0, 0.0, 0.0, 0.0};
   if (w < 2) {
     ln = log(v[0]);
-    if (in) lq = ((double)zi * (double)c - (double)m) * kLn2 - ln;
+    if (in) lq = (double)j.zs * ((double)zi - (double)m) - ln;
     double lnp = 0.0;
     if (bucket) {
       lnr = log(v[1]);
-      lqr = ((double)mr - (double)m) * kLn2 + lnr - ln;           // log of the others' probability
+      lqr = (double)j.zs * ((double)mr - (double)m) + lnr - ln;   // log of the others' probability
       pr = 1.0 - v[2]; pr = pr < 0.0 ? 0.0 : pr;
       if (mr == NEG && v[1] == 0.0) pr = 0.0;                     // (the list names all tokens)
       P = v[2] + pr;
@@ -742,7 +742,7 @@ __global__ __launch_bounds__(kTopThreads) void distill_row_kernel(DistillJob j) 
   if (nothing) kl = 0.0;
   const double coef = (double)j.scale * share, f = coef * (double)j.zs;
   if (tid == 0) {
-    if (j.lse) j.lse[row] = (float)((double)m * kLn2 + ln);
+    if (j.lse) j.lse[row] = (float)((double)j.zs * (double)m + ln);
     if (j.row_loss) j.row_loss[row] = (float)kl;
     j.term[tg] = coef * kl;
     j.info[tg] = left_out | (nothing ? 1 << 30 : 0);
@@ -750,8 +750,8 @@ __global__ __launch_bounds__(kTopThreads) void distill_row_kernel(DistillJob j) 
   if (!j.rows) return;
   // dS at the others, coef zs q (P - pr / q_r).  With a bucket relative to their own sum, q / q_r (P q_r - pr): nothing overflows where q_r is small
   if (tid == 0) {
-    DistillRow d{m, (float)(ln / kLn2), nothing ? 0.f : (float)(f * P), 0.f};
-    if (pr > 0.0 && !nothing) { d.k = mr; d.l2 = (float)(lnr / kLn2); d.f = (float)(f * (P * exp_near(lqr) - pr)); }
+    DistillRow d{m, (float)(ln * 1.4426950408889634), nothing ? 0.f : (float)(f * P), 0.f};
+    if (pr > 0.0 && !nothing) { d.m = mr; d.l2 = (float)(lnr * 1.4426950408889634); d.f = (float)(f * (P * exp_near(lqr) - pr)); }
     j.rows[t] = d;
   }
   if (tid < K) {
@@ -767,7 +767,7 @@ static void launch_distill_rows(const DistillJob& j, int64_t rows, hipStream_t s
 
 // ------------------------------------------------------------------ dS
 __device__ __attribute__((always_inline)) inline float ds_entry(float z, const DistillRow& d, float c) {
-  return d.f == 0.f ? 0.f : d.f * __builtin_amdgcn_exp2f(__builtin_fmaf(z, c, -d.k) - d.l2);
+  return d.f == 0.f ? 0.f : d.f * __builtin_amdgcn_exp2f((z - d.m) * c - d.l2);
 }
 
 struct DsJob { const float* z; int64_t ldz; const DistillRow* rows; const Ctrl* ctrl; int chunk_start, V; float zs; };

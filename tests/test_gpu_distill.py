@@ -2,13 +2,11 @@
 
 Inputs lie on grids of powers of two on which every logit is a sum without rounding, so that the order of the alternatives is that of the oracle to the bit, and what is
 left in the tolerances is what follows the logits.  With u = 2^-24 (half a step of f32, relative):
-  * c = log2(e) / temperature in f32: two roundings of its own and that of the temperature, 1.3 u at those used here (arithmetic; 0.5 u at 0.6).  It acts as another temperature:
-    lse moves by that share of the mean logit / temperature (below 40 here), a log-probability by that share of itself.
-  * an exponential 2^(z c - k): one rounding of the exponent, which changes e^-d by u d e^-d, <= 0.37 u summed; exp2 itself 2 u.  A group's 64 are added in chains of
-    18 at most: 18 u.  Groups differ by powers of two, exact, and are added in f64.  So a sum is off by less than 24 u of itself, its logarithm by 24 u.  SUM = 32 u.
-  * lse and log-probabilities: SUM, c, their own rounding.   * entropy: ln S (SUM) and sum e d / S, off by 32 u (1 + D) D with D = its value: SUM (2 + 2 D).
-  * dS: SUM from the sum, and for an entry d below the sum c, the exponent's rounding and that of the sum's logarithm: (32 + 3.3 d) u of each magnitude that it is the difference of,
-    d < 50 here: 2^-16.  Then one rounding, 2^-8 in bf16.
+  * an exponential: the difference to the maximum and its scaling round once each, which changes e = exp(-d) by 2 u d e, summed at most 2 u sum d e; exp2 itself 2 u.
+    A group's 64 are added in chains of 18 at most: 18 u.  Groups are added in f64, their weights are exponentials of the same kind: 2 u d + 2 u.  d e^-d <= 0.37,
+    so a sum is off by less than 26 u of itself, its logarithm by 26 u.  SUM = 32 u.
+  * lse and log-probabilities: SUM, and their own rounding.   * entropy: ln S (SUM) and sum e d / S, off by 32 u (1 + D) D with D = its value: SUM (2 + 2 D).
+  * dS: exponentials of the row's maximum, SUM more from the sum: (32 + 2 d) u of each magnitude that it is the difference of, d < 60 here: 2^-16.  Then one rounding, 2^-8 in bf16.
   * contractions of n terms: n u of the sum of magnitudes; one rounding at the end (2^-8 in bf16, u in f32)."""
 import numpy as np
 import pytest
@@ -168,3 +166,22 @@ def test_few_rows(R, H, V, dtype, dw, off):
         b.weight, b.hidden = off_grid(b.weight, off), off_grid(b.hidden, off)
     r = b.distill(ids, lp, aggregation="token", d_weight_dtype=DTYPES[dtype] if dw == "own" else torch.float32)
     check_distill(b, r, ids, lp, "bucket", 1.0, "token")
+
+
+# one token far above all others: it has all of the probability, to the last bit, at any temperature
+@pytest.mark.parametrize("R,H,V,dtype", [(1, 64, 300, "bf16"), (40, 128, 3000, "bf16"), (300, 136, 5001, "bf16"), (3, 36, 200, "f32"), (200, 68, 777, "f32")])
+@pytest.mark.parametrize("tau", [1.0, 0.7, 1.9])
+def test_certain_tokens(R, H, V, dtype, tau):
+    b = Batch(R, H, V, dtype, seed=R, masked=0.0)
+    b.weight[:, 0], b.hidden[:, 0] = 0.0, 37.0                 # (the others' logits are below 50 in size, this one is above 2000)
+    b.ids[:] = b.ids[0].clone()
+    b.weight[b.ids[0].long(), 0] = 64.0
+    r = b.score(2, tau)
+    for f in (r.logprob, r.entropy, r.top_logprob[:, 0]):
+        assert torch.equal(f, torch.zeros_like(f))
+    assert torch.equal(r.top_ids[:, 0], b.ids)
+    z = host(b.hidden).astype(np.float64) @ host(b.weight[b.ids[:1].long()]).astype(np.float64)[0]
+    near(r.lse, z / tau, 4 * U * np.abs(z / tau), "lse")
+    d = b.distill(b.ids[:, None].contiguous(), torch.zeros(R, 1, device="cuda"), temperature=tau, aggregation="token")
+    for f in (d.row_loss, d.loss, d.d_hidden, d.d_weight):
+        assert torch.equal(f, torch.zeros_like(f))
