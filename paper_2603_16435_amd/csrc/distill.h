@@ -428,15 +428,26 @@ __global__ __launch_bounds__(kTopThreads) void top_kernel(TopJob j) {
   __syncthreads();
 #pragma unroll
   for (int i = 0; i < kTopWaves; ++i) m = fmaxf(m, red_m[i]);
+  // The group of the largest logit once more, its logits added in f64: beside the largest's 1 an f32 sum keeps nothing of what a nearly certain token leaves to the others,
+  // and its entropy and log-probability are just that.  (Of equal ones a wavefront's first; there the 1s say all.)
   double s = 0.0, u = 0.0;
+  int top = -1;
 #pragma unroll
   for (int i = 0; i < REG; ++i) {
+    const unsigned long long at = __ballot(m > NEG && q[i].x == m);
+    if (at && top < 0) top = i * kTopThreads + w * 64 + __builtin_ctzll(at);
+  }
+  const float zt = top >= 0 && top * kGroup + lane < j.V ? j.z[tiled_index(t, top * kGroup + lane, j.ldz)] : NEG;
+#pragma unroll
+  for (int i = 0; i < REG; ++i) {
+    if (i * kTopThreads + tid == top) continue;
     if (q[i].x > NEG) {
       const float d = q[i].x - m, f = __builtin_amdgcn_exp2f(d * c);
       s += (double)f * (double)q[i].y;
       u += (double)f * ((double)q[i].z + (double)d * (double)q[i].y);
     } else if (q[i].y != q[i].y) s = __builtin_nan("");
   }
+  if (zt != NEG) { const float d = zt - m; const double e = __builtin_amdgcn_exp2f(d * c); s += e; u += e * (double)d; }
   s = wave_sum(s); u = wave_sum(u);
   if (lane == 0) { red_s[w] = s; red_u[w] = u; }
   __syncthreads();

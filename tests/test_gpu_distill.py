@@ -185,3 +185,19 @@ def test_certain_tokens(R, H, V, dtype, tau):
     d = b.distill(b.ids[:, None].contiguous(), torch.zeros(R, 1, device="cuda"), temperature=tau, aggregation="token")
     for f in (d.row_loss, d.loss, d.d_hidden, d.d_weight):
         assert torch.equal(f, torch.zeros_like(f))
+
+
+# a token nearly certain: entropy and its log-probability are small numbers of their own, not what is left of larger ones.  Both are sums of positive terms d^i e^-d over the others;
+# a difference to the maximum is exact, its product with c off by 1.3 u of itself (c 0.33 u at these temperatures), exp2 by 2 u, a group's sum by 24 u: with d below 100 each term by 156 u,
+# and 26 u for the sums' own roundings and the result's.  Where another token is the likely one, 26 u more from the logarithm of a sum.  (The oracle's differences in f64: 1e-13)
+@pytest.mark.parametrize("R,H,V,dtype", [(1, 64, 300, "bf16"), (40, 128, 3000, "bf16"), (300, 136, 65001, "bf16"), (3, 36, 200, "f32"), (200, 68, 777, "f32")])
+@pytest.mark.parametrize("lift,tau", [(1.0, 1.0), (1.5, 0.7), (2.0, 1.0)])
+def test_nearly_certain_tokens(R, H, V, dtype, lift, tau):
+    b = Batch(R, H, V, dtype, seed=R + 7, masked=0.0)
+    b.weight[:, 0], b.hidden[:, 0] = 0.0, 16.0
+    b.ids[:] = b.ids[0].clone()
+    b.weight[b.ids[0].long(), 0] = lift
+    r = b.score(2, tau)
+    want = orc.top_logprobs(host(b.hidden), host(b.weight), host(b.ids), host(b.mask), host(b.cu), 2, tau)
+    for f in ("entropy", "logprob"):
+        near(getattr(r, f), want[f], 182 * U * np.abs(want[f]) + (26 * U if f == "logprob" else 0) * (want[f] < -1) + 1e-13, f)
