@@ -1863,7 +1863,7 @@ rl_status rl_profile_read(rl_profile* out) {
   return st;
 }
 
-int32_t rl_version(void) { return 107; }
+int32_t rl_version(void) { return 108; }
 int32_t rl_default_chunk_rows(void) { return kDefaultChunkRows; }
 int32_t rl_default_chunk_rows_single_pass(void) { return kDefaultChunkRowsStash; }
 

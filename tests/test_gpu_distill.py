@@ -201,3 +201,25 @@ def test_nearly_certain_tokens(R, H, V, dtype, lift, tau):
     want = orc.top_logprobs(host(b.hidden), host(b.weight), host(b.ids), host(b.mask), host(b.cu), 2, tau)
     for f in ("entropy", "logprob"):
         near(getattr(r, f), want[f], 182 * U * np.abs(want[f]) + (26 * U if f == "logprob" else 0) * (want[f] < -1) + 1e-13, f)
+
+
+# lists that name next to nothing: with p, q ~ 1e-3 the divergence is ~ (p - q)^2 / q, far below the terms p (log p - log q) and p_r (log p_r - log q_r) that it is the sum of.  With each
+# log q_i off by e_i, at most SUM and 2 u d for the temperature's two roundings, 52 u at d < 10, KL moves by sum e_i (q_i p_r / q_r - p_i), and |p_r / q_r - 1| <= 1.25 sum |p - q|: at most
+# 1.25 x 52 u sum |p - q|.  The q_i that make q_r are exponentials, 4 u of each, times p_r / q_r <= 1.25
+@pytest.mark.parametrize("R,H,V,dtype", [(1, 64, 3000, "bf16"), (60, 128, 20000, "bf16"), (300, 136, 30001, "bf16"), (20, 68, 5000, "f32"), (150, 36, 7777, "f32")])
+@pytest.mark.parametrize("K", [1, 4])
+def test_lists_of_next_to_nothing(R, H, V, dtype, K):
+    tau = 2.9
+    b = Batch(R, H, V, dtype, seed=R + 3, masked=0.0, x_levels=16)
+    z = (b.hidden.double() @ b.weight.double().t()) / tau
+    lq = z - torch.logsumexp(z, 1, keepdim=True)
+    ids = torch.randint(V, (R, K), generator=b.g).cuda()
+    lp = (lq.gather(1, ids) + 0.1 * torch.randn(R, K, generator=b.g, dtype=torch.float64).cuda()).float()
+    ids = ids.int()
+    r = b.distill(ids, lp, temperature=tau, aggregation="token")
+    want = orc.distill(host(b.hidden), host(b.weight), host(ids), host(lp), host(b.mask), host(b.cu), "bucket", tau, "token", 1.0)
+    p, q = np.exp(host(lp).astype(np.float64)), np.exp(lq.gather(1, ids.long()).cpu().numpy())
+    both = (p + q).sum(1)
+    assert both.max() < 0.2
+    near(r.row_loss, want["row_loss"], 65 * U * np.abs(p - q).sum(1) + 5 * U * both + U * np.abs(want["row_loss"]), "row_loss")
+    check_distill(b, r, ids, lp, "bucket", tau, "token")
