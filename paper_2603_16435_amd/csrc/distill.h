@@ -1000,15 +1000,15 @@ struct HeadPlan {
   size_t off_z, off_rec, off_stats, off_term, off_info, off_rows, off_pids, off_pval, off_dw, off_few, total;
 };
 
-static int few_cols(int dtype) { return dtype == RL_BF16 ? 128 : 64; }       // of a wavefront
+static int few_cols(int dtype, int nt) { return dtype == RL_BF16 ? 128 : 16 * few_f32_blocks(nt); }       // of a wavefront
 // Batches of so few rows that both gradients are one pass over the weight, and their launch: a wavefront on each SIMD (us with 768, 1024, 1536, 2048 wavefronts: 36 rows, H 5120,
 // V 50257 266 233 269 242; 3 rows, H 3584, V 126849 368 355 409 358; 61 rows, H 2048, V 32000 69 67 85 85).
 static void few_plan(HeadPlan& h) {
   const Plan& p = h.p;
   h.few_nt = 0;
   if (p.R > (p.dtype == RL_BF16 ? kFewGradRows : kFewGradRowsF32)) return;
-  const int nt = p.R <= 16 ? 1 : p.R <= 32 ? 2 : 4;
-  const int cols = few_cols(p.dtype), step = p.dtype == RL_BF16 ? 32 : 16;
+  const int nt = p.R <= 16 ? 1 : p.R <= 32 ? 2 : p.dtype == RL_BF16 || (p.R > 48 && p.R <= 64) ? 4 : p.R <= 48 ? 3 : p.R <= 96 ? 6 : 8;
+  const int cols = few_cols(p.dtype, nt), step = p.dtype == RL_BF16 ? 32 : 16;
   const int hs = (p.H + cols - 1) / cols, all = (p.V + step - 1) / step;
   int splits = 4 * kHotSlots / hs;
   splits = splits < 1 ? 1 : splits > kFewSplits ? kFewSplits : splits;
@@ -1139,11 +1139,15 @@ static void run_few_grads(const rl_batch* b, const HeadPlan& h, const Ptrs& q, u
   }
   ProfScope ps(RL_PROF_GEMM_BWD, s);
   const FewGrads j{b->weight, b->hidden, p.V, p.H, q.row_map, &q.ctrl->n_real, ds1, ds2, out->d_weight, part, h.few_splits, h.few_steps};
-  const int cols = few_cols(p.dtype), hs = (p.H + cols - 1) / cols, waves = hs < 4 ? hs : 4, blocks = (hs + waves - 1) / waves * h.few_splits;
+  const int cols = few_cols(p.dtype, h.few_nt), hs = (p.H + cols - 1) / cols, waves = hs < 4 ? hs : 4, blocks = (hs + waves - 1) / waves * h.few_splits;
   if constexpr (sizeof(T) == 2) {
     auto kern = round ? few_grads_kernel<bf16_t>(h.few_nt) : few_grads_kernel<float>(h.few_nt);
     kern<<<blocks, 64 * waves, 0, s>>>(j);
-  } else (h.few_nt == 1 ? few_grads_f32_kernel<1> : few_grads_f32_kernel<2>)<<<blocks, 64 * waves, 0, s>>>(j);
+  } else {
+    auto kern = h.few_nt == 1 ? few_grads_f32_kernel<1> : h.few_nt == 2 ? few_grads_f32_kernel<2> : h.few_nt == 3 ? few_grads_f32_kernel<3> : h.few_nt == 4 ? few_grads_f32_kernel<4>
+                : h.few_nt == 6 ? few_grads_f32_kernel<6> : few_grads_f32_kernel<8>;
+    kern<<<blocks, 64 * waves, 0, s>>>(j);
+  }
   few_dx_kernel<T><<<(unsigned)(p.R * ((p.H + 63) / 64)), 256, 0, s>>>(part, h.few_splits, tokens, q.row_map, &q.ctrl->n_real, p.H, static_cast<T*>(out->d_hidden));
 }
 

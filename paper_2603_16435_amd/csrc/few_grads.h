@@ -1,13 +1,15 @@
 // few_grads.h - both gradients of a few rows, dX = dS W and dW = dS^T X, in one pass over the weight.
 //
-// With few rows (up to 64 in bf16, 32 in f32) both contractions are as large as the weight: W is read once, dW written once, and nothing else is of any size.
+// With few rows (up to 64 in bf16, 128 in f32) both contractions are as large as the weight: W is read once, dW written once, and nothing else is of any size; in f32 the
+// matrix unit bounds more than 48.
 // A wavefront takes 16 NB columns of W and a run of its rows, 32 (bf16) or 16 (f32) at a time, straight from memory into registers: the lane that loads eight (four)
 // consecutive columns of a row owns them as one column of each of eight (four) matrix blocks - which column of W a block's column is, is free to choose - so that the pieces of
 // a step are the operands of dX after a transpose of 8 x 8 values inside the lane (bf16), or as they are (f32).  Nothing passes through LDS and no
 // wavefront waits for another; the loads of the next two steps are out while a step is computed.  dW's blocks are laid such that a lane ends with
 // sixteen bytes of a row, and lane pairs exchange halves, so that a store writes whole lines.  dX is a sum over all rows of W: few_dx_kernel adds the runs'.
 // us of the pair of contractions, and here (TB/s of W and dW): 61 rows, H 2048, V 32000 86 and 67 (3.9); 36, 5120, 50257 357 and 233 (4.4); 20, 3584, 152064 679 and 444 (4.9);
-// 3, 3584, 126849 579 and 355 (5.1); f32 4 rows, 2048, 152064 1636 and 443 (5.6).
+// 3, 3584, 126849 579 and 355 (5.1); f32 4 rows, 2048, 152064 1636 and 443 (5.6); 48 rows, 3584, 152064 3070 and 1120 (3.9);
+// 64 and 128 rows 3110 and 1350, 3570 and 2620, 103 and 107 TF of the 152 that a large product reaches.
 // dS is wanted in the order of both operands, and small: few_ds_kernel writes two copies.  The wavefronts of a workgroup take the same run and
 // neighbouring columns, so that they find its dS in their L1.
 #pragma once
@@ -15,9 +17,10 @@
 
 namespace rlk {
 
-// Rows whose gradients these kernels take, by type.  More come as fast from the pair of contractions, whose tiles of 256 rows they fill better (us, pair and here: 100 rows, H 3584,
-// V 152064 685 and 691, 128 rows, H 1024, V 50000 68 and 74 with eight blocks of 16 tokens).
-constexpr int kFewGradRows = 64, kFewGradRowsF32 = 32;
+// Rows whose gradients these kernels take, by type.  bf16: more come as fast from the pair of contractions, whose tiles of 256 rows they fill better (us, pair and here: 100 rows, H 3584,
+// V 152064 685 and 691, 128 rows, H 1024, V 50000 68 and 74 with eight blocks of 16 tokens).  f32: eight blocks are what the registers hold; 128 rows, H 5120, V 151936 take 5100 and 3880,
+// H 2648, V 32000 580 and 430, H 512, V 1000 35 and 28.
+constexpr int kFewGradRows = 64, kFewGradRowsF32 = 128;
 constexpr int kFewSplits = 256;          // runs of the vocabulary, at most
 
 struct FewGrads {
@@ -36,17 +39,19 @@ template <class T> constexpr int few_step() { return sizeof(T) == 2 ? 32 : 16; }
 // A run's dX, to the partial buffer.  acc: [token block][column block]; column of block j, lane n: NB n + j.
 template <int NT, int NB>
 __device__ __attribute__((always_inline)) inline void few_dx_out(const floatx4 (&acc)[NT][NB], const FewGrads& j, int split, int h0) {
+  constexpr int PER = NB < 4 ? NB : 4;
+  typedef float piece __attribute__((ext_vector_type(PER)));
   const int lane = threadIdx.x & 63, g = lane >> 4, h = h0 + (lane & 15) * NB;
 #pragma unroll
   for (int b = 0; b < NT; ++b)
 #pragma unroll
     for (int i = 0; i < 4; ++i)
 #pragma unroll
-      for (int q = 0; q < NB / 4; ++q) {
-        floatx4 v;
+      for (int q = 0; q < NB; q += PER) {
+        piece v;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) v[e] = acc[b][q * 4 + e][i];
-        if (h + q * 4 < j.H) *reinterpret_cast<floatx4*>(j.part + ((int64_t)split * 16 * NT + b * 16 + g * 4 + i) * j.H + h + q * 4) = v;       // (H % 4 == 0)
+        for (int e = 0; e < PER; ++e) v[e] = acc[b][q + e][i];
+        if (h + q < j.H) *reinterpret_cast<piece*>(j.part + ((int64_t)split * 16 * NT + b * 16 + g * 4 + i) * j.H + h + q) = v;       // (H % 4 == 0)
       }
 }
 
@@ -187,9 +192,12 @@ __global__ __launch_bounds__(256, 1) void few_grads_bf16_kernel(FewGrads j) {
 }
 
 // f32: v_mfma_f32_16x16x4, 64 columns of a wavefront, 16 rows of W a step: lane group g loads rows 4 g .. 4 g + 3, and k-step s contracts row s of each group
+// (32 columns where there are more than 64 rows: what a wavefront holds of X and dX fits its registers)
+constexpr int few_f32_blocks(int nt) { return nt > 4 ? 2 : 4; }
 template <int NT>
 __global__ __launch_bounds__(256, 1) void few_grads_f32_kernel(FewGrads j) {
-  constexpr int T = 16 * NT, NB = 4, HW = 64;
+  constexpr int T = 16 * NT, NB = few_f32_blocks(NT), HW = 16 * NB;
+  typedef float wide __attribute__((ext_vector_type(NB)));
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane >> 4, n = lane & 15, odd = n & 1;
   const int hs = (j.H + HW - 1) / HW, waves = blockDim.x >> 6, cols = (hs + waves - 1) / waves, split = (int)blockIdx.x / cols;
   const int h0 = ((int)blockIdx.x % cols * waves + w) * HW;
@@ -210,7 +218,7 @@ __global__ __launch_bounds__(256, 1) void few_grads_f32_kernel(FewGrads j) {
       x[s][k] = row >= 0 && h < j.H ? X[(int64_t)row * j.H + h] : 0.f;
     }
   }
-  const int hl = h0 + n * 4 < j.H ? h0 + n * 4 : j.H - 4;
+  const int hl = h0 + n * NB < j.H ? h0 + n * NB : j.H - NB;
   const float* Wl = static_cast<const float*>(j.W) + hl;
   const floatx4* d1 = static_cast<const floatx4*>(j.ds1);
   const floatx4* d2 = static_cast<const floatx4*>(j.ds2);
@@ -222,14 +230,14 @@ __global__ __launch_bounds__(256, 1) void few_grads_f32_kernel(FewGrads j) {
 #pragma unroll
     for (int k = 0; k < NB; ++k) acc[b][k] = floatx4{0.f, 0.f, 0.f, 0.f};
 
-  struct Step { floatx4 w[4], a[NT], b[NT]; };
+  struct Step { wide w[4]; floatx4 a[NT], b[NT]; };
   auto load = [&](Step& s, int step) __attribute__((always_inline)) {
     step = step < last ? step : last - 1;
     const int v0 = step * 16;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       const int v = v0 + g * 4 + i;
-      s.w[i] = __builtin_nontemporal_load(reinterpret_cast<const floatx4*>(Wl + (int64_t)(v < j.V ? v : j.V - 1) * j.H));
+      s.w[i] = __builtin_nontemporal_load(reinterpret_cast<const wide*>(Wl + (int64_t)(v < j.V ? v : j.V - 1) * j.H));
     }
 #pragma unroll
     for (int b = 0; b < NT; ++b) {

@@ -79,7 +79,7 @@ def test_every_kernel_is_launched(trace):
                             calls.append(distill(R, H, V, dtype=dtype, off=off, dw=dw))
     calls += [score(70, 2048, 90000), distill(100000, 2816, 152064, chunk=40000, dw=1), score(9, 5200, 16000, dtype=0), score(20, 5200, 16000, dtype=0)]
     calls += [distill(800000, 3584, 1000), score(800000, 3584, 1000), score(800000, 3592, 1000), distill(100000, 1344, 152064, chunk=40000), distill(100000, 1344, 152064, chunk=40000, dw=1),
-              distill(50, 64, 300, bwd=0)]
+              distill(50, 64, 300, bwd=0), distill(60, 64, 300, dtype=0), distill(128, 64, 300, dtype=0)]
     calls += [score(R, H, V, B=B, dtype=dtype) for R in (1, 17, 33, 70) for H in (64, 300, 5200) for V in (3000, 16000, 20000, 40000, 98000, 140000) for B in (1, 100) for dtype in (0, 1)]
     met = {name for i in range(0, len(calls), 200) for _, _, launches in trace(calls[i:i + 200]) for _, _, name in launches}
     mine = {k for k in trace.kernels if re.search("EpiScore|top_kernel|distill|few_grads|few_ds|few_dx|few_patch|EpiDWRounded", k)}

@@ -223,3 +223,14 @@ def test_lists_of_next_to_nothing(R, H, V, dtype, K):
     assert both.max() < 0.2
     near(r.row_loss, want["row_loss"], 65 * U * np.abs(p - q).sum(1) + 5 * U * both + U * np.abs(want["row_loss"]), "row_loss")
     check_distill(b, r, ids, lp, "bucket", tau, "token")
+
+
+# f32, up to 128 rows: every number of token blocks, 64 and 32 columns of a wavefront, whole and not, vocabularies inside a step and past the last whole one, and a row more
+@pytest.mark.parametrize("R,H,V", [(48, 100, 1001), (49, 516, 300), (64, 64, 48), (65, 36, 777), (80, 1028, 40), (96, 132, 2003), (97, 4, 33), (128, 516, 5003), (128, 32, 16), (120, 92, 30001), (129, 68, 999)])
+@pytest.mark.parametrize("off", [0, 1])
+def test_few_rows_f32(R, H, V, off):
+    b = Batch(R, H, V, "f32", seed=R + H + 1, masked=0.1)
+    ids, lp = b.teacher(5)
+    if off:
+        b.weight, b.hidden = off_grid(b.weight, off), off_grid(b.hidden, off)
+    check_distill(b, b.distill(ids, lp), ids, lp, "bucket", 1.0, "sequence")
