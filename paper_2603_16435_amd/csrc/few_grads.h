@@ -237,7 +237,9 @@ __global__ __launch_bounds__(256, 1) void few_grads_f32_kernel(FewGrads j) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       const int v = v0 + g * 4 + i;
-      s.w[i] = __builtin_nontemporal_load(reinterpret_cast<const wide*>(Wl + (int64_t)(v < j.V ? v : j.V - 1) * j.H));
+      const wide* p = reinterpret_cast<const wide*>(Wl + (int64_t)(v < j.V ? v : j.V - 1) * j.H);
+      if (lines) s.w[i] = __builtin_nontemporal_load(p);                // (otherwise lines are shared with the neighbour: 2 rows, H 4904, V 151936 2340 -> 2130 us)
+      else s.w[i] = *p;
     }
 #pragma unroll
     for (int b = 0; b < NT; ++b) {
