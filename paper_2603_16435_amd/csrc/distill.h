@@ -580,6 +580,7 @@ struct DistillJob {
   float *row_loss, *lse;
   double* term;                         // [compact row] this row's part of the loss
   int* info;                            // [compact row] entries left out, bit 30: empty
+  int* x_rows;                          // [compact row] its row of hidden states, -1 if empty: a gradient of 0 times an infinity or a NaN would be one.  NULL without backward
   DistillRow* rows; int* p_ids; float* p_val;          // [chunk row], [chunk row][K]: the tokens that are listed and their dS (-1: none); NULL without backward
 };
 // Sequence of compact row t: the last i with cstart[i] <= t, 64 at a time.
@@ -773,6 +774,7 @@ __global__ __launch_bounds__(kTopThreads) void distill_row_kernel(DistillJob j) 
     DistillRow d{m, (float)(ln * 1.4426950408889634), nothing ? 0.f : (float)(f * P), 0.f};
     if (pr > 0.0 && !nothing) { d.m = mr; d.l2 = (float)(lnr * 1.4426950408889634); d.f = (float)(f * (P * qr - pr)); }
     j.rows[t] = d;
+    j.x_rows[tg] = nothing ? -1 : row;
   }
   if (tid < K) {
     j.p_ids[(int64_t)t * K + tid] = in && !nothing ? id : -1;
@@ -892,7 +894,7 @@ __global__ __launch_bounds__(1024) void distill_finish_kernel(FinishJob j) { dis
 
 // dS of a chunk, and beside it what else is wanted by then: X^T, in the first chunk's launch the rows of dX that do not count as 0, in the last one's the loss (term != NULL).  Workgroups, in
 // this order: the loss, n_ds, n_xt, and the rest.
-struct XtJob { const void* x; int64_t R; int H, cols, n_ds, n_xt, fast; const int *row_map, *cpos; void *xt, *dX; int tc; };
+struct XtJob { const void* x; int64_t R; int H, cols, n_ds, n_xt, fast; const int *x_rows, *cpos; void *xt, *dX; int tc; };
 template <class T>
 __global__ __launch_bounds__(256) void distill_ds_kernel(DsJob j, T* dS, int64_t ld_ds, T* dST, int64_t ld_dst, XtJob x, FinishJob fin) {
   __shared__ union { float f[64][65]; unsigned b[64][33]; bf16_t h[64][65]; } tile;
@@ -911,9 +913,9 @@ __global__ __launch_bounds__(256) void distill_ds_kernel(DsJob j, T* dS, int64_t
   if (b < x.n_xt) {
     const int bx = b % x.cols, by = b / x.cols;
     if constexpr (sizeof(T) == 2) {
-      if (x.fast) transpose_bf16_block(bx, by, tile.b, X, x.H, x.tc, x.H, x.row_map, j.ctrl, j.chunk_start, 1, nullptr, nullptr, XT, x.tc, x.tc);
-      else transpose_block(TransposeJob<T>{X, x.H, x.tc, x.H, x.row_map, j.ctrl, j.chunk_start, 1, nullptr, nullptr, XT, x.tc, x.tc, true}, bx, by, tile.h);
-    } else transpose_block(TransposeJob<T>{X, x.H, x.tc, x.H, x.row_map, j.ctrl, j.chunk_start, 1, nullptr, nullptr, XT, x.tc, x.tc, false}, bx, by, tile.f);
+      if (x.fast) transpose_bf16_block(bx, by, tile.b, X, x.H, x.tc, x.H, x.x_rows, j.ctrl, j.chunk_start, 1, nullptr, nullptr, XT, x.tc, x.tc);
+      else transpose_block(TransposeJob<T>{X, x.H, x.tc, x.H, x.x_rows, j.ctrl, j.chunk_start, 1, nullptr, nullptr, XT, x.tc, x.tc, true}, bx, by, tile.h);
+    } else transpose_block(TransposeJob<T>{X, x.H, x.tc, x.H, x.x_rows, j.ctrl, j.chunk_start, 1, nullptr, nullptr, XT, x.tc, x.tc, false}, bx, by, tile.f);
     return;
   }
   b -= x.n_xt;
@@ -997,7 +999,7 @@ struct HeadPlan {
   Plan p;
   int K, groups;
   int few_nt, few_splits, few_steps;        // few rows (few_grads.h): blocks of 16 tokens (0: not few), runs of the vocabulary, steps of a wavefront
-  size_t off_z, off_rec, off_stats, off_term, off_info, off_rows, off_pids, off_pval, off_dw, off_few, total;
+  size_t off_z, off_rec, off_stats, off_term, off_info, off_rows, off_pids, off_pval, off_xrows, off_dw, off_few, total;
 };
 
 static int few_cols(int dtype, int nt) { return dtype == RL_BF16 ? 128 : 16 * few_f32_blocks(nt); }       // of a wavefront
@@ -1040,7 +1042,7 @@ static rl_status head_plan(const rl_batch* b, int K, int chunk_rows, float tempe
   const size_t tc = (size_t)p.Tc, R = (size_t)p.R;
   h.off_z = take(4 * tc * (size_t)p.Vp);
   h.off_rec = take(sizeof(float4) * tc * (size_t)h.groups);
-  h.off_stats = h.off_term = h.off_info = h.off_rows = h.off_pids = h.off_pval = h.off_dw = h.off_few = 0;
+  h.off_stats = h.off_term = h.off_info = h.off_rows = h.off_pids = h.off_pval = h.off_xrows = h.off_dw = h.off_few = 0;
   h.few_nt = 0;
   if (distill) {
     h.off_stats = take(sizeof(rl_stats));
@@ -1048,6 +1050,7 @@ static rl_status head_plan(const rl_batch* b, int K, int chunk_rows, float tempe
     if (bwd) {
       h.off_rows = take(sizeof(DistillRow) * tc);
       h.off_pids = take(4 * tc * (size_t)K); h.off_pval = take(4 * tc * (size_t)K);
+      h.off_xrows = take(4 * R);
       few_plan(h);
       if (h.few_nt) h.off_few = take(4 * (size_t)h.few_splits * (size_t)h.few_nt * 16 * (size_t)p.H);
       if (round_dw && p.n_chunks > 1) h.off_dw = take(4 * (size_t)p.V * (size_t)p.H);
@@ -1135,10 +1138,10 @@ static void run_few_grads(const rl_batch* b, const HeadPlan& h, const Ptrs& q, u
   {
     ProfScope ps(RL_PROF_GEMM_DS, s);
     few_ds_kernel<T><<<1 + n_ds + zero, 256, 0, s>>>(ds, (const int*)(w + h.off_pids), (const float*)(w + h.off_pval), h.K, tokens, pitch, ds1, ds2,
-                                                     XtJob{nullptr, p.R, p.H, 0, n_ds, 0, 0, q.row_map, q.cpos, nullptr, out->d_hidden, p.Tc}, fin);
+                                                     XtJob{nullptr, p.R, p.H, 0, n_ds, 0, 0, nullptr, q.cpos, nullptr, out->d_hidden, p.Tc}, fin);
   }
   ProfScope ps(RL_PROF_GEMM_BWD, s);
-  const FewGrads j{b->weight, b->hidden, p.V, p.H, q.row_map, &q.ctrl->n_real, ds1, ds2, out->d_weight, part, h.few_splits, h.few_steps};
+  const FewGrads j{b->weight, b->hidden, p.V, p.H, (const int*)(w + h.off_xrows), &q.ctrl->n_real, ds1, ds2, out->d_weight, part, h.few_splits, h.few_steps};
   const int cols = few_cols(p.dtype, h.few_nt), hs = (p.H + cols - 1) / cols, waves = hs < 4 ? hs : 4, blocks = (hs + waves - 1) / waves * h.few_splits;
   if constexpr (sizeof(T) == 2) {
     auto kern = round ? few_grads_kernel<bf16_t>(h.few_nt) : few_grads_kernel<float>(h.few_nt);
@@ -1165,6 +1168,7 @@ static void run_distill(const rl_batch* b, const HeadPlan& h, const Ptrs& q, uns
   DistillRow* rows = bwd ? (DistillRow*)(w + h.off_rows) : nullptr;
   int* p_ids = (int*)(w + h.off_pids);
   float* p_val = (float*)(w + h.off_pval);
+  int* x_rows = bwd ? (int*)(w + h.off_xrows) : nullptr;
   const FinishJob fin{(const double*)(w + h.off_term), (const int*)(w + h.off_info), q.ctrl, (const rl_stats*)(w + h.off_stats), out->loss, out->stats};
   const bool few = bwd && h.few_nt && reinterpret_cast<uintptr_t>(W) % 16 == 0;
   if (bwd && !few && !p.k_major_w) {
@@ -1179,7 +1183,7 @@ static void run_distill(const rl_batch* b, const HeadPlan& h, const Ptrs& q, uns
       ProfScope ps(RL_PROF_COMBINE, s);
       launch_distill_rows(DistillJob{z, p.Vp, rec, p.Tc, h.groups, p.V, h.K, p.inv_tau, q.row_map, q.cstart, q.ctrl, c0, p.Tc, p.B, t_ids, t_lp, prm->rest,
                                      prm->aggregation == RL_AGG_TOKEN, prm->scale == 0.f ? 1.f : prm->scale, out->row_loss, out->lse,
-                                     (double*)(w + h.off_term), (int*)(w + h.off_info), rows, p_ids, p_val}, n, s);
+                                     (double*)(w + h.off_term), (int*)(w + h.off_info), x_rows, rows, p_ids, p_val}, n, s);
     }
     if (!bwd) continue;
     if (few) {
@@ -1195,7 +1199,7 @@ static void run_distill(const rl_batch* b, const HeadPlan& h, const Ptrs& q, uns
       const bool last = ch + 1 == p.n_chunks;
       distill_ds_kernel<T><<<(unsigned)(last + n_ds + n_xt + (zero < 16384 ? zero : 16384)), 256, 0, s>>>(
           DsJob{z, p.Vp, rows, q.ctrl, c0, p.V, p.inv_tau}, plain, p.Vp, dST, p.Tc,
-          XtJob{X, p.R, p.H, cols, n_ds, n_xt, reinterpret_cast<uintptr_t>(X) % 16 == 0, q.row_map, q.cpos, q.xt, out->d_hidden, p.Tc}, last ? fin : FinishJob{});
+          XtJob{X, p.R, p.H, cols, n_ds, n_xt, reinterpret_cast<uintptr_t>(X) % 16 == 0, x_rows, q.cpos, q.xt, out->d_hidden, p.Tc}, last ? fin : FinishJob{});
       distill_patch_kernel<T><<<(unsigned)((n * h.K + 255) / 256), 256, 0, s>>>(p_ids, p_val, h.K, q.ctrl, c0, p.Tc, plain, p.Vp, dST, p.Tc);
     }
     contract_grads<T>(b, p, q, ch, out->d_hidden, dw, s, round ? static_cast<bf16_t*>(out->d_weight) : nullptr);

@@ -25,7 +25,7 @@ constexpr int kFewSplits = 256;          // runs of the vocabulary, at most
 
 struct FewGrads {
   const void* W; const void* X; int V, H;
-  const int* row_map; const int* n_real;
+  const int* x_rows; const int* n_real;  // [compact row] its row of X (-1: one of zeros)
   const void* ds1;                       // bf16 [V / 32][tokens][32], f32 [V / 16][tokens][16]
   const void* ds2;                       // [V][tokens rounded up to 32 (bf16)]
   void* dW;
@@ -102,7 +102,7 @@ __global__ __launch_bounds__(256, 1) void few_grads_bf16_kernel(FewGrads j) {
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
       const int t = s * 32 + g * 8 + i;
-      const int row = t < rows ? j.row_map[t] : -1;
+      const int row = t < rows ? j.x_rows[t] : -1;
 #pragma unroll
       for (int k = 0; k < NB; ++k) {
         const int h = h0 + 32 * (k >> 1) + 8 * (n >> 2) + 4 * (k & 1) + (n & 3);
@@ -211,7 +211,7 @@ __global__ __launch_bounds__(256, 1) void few_grads_f32_kernel(FewGrads j) {
 #pragma unroll
   for (int s = 0; s < 4 * NT; ++s) {
     const int t = (s >> 2) * 16 + g * 4 + (s & 3);
-    const int row = t < rows ? j.row_map[t] : -1;
+    const int row = t < rows ? j.x_rows[t] : -1;
 #pragma unroll
     for (int k = 0; k < NB; ++k) {
       const int h = h0 + 16 * k + n;

@@ -1048,8 +1048,8 @@ __device__ inline void transpose_block(const TransposeJob<T>& j, int bx, int by,
   for (int k = ty; k < 64; k += 4) {
     const int r = r0 + k, c = c0 + tx;
     T v = (T)0.f;
-    if (r < rv && c < j.cols) {
-      const int64_t sr = j.row_idx ? (int64_t)j.row_idx[chunk_start + r] : (int64_t)r;
+    const int64_t sr = r < rv ? (j.row_idx ? (int64_t)j.row_idx[chunk_start + r] : (int64_t)r) : -1;       // (-1: a row of zeros)
+    if (sr >= 0 && c < j.cols) {
       v = j.src[sr * j.ld_src + c];
       if (j.row_scale) v = (T)((float)v * j.row_scale[r]);
     }
@@ -1114,8 +1114,8 @@ __device__ __attribute__((always_inline)) inline void transpose_bf16_block(int b
   for (int p = 0; p < 2; ++p) {
     const int k = k0 + 32 * p, r = r0 + k, c = c0 + 8 * ch;
     uint4 v = make_uint4(0, 0, 0, 0);
-    if (r < rv && c < cols) {
-      const int64_t sr = row_idx ? (int64_t)row_idx[chunk_start + r] : (int64_t)r;
+    const int64_t sr = r < rv ? (row_idx ? (int64_t)row_idx[chunk_start + r] : (int64_t)r) : -1;           // (-1: a row of zeros)
+    if (sr >= 0 && c < cols) {
       v = *reinterpret_cast<const uint4*>(src + sr * ld_src + c);
       if (row_scale) {
         const float f = row_scale[r];
