@@ -580,7 +580,7 @@ struct DistillJob {
   float *row_loss, *lse;
   double* term;                         // [compact row] this row's part of the loss
   int* info;                            // [compact row] entries left out, bit 30: empty
-  int* x_rows;                          // [compact row] its row of hidden states, -1 if empty: a gradient of 0 times an infinity or a NaN would be one.  NULL without backward
+  int* x_rows;                          // [compact row] its row of hidden states, -1 if empty: a gradient of 0 times what is no number would be none.  NULL without backward
   DistillRow* rows; int* p_ids; float* p_val;          // [chunk row], [chunk row][K]: the tokens that are listed and their dS (-1: none); NULL without backward
 };
 // Sequence of compact row t: the last i with cstart[i] <= t, 64 at a time.
@@ -1151,7 +1151,7 @@ static void run_few_grads(const rl_batch* b, const HeadPlan& h, const Ptrs& q, u
                 : h.few_nt == 6 ? few_grads_f32_kernel<6> : few_grads_f32_kernel<8>;
     kern<<<blocks, 64 * waves, 0, s>>>(j);
   }
-  few_dx_kernel<T><<<(unsigned)(p.R * ((p.H + 63) / 64)), 256, 0, s>>>(part, h.few_splits, tokens, q.row_map, &q.ctrl->n_real, p.H, static_cast<T*>(out->d_hidden));
+  few_dx_kernel<T><<<(unsigned)(p.R * ((p.H + 63) / 64)), 256, 0, s>>>(part, h.few_splits, tokens, q.row_map, j.x_rows, &q.ctrl->n_real, p.H, static_cast<T*>(out->d_hidden));
 }
 
 template <class T>
@@ -1202,7 +1202,7 @@ static void run_distill(const rl_batch* b, const HeadPlan& h, const Ptrs& q, uns
           XtJob{X, p.R, p.H, cols, n_ds, n_xt, reinterpret_cast<uintptr_t>(X) % 16 == 0, x_rows, q.cpos, q.xt, out->d_hidden, p.Tc}, last ? fin : FinishJob{});
       distill_patch_kernel<T><<<(unsigned)((n * h.K + 255) / 256), 256, 0, s>>>(p_ids, p_val, h.K, q.ctrl, c0, p.Tc, plain, p.Vp, dST, p.Tc);
     }
-    contract_grads<T>(b, p, q, ch, out->d_hidden, dw, s, round ? static_cast<bf16_t*>(out->d_weight) : nullptr);
+    contract_grads<T>(b, p, q, ch, out->d_hidden, dw, s, round ? static_cast<bf16_t*>(out->d_weight) : nullptr, x_rows);
   }
   if (bwd) return;
   ProfScope ps(RL_PROF_LOSS, s);

@@ -754,14 +754,15 @@ struct EpiDX {
 };
 
 // The slices of a split dX contraction added up in order, scaled and scattered to the original rows (four columns per
-// thread, H % 4 == 0; `step`: elements of K per step of the cut).  Works the number of slices out like the contraction itself; returns at once if there was one.
-template <class T>
-__global__ __launch_bounds__(256) void splitk_reduce_kernel(GemmDims d, EpiDX<T> e, int bm, int bn, int step) {
+// thread, H % 4 == 0; `step`: elements of K per step of the cut).  Works the number of slices out like the contraction itself, and is done if there was one.
+// empty(m): rows that read 0 whatever the slices hold.  Rows that the contraction wrote itself are left: how many there are comes back, 0 where they were added up here.
+template <class T, class EMPTY>
+__device__ __attribute__((always_inline)) inline int splitk_reduce(GemmDims& d, const EpiDX<T>& e, int bm, int bn, int step, EMPTY empty) {
   int M, N, K;
-  if (!resolve_dims(d, M, N, K)) return;
+  if (!resolve_dims(d, M, N, K)) return 0;
   const int tiles_m = (M + bm - 1) / bm;
   const SplitK sk = split_k(tiles_m * ((d.N + bn - 1) / bn), (K + step - 1) / step, d.split_slots, fill_steps(d, M));
-  if (sk.slices == 1) return;
+  if (sk.slices == 1) return M;
   const int64_t stride = (int64_t)tiles_m * bm * e.H;
   const int h4 = e.H / 4;
   for (int64_t q = (int64_t)blockIdx.x * 256 + threadIdx.x; q < (int64_t)M * h4; q += (int64_t)gridDim.x * 256) {
@@ -777,9 +778,21 @@ __global__ __launch_bounds__(256) void splitk_reduce_kernel(GemmDims d, EpiDX<T>
     }
     const float f = e.row_scale ? e.row_scale[m] : 1.f;
     T* o = e.dX + (int64_t)e.row_map[d.chunk_start + m] * e.ldx + n;
+    const bool zero = empty(m);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) o[i] = (T)(f * s[i]);
+    for (int i = 0; i < 4; ++i) o[i] = zero ? (T)0.f : (T)(f * s[i]);
   }
+  return 0;
+}
+template <class T>
+__global__ __launch_bounds__(256) void splitk_reduce_kernel(GemmDims d, EpiDX<T> e, int bm, int bn, int step) { splitk_reduce(d, e, bm, bn, step, [](int) { return false; }); }
+// ... of distillation: rows without entries (x_rows[compact row] < 0) become 0, also where nothing was cut: 0 times an infinity or a NaN of W is no number
+template <class T>
+__global__ __launch_bounds__(256) void distill_splitk_reduce_kernel(GemmDims d, EpiDX<T> e, int bm, int bn, int step, const int* x_rows) {
+  const int M = splitk_reduce(d, e, bm, bn, step, [&](int m) { return x_rows[d.chunk_start + m] < 0; });
+  for (int m = (int)blockIdx.x * 4 + (int)(threadIdx.x >> 6); m < M; m += (int)gridDim.x * 4)
+    if (x_rows[d.chunk_start + m] < 0)
+      for (int n = threadIdx.x & 63; n < e.H; n += 64) e.dX[(int64_t)e.row_map[d.chunk_start + m] * e.ldx + n] = (T)0.f;
 }
 
 // ---- backward, stage 3: dW tile, f32, overwritten by the first chunk and accumulated after.

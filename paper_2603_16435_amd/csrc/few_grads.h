@@ -278,9 +278,9 @@ __global__ __launch_bounds__(256, 1) void few_grads_f32_kernel(FewGrads j) {
   few_dx_out<NT, NB>(acc, j, split, h0);
 }
 
-// dX: the runs' sums added in a fixed order, to the rows that count: 64 columns of a row by a workgroup, thread (q, k) = (i % 16, i / 16) adds up runs k, k + 16, ... of four of them
+// dX: the runs' sums added in a fixed order, to the rows that count, 0 to those without entries (x_rows < 0) whatever W holds: 64 columns of a row by a workgroup, thread (q, k) = (i % 16, i / 16) adds up runs k, k + 16, ... of four of them
 template <class T>
-__global__ __launch_bounds__(256) void few_dx_kernel(const float* part, int splits, int tokens, const int* row_map, const int* n_real, int H, T* dX) {
+__global__ __launch_bounds__(256) void few_dx_kernel(const float* part, int splits, int tokens, const int* row_map, const int* x_rows, const int* n_real, int H, T* dX) {
   __shared__ floatx4 sum[16][16];
   const int hb = (H + 63) / 64, t = (int)blockIdx.x / hb, q = threadIdx.x & 15, k = threadIdx.x >> 4, h = ((int)blockIdx.x % hb) * 64 + q * 4;
   if (t >= *n_real) return;
@@ -299,8 +299,9 @@ __global__ __launch_bounds__(256) void few_dx_kernel(const float* part, int spli
 #pragma unroll
   for (int i = 1; i < 16; ++i) s += sum[i][q];
   T* o = dX + (int64_t)row_map[t] * H + h;
+  const bool empty = x_rows[t] < 0;
 #pragma unroll
-  for (int e = 0; e < 4; ++e) o[e] = (T)s[e];
+  for (int e = 0; e < 4; ++e) o[e] = empty ? (T)0.f : (T)s[e];
 }
 
 }  // namespace rlk

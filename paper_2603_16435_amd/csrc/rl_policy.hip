@@ -1460,12 +1460,18 @@ static void launch_gemm(const float* A, const float* B, const GemmDims& d, const
   else gemm_nt_kernel<float, Epi, kBM, kF32SmallBN, 4, 1><<<tiles, 256, 0, s>>>(A, B, d, epi);
 }
 
+template <class T>
+static void launch_splitk_reduce(const GemmDims& dx, const EpiDX<T>& ex, int bm, int bn, int step, const int* x_rows, hipStream_t s) {
+  if (x_rows) distill_splitk_reduce_kernel<T><<<512, 256, 0, s>>>(dx, ex, bm, bn, step, x_rows);
+  else splitk_reduce_kernel<T><<<512, 256, 0, s>>>(dx, ex, bm, bn, step);
+}
+
 // dX = diag(f) dS W  (A = dS or E' [Tc][Vp], B = W^T [H][Vp]) and dW (+)= dS^T (diag(f) X)  (A = the same array read as a K-major
 // operand, B = X^T [H][Tc]) of a bf16 chunk in one launch: dX alone has few (long) tiles, whose last round would leave CUs
 // idle; the dW tiles fill them.  dX is cut along K where its tiles are fewer still.
 template <class EDW>
 static void launch_dx_dw(const bf16_t* E, const bf16_t* W, const bf16_t* WT, GemmDims dx, EpiDX<bf16_t> ex, const bf16_t* XT, const GemmDims& dw,
-                         const EDW& ew, hipStream_t s) {
+                         const EDW& ew, const int* x_rows, hipStream_t s) {
   const int tn = (dx.N + kBN - 1) / kBN;
   dx.split_slots = kHotSlots; dx.fill_tiles = (dw.M + kBM - 1) / kBM * tn;
   const int n1 = split_launch((dx.M + kBM - 1) / kBM, tn, kHotSlots);
@@ -1478,7 +1484,7 @@ static void launch_dx_dw(const bf16_t* E, const bf16_t* W, const bf16_t* WT, Gem
     dx.ldb = dx.N; dx.b_k_rows = dw.M;
     gemm_nt_bf16_pair_kernel<EpiDX<bf16_t>, TuneDX, EDW, TuneDW, true><<<n1 + n2, 256, 0, s>>>(E, W, dx, ex, n1, E, XT, dw, ew, 0, 0);
   }
-  splitk_reduce_kernel<bf16_t><<<512, 256, 0, s>>>(dx, ex, kBM, kBN, kHotStep);
+  launch_splitk_reduce(dx, ex, kBM, kBN, kHotStep, x_rows, s);
 }
 
 // The combine of a small f32 batch inside its loss launch, also where no gradients are asked for: up to 1024 rows, which are four tokens of a thread at most.
@@ -1626,8 +1632,9 @@ static void run_forward(const rl_batch* b, const Plan& p, const Ptrs& q, float* 
 }
 
 // dX and dW (+)= of chunk ch, out of its dS (and dS^T for f32 inputs), X^T and W or W^T.  rounded (bf16): where the last chunk's dW goes, d_weight having the sums of the others.
+// x_rows: [compact row] -1 where a row's dX is 0 whatever W holds (NULL: none).
 template <class T>
-static void contract_grads(const rl_batch* b, const Plan& p, const Ptrs& q, int ch, void* d_hidden, float* d_weight, hipStream_t s, bf16_t* rounded = nullptr) {
+static void contract_grads(const rl_batch* b, const Plan& p, const Ptrs& q, int ch, void* d_hidden, float* d_weight, hipStream_t s, bf16_t* rounded = nullptr, const int* x_rows = nullptr) {
   const T* W = static_cast<const T*>(b->weight);
   T* WT = static_cast<T*>(q.wt); T* XT = static_cast<T*>(q.xt);
   T* dS = static_cast<T*>(q.ds); T* dST = static_cast<T*>(q.dst);
@@ -1649,22 +1656,22 @@ static void contract_grads(const rl_batch* b, const Plan& p, const Ptrs& q, int 
     ProfScope ps(RL_PROF_GEMM_BWD, s);
     if (rounded && ch + 1 == p.n_chunks) {
       dw.zero_if_empty = true;
-      launch_dx_dw(dS, W, p.k_major_w ? nullptr : WT, dx, ex, XT, dw, EpiDWRounded{rounded, p.H, p.V, p.H, ch > 0 ? d_weight : nullptr}, s);
-    } else launch_dx_dw(dS, W, p.k_major_w ? nullptr : WT, dx, ex, XT, dw, ew, s);
+      launch_dx_dw(dS, W, p.k_major_w ? nullptr : WT, dx, ex, XT, dw, EpiDWRounded{rounded, p.H, p.V, p.H, ch > 0 ? d_weight : nullptr}, x_rows, s);
+    } else launch_dx_dw(dS, W, p.k_major_w ? nullptr : WT, dx, ex, XT, dw, ew, x_rows, s);
   } else {
     dx.split_slots = kF32Slots;
     if (p.small_pair) {
       ProfScope ps(RL_PROF_GEMM_BWD, s);
       const int n1 = split_launch((dx.M + 63) / 64, (dx.N + kF32SmallBN - 1) / kF32SmallBN, kF32Slots);
       gemm_nt_small_pair_kernel<<<n1 + launch_tiles((dw.M + 63) / 64, (dw.N + kF32SmallBN - 1) / kF32SmallBN), 1024, 0, s>>>(dS, WT, dx, ex, n1, dST, XT, dw, ew);
-      splitk_reduce_kernel<T><<<512, 256, 0, s>>>(dx, ex, 64, kF32SmallBN, 128);
+      launch_splitk_reduce(dx, ex, 64, kF32SmallBN, 128, x_rows, s);
       return;
     }
     {
       ProfScope ps(RL_PROF_GEMM_DX, s);
       if (p.k_major_w) { dx.lda = p.Tc; dx.ldb = p.H; dx.b_k_rows = p.V; }
       launch_gemm<TuneDX>(p.k_major_w ? dST : dS, p.k_major_w ? W : WT, dx, ex, s);
-      splitk_reduce_kernel<T><<<512, 256, 0, s>>>(dx, ex, kBM, f32_tile_n(dx.M, dx.N, dx.K, true), 32);
+      launch_splitk_reduce(dx, ex, kBM, f32_tile_n(dx.M, dx.N, dx.K, true), 32, x_rows, s);
     }
     ProfScope ps(RL_PROF_GEMM_DW, s);
     launch_gemm<TuneDW>(dST, XT, dw, ew, s);
@@ -1814,7 +1821,7 @@ static void run_fused(const rl_batch* b, const rl_params* prm, int objective, co
       dw.chunk = chunk; dw.dyn = 3; dw.k_round = 256; dw.zero_if_empty = (k == 0); dw.group_m = TuneDW::kBand;
       EpiDW ew{out->d_weight, p.H, p.V, p.H, k > 0 ? 1 : 0};
       ProfScope ps(RL_PROF_GEMM_BWD, s);
-      launch_dx_dw(E, W, p.k_major_w ? nullptr : WT, dx, ex, XT, dw, ew, s);
+      launch_dx_dw(E, W, p.k_major_w ? nullptr : WT, dx, ex, XT, dw, ew, nullptr, s);
     }
   }
   ProfScope ps(RL_PROF_LOSS, s);

@@ -2,6 +2,7 @@
 import pytest
 import torch
 
+from paper_2603_16435_amd import binding
 from test_gpu_distill import Batch, DTYPES, off_grid
 
 pytestmark = pytest.mark.gpu
@@ -44,3 +45,26 @@ def test_a_row_without_a_list_has_no_part_in_the_weight_gradient(R, H, V, dtype,
     for f in ("loss", "row_loss", "d_hidden", "d_weight", "stats"):
         assert torch.equal(getattr(got, f), getattr(want, f)), f
     assert not got.d_hidden[gone].any() and not got.row_loss[gone].any() and int(got.stats[2]) >= int((gone & (b.mask != 0)).sum())
+
+
+@pytest.mark.parametrize("R,H,V,dtype,chunk,off", ROUTES)
+def test_a_row_without_a_list_has_no_gradient_whatever_the_weight_holds(R, H, V, dtype, chunk, off):
+    b = Batch(R, H, V, dtype, seed=R + 1, masked=0.1)
+    ids, lp = b.teacher(5)
+    if off:
+        b.weight = off_grid(b.weight, off)
+    without_lists(b, ids, lp, "bucket")
+    gone = ((ids < 0) | (ids >= V)).all(1)
+    b.weight[V // 2, 1], b.weight[V - 1, 0] = float("nan"), float("inf")
+    kw = dict(chunk_rows=chunk, d_weight_dtype=DTYPES[dtype])
+    r = b.distill(ids, lp, **kw)
+    counts = b.mask != 0
+    assert not r.d_hidden[gone | ~counts].any() and not r.row_loss[gone | ~counts].any()
+    assert bool(r.row_loss[counts & ~gone].isnan().all())
+    x = b.hidden.clone()
+    over = binding.rl_distill_loss_fwd_bwd(x, b.weight, ids, lp, b.mask, b.cu, d_hidden=x, **kw)
+    assert not over.d_hidden[gone | ~counts].any()
+    ids.fill_(-1)
+    r = b.distill(ids, lp, **kw)
+    for f in (r.loss, r.row_loss, r.d_hidden, r.d_weight):
+        assert not f.any()
