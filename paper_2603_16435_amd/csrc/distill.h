@@ -10,7 +10,7 @@
 //    all of the probability.
 // What is read of the logits once more is the whole chunk, by the backward, which turns it into dS in one pass.
 //
-// Sums: those of a group in f32, of groups in f64, scoring's largest group once more in f64; each exponential is taken of a difference to the group's or the row's maximum (formed before it is
+// Sums: those of a group in f32, of groups in f64, the group of the largest logit once more in f64; each exponential is taken of a difference to the group's or the row's maximum (formed before it is
 // scaled), so that what carries the sum carries no error of the shift.
 #pragma once
 #include "../../include/rl_distill.h"
@@ -310,12 +310,6 @@ __global__ __launch_bounds__(256 * KS) void score_few_f32_kernel(const float* __
 // ------------------------------------------------------------------ a row, by a workgroup
 __device__ inline float wave_max(float v) { for (int o = 32; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor(v, o)); return v; }
 
-// e^x, to 2^-23 of itself: the hardware's exponential of what is left of x beside a power of two
-__device__ inline double exp_near(double x) {
-  const double v = x * 1.4426950408889634, n = rint(v);
-  return v < -1000.0 ? 0.0 : ldexp((double)__builtin_amdgcn_exp2f((float)(v - n)), (int)n);
-}
-
 // Order of logits as unsigned numbers: -0 is 0, what is no number comes before everything.
 __device__ inline unsigned order_key(float z) {
   const unsigned u = __float_as_uint(z + 0.f);
@@ -385,6 +379,19 @@ __device__ __attribute__((always_inline)) inline X least_of_best(int bit, int K,
   return x;
 }
 
+// The group of the largest logit m is added once more, logit by logit in f64: beside the largest's 1 an f32 sum keeps nothing of what a nearly certain token leaves to the others, and its entropy,
+// its log-probability and the gradient of a list that names it are just that.  A wavefront's first such group, -1 where it has none (of equal ones in several wavefronts each its own; there the 1s say all).
+template <int REG>
+__device__ __attribute__((always_inline)) inline int top_group(const float4 (&q)[REG], float m, int w) {
+  int top = -1;
+#pragma unroll
+  for (int i = 0; i < REG; ++i) {
+    const unsigned long long at = __ballot(m > -__builtin_inff() && q[i].x == m);
+    if (at && top < 0) top = i * kTopThreads + w * 64 + __builtin_ctzll(at);
+  }
+  return top;
+}
+
 // A row by a workgroup of 256: every thread holds up to REG records.  Bound by the latency of a chain of short steps, so a row is spread over a
 // workgroup and its records are read once; neighbouring rows, which share the records' lines, go to one XCD.  Where maxima or logits are equal the lower index is
 // the better one: a second search, over the index, parts the groups, and candidates are pairs (key, token) that are all different.
@@ -432,15 +439,8 @@ __global__ __launch_bounds__(kTopThreads) void top_kernel(TopJob j) {
   __syncthreads();
 #pragma unroll
   for (int i = 0; i < kTopWaves; ++i) m = fmaxf(m, red_m[i]);
-  // The group of the largest logit once more, its logits added in f64: beside the largest's 1 an f32 sum keeps nothing of what a nearly certain token leaves to the others,
-  // and its entropy and log-probability are just that.  (Of equal ones a wavefront's first; there the 1s say all.)
   double s = 0.0, u = 0.0;
-  int top = -1;
-#pragma unroll
-  for (int i = 0; i < REG; ++i) {
-    const unsigned long long at = __ballot(m > NEG && q[i].x == m);
-    if (at && top < 0) top = i * kTopThreads + w * 64 + __builtin_ctzll(at);
-  }
+  const int top = top_group(q, m, w);
   const float zt = top >= 0 && top * kGroup + lane < j.V ? j.z[tiled_index(t, top * kGroup + lane, j.ldz)] : NEG;
 #pragma unroll
   for (int i = 0; i < REG; ++i) {
@@ -703,15 +703,19 @@ __global__ __launch_bounds__(kTopThreads) void distill_row_kernel(DistillJob j) 
   __syncthreads();
 #pragma unroll
   for (int i = 0; i < kTopWaves; ++i) { m = fmaxf(m, red_m[0][i]); mr = fmaxf(mr, red_m[1][i]); ml = fmaxf(ml, red_m[2][i]); }
+  const int top = top_group(q, m, w);
+  const float zt = top >= 0 && top * kGroup + lane < j.V ? j.z[tiled_index(t, top * kGroup + lane, j.ldz)] : NEG;
   Online o;
   o.m = m;
   r.raise(mr, c);
 #pragma unroll
   for (int i = 0; i < REG; ++i) {
-    if (i * kTopThreads + tid >= j.groups) continue;
-    o.add(q[i], c);
+    const int b = i * kTopThreads + tid;
+    if (b >= j.groups) continue;
+    if (b != top) o.add(q[i], c);
     if (plain[i]) r.add(q[i], c);
   }
+  if (zt != NEG) o.s += (double)__builtin_amdgcn_exp2f((zt - m) * c);
   auto sum4 = [&](int half, double (&v)[4]) __attribute__((always_inline)) {
 #pragma unroll
     for (int k = 0; k < 4; ++k) v[k] = wave_sum(v[k]);
@@ -735,7 +739,8 @@ __global__ __launch_bounds__(kTopThreads) void distill_row_kernel(DistillJob j) 
   double ln = 0.0, lnr = 0.0, lq = 0.0, q_in = 0.0, lqr = 0.0, P = 0.0, pr = 0.0, part[4] = {0.0, 0.0, 0.0, 0.0};
   if (w < 2) {
     ln = log(v[0]);
-    if (in) { lq = (double)j.zs * ((double)zi - (double)m) - ln; q_in = exp_near(lq); part[1] = q_in; }
+    // (q in f64: P q - p of a token that both are nearly certain of is far below either)
+    if (in) { lq = (double)j.zs * ((double)zi - (double)m) - ln; q_in = exp(lq); part[1] = q_in; }
     double lnp = 0.0;
     if (bucket) {
       lnr = log(v[1]);
@@ -757,7 +762,7 @@ __global__ __launch_bounds__(kTopThreads) void distill_row_kernel(DistillJob j) 
   // a list of next to nothing, whose KL is smaller still, is not drowned by it.
   double qr;
   if (part[1] <= 0.5) { qr = 1.0 - part[1]; lqr = log1p(-part[1]); }
-  else qr = exp_near(lqr);
+  else qr = exp(lqr);
   double kl = part[0];
   if (pr > 0.0) kl += pr * (log(pr) - lqr);
   if (nothing) kl = 0.0;

@@ -1,9 +1,11 @@
 """Scoring with top alternatives and distillation where rows, weights or logits are out of the ordinary: rows without a list, numbers that are none, a token that is nearly certain."""
+import numpy as np
 import pytest
 import torch
 
+from oracle import distill_oracle as orc
 from paper_2603_16435_amd import binding
-from test_gpu_distill import Batch, DTYPES, off_grid
+from test_gpu_distill import Batch, DTYPES, U, host, near, off_grid
 
 pytestmark = pytest.mark.gpu
 
@@ -68,3 +70,27 @@ def test_a_row_without_a_list_has_no_gradient_whatever_the_weight_holds(R, H, V,
     r = b.distill(ids, lp, **kw)
     for f in (r.loss, r.row_loss, r.d_hidden, r.d_weight):
         assert not f.any()
+
+
+# a token nearly certain, and the list says so: what is left to learn, 1 - q and its logarithm, is a sum of positive terms over the other tokens, and is right relative to itself.  Column 0 of the weight
+# is that token's alone, so that column 0 of d_hidden is its dS times a number.  With e^-d of the others off by 156 u and the sums by 26 u (see test_nearly_certain_tokens), 1 - q and KL are off by
+# 182 u of themselves (where another token is the likelier one, 26 u more of a KL above one); then dS and d_hidden round once each.  (1e-13: the oracle's own differences.)
+@pytest.mark.parametrize("R,H,V,dtype", [(1, 64, 300, "bf16"), (40, 128, 3000, "bf16"), (300, 136, 5001, "bf16"), (3, 36, 200, "f32"), (100, 68, 5001, "f32"), (200, 68, 777, "f32"), (1100, 100, 900, "f32")])
+@pytest.mark.parametrize("lift,tau", [(1.0, 1.0), (1.0, 0.7), (1.25, 1.0), (1.5, 1.0)])
+@pytest.mark.parametrize("runner_up", [False, True])
+@pytest.mark.parametrize("rest", ["bucket", "renormalise"])
+def test_a_list_of_a_nearly_certain_token(R, H, V, dtype, lift, tau, runner_up, rest):
+    b = Batch(R, H, V, dtype, seed=R + 7, masked=0.0)
+    y = int(b.ids[0])
+    b.weight[:, :2], b.hidden[:, :2] = 0.0, 16.0
+    b.weight[y, 0] = lift
+    if runner_up:                                              # eight below it in the same group
+        b.weight[y - 1 if y % 64 else y + 1, 1] = lift - 0.5
+    ids, lp = torch.full((R, 1), y, dtype=torch.int32, device="cuda"), torch.zeros(R, 1, device="cuda")
+    r = b.distill(ids, lp, rest=rest, temperature=tau, aggregation="token", d_weight_dtype=DTYPES[dtype])
+    want = orc.distill(host(b.hidden), host(b.weight), host(ids), host(lp), host(b.mask), host(b.cu), rest, tau, "token")
+    kl = want["row_loss"]
+    near(r.row_loss, kl, 182 * U * kl + 26 * U * (kl > 1) + 1e-13, "row_loss")
+    ref = want["dS"][:, y] * lift
+    half = 2.0 ** -8 if dtype == "bf16" else U
+    near(r.d_hidden[:, 0], ref, (182 * U + 2.01 * half) * np.abs(ref) + 2e-13 / R, "d_hidden")
