@@ -458,6 +458,21 @@ __global__ __launch_bounds__(kTopThreads) void top_kernel(TopJob j) {
   s = red_s[0]; u = red_u[0];
 #pragma unroll
   for (int i = 1; i < kTopWaves; ++i) { s += red_s[i]; u += red_u[i]; }
+  if (u != u && s == s && j.entropy) {
+    // A logit, or a difference to the largest, is -inf: e d was 0 times that.  Its probability is 0, and so is its part: the row once more, by its logits.
+    u = 0.0;
+    for (int v = tid; v < j.V; v += kTopThreads) {
+      const float d = j.z[tiled_index(t, v, j.ldz)] - m, e = __builtin_amdgcn_exp2f(d * c);
+      if (e > 0.f) u += (double)e * (double)d;
+    }
+    u = wave_sum(u);
+    __syncthreads();                                              // (red_u has been read)
+    if (lane == 0) red_u[w] = u;
+    __syncthreads();
+    u = red_u[0];
+#pragma unroll
+    for (int i = 1; i < kTopWaves; ++i) u += red_u[i];
+  }
   const double ln = log(s);
   if (tid == 0) {
     if (j.lse) j.lse[row] = (float)((double)j.zs * (double)m + ln);

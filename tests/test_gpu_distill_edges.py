@@ -94,3 +94,27 @@ def test_a_list_of_a_nearly_certain_token(R, H, V, dtype, lift, tau, runner_up, 
     ref = want["dS"][:, y] * lift
     half = 2.0 ** -8 if dtype == "bf16" else U
     near(r.d_hidden[:, 0], ref, (182 * U + 2.01 * half) * np.abs(ref) + 2e-13 / R, "d_hidden")
+
+
+# scoring: few tokens in bf16 and in f32, tiles of both, a weight off the 16-byte grid
+@pytest.mark.parametrize("R,H,V,dtype,off", [(1, 64, 300, "bf16", 0), (60, 128, 3000, "bf16", 0), (100, 136, 20000, "bf16", 0), (300, 128, 1000, "bf16", 0), (300, 72, 1000, "bf16", 0),
+                                             (200, 64, 700, "bf16", 1), (3, 36, 200, "f32", 0), (60, 68, 777, "f32", 0), (200, 68, 777, "f32", 0), (1100, 100, 20011, "f32", 0), (200, 36, 700, "f32", 1)])
+@pytest.mark.parametrize("where", ["group", "far"])
+def test_a_logit_below_all_numbers_has_no_part_in_the_entropy(R, H, V, dtype, off, where):
+    """Logits that overflow to -inf, in the group of the largest and in others; and logits so far apart that their difference overflows.  Their tokens have probability 0.  (A sum
+    of e d over the others: an exponential as in test_gpu_distill.py, sums in f64, entropy within 32 u (2 + 2 x 60).)"""
+    b = Batch(R, H, V, dtype, seed=R + 5, masked=0.0)
+    b.weight[:, 0], b.hidden[:, 0] = 0.0, 4.0
+    low = torch.tensor([1, 70, V // 2, V - 1], device="cuda") % V
+    if where == "group":
+        b.weight[low, 0] = -3e38
+        b.weight[low, 1:] = 0.0
+    else:
+        b.weight[64:128, 0], b.weight[5, 0] = -7.5e37, 7.5e37
+    if off:
+        b.weight = off_grid(b.weight, off)
+    r = b.score(3, 1.0)
+    want = orc.top_logprobs(host(b.hidden), host(b.weight), host(b.ids), host(b.mask), host(b.cu), 3, 1.0)
+    assert bool(r.entropy.isfinite().all()) and bool(r.lse.isfinite().all())
+    near(r.entropy, want["entropy"], 32 * U * (2 + 2 * 60), "entropy")
+    assert np.array_equal(host(r.top_ids), want["top_ids"])
