@@ -27,7 +27,7 @@ typedef struct rl_top_params {
   int32_t top_k;                  /* alternatives, 1 <= top_k <= min(RL_TOP_MAX_K, V)                             */
   int32_t chunk_rows;             /* rows whose logits are held at once (4 bytes per row and vocabulary entry);   */
                                   /* 0 = rl_default_chunk_rows_distill; rounded up to a multiple of 256, 2^20 at most */
-  float   temperature;            /* 0 = 1.0; otherwise finite and > 0                                            */
+  float   temperature;            /* 0 = 1.0; otherwise 4.3e-39 to 3e38 (log2(e) / temperature is finite in f32)  */
 } rl_top_params;
 
 typedef struct rl_top_outputs {   /* NULL = not wanted; one at least                                              */
@@ -63,7 +63,7 @@ typedef struct rl_distill_params {
   int32_t rest;                   /* rl_distill_rest                                                              */
   int32_t aggregation;            /* rl_aggregation                                                               */
   int32_t chunk_rows;             /* as above; sizes the workspace                                                */
-  float   temperature;            /* of the student; the lists are taken as they are.  0 = 1.0                    */
+  float   temperature;            /* of the student, as above; the lists are taken as they are                    */
   float   scale;                  /* 0 = 1.0; otherwise finite                                                    */
   int32_t d_weight_dtype;         /* rl_dtype of d_weight: RL_F32, or RL_BF16 with bf16 inputs (else RL_ERR_DTYPE)  */
 } rl_distill_params;

@@ -1039,7 +1039,8 @@ static void few_plan(HeadPlan& h) {
   h.few_nt = nt;
 }
 
-static bool good_temperature(float t) { return t == 0.f || (t > 0.f && t <= 3.0e38f); }
+// (log2(e) / t is what differences of logits are multiplied with: 0 times an infinity is no number)
+static bool good_temperature(float t) { return t == 0.f || (t > 0.f && t <= 3.0e38f && 1.f / t * kLog2e <= 3.4028234e38f); }
 
 static rl_status head_plan(const rl_batch* b, int K, int chunk_rows, float temperature, bool bwd, bool distill, bool round_dw, HeadPlan& h) {
   if (!b) return RL_ERR_NULL;

@@ -118,3 +118,18 @@ def test_a_logit_below_all_numbers_has_no_part_in_the_entropy(R, H, V, dtype, of
     assert bool(r.entropy.isfinite().all()) and bool(r.lse.isfinite().all())
     near(r.entropy, want["entropy"], 32 * U * (2 + 2 * 60), "entropy")
     assert np.array_equal(host(r.top_ids), want["top_ids"])
+
+
+@pytest.mark.parametrize("R,H,V,dtype", [(40, 128, 3000, "bf16"), (300, 136, 5001, "bf16"), (20, 36, 700, "f32"), (200, 68, 777, "f32")])
+def test_the_lowest_temperatures(R, H, V, dtype):
+    """At the lowest that is taken a row's largest logit has all of the probability, shared out among equal ones: numbers everywhere, and those of the definition."""
+    tau = 4.3e-39
+    b = Batch(R, H, V, dtype, seed=R + 9, masked=0.0)
+    r = b.score(2, tau)
+    want = orc.top_logprobs(host(b.hidden), host(b.weight), host(b.ids), host(b.mask), host(b.cu), 2, tau)
+    assert np.array_equal(host(r.top_ids), want["top_ids"])
+    near(r.top_logprob[:, 0], want["top_logprob"][:, 0], 32 * U, "top_logprob")
+    near(r.entropy, want["entropy"], 64 * U, "entropy")
+    d = b.distill(r.top_ids[:, :1].contiguous(), torch.zeros(R, 1, device="cuda"), temperature=tau, rest="renormalise", aggregation="token")
+    near(d.row_loss, -want["top_logprob"][:, 0], 32 * U, "row_loss")
+    assert bool(d.d_hidden.isfinite().all()) and bool(d.d_weight.isfinite().all())
