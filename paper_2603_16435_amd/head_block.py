@@ -74,7 +74,12 @@ class HeadBlock:
         return binding.rl_token_top_logprobs(self.hidden(x), self.lm_head, token_ids, mask, top_k, **options)
 
     def distill_step(self, x, teacher_ids, teacher_logprob, mask, cu_seqlens=None, overwrite=False, **options):
-        """One pass over a batch that a teacher has scored: (DistillResult, HeadGrads).  options: those of rl_distill_loss_fwd_bwd."""
+        """One pass over a batch that a teacher has scored: (DistillResult, HeadGrads).  options: those of rl_distill_loss_fwd_bwd, but d_hidden; with backward=False, the loss
+        alone (held-out text), x is left as it is and the gradients are None."""
+        if "d_hidden" in options:
+            raise ValueError("d_hidden: the gradient of the LM head's input is the block's own")
+        if not options.get("backward", True):
+            return binding.rl_distill_loss_fwd_bwd(self.hidden(x), self.lm_head, teacher_ids, teacher_logprob, mask, cu_seqlens, **options), None
         hidden, kept = self.forward(x, overwrite)
         res = binding.rl_distill_loss_fwd_bwd(hidden, self.lm_head, teacher_ids, teacher_logprob, mask, cu_seqlens, d_hidden=hidden, **options)
         dx, dgamma, dbeta, dweight = self.backward(res.d_hidden, kept)
