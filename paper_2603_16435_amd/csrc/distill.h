@@ -397,7 +397,7 @@ __device__ __attribute__((always_inline)) inline int top_group(const float4 (&q)
 // the better one: a second search, over the index, parts the groups, and candidates are pairs (key, token) that are all different.
 // 5.7 k rows, V 152064, K 20 112 us (the records alone 215 MB, 1.9 TB/s), 4.1 k rows, K 128 135; one row 17, 48 rows of V 32000 10.
 template <int REG>
-__global__ __launch_bounds__(kTopThreads) void top_kernel(TopJob j) {
+__global__ __launch_bounds__(kTopThreads, REG <= 10 ? 7 : 2) void top_kernel(TopJob j) {
   __shared__ float red_m[kTopWaves];
   __shared__ double red_s[kTopWaves], red_u[kTopWaves];
   __shared__ int words[2][kTopWaves];
