@@ -33,7 +33,7 @@ typedef struct rl_top_params {
 typedef struct rl_top_outputs {   /* NULL = not wanted; one at least                                              */
   float*   logprob;               /* [R]  log q_t[token_ids[t]]; needs token_ids, which may be NULL without it    */
   float*   lse;                   /* [R]  logsumexp of z / temperature                                            */
-  float*   entropy;               /* [R]                                                                          */
+  float*   entropy;               /* [R]  a logit of -inf has probability 0 and no part in it                       */
   int32_t* top_ids;               /* [R, top_k]  the most probable tokens, most probable first; among equal logits the lower token first; */
                                   /*             -1 on rows that do not count, and where a row's logits are not numbers                   */
   float*   top_logprob;           /* [R, top_k]  their log-probabilities; 0 on rows that do not count             */
@@ -57,7 +57,7 @@ typedef enum rl_distill_rest {
  *                                       or 1 / T (RL_AGG_TOKEN)
  *     dS[t,v] = scale c_t / temperature (P q_t[v] - p_v) for listed v, scale c_t / temperature q_t[v] (P - p_r / q_r) for others,  P = sum p_i + p_r
  * and d_hidden = dS W, d_weight = dS^T X.  A row with an empty list, or whose entries all have p = 0 under RL_REST_RENORMALISE, counts with
- * KL_t = 0 and no gradient. */
+ * KL_t = 0 and no gradient, whatever its hidden states or the weight hold. */
 typedef struct rl_distill_params {
   int32_t top_k;                  /* length of the lists, 1 <= top_k <= RL_TOP_MAX_K                              */
   int32_t rest;                   /* rl_distill_rest                                                              */

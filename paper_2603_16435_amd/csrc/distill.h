@@ -23,8 +23,8 @@ constexpr int kMostChunkRows = 1 << 20;           // (launches of a chunk stay b
 constexpr int kGroup = 64;                        // vocabulary entries of a record
 
 // ------------------------------------------------------------------ logits and records
-// Bound by the contraction, whose tile the epilogue ends: 1290 TF at 5.7 k rows of the 7B head (H 3584, V 152064), 4780 us, 9 to 12 % behind the forward that keeps no logits (4420).
-// Keeping them is most of that (3.4 GB of f32; the policy's own forward that keeps them takes 8 % more), three operations and an exponential for each logit the rest.
+// Bound by the contraction, whose tile the epilogue ends.  us in turn with the forward that keeps no logits: 5664 rows at the 7B head (H 3584, V 152064) 4660 (1325 TF) and 4236, 10 % behind it, 4099 rows,
+// H 5120, V 151936 4667 (1366 TF) and 4350, 7 %: the store of the logits (3.4 GB of f32) and three operations and an exponential for each.
 //
 // Record of 64 logits of a token, x largest (raw), y sum exp(zs (z - x)), z sum of those times (z - x); w unused.
 //
@@ -193,7 +193,7 @@ void score_few_kernel(const bf16_t* __restrict__ W, const bf16_t* __restrict__ X
 // f32 logits of a few tokens, up to 64.  Bound by reading the weight once, which the tiles of gemm_f32.h, 64 tokens wide, and the narrow ones, which leave most CUs without work where the
 // vocabulary is small, are far from (us, TB/s of W: 4 tokens, H 2048, V 152064 366, 3.4; 2 tokens, H 5120, V 32000 216, 3.0; 3 tokens, V 5726 169, 0.7).  A workgroup takes a group of
 // 64 vocabulary entries; KS sets of four wavefronts share K, each wavefront 16 entries.  Slabs of 32 k go straight into LDS, as whole lines (loaded into the operands' registers, 64 bytes of a row by
-// four lanes, L1 bounds it: 325 us for the first of the three), two ahead of the one computed on; five workgroups fit a CU.  v_mfma_f32_16x16x4, lane group g with k = 16 s + 4 g + e of a slab in its
+// four lanes, L1 bounds it: 325 us for the first of the three), two ahead of the one computed on; of up to 16 tokens in one set five workgroups fit a CU's LDS (four with the preparation inside), of 32 tokens in four sets or 64 in two one.  v_mfma_f32_16x16x4, lane group g with k = 16 s + 4 g + e of a slab in its
 // k-step (s, e).  What the sets found is added in order in LDS, and the record made there.  (The order of a logit's sum is not that of the other f32 kernels: scored with more than 64
 // rows, a token's last bit may be another.)
 constexpr int kFewF32Stages = 3;
@@ -395,7 +395,8 @@ __device__ __attribute__((always_inline)) inline int top_group(const float4 (&q)
 // A row by a workgroup of 256: every thread holds up to REG records.  Bound by the latency of a chain of short steps, so a row is spread over a
 // workgroup and its records are read once; neighbouring rows, which share the records' lines, go to one XCD.  Where maxima or logits are equal the lower index is
 // the better one: a second search, over the index, parts the groups, and candidates are pairs (key, token) that are all different.
-// 5.7 k rows, V 152064, K 20 112 us (the records alone 215 MB, 1.9 TB/s), 4.1 k rows, K 128 135; one row 17, 48 rows of V 32000 10.
+// 5.7 k rows, V 152064, K 20 108 us (the records alone 215 MB, 2.0 TB/s; 114 with six workgroups a CU instead of seven, which the part for logits of -inf takes where it may), 4.1 k rows,
+// K 128 135; one row 17, 48 rows of V 32000 10.
 template <int REG>
 __global__ __launch_bounds__(kTopThreads, REG <= 10 ? 7 : 2) void top_kernel(TopJob j) {
   __shared__ float red_m[kTopWaves];
@@ -815,7 +816,8 @@ __device__ __attribute__((always_inline)) inline float ds_entry(float z, const D
 struct DsJob { const float* z; int64_t ldz; const DistillRow* rows; const Ctrl* ctrl; int chunk_start, V; float zs; };
 
 // bf16: logits and dS are both slab-tiled, a pass over memory in order; a workgroup takes a slab (256 rows, 64 vocabulary entries).  Rows of a slab without a token become 0,
-// as does the padding of the vocabulary.  Bound by memory, six bytes a logit: 4.5 k rows, V 152064 780 us, 5.3 TB/s.
+// as does the padding of the vocabulary.  dS is rounded to bf16, once, by at most 2^-8 of each entry: it is an operand of both contractions, and the matrix unit's rate for f32 operands is a tenth of
+// that for bf16; two bf16 terms of each entry would double the two contractions, 60 % of a call.  Both gradients are off by 2.2e-3 to 2.5e-3 of their norm where rounding the exact result gives 1.7e-3.  Bound by memory, six bytes a logit: 4.5 k rows, V 152064 780 us, 5.3 TB/s.
 __device__ __attribute__((always_inline)) inline void ds_block(int block, const DsJob& j, bf16_t* dS) {
   const int slabs = (int)(j.ldz / 64), tile = block / slabs, slab = block % slabs;
   const int left = j.ctrl->n_real - j.chunk_start - tile * 256;
